@@ -383,6 +383,123 @@ hack_status hack_step_final(hack_ctx* ctx, hack_kvcache* cache, int32_t B,
                             void* out, int32_t* kept_idx_opt, int64_t idx_stride,
                             hack_stream stream);
 
+/* ---- rotary positions, norms of queries and keys -----------------------------
+ * What stands in front of a step: queries and keys as a projection leaves them become
+ * the q and k_new of the calls above.  These calls read rows with any strides and
+ * write [B, heads, N, head_dim]; the number of heads is the operand's own (queries
+ * may have more heads than the caches, see hack_attn_packed).
+ *
+ * A pair (a, b) of a head's row at position p becomes
+ *   (gain (a cos(p f) - b sin(p f)), gain (a sin(p f) + b cos(p f))),
+ * f its frequency in radians per position.  Angles are exact to 1e-8 for every
+ * 32-bit position, negative ones too: -p undoes p where gain is 1.  Elements from
+ * rot_dim on pass through.  Everything is formed in float32 and rounded once. */
+enum { HACK_ROPE_HALF = 0, HACK_ROPE_INTERLEAVED = 1 };
+
+typedef struct {
+  int32_t layout;     /* HACK_ROPE_HALF: pairs (i, i + S/2) of an axis' S elements; HACK_ROPE_INTERLEAVED: (2i, 2i + 1) */
+  int32_t rot_dim;    /* elements of a head that rotate, the first ones; at most head_dim, a multiple of 16 for each axis */
+  int32_t axes;       /* 1, or 2 (rows and columns of an image): axis a has the S = rot_dim / axes elements from a S on */
+  float gain;         /* factor on cosine and sine, 1 as a rule */
+  const double* freq; /* HOST [rot_dim / 2], axis after axis; read during the call */
+} hack_rope;
+
+typedef struct {
+  const void* x;        /* DEVICE element (b, h, n, i) at b stride_b + h stride_h + n stride_n + i */
+  void* out;            /* DEVICE [B, heads, N, head_dim]; may be x if x lies in that layout, must not share memory with
+                           rows that are read otherwise */
+  int32_t heads;
+  int64_t stride_b, stride_h, stride_n;   /* elements, not negative, multiples of 16 bytes */
+  const float* weight;  /* DEVICE [head_dim] or [heads, weight_stride_h], NULL = ones (hack_norm_rotate only) */
+  int64_t weight_stride_h;   /* 0: one weight for all heads; else elements from one head's to the next's, a multiple of 4 */
+} hack_rows;
+
+/* The frequencies of common scalings, base^(-2i/S) for pair i of an axis, into freq
+ * [rot_dim / 2]; *gain (may be NULL) gets the gain that belongs to them.  factor >= 1
+ * is the ratio of the context to the one trained on.
+ *   HACK_ROPE_PLAIN   as they are
+ *   HACK_ROPE_LINEAR  all divided by factor
+ *   HACK_ROPE_BASE    base raised by factor^(S / (S - 2)): the slowest pair is divided by factor, the fastest stays
+ *   HACK_ROPE_PARTS   pairs that turn more than 32 times over trained_len positions stay, those that turn less than
+ *                     once are divided by factor, a linear ramp over the pairs between; gain 0.1 ln(factor) + 1
+ * Host arithmetic, no context.  Errors: HACK_EINVAL. */
+enum { HACK_ROPE_PLAIN = 0, HACK_ROPE_LINEAR = 1, HACK_ROPE_BASE = 2, HACK_ROPE_PARTS = 3 };
+hack_status hack_rope_freqs(int32_t rot_dim, int32_t axes, int32_t scaling, double base, double factor,
+                            double trained_len, double* freq, float* gain);
+
+/* Rotates the rows of x.
+ *   pos  DEVICE int32: row n of batch element b has position pos[b pos_stride_b + a N + n]
+ *        on axis a (pos_stride_b 0: the same for every batch element); NULL: pos0 + n (one axis)
+ * Errors: HACK_EINVAL (NULL/misaligned pointers, strides, layout, frequencies that are not finite, overlap, the current
+ * device is not the context's), HACK_EUNSUPPORTED (rot_dim no multiple of 16 for each axis), HACK_ECAPACITY. */
+hack_status hack_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* x, const hack_rope* rope,
+                        const int32_t* pos, int64_t pos_stride_b, int32_t pos0, hack_stream stream);
+
+/* Norms of the rows of q and k, head by head, and their rotation, in one launch.
+ *   HACK_NORM_RMS   x / sqrt(mean(x^2) + eps) * weight
+ *   HACK_NORM_UNIT  x / max(|x|, eps) * weight (a weight per head: unit rows times a learned scale)
+ * over all head_dim elements, sums of squares in float32.  k may be NULL, rope may be
+ * NULL (norms alone; pos is not read then).  eps > 0.  Errors as hack_rotate. */
+enum { HACK_NORM_RMS = 0, HACK_NORM_UNIT = 1 };
+hack_status hack_norm_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, int32_t norm,
+                             float eps, const hack_rope* rope, const int32_t* pos, int64_t pos_stride_b, int32_t pos0,
+                             hack_stream stream);
+
+/* ---- caches in 4 bits ----------------------------------------------------------
+ * A packed cache holds a row in 17/32 of a byte an element: groups of 32 elements
+ * along the head share an exponent s; an element is 2^(s - 127) times one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 or its negative.  s is the smallest in [3, 252] for which no
+ * magnitude of the group exceeds 7 of that unit (252 for what is larger still); elements are
+ * rounded to the nearest value, ties to the even code.  A group that holds an infinity or a NaN
+ * reads as NaN throughout, magnitudes below 2^-126 as zero.  Rows read back are bf16
+ * numbers exactly, and packing them again gives the same bytes: unpack, score, select and
+ * pack compress a packed cache without a second rounding.
+ * Memory is laid out in blocks of 64 rows, for the matrix cores; it means nothing to
+ * the caller beyond its size: hack_packed_bytes for K and the same for V. */
+typedef struct {
+  void* k;            /* DEVICE hack_packed_bytes(head_dim, rows) bytes, 16-byte aligned */
+  void* v;            /* DEVICE the same */
+  int32_t* pos;       /* DEVICE [rows] global token id of every row, or NULL */
+  int64_t rows;       /* a multiple of 64 */
+  const int64_t* off; /* HOST [B*H] first row of each unit; multiples of 64 */
+  const int32_t* len; /* HOST [B*H] valid rows of each unit */
+} hack_packed_cache;
+
+/* Bytes of k (and of v) for `rows` rows, rounded up to whole blocks. */
+hack_status hack_packed_bytes(int32_t head_dim, int64_t rows, int64_t* bytes);
+
+/* hack_compact into a packed cache: row first[u] + i of unit u becomes row
+ * kept_idx[u, i] of the virtual concatenation (in rows, then k_new/v_new rows), for
+ * first[u] + i < out->len[u].  Without kept_idx it becomes row i of it, so packing
+ * the new rows of a step behind those a unit has is in = NULL, first[u] = the length
+ * before, out->len[u] = the length after.  Other rows stay as they are.
+ *   in        NULL: no cached rows
+ *   kept_idx  DEVICE int32 [B*H, idx_stride], entries in [0, in->len[u] + N_k) (clamped to it), or NULL
+ *   first     HOST [B*H], NULL = 0 for all
+ * `pos` is written for rows from k_new (pos_new + row number), and for cached rows
+ * if `in` carries it too.  bf16 and fp32 contexts.
+ * Errors: HACK_EINVAL (NULL/misaligned pointers, more rows than there are, units outside out or overlapping in it, the
+ * current device is not the context's), HACK_ECAPACITY. */
+hack_status hack_pack(hack_ctx* ctx, int32_t B, int32_t N_k, const hack_cache* in, const void* k_new, const void* v_new,
+                      int32_t pos_new, const int32_t* kept_idx, int64_t idx_stride, const int32_t* first,
+                      const hack_packed_cache* out, hack_stream stream);
+
+/* Rows first[u] .. first[u] + out->len[u] of unit u of a packed cache (first NULL: from
+ * row 0), as rows of the context's element type, exactly; pos too when both carry it.
+ * Errors as hack_pack. */
+hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_cache* in, const int32_t* first,
+                        const hack_cache* out, hack_stream stream);
+
+/* hack_attn over a packed cache: O = Softmax(scale * Q K^T) V for every unit over its
+ * own kv->len[u] rows, no mask.  Every unit must have at least one row; out must not
+ * share memory with q.  Units are not limited by max_cache_len.  Heads that share a
+ * cache: queries [B, G H, N, d] of G heads to each of the H caches are [B, H, G N, d],
+ * so N_k = G N.  The values that packing rounds to are bf16 numbers, so the accuracy is
+ * hack_attn's over the rows that hack_unpack gives.  Results are reproducible bit for bit.
+ * bf16 contexts only (HACK_EUNSUPPORTED).  Errors: HACK_EINVAL, HACK_ECAPACITY as above. */
+hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, const void* q, const hack_packed_cache* kv,
+                             float scale, void* out, hack_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

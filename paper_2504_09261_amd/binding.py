@@ -25,6 +25,7 @@ EXPORTS = [
     "hack_kvcache_rows_required", "hack_kvcache_create", "hack_kvcache_destroy",
     "hack_kvcache_reset", "hack_kvcache_view", "hack_kvcache_step_form", "hack_step", "hack_head_variance",
     "hack_set_score_mode", "hack_get_score_mode", "hack_score_static", "hack_score_item_keys", "hack_merge", "hack_step_final",
+    "hack_rope_freqs", "hack_rotate", "hack_norm_rotate", "hack_packed_bytes", "hack_pack", "hack_unpack", "hack_attn_packed",
 ]
 
 
@@ -49,6 +50,15 @@ class _raw_cache(C.Structure):
     """The same memory with the host arrays as plain addresses (making a pointer object takes longer than a call)."""
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pos", C.c_void_p), ("rows", C.c_int64),
                 ("off", C.c_void_p), ("len", C.c_void_p)]
+
+
+class hack_rope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("axes", C.c_int32), ("gain", C.c_float), ("freq", C.POINTER(C.c_double))]
+
+
+class hack_rows(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("heads", C.c_int32), ("stride_b", C.c_int64), ("stride_h", C.c_int64),
+                ("stride_n", C.c_int64), ("weight", C.c_void_p), ("weight_stride_h", C.c_int64)]
 
 
 _lib = None
@@ -108,6 +118,14 @@ def load_library() -> C.CDLL:
     lib.hack_kvcache_step_form.argtypes = [vp]
     lib.hack_kvcache_step_form.restype = i32
     lib.hack_step.argtypes = [vp, vp, i32, i32, vp, vp, vp, pu8, pi32, i32, f32, vp, vp, i64, vp]
+    pd, prows, prope = C.POINTER(C.c_double), C.POINTER(hack_rows), C.POINTER(hack_rope)
+    lib.hack_rope_freqs.argtypes = [i32, i32, i32, C.c_double, C.c_double, C.c_double, pd, C.POINTER(f32)]
+    lib.hack_rotate.argtypes = [vp, i32, i32, prows, prope, vp, i64, i32, vp]
+    lib.hack_norm_rotate.argtypes = [vp, i32, i32, prows, prows, i32, f32, prope, vp, i64, i32, vp]
+    lib.hack_packed_bytes.argtypes = [i32, i64, pi64]
+    lib.hack_pack.argtypes = [vp, i32, i32, pcache, vp, vp, i32, vp, i64, pi32, pcache, vp]
+    lib.hack_unpack.argtypes = [vp, i32, pcache, pi32, pcache, vp]
+    lib.hack_attn_packed.argtypes = [vp, i32, i32, vp, pcache, f32, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int and name not in ("hack_strerror", "hack_last_error"):
@@ -180,6 +198,71 @@ class Cache:
     def struct(self) -> hack_cache:
         return hack_cache.from_buffer(_raw_cache(_dev(self.k), _dev(self.v), _dev(self.pos), self.rows,
                                                  _addr(self.off), _addr(self.len)))
+
+
+PACK_ROWS = 64   # rows of a block of a packed cache
+
+
+def packed_bytes(head_dim: int, rows: int) -> int:
+    """Bytes of the K (and of the V) of `rows` rows of a packed cache."""
+    n = C.c_int64()
+    st = load_library().hack_packed_bytes(head_dim, rows, C.byref(n))
+    if st != 0:
+        raise HackError(st, load_library().hack_strerror(st).decode())
+    return n.value
+
+
+class PackedCache:
+    """A hack_packed_cache view: device byte tensors of K and V (hack_packed_bytes each), host offsets (multiples of 64 rows) and lengths."""
+
+    def __init__(self, k, v, off, length, pos=None):
+        import torch
+        self.k, self.v, self.pos = k, v, pos
+        self.off, self.len = _i64(off), _i32(length)
+        assert k.dtype == v.dtype == torch.uint8 and k.shape == v.shape and k.dim() == 2, "K and V: byte tensors [rows / 64, bytes of 64 rows]"
+        assert k.shape[1] in (34 * 64, 34 * 128), "a block of 64 rows has 34 bytes an element of the head"
+        assert pos is None or pos.dtype == torch.int32 and pos.numel() >= PACK_ROWS * k.shape[0], "pos: an int32 for every row"
+        self.head_dim, self.rows = int(k.shape[1]) // 34, PACK_ROWS * int(k.shape[0])
+
+    @classmethod
+    def empty(cls, head_dim: int, cap, device="cuda", with_pos: bool = False) -> "PackedCache":
+        """Room for units of up to cap[u] rows, all of them empty."""
+        import torch
+        blocks = -(-_i64(cap) // PACK_ROWS)
+        n = int(blocks.sum())
+        k, v = (torch.empty((n, packed_bytes(head_dim, PACK_ROWS)), dtype=torch.uint8, device=device) for _ in range(2))
+        pos = torch.empty((n * PACK_ROWS,), dtype=torch.int32, device=device) if with_pos else None
+        return cls(k, v, PACK_ROWS * (np.cumsum(blocks) - blocks), np.zeros(len(blocks), np.int32), pos)
+
+    def struct(self) -> hack_cache:   # the two structures have the same members
+        return hack_cache.from_buffer(_raw_cache(_dev(self.k), _dev(self.v), _dev(self.pos), self.rows,
+                                                 _addr(self.off), _addr(self.len)))
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+NORMS = {"rms": 0, "l2": 1}
+
+
+class Rope:
+    """A hack_rope: frequencies (radians per position, axis after axis), which elements rotate and how they pair."""
+
+    def __init__(self, freq, rot_dim: int, axes: int = 1, layout: str = "half", gain: float = 1.0):
+        self.freq = np.ascontiguousarray(freq, np.float64)
+        assert self.freq.shape == (rot_dim // 2,), "one frequency for every pair"
+        self.rot_dim, self.axes, self.layout, self.gain = rot_dim, axes, layout, gain
+        self._struct = hack_rope(ROPE_LAYOUTS[layout], rot_dim, axes, gain, self.freq.ctypes.data_as(C.POINTER(C.c_double)))
+
+    @classmethod
+    def scaled(cls, rot_dim: int, axes: int = 1, layout: str = "half", scaling: str = "plain", base: float = 10000.0, factor: float = 1.0,
+               trained_len: float = 0.0) -> "Rope":
+        """The frequencies and the gain of hack_rope_freqs."""
+        lib = load_library()
+        freq, gain = np.zeros(max(rot_dim // 2, 0)), C.c_float()
+        st = lib.hack_rope_freqs(rot_dim, axes, ROPE_SCALINGS[scaling], base, factor, trained_len, freq.ctypes.data_as(C.POINTER(C.c_double)), C.byref(gain))
+        if st != 0:
+            raise HackError(st, lib.hack_strerror(st).decode())
+        return cls(freq, rot_dim, axes, layout, gain.value)
 
 
 class ManagedCache:
@@ -351,6 +434,70 @@ class Hack:
         B, H, Nk, d = q.shape
         cs = cache.struct()
         self._check(self.lib.hack_head_variance(self.ctx, B, Nk, _dev(q), C.byref(cs), scale, _dev(sigma), _stream()))
+
+    # ---- rotary positions, norms ----
+    def _rows(self, x, out, weight=None) -> hack_rows:
+        """x: [B, heads, N, head_dim] in any strides with the head's elements side by side; out: the same shape, contiguous."""
+        assert x.is_cuda and x.dim() == 4 and x.stride(3) == 1 and x.shape[3] == self.head_dim and x.dtype == self.torch_dtype, \
+            "rows: [B, heads, N, head_dim] of the context's element type, head_dim side by side"
+        assert out.shape == x.shape and out.dtype == x.dtype, "out: the shape and element type of x"
+        ws = 0
+        if weight is not None:
+            assert weight.is_cuda and weight.dtype.itemsize == 4 and weight.is_floating_point(), "weight: float32"
+            assert weight.shape[-1] == self.head_dim and weight.stride(-1) == 1 and (weight.dim() == 1 or weight.dim() == 2 and weight.shape[0] == x.shape[1])
+            ws = weight.stride(0) if weight.dim() == 2 else 0
+        # a dimension of one element may have any stride
+        s = [x.stride(i) if x.shape[i] > 1 else 0 for i in (0, 1, 2)]
+        return hack_rows(x.data_ptr(), _dev(out), x.shape[1], s[0], s[1], s[2], None if weight is None else weight.data_ptr(), ws)
+
+    @staticmethod
+    def _positions(pos, B: int, N: int, axes: int):
+        """(address, stride) of positions [axes, N], the same for all batch elements, or [B, axes, N]; with one axis also [N]."""
+        if pos is None:
+            return None, 0
+        assert pos.dtype.itemsize == 4 and not pos.is_floating_point(), "positions: int32"
+        shape = tuple(pos.shape)
+        assert shape in ((axes, N), (B, axes, N)) or axes == 1 and shape == (N,), "positions: [axes, N] or [B, axes, N]"
+        return _dev(pos), axes * N if len(shape) == 3 else 0
+
+    def rotate(self, x, rope: Rope, out, pos=None, pos0: int = 0):
+        """out <- the rows of x rotated (x: [B, heads, N, head_dim], any strides; out may be x if that is contiguous)."""
+        B, _, N, _ = x.shape
+        p, stride = self._positions(pos, B, N, rope.axes)
+        self._check(self.lib.hack_rotate(self.ctx, B, N, C.byref(self._rows(x, out)), C.byref(rope._struct), p, stride, pos0, _stream()))
+
+    def norm_rotate(self, q, k, norm: str, eps: float, q_weight, k_weight, rope: Optional[Rope], q_out, k_out, pos=None, pos0: int = 0):
+        """Norms ("rms" or "l2") of the rows of q and k (or None), then their rotation (rope None: norms alone)."""
+        B, _, N, _ = q.shape
+        assert k is None or (k.shape[0], k.shape[2]) == (B, N)
+        p, stride = self._positions(pos, B, N, rope.axes) if rope is not None else (None, 0)
+        self._check(self.lib.hack_norm_rotate(self.ctx, B, N, C.byref(self._rows(q, q_out, q_weight)),
+                                              None if k is None else C.byref(self._rows(k, k_out, k_weight)), NORMS[norm], eps,
+                                              None if rope is None else C.byref(rope._struct), p, stride, pos0, _stream()))
+
+    # ---- caches in 4 bits ----
+    def pack(self, B: int, Nk: int, packed: PackedCache, cache_in: Optional[Cache] = None, kept_idx=None, k_new=None, v_new=None,
+             pos_new: int = 0, at=None):
+        """Rows of cache_in and new ones, all in order or those of kept_idx, become rows at[u] .. packed.len[u] of unit u."""
+        assert packed.head_dim == self.head_dim
+        ci, cp = None if cache_in is None else cache_in.struct(), packed.struct()
+        a = None if at is None else _i32(at)
+        self._check(self.lib.hack_pack(self.ctx, B, Nk, None if ci is None else C.byref(ci), _dev(k_new), _dev(v_new), pos_new, _dev(kept_idx),
+                                       0 if kept_idx is None else kept_idx.stride(0), _p(a, C.c_int32), C.byref(cp), _stream()))
+
+    def unpack(self, B: int, packed: PackedCache, cache_out: Cache, first=None):
+        """Rows first[u] .. first[u] + cache_out.len[u] of every unit, as rows of the context's element type."""
+        assert packed.head_dim == self.head_dim
+        cp, co = packed.struct(), cache_out.struct()
+        f = None if first is None else _i32(first)
+        self._check(self.lib.hack_unpack(self.ctx, B, C.byref(cp), _p(f, C.c_int32), C.byref(co), _stream()))
+
+    def attn_packed(self, q, packed: PackedCache, scale: float, out):
+        """q: [B, G heads, N, head_dim], G query heads to each cache."""
+        B, H, N, d = q.shape
+        assert packed.head_dim == self.head_dim == d and H % self.heads == 0 and out.shape == q.shape
+        cp = packed.struct()
+        self._check(self.lib.hack_attn_packed(self.ctx, B, H // self.heads * N, _dev(q), C.byref(cp), scale, _dev(out), _stream()))
 
     # ---- a5 ----
     def managed_cache(self, cap, with_pos: bool = True) -> ManagedCache:

@@ -13,7 +13,7 @@ LIB_NAME = "libhack_mi355x.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
 STEP_CALL_PATH = os.path.join(HERE, "_step_call.so")   # CPython entry to hack_step
 SOURCES = ["hack_api.cpp", "kernels_move.hip", "kernels_select.hip", "kernels_score.hip", "kernels_attn.hip", "kernels_attn_split.hip", "kernels_attn_f32.hip", "kernels_step.hip",
-           "kernels_headvar.hip", "kernels_merge.hip"]
+           "kernels_headvar.hip", "kernels_merge.hip", "ops_api.cpp", "kernels_rotate.hip", "kernels_packed.hip", "kernels_attn_packed.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms are switched off for all device code.

@@ -1,0 +1,196 @@
+// Rotary positions of queries and keys, alone or behind the norm of each head's row.
+//
+// A pair (a, b) of a head's row at position p turns by p f: (a c - b s, a s + b c) with c, s = gain cos(p f), gain sin(p f).  Pairs are (i, i + S/2)
+// or (2i, 2i + 1) of a section of S elements; with two axes a head has two sections, each turned by a position of its own.  In front of it, RMS norm
+// x / sqrt(mean x^2 + eps) w or unit norm x / max(|x|, eps) w over the whole row.
+//
+// Memory-bound: a row is read and written once, whatever the strides it is read with.  A lane holds 16 elements of a row, two runs of eight chosen so
+// that its pairs are its own: no exchange but the sum of squares over the 8 (head_dim 128) or 4 lanes of a row.  Angles are formed
+// once for a token and used for all heads that the thread walks over.  They are exact where it matters: the frequency is held in units of 2^-64
+// turns, so the product with a position wraps to its fraction of a turn in integers, however far the position.
+#include "device_util.h"
+#include "ops_internal.h"
+
+namespace hack {
+
+namespace {
+
+using namespace dev;
+
+constexpr int kThreads = 256;
+constexpr int kMaxSteps = 8;
+constexpr int kWantGroups = 2048;   // work-groups that fill the chip: eight a compute unit
+
+// 2^32 u turns -> cosine and sine.  The nearest quarter turn, then the Taylor series of the rest (at most pi / 4: the first terms
+// left out are 2e-9 and 2e-11).
+__device__ __forceinline__ void cos_sin(unsigned u, float& c, float& s) {
+  const unsigned q = (u + 0x20000000u) >> 30;
+  const float x = (float)(int)(u - (q << 30)) * 1.4629180792671596e-9f;   // 2 pi 2^-32
+  const float y = x * x;
+  const float sx = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), x);
+  const float cx = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
+  const float a = (q & 1) ? sx : cx, b = (q & 1) ? cx : sx;
+  c = ((q + 1) & 2) ? -a : a;
+  s = (q & 2) ? -b : b;
+}
+
+template <typename T> struct Run;   // eight elements
+template <> struct Run<float> {
+  static __device__ __forceinline__ void load(const float* p, float* v) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float* v) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+};
+template <> struct Run<__bf16> {
+  static __device__ __forceinline__ void load(const __bf16* p, float* v) {
+    const bf16x8 x = *reinterpret_cast<const bf16x8*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
+  }
+  static __device__ __forceinline__ void store(__bf16* p, const float* v) {
+    bf16x8 x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (__bf16)v[i];
+    *reinterpret_cast<bf16x8*>(p) = x;
+  }
+};
+
+template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+
+template <typename T, int D, bool HALF, int NORM>
+__global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
+  constexpr int LPR = D / 16;             // lanes of a row
+  constexpr int SLOTS = kThreads / LPR;   // rows of a work-group at a time
+  const int j = threadIdx.x % LPR, slot = threadIdx.x / LPR;
+  unsigned x = blockIdx.x;
+  const int tile = x % (unsigned)a.tiles;
+  x /= (unsigned)a.tiles;
+  const unsigned chunks = a.t[0].chunks + a.t[1].chunks;
+  int chunk = x % chunks;
+  const int64_t b = x / chunks;
+  const bool second = chunk >= a.t[0].chunks;
+  if (second) chunk -= a.t[0].chunks;
+  const RotateTensor& t = a.t[second ? 1 : 0];
+  const int64_t n = (int64_t)(tile << a.tokens_log2) + (slot & ((1 << a.tokens_log2) - 1));
+  if (n >= a.n) return;   // all lanes of a row
+
+  // this lane's two runs of eight elements, and the first of its eight pairs
+  const bool turns = 16 * j < a.rot_dim;
+  int lo = 16 * j, hi = 16 * j + 8, axis = 0, pair = 8 * j;
+  if (turns) {
+    axis = 16 * j >= a.section ? 1 : 0;
+    if (HALF) {
+      lo = axis * a.section + (16 * j - axis * a.section) / 2;
+      hi = lo + a.section / 2;
+    }
+  }
+  float c[8], s[8];
+  if (turns) {
+    const int p = a.pos ? a.pos[b * a.pos_b + (int64_t)axis * a.n + n] : a.pos0 + (int)n;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint64_t f = a.turns[pair + i];
+      // upper half of the low 64 bits of p f; the low half of f makes up for p < 0 standing for p + 2^32
+      const unsigned u = __umulhi((unsigned)p, (unsigned)f) + (unsigned)p * (unsigned)(f >> 32) - (p < 0 ? (unsigned)f : 0u);
+      cos_sin(u, c[i], s[i]);
+      c[i] *= a.gain;
+      s[i] *= a.gain;
+    }
+  }
+  const T* src = static_cast<const T*>(t.x) + b * t.sb + n * t.sn;
+  T* dst = static_cast<T*>(t.out) + (b * t.heads * a.n + n) * D;
+  const int across = SLOTS >> a.tokens_log2;   // heads at a time
+  const int h0 = chunk * across * a.steps + (slot >> a.tokens_log2);
+  const int h1 = min(t.heads, (chunk + 1) * across * a.steps);
+  float w[16];
+  if (NORM != kNormNone && t.w != nullptr && t.w_stride == 0) {
+    Run<float>::load(t.w + lo, w);
+    Run<float>::load(t.w + hi, w + 8);
+  }
+  for (int h = h0; h < h1; h += across) {
+    float v[16];
+    Run<T>::load(src + h * t.sh + lo, v);
+    Run<T>::load(src + h * t.sh + hi, v + 8);
+    if (NORM != kNormNone) {
+      if (t.w != nullptr && t.w_stride != 0) {
+        Run<float>::load(t.w + (int64_t)h * t.w_stride + lo, w);
+        Run<float>::load(t.w + (int64_t)h * t.w_stride + hi, w + 8);
+      }
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ss = fmaf(v[i], v[i], ss);
+      ss = dpp_add<0xB1>(ss);    // lane ^ 1
+      ss = dpp_add<0x4E>(ss);    // lane ^ 2
+      if (LPR == 8) ss = dpp_add<0x141>(ss);   // mirrored within eight lanes
+      const float r = NORM == kNormRms ? 1.f / sqrtf(ss * (1.f / D) + a.eps) : 1.f / fmaxf(sqrtf(ss), a.eps);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        v[i] *= r;
+        if (t.w != nullptr) v[i] *= w[i];
+      }
+    }
+    if (turns) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int ia = HALF ? i : 2 * i, ib = HALF ? 8 + i : 2 * i + 1;
+        const float p = v[ia], q = v[ib];
+        v[ia] = fmaf(p, c[i], -(q * s[i]));
+        v[ib] = fmaf(p, s[i], q * c[i]);
+      }
+    }
+    T* o = dst + (int64_t)h * a.n * D;
+    Run<T>::store(o + lo, v);
+    Run<T>::store(o + hi, v + 8);
+  }
+}
+
+template <typename T, int D>
+void launch_typed(hipStream_t s, bool half_layout, int norm, unsigned groups, const RotateArgs& a) {
+#define HACK_ROTATE(HALF, NORM) hipLaunchKernelGGL((rotate_rows<T, D, HALF, NORM>), dim3(groups), dim3(kThreads), 0, s, a)
+  if (half_layout) {
+    if (norm == kNormNone) HACK_ROTATE(true, kNormNone);
+    else if (norm == kNormRms) HACK_ROTATE(true, kNormRms);
+    else HACK_ROTATE(true, kNormL2);
+  } else {
+    if (norm == kNormNone) HACK_ROTATE(false, kNormNone);
+    else if (norm == kNormRms) HACK_ROTATE(false, kNormRms);
+    else HACK_ROTATE(false, kNormL2);
+  }
+#undef HACK_ROTATE
+}
+
+}  // namespace
+
+void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout, int norm, int batch, int n_tensors, RotateArgs a) {
+  const int slots = kThreads / (head_dim / 16);
+  int log2 = 0;
+  while ((1 << log2) < slots && (1 << log2) < a.n) ++log2;
+  a.tokens_log2 = log2;
+  a.tiles = (a.n + (1 << log2) - 1) >> log2;
+  const int across = slots >> log2;
+  // A thread walks over as many heads as leave enough work-groups: it forms its angles once for all of them.
+  int64_t groups = 0;
+  for (a.steps = kMaxSteps;; a.steps /= 2) {
+    groups = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+      a.t[i].chunks = (a.t[i].heads + across * a.steps - 1) / (across * a.steps);
+      groups += (int64_t)a.t[i].chunks * a.tiles * batch;
+    }
+    if (a.steps == 1 || groups >= kWantGroups) break;
+  }
+  if (elem_bytes == 4) {
+    if (head_dim == 64) launch_typed<float, 64>(s, half_layout, norm, (unsigned)groups, a);
+    else launch_typed<float, 128>(s, half_layout, norm, (unsigned)groups, a);
+  } else {
+    if (head_dim == 64) launch_typed<__bf16, 64>(s, half_layout, norm, (unsigned)groups, a);
+    else launch_typed<__bf16, 128>(s, half_layout, norm, (unsigned)groups, a);
+  }
+}
+
+}  // namespace hack

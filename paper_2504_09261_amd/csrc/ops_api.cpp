@@ -1,0 +1,347 @@
+// Host side of the operators around the cache that include/hack.h declares: rotary positions and norms of queries and keys, rows
+// packed into 4 bits and read back, attention over them.  Arguments are checked here, launches take everything by value.
+#include <algorithm>
+#include <climits>
+#include <utility>
+#include <vector>
+
+#include "hack_ctx.h"
+#include "ops_internal.h"
+
+using namespace hack;
+
+namespace {
+
+// Kernels run on the device that is current when they are launched; the context's memory lies on its own.
+hack_status check_device(hack_ctx* ctx) {
+  int dev = -1;
+  HIP_TRY(ctx, hipGetDevice(&dev));
+  if (dev != ctx->cfg.device) return fail(ctx, HACK_EINVAL, "the current device is %d, the context's is %d", dev, ctx->cfg.device);
+  return HACK_OK;
+}
+
+// ---- rotary positions, norms ------------------------------------------------
+
+struct Range {   // bytes
+  uintptr_t lo, hi;
+  bool meets(const Range& o) const { return lo < o.hi && o.lo < hi; }
+};
+
+// Checks one operand and fills in its part of the launch.
+hack_status take_rows(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* r, const char* name, RotateTensor* t, Range* in, Range* out) {
+  if (!r) return fail(ctx, HACK_EINVAL, "%s is NULL", name);
+  if (!r->x || !r->out) return fail(ctx, HACK_EINVAL, "%s has a NULL member", name);
+  if (r->heads < 1) return fail(ctx, HACK_EINVAL, "%s heads must be >= 1 (got %d)", name, r->heads);
+  const int d = ctx->cfg.head_dim, e = ctx->elem_bytes, piece = 16 / e;
+  if (!aligned16(r->x) || !aligned16(r->out)) return fail(ctx, HACK_EINVAL, "%s x/out must be 16-byte aligned", name);
+  const int64_t strides[3] = {r->stride_b, r->stride_h, r->stride_n}, counts[3] = {B, r->heads, N};
+  int64_t span = d;   // elements from the first to behind the last
+  for (int i = 0; i < 3; ++i) {
+    if (strides[i] < 0 || strides[i] % piece != 0)
+      return fail(ctx, HACK_EINVAL, "%s strides must be non-negative multiples of 16 bytes (got %lld elements)", name, (long long)strides[i]);
+    if (strides[i] > (INT64_MAX >> 4) / counts[i]) return fail(ctx, HACK_EINVAL, "%s strides are too large", name);
+    span += strides[i] * (counts[i] - 1);
+  }
+  if (r->weight && ((uintptr_t)r->weight & 15)) return fail(ctx, HACK_EINVAL, "%s weight must be 16-byte aligned", name);
+  if (r->weight && r->weight_stride_h != 0 && (r->weight_stride_h < d || r->weight_stride_h % 4 != 0 || r->weight_stride_h > INT32_MAX))
+    return fail(ctx, HACK_EINVAL, "%s weight_stride_h must be 0 or a multiple of 4 from head_dim on (got %lld)", name, (long long)r->weight_stride_h);
+  t->x = r->x;
+  t->out = r->out;
+  t->w = r->weight;
+  t->w_stride = (int32_t)r->weight_stride_h;
+  t->sb = r->stride_b;
+  t->sh = r->stride_h;
+  t->sn = r->stride_n;
+  t->heads = r->heads;
+  const int64_t rows = (int64_t)B * r->heads * N;
+  if (rows > (int64_t)1 << 34) return fail(ctx, HACK_ECAPACITY, "%s has %lld rows, more than a launch takes", name, (long long)rows);
+  *in = Range{(uintptr_t)r->x, (uintptr_t)r->x + (uintptr_t)span * e};
+  *out = Range{(uintptr_t)r->out, (uintptr_t)r->out + (uintptr_t)(rows * d) * e};
+  return HACK_OK;
+}
+
+// Whether a thread that reads an element of x is the one that writes that place of out.
+bool in_place(const hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* r) {
+  const int64_t d = ctx->cfg.head_dim;
+  return r->x == r->out && (N == 1 || r->stride_n == d) && (r->heads == 1 || r->stride_h == d * N) && (B == 1 || r->stride_b == d * N * r->heads);
+}
+
+hack_status take_rope(hack_ctx* ctx, const hack_rope* rope, int32_t N, const int32_t* pos, int64_t pos_stride_b, int32_t pos0, RotateArgs* a) {
+  const int d = ctx->cfg.head_dim;
+  if (rope->layout != HACK_ROPE_HALF && rope->layout != HACK_ROPE_INTERLEAVED) return fail(ctx, HACK_EINVAL, "bad rope layout %d", rope->layout);
+  if (rope->axes != 1 && rope->axes != 2) return fail(ctx, HACK_EINVAL, "rope axes must be 1 or 2 (got %d)", rope->axes);
+  if (rope->rot_dim < 1 || rope->rot_dim > d) return fail(ctx, HACK_EINVAL, "rot_dim %d outside [1, head_dim]", rope->rot_dim);
+  if (rope->rot_dim % (16 * rope->axes) != 0) return fail(ctx, HACK_EUNSUPPORTED, "rot_dim %d is no multiple of 16 for each axis", rope->rot_dim);
+  if (!rope->freq) return fail(ctx, HACK_EINVAL, "rope freq is NULL");
+  if (!std::isfinite(rope->gain)) return fail(ctx, HACK_EINVAL, "rope gain must be finite");
+  if (!pos && rope->axes != 1) return fail(ctx, HACK_EINVAL, "two axes need positions");
+  if ((uintptr_t)pos & 3) return fail(ctx, HACK_EINVAL, "pos must be 4-byte aligned");
+  if (pos && pos_stride_b != 0 && pos_stride_b < (int64_t)rope->axes * N)
+    return fail(ctx, HACK_EINVAL, "pos_stride_b must be 0 or at least axes * N (got %lld)", (long long)pos_stride_b);
+  if (!pos && (int64_t)pos0 + N - 1 > INT32_MAX) return fail(ctx, HACK_EINVAL, "positions from %d on leave 32 bits", pos0);
+  for (int i = 0; i < rope->rot_dim / 2; ++i) {
+    if (!std::isfinite(rope->freq[i])) return fail(ctx, HACK_EINVAL, "freq[%d] is not finite", i);
+    // whole turns per position do not matter
+    long double t = (long double)rope->freq[i] / 6.283185307179586476925286766559L;
+    t -= floorl(t);
+    const long double high = floorl(t * 4294967296.0L);
+    a->turns[i] = ((uint64_t)high << 32) + (uint64_t)floorl((t * 4294967296.0L - high) * 4294967296.0L);
+  }
+  a->pos = pos;
+  a->pos_b = pos_stride_b;
+  a->pos0 = pos0;
+  a->rot_dim = rope->rot_dim;
+  a->section = rope->rot_dim / rope->axes;
+  a->gain = rope->gain;
+  return HACK_OK;
+}
+
+hack_status rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, int norm, float eps, const hack_rope* rope,
+                   const int32_t* pos, int64_t pos_stride_b, int32_t pos0, hack_stream stream) {
+  hack_status st = check_common(ctx, B, N, true);
+  if (st != HACK_OK) return st;
+  RotateArgs a{};
+  const int n = k ? 2 : 1;
+  const hack_rows* r[2] = {q, k};
+  Range in[2], out[2];
+  for (int i = 0; i < n; ++i)
+    if ((st = take_rows(ctx, B, N, r[i], i ? "k" : norm == kNormNone ? "x" : "q", &a.t[i], &in[i], &out[i])) != HACK_OK) return st;
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j)
+      if (out[i].meets(in[j]) && !(i == j && in_place(ctx, B, N, r[i])))
+        return fail(ctx, HACK_EINVAL, "outputs overlap rows that are read (in place: x in the layout of out, from the same address)");
+  if (n == 2 && out[0].meets(out[1])) return fail(ctx, HACK_EINVAL, "the outputs overlap each other");
+  a.n = N;
+  a.eps = eps;
+  if (rope && (st = take_rope(ctx, rope, N, pos, pos_stride_b, pos0, &a)) != HACK_OK) return st;
+  if ((st = check_device(ctx)) != HACK_OK) return st;
+  launch_rotate(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, !rope || rope->layout == HACK_ROPE_HALF, norm, B, n, a);
+  HIP_TRY(ctx, hipGetLastError());
+  return HACK_OK;
+}
+
+// ---- packed cache -----------------------------------------------------------
+
+hack_status check_packed(hack_ctx* ctx, const hack_packed_cache* c, int n_units, const char* name) {
+  if (!c) return fail(ctx, HACK_EINVAL, "%s is NULL", name);
+  if (!c->k || !c->v || !c->off || !c->len) return fail(ctx, HACK_EINVAL, "%s has a NULL member", name);
+  if (!aligned16(c->k) || !aligned16(c->v) || ((uintptr_t)c->pos & 3)) return fail(ctx, HACK_EINVAL, "%s k/v must be 16-byte, pos 4-byte aligned", name);
+  if (c->rows < 0 || c->rows % kPackRows != 0) return fail(ctx, HACK_EINVAL, "%s rows must be a non-negative multiple of %d", name, kPackRows);
+  if (c->rows / kPackRows > INT32_MAX) return fail(ctx, HACK_ECAPACITY, "%s has more than 2^31 blocks of %d rows", name, kPackRows);
+  for (int u = 0; u < n_units; ++u)
+    if (c->len[u] < 0 || c->off[u] < 0 || c->off[u] % kPackRows != 0 || c->off[u] > c->rows || c->len[u] > c->rows - c->off[u])
+      return fail(ctx, HACK_EINVAL, "%s unit %d: off %lld len %d outside [0, %lld) or off not a multiple of %d", name, u, (long long)c->off[u],
+                  c->len[u], (long long)c->rows, kPackRows);
+  return HACK_OK;
+}
+
+// Whether two units' rows [off + first, off + len), rounded out to `step`, share any.
+template <typename Lo, typename Hi>
+bool units_overlap(int n_units, Lo lo, Hi hi) {
+  bool sorted = true;
+  int64_t end = INT64_MIN;
+  for (int u = 0; u < n_units && sorted; ++u) {
+    if (hi(u) <= lo(u)) continue;
+    sorted = lo(u) >= end;
+    end = hi(u);
+  }
+  if (sorted) return false;
+  std::vector<std::pair<int64_t, int64_t>> r;
+  for (int u = 0; u < n_units; ++u)
+    if (hi(u) > lo(u)) r.emplace_back(lo(u), hi(u));
+  std::sort(r.begin(), r.end());
+  for (size_t i = 1; i < r.size(); ++i)
+    if (r[i].first < r[i - 1].second) return true;
+  return false;
+}
+
+template <typename Launch>
+void launch_units(const std::vector<PackUnit>& units, PackArgs* a, Launch launch) {
+  for (size_t u0 = 0; u0 < units.size(); u0 += kPackUnits) {
+    a->unit0 = (int32_t)u0;
+    a->n_units = (int32_t)std::min<size_t>(kPackUnits, units.size() - u0);
+    int rows = 0;
+    for (int i = 0; i < a->n_units; ++i) {
+      a->unit[i] = units[u0 + i];
+      rows = std::max(rows, a->unit[i].n);
+    }
+    if (rows > 0) launch(rows);
+  }
+}
+
+}  // namespace
+
+extern "C" hack_status hack_rope_freqs(int32_t rot_dim, int32_t axes, int32_t scaling, double base, double factor, double trained_len, double* freq,
+                                       float* gain) {
+  if (!freq || (axes != 1 && axes != 2) || rot_dim < 2 || rot_dim > 2 * kMaxPairs || rot_dim % (2 * axes) != 0) return HACK_EINVAL;
+  if (!std::isfinite(base) || base <= 1.0 || !std::isfinite(factor) || factor < 1.0) return HACK_EINVAL;
+  if (scaling < HACK_ROPE_PLAIN || scaling > HACK_ROPE_PARTS) return HACK_EINVAL;
+  if (scaling == HACK_ROPE_PARTS && (!std::isfinite(trained_len) || trained_len < 1.0)) return HACK_EINVAL;
+  const int size = rot_dim / axes, n = size / 2;
+  double g = 1.0;
+  if (scaling == HACK_ROPE_BASE && size > 2) base *= std::pow(factor, (double)size / (size - 2));
+  double low = 0.0, high = 0.0;
+  if (scaling == HACK_ROPE_PARTS) {
+    // pair that makes `turns` turns over the length trained on
+    const auto at = [&](double turns) { return size * std::log(trained_len / (turns * 6.283185307179586)) / (2.0 * std::log(base)); };
+    low = std::max(std::floor(at(32.0)), 0.0);
+    high = std::min(std::ceil(at(1.0)), size - 1.0);
+    g = 0.1 * std::log(factor) + 1.0;
+  }
+  for (int i = 0; i < n; ++i) {
+    double f = std::pow(base, -2.0 * i / size);
+    if (scaling == HACK_ROPE_LINEAR) f /= factor;
+    if (scaling == HACK_ROPE_PARTS) {
+      const double ramp = std::min(std::max((i - low) / std::max(high - low, 0.001), 0.0), 1.0);
+      f = f * (1.0 - ramp) + f / factor * ramp;
+    }
+    for (int a = 0; a < axes; ++a) freq[a * n + i] = f;
+  }
+  if (gain) *gain = (float)g;
+  return HACK_OK;
+}
+
+extern "C" hack_status hack_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* x, const hack_rope* rope, const int32_t* pos,
+                                   int64_t pos_stride_b, int32_t pos0, hack_stream stream) {
+  if (!ctx) return HACK_EINVAL;
+  if (!rope) return fail(ctx, HACK_EINVAL, "rope is NULL");
+  if (x && x->weight) return fail(ctx, HACK_EINVAL, "a rotation without a norm takes no weight");
+  return rotate(ctx, B, N, x, nullptr, kNormNone, 0.f, rope, pos, pos_stride_b, pos0, stream);
+}
+
+extern "C" hack_status hack_norm_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, int32_t norm, float eps,
+                                        const hack_rope* rope, const int32_t* pos, int64_t pos_stride_b, int32_t pos0, hack_stream stream) {
+  if (!ctx) return HACK_EINVAL;
+  if (norm != HACK_NORM_RMS && norm != HACK_NORM_UNIT) return fail(ctx, HACK_EINVAL, "bad norm %d", norm);
+  if (!std::isfinite(eps) || eps <= 0.f) return fail(ctx, HACK_EINVAL, "eps must be finite and > 0");
+  return rotate(ctx, B, N, q, k, norm == HACK_NORM_RMS ? kNormRms : kNormL2, eps, rope, pos, pos_stride_b, pos0, stream);
+}
+
+extern "C" hack_status hack_packed_bytes(int32_t head_dim, int64_t rows, int64_t* bytes) {
+  if (!bytes || (head_dim != 64 && head_dim != 128) || rows < 0 || rows > ((int64_t)INT32_MAX) * kPackRows) return HACK_EINVAL;
+  *bytes = (rows + kPackRows - 1) / kPackRows * packed_block_bytes(head_dim);
+  return HACK_OK;
+}
+
+extern "C" hack_status hack_pack(hack_ctx* ctx, int32_t B, int32_t N_k, const hack_cache* in, const void* k_new, const void* v_new, int32_t pos_new,
+                                 const int32_t* kept_idx, int64_t idx_stride, const int32_t* first, const hack_packed_cache* out,
+                                 hack_stream stream) try {
+  const bool has_new = k_new != nullptr;
+  hack_status st = check_common(ctx, B, N_k, has_new);
+  if (st != HACK_OK) return st;
+  const int U = B * ctx->cfg.heads;
+  if (has_new != (v_new != nullptr)) return fail(ctx, HACK_EINVAL, "k_new and v_new must both be given or both be NULL");
+  if (!has_new && !in) return fail(ctx, HACK_EINVAL, "neither cached nor new rows are given");
+  if (has_new && (!aligned16(k_new) || !aligned16(v_new))) return fail(ctx, HACK_EINVAL, "k_new/v_new must be 16-byte aligned");
+  if ((uintptr_t)kept_idx & 3) return fail(ctx, HACK_EINVAL, "kept_idx must be 4-byte aligned");
+  if (in && (st = check_cache(ctx, in, U, "in", true)) != HACK_OK) return st;
+  if ((st = check_packed(ctx, out, U, "out")) != HACK_OK) return st;
+  const int n_new = has_new ? N_k : 0;
+  std::vector<PackUnit> units(U);
+  bool any = false;
+  for (int u = 0; u < U; ++u) {
+    const int at = first ? first[u] : 0, there = in ? in->len[u] : 0;
+    if (at < 0 || at > out->len[u]) return fail(ctx, HACK_EINVAL, "first[%d] = %d outside [0, out->len = %d]", u, at, out->len[u]);
+    const int n = out->len[u] - at;
+    if (n > (int64_t)there + n_new) return fail(ctx, HACK_EINVAL, "unit %d takes %d rows of %lld", u, n, (long long)there + n_new);
+    if (kept_idx && n > idx_stride) return fail(ctx, HACK_ECAPACITY, "idx_stride %lld < the %d rows of unit %d", (long long)idx_stride, n, u);
+    if ((int64_t)there + n_new > INT32_MAX) return fail(ctx, HACK_ECAPACITY, "unit %d has more than 2^31 rows", u);
+    units[u] = PackUnit{in ? in->off[u] : 0, there, (int32_t)(out->off[u] / kPackRows), at, n};
+    any |= n > 0;
+  }
+  if (!any) return HACK_OK;
+  if (units_overlap(U, [&](int u) { return out->off[u] + units[u].first; }, [&](int u) { return out->off[u] + out->len[u]; }))
+    return fail(ctx, HACK_EINVAL, "units of out overlap");
+  if ((st = check_device(ctx)) != HACK_OK) return st;
+  PackArgs a{};
+  if (in) a.plain = CachePtrs{in->k, in->v, in->pos};
+  a.packed = CachePtrs{out->k, out->v, out->pos};
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.kept = kept_idx;
+  a.kept_stride = idx_stride;
+  a.n_new = n_new;
+  a.pos_new = pos_new;
+  launch_units(units, &a, [&](int rows) { launch_pack(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, rows, a); });
+  HIP_TRY(ctx, hipGetLastError());
+  return HACK_OK;
+} HACK_NO_THROW(ctx)
+
+extern "C" hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_cache* in, const int32_t* first, const hack_cache* out,
+                                   hack_stream stream) try {
+  hack_status st = check_common(ctx, B, 0, false);
+  if (st != HACK_OK) return st;
+  const int U = B * ctx->cfg.heads;
+  if ((st = check_packed(ctx, in, U, "in")) != HACK_OK) return st;
+  if ((st = check_cache(ctx, out, U, "out", true)) != HACK_OK) return st;
+  std::vector<PackUnit> units(U);
+  bool any = false;
+  for (int u = 0; u < U; ++u) {
+    const int at = first ? first[u] : 0;
+    if (at < 0 || at > in->len[u] || out->len[u] > in->len[u] - at)
+      return fail(ctx, HACK_EINVAL, "unit %d: rows %d to %lld of %d", u, at, (long long)at + out->len[u], in->len[u]);
+    units[u] = PackUnit{out->off[u], 0, (int32_t)(in->off[u] / kPackRows), at, out->len[u]};
+    any |= out->len[u] > 0;
+  }
+  if (!any) return HACK_OK;
+  if (units_overlap(U, [&](int u) { return out->off[u]; }, [&](int u) { return out->off[u] + out->len[u]; }))
+    return fail(ctx, HACK_EINVAL, "units of out overlap");
+  if ((st = check_device(ctx)) != HACK_OK) return st;
+  PackArgs a{};
+  a.plain = CachePtrs{out->k, out->v, out->pos};
+  a.packed = CachePtrs{in->k, in->v, in->pos};
+  launch_units(units, &a, [&](int rows) { launch_unpack(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, rows, a); });
+  HIP_TRY(ctx, hipGetLastError());
+  return HACK_OK;
+} HACK_NO_THROW(ctx)
+
+extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, const void* q, const hack_packed_cache* kv, float scale, void* out,
+                                        hack_stream stream) try {
+  hack_status st = check_common(ctx, B, N_k, true);
+  if (st != HACK_OK) return st;
+  if (ctx->cfg.dtype != HACK_BF16) return fail(ctx, HACK_EUNSUPPORTED, "attention over a packed cache is implemented for bf16 contexts");
+  const int U = B * ctx->cfg.heads, d = ctx->cfg.head_dim;
+  if (!q || !out) return fail(ctx, HACK_EINVAL, "q and out must not be NULL");
+  if (!aligned16(q) || !aligned16(out)) return fail(ctx, HACK_EINVAL, "q/out must be 16-byte aligned");
+  if (!scale_ok(scale)) return fail(ctx, HACK_EINVAL, "scale must be finite and > 0");
+  if ((st = check_packed(ctx, kv, U, "kv")) != HACK_OK) return st;
+  for (int u = 0; u < U; ++u)
+    if (kv->len[u] < 1) return fail(ctx, HACK_EINVAL, "unit %d has an empty cache", u);
+  const int64_t bytes = (int64_t)U * N_k * d * 2;
+  const Range rq{(uintptr_t)q, (uintptr_t)q + (uintptr_t)bytes}, ro{(uintptr_t)out, (uintptr_t)out + (uintptr_t)bytes};
+  if (rq.meets(ro)) return fail(ctx, HACK_EINVAL, "q and out overlap");
+  if ((st = check_device(ctx)) != HACK_OK) return st;
+  AttnPackedArgs a{};
+  a.k = static_cast<const uint8_t*>(kv->k);
+  a.v = static_cast<const uint8_t*>(kv->v);
+  a.part_o = ctx->part_o;
+  a.part_ml = ctx->part_ml;
+  a.q = q;
+  a.out = out;
+  a.N_k = N_k;
+  a.scale = scale;
+  const int queries = N_k <= 16 ? 16 : 32;
+  a.q_tiles = (N_k + queries - 1) / queries;
+  const int64_t slots = 2 * (int64_t)std::max(ctx->attn_slots, 1) * 128 / queries;   // partial results that the workspace holds
+  for (int u0 = 0; u0 < U; u0 += kAttnPackedUnits) {
+    a.unit0 = u0;
+    a.n_units = std::min(kAttnPackedUnits, U - u0);
+    int64_t blocks = 0;
+    int longest = 0;
+    for (int i = 0; i < a.n_units; ++i) {
+      a.unit[i] = AttnPackedUnit{(int32_t)(kv->off[u0 + i] / kPackRows), kv->len[u0 + i]};
+      const int n = (kv->len[u0 + i] + kPackRows - 1) / kPackRows;
+      blocks += (int64_t)n * a.q_tiles;
+      longest = std::max(longest, n);
+    }
+    // chunks of the work that fill the chip four times over, of at least eight blocks, no more than the workspace holds
+    int64_t chunk = std::max<int64_t>(8, (blocks + 4 * ctx->cus - 1) / (4 * ctx->cus));
+    const int64_t most = std::max<int64_t>(1, slots / ((int64_t)a.n_units * a.q_tiles));
+    chunk = std::max<int64_t>(chunk, (longest + most - 1) / most);
+    a.chunk = (int32_t)std::min<int64_t>(chunk, longest);
+    a.n_chunks = (longest + a.chunk - 1) / a.chunk;
+    launch_attn_packed(static_cast<hipStream_t>(stream), d, queries, a);
+  }
+  HIP_TRY(ctx, hipGetLastError());
+  return HACK_OK;
+} HACK_NO_THROW(ctx)

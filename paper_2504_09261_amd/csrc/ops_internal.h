@@ -1,0 +1,99 @@
+// Internal declarations of the operators around the cache: rotary positions, norms of queries and keys, the cache packed
+// into 4 bits and attention over it (ops_api.cpp and the kernels behind it).  Nothing here is part of the C ABI.
+// Everything a launch needs travels by value: lengths that grow by a token a call would fill a store of launch tables.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "hack_internal.h"
+
+namespace hack {
+
+// ---- rotary positions, norms ------------------------------------------------
+constexpr int kMaxPairs = 64;   // rotating pairs of a head
+enum : int32_t { kNormNone = 0, kNormRms = 1, kNormL2 = 2 };
+
+struct RotateTensor {
+  const void* x;        // element (b, h, n, i) at b sb + h sh + n sn + i
+  void* out;            // [B, heads, N, head_dim]
+  const float* w;       // weight of element i of head h at h w_stride + i, NULL: ones
+  int64_t sb, sh, sn;
+  int32_t heads;
+  int32_t w_stride;
+  int32_t chunks;       // work-groups that share a tile's heads
+  int32_t pad;
+};
+struct RotateArgs {
+  RotateTensor t[2];
+  const int32_t* pos;   // position of row n of batch element b on axis a at b pos_b + a N + n, NULL: pos0 + n
+  int64_t pos_b;
+  int32_t pos0;
+  int32_t n;            // N
+  int32_t rot_dim;      // rotating elements of a head, 0: none
+  int32_t section;      // of an axis
+  float gain, eps;
+  // launch shape, set by launch_rotate
+  int32_t tokens_log2;  // rows of one head a work-group takes (power of two)
+  int32_t tiles;        // of rows
+  int32_t steps;        // heads a thread takes, one after the other
+  int32_t pad;
+  uint64_t turns[kMaxPairs];   // of a pair per position, in units of 2^-64 of a turn
+};
+void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout, int norm, int batch, int n_tensors, RotateArgs a);
+
+// ---- rows in 4 bits ---------------------------------------------------------
+constexpr int kPackRows = 64;    // rows of a block
+constexpr int kPackGroup = 32;   // elements of a row that share a scale
+inline int packed_block_bytes(int head_dim) { return kPackRows * (head_dim / 2 + head_dim / kPackGroup); }
+constexpr int kPackUnits = 96;   // units of a launch
+struct PackUnit {
+  int64_t row0;     // first row in the arrays of plain rows
+  int32_t len_in;   // pack: cached rows there, which the new ones follow
+  int32_t block;    // first block in the packed arrays
+  int32_t first;    // row of the unit there
+  int32_t n;        // rows
+};
+struct PackArgs {
+  CachePtrs plain;       // rows read (pack) or written (unpack)
+  CachePtrs packed;
+  const void* k_new;
+  const void* v_new;
+  const int32_t* kept;   // [unit, kept_stride], NULL: all rows in order
+  int64_t kept_stride;
+  int32_t n_new;         // rows of k_new / v_new of a unit
+  int32_t pos_new;
+  int32_t unit0;         // of the launch
+  int32_t n_units;
+  PackUnit unit[kPackUnits];
+};
+void launch_pack(hipStream_t s, int elem_bytes, int head_dim, int max_rows, const PackArgs& a);
+void launch_unpack(hipStream_t s, int elem_bytes, int head_dim, int max_rows, const PackArgs& a);
+
+// ---- attention over them (bf16 queries and outputs) -------------------------
+constexpr int kAttnPackedUnits = 384;   // units of a launch
+struct AttnPackedUnit {
+  int32_t block;   // first block
+  int32_t len;     // rows
+};
+struct AttnPackedArgs {
+  const uint8_t* k;
+  const uint8_t* v;
+  const void* q;      // bf16
+  void* out;
+  float* part_o;      // [slot, queries of a work-group, head_dim] unnormalised partial outputs
+  float* part_ml;     // [slot, queries of a work-group, 2] their references and normalisers
+  int32_t N_k;
+  float scale;
+  int32_t unit0;      // of the launch
+  int32_t n_units;
+  int32_t q_tiles;    // of a unit's queries
+  int32_t n_chunks;   // most chunks that a unit's keys are cut into
+  int32_t chunk;      // blocks of kPackRows keys of one
+  int32_t pad;
+  AttnPackedUnit unit[kAttnPackedUnits];
+};
+// queries: of a work-group, 16 or 32
+void launch_attn_packed(hipStream_t s, int head_dim, int queries, const AttnPackedArgs& a);
+
+}  // namespace hack
