@@ -10,6 +10,7 @@
 // probabilities and the PV product of 32 keys are those of SplitStage.  The partial results of the waves are merged through LDS, those of several chunks
 // of a unit in memory, by a launch of their own.
 #include <cfloat>
+#include <type_traits>
 
 #include "packed_device.h"
 #include "split_stage.h"
@@ -36,9 +37,23 @@ template <int D> struct PackedRows {   // a lane's share of a block of 64 rows
   __device__ __forceinline__ float scale(int t) const { return scale_of((exponents >> (8 * t)) & 255u); }
 };
 
-template <int D, int NQ>
-__global__ __launch_bounds__(64 * kWaves, 2) void attn_packed(const AttnPackedArgs a) {
-  constexpr int KC = D / 32, MT = D / 16, CPR = D / 8, QROWS = 16 * NQ;
+template <int N> struct AttnPackedArgs : AttnPackedHead { AttnPackedUnit unit[N]; };
+
+// Blocks [lo, hi) of chunk c of a unit of n blocks: as even as they can be.
+__device__ __forceinline__ int chunks_of(int n, int most) { return (n + most - 1) / most; }
+__device__ __forceinline__ int chunk_at(int n, int chunks, int c) { return (int)((unsigned)n / chunks * c + ((unsigned)n % chunks) * c / chunks); }
+
+// LDS layout of converted rows of V: groups of four, a group's 64-byte pieces row after row, the 16-byte chunks of a piece permuted by the group.
+// All operands of the PV product stand at constant distances from two addresses, a lane's share of a row at constant distances from two others, and
+// neither the writes (16 rows, one chunk) nor the transposing reads (8 rows, 32 bytes) meet a bank twice.
+__device__ __forceinline__ int v_flip(int row) { return 2 * ((row >> 2) & 1) | ((row >> 3) & 1); }
+template <int D> __device__ __forceinline__ int v_chunk(int row, int chunk) {   // element offset of a chunk
+  return (row >> 2) * 4 * D + (chunk >> 2) * 128 + (row & 3) * 32 + ((chunk & 3) ^ v_flip(row)) * 8;
+}
+
+template <int D, int NQ, int N>
+__global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void attn_packed(const AttnPackedArgs<N> a) {
+  constexpr int KC = D / 32, MT = D / 16, QROWS = 16 * NQ;
   constexpr int SLOT = (NQ == 2 ? 64 : 32) * D;   // elements: 32 rows of V, then the wave's partial results
   // The query tiles of a unit and a chunk follow each other on an XCD (work-group id mod 8).
   const int local = blockIdx.x >> 3, pair = (local / a.q_tiles) * 8 + (blockIdx.x & 7), q_tile = local % a.q_tiles;
@@ -46,25 +61,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_packed(const AttnPackedAr
   const int ui = pair % a.n_units, chunk = pair / a.n_units;
   const AttnPackedUnit u = a.unit[ui];
   const int len = u.len, n_blocks = (len + kPackRows - 1) / kPackRows;
-  const int first = chunk * a.chunk;
-  if (first >= n_blocks) return;
-  const int last = min(first + a.chunk, n_blocks);
+  const int chunks = chunks_of(n_blocks, a.chunk);
+  if (chunk >= chunks) return;
+  const int first = chunk_at(n_blocks, chunks, chunk), last = chunk_at(n_blocks, chunks, chunk + 1);
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int q0 = q_tile * QROWS;
-  const int64_t row0 = (int64_t)(a.unit0 + ui) * a.N_k;
+  const int64_t row0 = (int64_t)u.unit * a.N_k;
 
   __shared__ __attribute__((aligned(1024))) __bf16 ring[kWaves][SLOT];
   __shared__ float m_sh[kWaves][QROWS], l_sh[kWaves][QROWS];
 
-  const uint8_t* const kb = a.k + (int64_t)u.block * kPackBytes<D>;
-  const uint8_t* const vb = a.v + (int64_t)u.block * kPackBytes<D>;
-  PackedRows<D> kr, vr;
+  // This wave's blocks: first + w, first + w + kWaves, ...  A block's K is needed until its scores are formed, its V until it lies in LDS: the
+  // next ones are loaded into the same registers then and have the rest of the iteration to arrive.
   int b = first + w;
+  const uint8_t* kb = a.k + ((int64_t)u.block + b) * kPackBytes<D>;
+  const uint8_t* vb = a.v + ((int64_t)u.block + b) * kPackBytes<D>;
+  PackedRows<D> kr, vr;
   if (b < last) {
-    kr.load(kb + (int64_t)b * kPackBytes<D>, lane);
-    vr.load(vb + (int64_t)b * kPackBytes<D>, lane);
+    kr.load(kb, lane);
+    vr.load(vb, lane);
   }
   // Queries as the B operand, in the order in which the lane's quarter of a key comes: element 8 s + j of quarter g
   bf16x8 qf[NQ][KC];
@@ -76,52 +93,108 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_packed(const AttnPackedAr
   }
   SplitStage<D, NQ> att;
   att.init(a.scale, lane);
+  // V^T operand: rows 4 g + e and 16 + 4 g + e, head-dim 16 mt + 4 qd; even and odd mt
+  const int qd = col & 3, v_even = v_chunk<D>(4 * g + (col >> 2), qd >> 1) + 4 * (qd & 1), v_odd = v_even ^ 16;
   __bf16* const slot = &ring[w][0];
 
-  for (; b < last; b += kWaves) {
-    const PackedRows<D> kc = kr, vc = vr;
-    if (b + kWaves < last) {
-      kr.load(kb + (int64_t)(b + kWaves) * kPackBytes<D>, lane);
-      vr.load(vb + (int64_t)(b + kWaves) * kPackBytes<D>, lane);
-    }
+  // RAGGED: rows of this block lie behind the unit's last one.  They may hold anything: their scores are masked, and as their probabilities are
+  // zero, V is zero there too, since the product must not meet a NaN.
+  auto block = [&](auto ragged_tag) {
+    constexpr bool RAGGED = decltype(ragged_tag)::value;
+    const bool more = b + kWaves < last;
+    floatx4 sc[4][NQ];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {   // 32 keys
-      if (b * kPackRows + 32 * h >= len) break;
-      floatx4 sc[2][NQ];
+    for (int t = 0; t < 4; ++t) {
+      const float scale = kr.scale(t);
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const float scale = kc.scale(2 * h + kt);
+      for (int qt = 0; qt < NQ; ++qt) sc[t][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) sc[kt][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < KC; ++s) {
+        const bf16x8 kf = codes_bf16(kr.slice(t, s), scale);
 #pragma unroll
-        for (int s = 0; s < KC; ++s) {
-          const bf16x8 kf = codes_bf16(kc.slice(2 * h + kt, s), scale);
-#pragma unroll
-          for (int qt = 0; qt < NQ; ++qt) sc[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qt][s], sc[kt][qt], 0, 0, 0);
-        }
+        for (int qt = 0; qt < NQ; ++qt) sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qt][s], sc[t][qt], 0, 0, 0);
       }
-      att.mask(sc, 2 * b + h, len);
+    }
+    const int left = len - b * kPackRows;   // rows of this block and behind it
+    auto v_rows = [&](int h) {   // rows 32 h ... of V, as bf16
       wave_lds_order();   // the last reads of the slot
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
-        const int r = 16 * kt + col;
-        // What lies behind the last row may be anything, and its probability is zero: the product must not meet a NaN there.
-        const bool there = b * kPackRows + 32 * h + r < len;
-        const float scale = there ? vc.scale(2 * h + kt) : 1.f;
+        const int t = 2 * h + kt, r = 16 * kt + col;
+        const bool there = !RAGGED || 32 * h + r < left;
+        const float scale = there ? vr.scale(t) : 1.f;
 #pragma unroll
         for (int s = 0; s < KC; ++s)
-          *reinterpret_cast<bf16x8*>(&slot[r * D + (((KC * g + s) ^ swz_v16<D>(r)) & (CPR - 1)) * 8]) =
-              codes_bf16(there ? vc.slice(2 * h + kt, s) : 0u, scale);
+          *reinterpret_cast<bf16x8*>(&slot[v_chunk<D>(r, KC * g + s)]) = codes_bf16(there ? vr.slice(t, s) : 0u, scale);
+      }
+      wave_lds_order();
+    };
+    v_rows(0);
+    if constexpr (RAGGED) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (16 * t + 4 * g + r >= left) {
+#pragma unroll
+            for (int qt = 0; qt < NQ; ++qt) sc[t][qt][r] = -INFINITY;
+          }
+    }
+    // The reference is the largest score so far (see SplitStage::follow).
+    float m_new[NQ];
+    bool moved = false;
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) {
+      float mx = sc[0][qt][0];
+#pragma unroll
+      for (int j = 1; j < 16; ++j) mx = maximum(mx, sc[j >> 2][qt][j & 3]);
+      m_new[qt] = maximum(att.mc[qt], quad_maximum(mx) * att.c2);
+      moved |= m_new[qt] != att.mc[qt];
+    }
+    if (__any(moved)) {
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+        const float f = __builtin_amdgcn_exp2f(att.mc[qt] - m_new[qt]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          att.ls[qt][r] *= f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) att.o[mt][qt][r] *= f;
+        }
+        att.mc[qt] = m_new[qt];
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (h == 1) {
+        if (RAGGED && left <= 32) break;
+        v_rows(1);
+        vb += kWaves * kPackBytes<D>;
+        if (more) vr.load(vb, lane);
       }
       bf16x8 pf[NQ];
-      att.follow(sc, b == first + w && h == 0);
-      att.probs(sc, pf);
-      wave_lds_order();
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pf[qt][j] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[2 * h + (j >> 2)][qt][j & 3], att.c2, -att.mc[qt]));
+      if (h == 0) {
+        kb += kWaves * kPackBytes<D>;
+        if (more) kr.load(kb, lane);
+      }
       att.row_sums(pf);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) att.pv(slot, pf, mt);
+      for (int mt = 0; mt < MT; ++mt) {
+        const __bf16* const at = slot + 128 * (mt >> 1) + (mt & 1 ? v_odd : v_even);
+        const bf16x4 v0 = lds_read_tr(at), v1 = lds_read_tr(at + 16 * D);
+        const bf16x8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) att.o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], att.o[mt][qt], 0, 0, 0);
+      }
     }
-  }
+  };
+  const int full = min(last, len / kPackRows);
+  for (; b < full; b += kWaves) block(std::false_type{});
+  if (b < last) block(std::true_type{});
 
   // ---- merge the waves' partial results ----
   constexpr int kPart = SLOT * 2 / 16;   // float4 per wave
@@ -151,7 +224,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_packed(const AttnPackedAr
     f[x] = __builtin_amdgcn_exp2f(m_sh[x][16 * qt + col] - M);   // a wave without blocks has summed nothing
     L = fmaf(f[x], l_sh[x][16 * qt + col], L);
   }
-  const bool whole = n_blocks <= a.chunk;
+  const bool whole = chunks == 1;
   const float inv = whole ? 1.f / L : 1.f;
   const int qi = q0 + 16 * qt + col;
   const int64_t part = (((int64_t)ui * a.q_tiles + q_tile) * a.n_chunks + chunk) * QROWS + 16 * qt + col;
@@ -180,32 +253,50 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_packed(const AttnPackedAr
 }
 
 // Rows of units that were cut: a work-group takes one query, D / 4 lanes a chunk.
-template <int D>
-__global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs a, int q_rows) {
+constexpr int kFactors = 1024;   // chunks whose factors are kept in LDS at a time
+template <int D, int N>
+__global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N> a, int q_rows) {
   constexpr int LPR = D / 4, SIDE = 256 / LPR;   // chunks at a time
-  const int ui = blockIdx.y, n_blocks = (a.unit[ui].len + kPackRows - 1) / kPackRows;
-  if (n_blocks <= a.chunk) return;
-  const int n = (n_blocks + a.chunk - 1) / a.chunk;
-  const int qi = blockIdx.x, c0 = threadIdx.x / LPR, lane = threadIdx.x % LPR;
+  const int ui = blockIdx.y, n = chunks_of((a.unit[ui].len + kPackRows - 1) / kPackRows, a.chunk);
+  if (n == 1) return;
+  const int tid = threadIdx.x, qi = blockIdx.x, c0 = tid / LPR, lane = tid % LPR;
   const int64_t part0 = ((int64_t)ui * a.q_tiles + qi / q_rows) * a.n_chunks * q_rows + qi % q_rows;
+  const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + part0;
+  const float4* const po = reinterpret_cast<const float4*>(a.part_o + part0 * D) + lane;
   __shared__ float4 o_sh[SIDE][LPR];
-  __shared__ float l_sh[SIDE];
-  float M = -FLT_MAX;
-  for (int c = 0; c < n; ++c) M = fmaxf(M, a.part_ml[2 * (part0 + (int64_t)c * q_rows)]);
+  __shared__ float f_sh[kFactors], m_sh[4], l_sh[4];
+  float M = -FLT_MAX, L = 0.f;
+  for (int c = tid; c < n; c += 256) M = fmaxf(M, ml[(int64_t)c * q_rows].x);
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x, 64));
+  if ((tid & 63) == 0) m_sh[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(m_sh[0], m_sh[1]), fmaxf(m_sh[2], m_sh[3]));
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float L = 0.f;
-  for (int c = c0; c < n; c += SIDE) {
-    const int64_t p = part0 + (int64_t)c * q_rows;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - M);
-    const float4 x = reinterpret_cast<const float4*>(a.part_o + p * D)[lane];
-    L = fmaf(f, a.part_ml[2 * p + 1], L);
-    o.x = fmaf(f, x.x, o.x);
-    o.y = fmaf(f, x.y, o.y);
-    o.z = fmaf(f, x.z, o.z);
-    o.w = fmaf(f, x.w, o.w);
+  for (int base = 0; base < n; base += kFactors) {
+    const int here = min(kFactors, n - base);
+    __syncthreads();   // the last ones have been used
+    for (int c = tid; c < here; c += 256) {
+      const float2 x = ml[(int64_t)(base + c) * q_rows];
+      const float f = __builtin_amdgcn_exp2f(x.x - M);
+      f_sh[c] = f;
+      L = fmaf(f, x.y, L);
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int c = c0; c < here; c += SIDE) {
+      const float f = f_sh[c];
+      const float4 x = po[(int64_t)(base + c) * q_rows * LPR];
+      o.x = fmaf(f, x.x, o.x);
+      o.y = fmaf(f, x.y, o.y);
+      o.z = fmaf(f, x.z, o.z);
+      o.w = fmaf(f, x.w, o.w);
+    }
   }
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) L += __shfl_xor(L, x, 64);
+  if ((tid & 63) == 0) l_sh[tid >> 6] = L;
   o_sh[c0][lane] = o;
-  if (lane == 0) l_sh[c0] = L;
   __syncthreads();
   if (c0 != 0) return;
 #pragma unroll
@@ -215,27 +306,32 @@ __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs a,
     o.y += p.y;
     o.z += p.z;
     o.w += p.w;
-    L += l_sh[x];
   }
-  const float inv = 1.f / L;
-  __bf16* row = static_cast<__bf16*>(a.out) + ((int64_t)(a.unit0 + ui) * a.N_k + qi) * D;
+  const float inv = 1.f / (l_sh[0] + l_sh[1] + l_sh[2] + l_sh[3]);
+  __bf16* row = static_cast<__bf16*>(a.out) + ((int64_t)a.unit[ui].unit * a.N_k + qi) * D;
   *reinterpret_cast<bf16x4*>(row + 4 * lane) = bf16x4{(__bf16)(o.x * inv), (__bf16)(o.y * inv), (__bf16)(o.z * inv), (__bf16)(o.w * inv)};
 }
 
-template <int D>
-void launch_dim(hipStream_t s, int queries, const AttnPackedArgs& a) {
-  const int pairs = a.n_units * a.n_chunks;
-  const dim3 grid((pairs + 7) / 8 * 8 * a.q_tiles), block(64 * kWaves);
-  if (queries == 16) hipLaunchKernelGGL((attn_packed<D, 1>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((attn_packed<D, 2>), grid, block, 0, s, a);
-  if (a.n_chunks > 1) hipLaunchKernelGGL((attn_packed_merge<D>), dim3(a.N_k, a.n_units), dim3(256), 0, s, a, queries);
+template <int D, int N>
+void launch_some(hipStream_t s, int queries, const AttnPackedHead& h, const AttnPackedUnit* units) {
+  AttnPackedArgs<N> a;
+  static_cast<AttnPackedHead&>(a) = h;
+  for (int i = 0; i < h.n_units; ++i) a.unit[i] = units[i];
+  const int pairs = h.n_units * h.n_chunks;
+  const dim3 grid((pairs + 7) / 8 * 8 * h.q_tiles), block(64 * kWaves);
+  if (queries == 16) hipLaunchKernelGGL((attn_packed<D, 1, N>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attn_packed<D, 2, N>), grid, block, 0, s, a);
+  if (h.n_chunks > 1) hipLaunchKernelGGL((attn_packed_merge<D, N>), dim3(h.N_k, h.n_units), dim3(256), 0, s, a, queries);
 }
 
 }  // namespace
 
-void launch_attn_packed(hipStream_t s, int head_dim, int queries, const AttnPackedArgs& a) {
-  if (head_dim == 64) launch_dim<64>(s, queries, a);
-  else launch_dim<128>(s, queries, a);
+void launch_attn_packed(hipStream_t s, int head_dim, int queries, const AttnPackedHead& h, const AttnPackedUnit* units) {
+  const bool few = h.n_units <= kFewUnits;
+  if (head_dim == 64 && few) launch_some<64, kFewUnits>(s, queries, h, units);
+  else if (head_dim == 64) launch_some<64, kAttnPackedUnits>(s, queries, h, units);
+  else if (few) launch_some<128, kFewUnits>(s, queries, h, units);
+  else launch_some<128, kAttnPackedUnits>(s, queries, h, units);
 }
 
 }  // namespace hack

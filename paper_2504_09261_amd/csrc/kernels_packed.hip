@@ -3,6 +3,8 @@
 // Memory-bound.  Packing reads a row of K and one of V (bf16 or float32), in order or through a unit's list of kept rows, cached rows
 // and new ones in one numbering, and writes 17/64 of a byte for every bit less; reading back is the same the other way, and exact.
 // Eight elements a lane: four lanes share a group's scale.
+#include <algorithm>
+
 #include "packed_device.h"
 
 namespace hack {
@@ -51,8 +53,10 @@ __device__ __forceinline__ unsigned encode8(const float* v, unsigned& exponent) 
   return w;
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void pack_rows(const PackArgs a) {
+template <int N> struct PackArgs : PackHead { PackUnit unit[N]; };
+
+template <typename T, int D, int N>
+__global__ __launch_bounds__(kThreads) void pack_rows(const PackArgs<N> a) {
   constexpr int LPR = D / 8, RPG = kThreads / LPR;   // lanes of a row, rows of a work-group
   const PackUnit u = a.unit[blockIdx.y];
   const int i = blockIdx.x * RPG + threadIdx.x / LPR, c = threadIdx.x % LPR;
@@ -90,8 +94,8 @@ __device__ __forceinline__ void store8(float* p, unsigned w, float scale) {
   reinterpret_cast<float4*>(p)[1] = make_float4(c[0], c[1], d[0], d[1]);
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void unpack_rows(const PackArgs a) {
+template <typename T, int D, int N>
+__global__ __launch_bounds__(kThreads) void unpack_rows(const PackArgs<N> a) {
   constexpr int LPR = D / 8, RPG = kThreads / LPR;
   const PackUnit u = a.unit[blockIdx.y];
   const int i = blockIdx.x * RPG + threadIdx.x / LPR, c = threadIdx.x % LPR;
@@ -109,20 +113,49 @@ __global__ __launch_bounds__(kThreads) void unpack_rows(const PackArgs a) {
   if (a.plain.pos != nullptr && a.packed.pos != nullptr && c == 0) a.plain.pos[row] = a.packed.pos[(int64_t)u.block * kPackRows + from];
 }
 
+template <typename T, int D, int N>
+void launch_some(hipStream_t s, bool pack, const PackHead& h, const PackUnit* units, int n_units) {
+  PackArgs<N> a;
+  static_cast<PackHead&>(a) = h;
+  int rows = 0;
+  for (int i = 0; i < n_units; ++i) {
+    a.unit[i] = units[i];
+    rows = std::max(rows, units[i].n);
+  }
+  if (rows == 0) return;
+  constexpr int per = kThreads / (D / 8);
+  const dim3 grid((rows + per - 1) / per, n_units);
+  if (pack) hipLaunchKernelGGL((pack_rows<T, D, N>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((unpack_rows<T, D, N>), grid, dim3(kThreads), 0, s, a);
+}
+
+template <typename T, int D>
+void launch_all(hipStream_t s, bool pack, PackHead h, const PackUnit* units, int n_units) {
+  for (int u = 0; u < n_units; u += kPackUnits) {
+    h.unit0 = u;
+    const int n = std::min(kPackUnits, n_units - u);
+    if (n <= kFewUnits) launch_some<T, D, kFewUnits>(s, pack, h, units + u, n);
+    else launch_some<T, D, kPackUnits>(s, pack, h, units + u, n);
+  }
+}
+
+void launch(hipStream_t s, int elem_bytes, int head_dim, bool pack, const PackHead& h, const PackUnit* units, int n_units) {
+  if (elem_bytes == 4) {
+    if (head_dim == 64) launch_all<float, 64>(s, pack, h, units, n_units);
+    else launch_all<float, 128>(s, pack, h, units, n_units);
+  } else {
+    if (head_dim == 64) launch_all<__bf16, 64>(s, pack, h, units, n_units);
+    else launch_all<__bf16, 128>(s, pack, h, units, n_units);
+  }
+}
+
 }  // namespace
 
-#define HACK_PACKED(KERNEL)                                                                                             \
-  const int rows = kThreads / (head_dim / 8);                                                                           \
-  const dim3 grid((max_rows + rows - 1) / rows, a.n_units), block(kThreads);                                            \
-  if (elem_bytes == 4) {                                                                                                \
-    if (head_dim == 64) hipLaunchKernelGGL((KERNEL<float, 64>), grid, block, 0, s, a);                                  \
-    else hipLaunchKernelGGL((KERNEL<float, 128>), grid, block, 0, s, a);                                                \
-  } else {                                                                                                              \
-    if (head_dim == 64) hipLaunchKernelGGL((KERNEL<__bf16, 64>), grid, block, 0, s, a);                                 \
-    else hipLaunchKernelGGL((KERNEL<__bf16, 128>), grid, block, 0, s, a);                                               \
-  }
-void launch_pack(hipStream_t s, int elem_bytes, int head_dim, int max_rows, const PackArgs& a) { HACK_PACKED(pack_rows) }
-void launch_unpack(hipStream_t s, int elem_bytes, int head_dim, int max_rows, const PackArgs& a) { HACK_PACKED(unpack_rows) }
-#undef HACK_PACKED
+void launch_pack(hipStream_t s, int elem_bytes, int head_dim, PackHead h, const PackUnit* units, int n_units) {
+  launch(s, elem_bytes, head_dim, true, h, units, n_units);
+}
+void launch_unpack(hipStream_t s, int elem_bytes, int head_dim, PackHead h, const PackUnit* units, int n_units) {
+  launch(s, elem_bytes, head_dim, false, h, units, n_units);
+}
 
 }  // namespace hack

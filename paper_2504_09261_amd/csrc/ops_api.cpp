@@ -81,11 +81,12 @@ hack_status take_rope(hack_ctx* ctx, const hack_rope* rope, int32_t N, const int
   if (!pos && (int64_t)pos0 + N - 1 > INT32_MAX) return fail(ctx, HACK_EINVAL, "positions from %d on leave 32 bits", pos0);
   for (int i = 0; i < rope->rot_dim / 2; ++i) {
     if (!std::isfinite(rope->freq[i])) return fail(ctx, HACK_EINVAL, "freq[%d] is not finite", i);
-    // whole turns per position do not matter
-    long double t = (long double)rope->freq[i] / 6.283185307179586476925286766559L;
-    t -= floorl(t);
-    const long double high = floorl(t * 4294967296.0L);
-    a->turns[i] = ((uint64_t)high << 32) + (uint64_t)floorl((t * 4294967296.0L - high) * 4294967296.0L);
+    // In 64 bits of mantissa.  Whole turns per position do not matter.
+    long double t = (long double)rope->freq[i] * 0.15915494309189533576888376337251436L;
+    if (fabsl(t) >= 9.0e18L) t = fmodl(t, 1.0L);
+    t -= (long double)(int64_t)t;
+    const uint64_t turn = (uint64_t)(fabsl(t) * 18446744073709551616.0L);
+    a->turns[i] = t < 0 ? 0 - turn : turn;
   }
   a->pos = pos;
   a->pos_b = pos_stride_b;
@@ -155,18 +156,50 @@ bool units_overlap(int n_units, Lo lo, Hi hi) {
   return false;
 }
 
-template <typename Launch>
-void launch_units(const std::vector<PackUnit>& units, PackArgs* a, Launch launch) {
-  for (size_t u0 = 0; u0 < units.size(); u0 += kPackUnits) {
-    a->unit0 = (int32_t)u0;
-    a->n_units = (int32_t)std::min<size_t>(kPackUnits, units.size() - u0);
-    int rows = 0;
-    for (int i = 0; i < a->n_units; ++i) {
-      a->unit[i] = units[u0 + i];
-      rows = std::max(rows, a->unit[i].n);
-    }
-    if (rows > 0) launch(rows);
+int blocks_of(int len) { return (int)(((int64_t)len + kPackRows - 1) / kPackRows); }
+
+// How units are cut: into chunks that give each compute unit two work-groups (two are enough to read at the rate of the memory, and more start and end more
+// often), but not where cutting costs more than it gains: merging the parts is a launch of its own, 5 us, which is what a work-group alone on its compute unit
+// takes for 16 blocks, and a work-group whose neighbour has finished runs 1.7 times as fast, so that units of up to twice the mean need no cut.
+void plan_chunks(const hack_ctx* ctx, const int32_t* len, int64_t slots, AttnPackedHead* a) {
+  int64_t blocks = 0;
+  int longest = 0;
+  for (int i = 0; i < a->n_units; ++i) {
+    const int n = blocks_of(len[i]);
+    blocks += n;
+    longest = std::max(longest, n);
   }
+  const int64_t fill = 2 * (int64_t)ctx->cus;
+  int64_t chunk = std::max<int64_t>(8, (blocks * a->q_tiles + fill - 1) / fill);
+  if (longest <= std::max(2 * chunk, chunk + 16)) chunk = longest;
+  const int64_t most = std::max<int64_t>(1, slots / ((int64_t)a->n_units * a->q_tiles));   // chunks whose partial results the workspace holds
+  chunk = std::max(chunk, (longest + most - 1) / most);
+  a->chunk = (int32_t)std::min<int64_t>(chunk, longest);
+  a->n_chunks = (longest + a->chunk - 1) / a->chunk;
+}
+
+// In what order units start: the longest first, except that where all work-groups start at once, two to a compute unit (one on each first, then a second
+// one in the same order), the long ones get the short ones beside them.
+void order_units(const hack_ctx* ctx, const int32_t* len, const AttnPackedHead& a, std::vector<int32_t>* order, std::vector<int32_t>* count) {
+  const int n = a.n_units;
+  int lo = INT_MAX, hi = 0;
+  for (int i = 0; i < n; ++i) {
+    lo = std::min(lo, blocks_of(len[i]));
+    hi = std::max(hi, blocks_of(len[i]));
+  }
+  std::vector<int32_t>& o = *order;
+  if (lo == hi || n == 1) {
+    for (int i = 0; i < n; ++i) o[i] = i;
+    return;
+  }
+  // by length in steps of a 255th of the range, equal ones in the order of the units
+  constexpr int kSteps = 256;
+  const auto step = [&](int i) { return (int)((int64_t)(hi - blocks_of(len[i])) * (kSteps - 1) / (hi - lo)); };
+  count->assign(kSteps + 1, 0);
+  for (int i = 0; i < n; ++i) ++(*count)[step(i) + 1];
+  for (int i = 0; i < kSteps; ++i) (*count)[i + 1] += (*count)[i];
+  for (int i = 0; i < n; ++i) o[(*count)[step(i)]++] = i;
+  if (a.q_tiles == 1 && a.n_chunks == 1 && n > ctx->cus && n <= 2 * ctx->cus) std::reverse(o.begin() + ctx->cus, o.begin() + n);
 }
 
 }  // namespace
@@ -253,7 +286,7 @@ extern "C" hack_status hack_pack(hack_ctx* ctx, int32_t B, int32_t N_k, const ha
   if (units_overlap(U, [&](int u) { return out->off[u] + units[u].first; }, [&](int u) { return out->off[u] + out->len[u]; }))
     return fail(ctx, HACK_EINVAL, "units of out overlap");
   if ((st = check_device(ctx)) != HACK_OK) return st;
-  PackArgs a{};
+  PackHead a{};
   if (in) a.plain = CachePtrs{in->k, in->v, in->pos};
   a.packed = CachePtrs{out->k, out->v, out->pos};
   a.k_new = k_new;
@@ -262,7 +295,7 @@ extern "C" hack_status hack_pack(hack_ctx* ctx, int32_t B, int32_t N_k, const ha
   a.kept_stride = idx_stride;
   a.n_new = n_new;
   a.pos_new = pos_new;
-  launch_units(units, &a, [&](int rows) { launch_pack(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, rows, a); });
+  launch_pack(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, a, units.data(), U);
   HIP_TRY(ctx, hipGetLastError());
   return HACK_OK;
 } HACK_NO_THROW(ctx)
@@ -287,10 +320,10 @@ extern "C" hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_c
   if (units_overlap(U, [&](int u) { return out->off[u]; }, [&](int u) { return out->off[u] + out->len[u]; }))
     return fail(ctx, HACK_EINVAL, "units of out overlap");
   if ((st = check_device(ctx)) != HACK_OK) return st;
-  PackArgs a{};
+  PackHead a{};
   a.plain = CachePtrs{out->k, out->v, out->pos};
   a.packed = CachePtrs{in->k, in->v, in->pos};
-  launch_units(units, &a, [&](int rows) { launch_unpack(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, rows, a); });
+  launch_unpack(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, a, units.data(), U);
   HIP_TRY(ctx, hipGetLastError());
   return HACK_OK;
 } HACK_NO_THROW(ctx)
@@ -311,7 +344,8 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
   const Range rq{(uintptr_t)q, (uintptr_t)q + (uintptr_t)bytes}, ro{(uintptr_t)out, (uintptr_t)out + (uintptr_t)bytes};
   if (rq.meets(ro)) return fail(ctx, HACK_EINVAL, "q and out overlap");
   if ((st = check_device(ctx)) != HACK_OK) return st;
-  AttnPackedArgs a{};
+  AttnPackedHead a{};
+  AttnPackedUnit units[kAttnPackedUnits];
   a.k = static_cast<const uint8_t*>(kv->k);
   a.v = static_cast<const uint8_t*>(kv->v);
   a.part_o = ctx->part_o;
@@ -323,24 +357,14 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
   const int queries = N_k <= 16 ? 16 : 32;
   a.q_tiles = (N_k + queries - 1) / queries;
   const int64_t slots = 2 * (int64_t)std::max(ctx->attn_slots, 1) * 128 / queries;   // partial results that the workspace holds
+  std::vector<int32_t> order(std::min(U, kAttnPackedUnits)), count;
   for (int u0 = 0; u0 < U; u0 += kAttnPackedUnits) {
-    a.unit0 = u0;
     a.n_units = std::min(kAttnPackedUnits, U - u0);
-    int64_t blocks = 0;
-    int longest = 0;
-    for (int i = 0; i < a.n_units; ++i) {
-      a.unit[i] = AttnPackedUnit{(int32_t)(kv->off[u0 + i] / kPackRows), kv->len[u0 + i]};
-      const int n = (kv->len[u0 + i] + kPackRows - 1) / kPackRows;
-      blocks += (int64_t)n * a.q_tiles;
-      longest = std::max(longest, n);
-    }
-    // chunks of the work that fill the chip four times over, of at least eight blocks, no more than the workspace holds
-    int64_t chunk = std::max<int64_t>(8, (blocks + 4 * ctx->cus - 1) / (4 * ctx->cus));
-    const int64_t most = std::max<int64_t>(1, slots / ((int64_t)a.n_units * a.q_tiles));
-    chunk = std::max<int64_t>(chunk, (longest + most - 1) / most);
-    a.chunk = (int32_t)std::min<int64_t>(chunk, longest);
-    a.n_chunks = (longest + a.chunk - 1) / a.chunk;
-    launch_attn_packed(static_cast<hipStream_t>(stream), d, queries, a);
+    const int32_t* len = kv->len + u0;
+    plan_chunks(ctx, len, slots, &a);
+    order_units(ctx, len, a, &order, &count);
+    for (int i = 0; i < a.n_units; ++i) units[i] = AttnPackedUnit{(int32_t)(kv->off[u0 + order[i]] / kPackRows), len[order[i]], u0 + order[i]};
+    launch_attn_packed(static_cast<hipStream_t>(stream), d, queries, a, units);
   }
   HIP_TRY(ctx, hipGetLastError());
   return HACK_OK;

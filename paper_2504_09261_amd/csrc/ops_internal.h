@@ -46,7 +46,6 @@ void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout
 constexpr int kPackRows = 64;    // rows of a block
 constexpr int kPackGroup = 32;   // elements of a row that share a scale
 inline int packed_block_bytes(int head_dim) { return kPackRows * (head_dim / 2 + head_dim / kPackGroup); }
-constexpr int kPackUnits = 96;   // units of a launch
 struct PackUnit {
   int64_t row0;     // first row in the arrays of plain rows
   int32_t len_in;   // pack: cached rows there, which the new ones follow
@@ -54,7 +53,7 @@ struct PackUnit {
   int32_t first;    // row of the unit there
   int32_t n;        // rows
 };
-struct PackArgs {
+struct PackHead {
   CachePtrs plain;       // rows read (pack) or written (unpack)
   CachePtrs packed;
   const void* k_new;
@@ -63,20 +62,19 @@ struct PackArgs {
   int64_t kept_stride;
   int32_t n_new;         // rows of k_new / v_new of a unit
   int32_t pos_new;
-  int32_t unit0;         // of the launch
-  int32_t n_units;
-  PackUnit unit[kPackUnits];
+  int32_t unit0;         // of the launch, set by the launchers
+  int32_t pad;
 };
-void launch_pack(hipStream_t s, int elem_bytes, int head_dim, int max_rows, const PackArgs& a);
-void launch_unpack(hipStream_t s, int elem_bytes, int head_dim, int max_rows, const PackArgs& a);
+void launch_pack(hipStream_t s, int elem_bytes, int head_dim, PackHead h, const PackUnit* units, int n_units);
+void launch_unpack(hipStream_t s, int elem_bytes, int head_dim, PackHead h, const PackUnit* units, int n_units);
 
 // ---- attention over them (bf16 queries and outputs) -------------------------
-constexpr int kAttnPackedUnits = 384;   // units of a launch
 struct AttnPackedUnit {
   int32_t block;   // first block
   int32_t len;     // rows
+  int32_t unit;    // u = b*H + h
 };
-struct AttnPackedArgs {
+struct AttnPackedHead {
   const uint8_t* k;
   const uint8_t* v;
   const void* q;      // bf16
@@ -85,15 +83,14 @@ struct AttnPackedArgs {
   float* part_ml;     // [slot, queries of a work-group, 2] their references and normalisers
   int32_t N_k;
   float scale;
-  int32_t unit0;      // of the launch
-  int32_t n_units;
+  int32_t n_units;    // of the launch
   int32_t q_tiles;    // of a unit's queries
   int32_t n_chunks;   // most chunks that a unit's keys are cut into
-  int32_t chunk;      // blocks of kPackRows keys of one
-  int32_t pad;
-  AttnPackedUnit unit[kAttnPackedUnits];
+  int32_t chunk;      // most blocks of kPackRows keys of one
 };
+// Units of a launch.  They travel by value; a launch takes 2.5 us to issue and 0.3 to 0.5 more for every KiB of arguments up to 8 (a table in memory
+// would be another copy each time a length grows), so there is a short list too.
+constexpr int kFewUnits = 64, kPackUnits = 640, kAttnPackedUnits = 1024;
 // queries: of a work-group, 16 or 32
-void launch_attn_packed(hipStream_t s, int head_dim, int queries, const AttnPackedArgs& a);
-
+void launch_attn_packed(hipStream_t s, int head_dim, int queries, const AttnPackedHead& h, const AttnPackedUnit* units);
 }  // namespace hack

@@ -9,8 +9,10 @@
 namespace stub {
 int device = 0;
 std::vector<RotateArgs> rotations;
-std::vector<PackArgs> packs, unpacks;
-std::vector<AttnPackedArgs> attentions;
+struct Pack : PackHead { std::vector<PackUnit> unit; };
+struct Attention : AttnPackedHead { std::vector<AttnPackedUnit> unit; };
+std::vector<Pack> packs, unpacks;
+std::vector<Attention> attentions;
 std::vector<int> queries;
 size_t calls() { return rotations.size() + packs.size() + unpacks.size() + attentions.size(); }
 }  // namespace stub
@@ -19,9 +21,13 @@ extern "C" hipError_t hipGetDevice(int* d) { *d = stub::device; return hipSucces
 
 namespace hack {
 void launch_rotate(hipStream_t, int, int, bool, int, int, int, RotateArgs a) { stub::Quiet q; stub::rotations.push_back(a); }
-void launch_pack(hipStream_t, int, int, int, const PackArgs& a) { stub::Quiet q; stub::packs.push_back(a); }
-void launch_unpack(hipStream_t, int, int, int, const PackArgs& a) { stub::Quiet q; stub::unpacks.push_back(a); }
-void launch_attn_packed(hipStream_t, int, int n, const AttnPackedArgs& a) { stub::Quiet q; stub::attentions.push_back(a); stub::queries.push_back(n); }
+void launch_pack(hipStream_t, int, int, PackHead h, const PackUnit* u, int n) { stub::Quiet q; stub::packs.push_back({h, {u, u + n}}); }
+void launch_unpack(hipStream_t, int, int, PackHead h, const PackUnit* u, int n) { stub::Quiet q; stub::unpacks.push_back({h, {u, u + n}}); }
+void launch_attn_packed(hipStream_t, int, int n, const AttnPackedHead& h, const AttnPackedUnit* u) {
+  stub::Quiet q;
+  stub::attentions.push_back({h, {u, u + h.n_units}});
+  stub::queries.push_back(n);
+}
 }  // namespace hack
 
 #define CHECK(c)                                    \
@@ -206,8 +212,8 @@ int pack_refusals() {
   uint8_t *const k = at(0x50000000), *const v = at(0x60000000);
   int32_t* const kept = at<int32_t>(0x70000000);
   CHECK(pack(&in, k, v, nullptr, 0, nullptr, &out) == HACK_OK && stub::packs.size() == 1);
-  const PackArgs& a = stub::packs[0];
-  CHECK(a.n_units == 4 && a.unit[3].row0 == 288 && a.unit[3].len_in == 33 && a.unit[3].block == 6 && a.unit[3].first == 0 && a.unit[3].n == 43 && a.n_new == 10);
+  const stub::Pack& a = stub::packs[0];
+  CHECK(a.unit.size() == 4 && a.unit[3].row0 == 288 && a.unit[3].len_in == 33 && a.unit[3].block == 6 && a.unit[3].first == 0 && a.unit[3].n == 43 && a.n_new == 10);
   CHECK(pack(nullptr, k, v, nullptr, 0, first, &out) == HACK_OK && stub::packs.back().unit[0].n == 0 && stub::packs.back().unit[1].n == 10);
   CHECK(pack(&in, k, v, kept, 100, nullptr, &out) == HACK_OK);
   REFUSED(HACK_ECAPACITY, pack(&in, k, v, kept, 99, nullptr, &out));
@@ -273,7 +279,7 @@ int pack_refusals() {
 
 // Every unit once, whatever their number.
 int many_units() {
-  constexpr int n = 1000;
+  constexpr int n = 3000;
   Context c(HACK_BF16, 10, n);
   std::vector<int64_t> off(n);
   std::vector<int32_t> len(n), first(n, 0);
@@ -289,18 +295,20 @@ int many_units() {
   const hack_cache in{at(kA), at(kB), nullptr, rows, in_off.data(), len.data()};
   CHECK(hack_pack(c.ctx, n / 10, 1, &in, nullptr, nullptr, 0, nullptr, 0, nullptr, &out, kStream) == HACK_OK);
   int u = 0;
-  for (const PackArgs& a : stub::packs) {
-    CHECK(a.unit0 == u && a.n_units >= 1 && a.n_units <= kPackUnits);
-    for (int i = 0; i < a.n_units; ++i, ++u) CHECK(a.unit[i].row0 == off[u] && a.unit[i].n == len[u] && a.unit[i].block == off[u] / 64);
-  }
+  for (const auto& a : stub::packs)
+    for (size_t i = 0; i < a.unit.size(); ++i, ++u) CHECK(a.unit[i].row0 == off[u] && a.unit[i].n == len[u] && a.unit[i].block == off[u] / 64);
   CHECK(u == n);
   CHECK(hack_attn_packed(c.ctx, n / 10, 5, at(0x50000000), &out, 0.1f, at(0x60000000), kStream) == HACK_OK);
-  u = 0;
-  for (const AttnPackedArgs& a : stub::attentions) {
-    CHECK(a.unit0 == u && a.n_units >= 1 && a.n_units <= kAttnPackedUnits);
-    for (int i = 0; i < a.n_units; ++i, ++u) CHECK(a.unit[i].len == len[u] && a.unit[i].block == off[u] / 64);
+  std::vector<int> seen(n, 0);
+  CHECK(stub::attentions.size() == (n + kAttnPackedUnits - 1) / kAttnPackedUnits);
+  for (const auto& a : stub::attentions) {
+    CHECK(a.n_units >= 1 && a.n_units <= kAttnPackedUnits);
+    for (const AttnPackedUnit& x : a.unit) {
+      CHECK(x.unit >= 0 && x.unit < n && x.len == len[x.unit] && x.block == off[x.unit] / 64);
+      ++seen[x.unit];
+    }
   }
-  CHECK(u == n);
+  for (int i = 0; i < n; ++i) CHECK(seen[i] == 1);
   return 0;
 }
 
@@ -353,7 +361,7 @@ int attn_plan() {
       stub::attentions.clear();
       stub::queries.clear();
       CHECK(attn(kv, N) == HACK_OK && stub::attentions.size() == 1);
-      const AttnPackedArgs& a = stub::attentions[0];
+      const auto& a = stub::attentions[0];
       const int64_t queries = stub::queries[0], longest = (*std::max_element(s.begin(), s.end()) + 63LL) / 64;
       CHECK(a.q_tiles == (N + queries - 1) / queries && a.chunk >= 1 && a.n_chunks >= 1);
       CHECK((int64_t)a.chunk * a.n_chunks >= longest && (int64_t)a.chunk * (a.n_chunks - 1) < longest);

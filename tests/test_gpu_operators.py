@@ -470,8 +470,8 @@ def test_attention_says_nan_where_a_row_holds_one(contexts):
 
 def test_many_units(contexts):
     """More units than a launch takes, on a stream of their own."""
-    heads, B, d = 20, 25, 64
-    hk = contexts(heads, d, "bf16", units=500)
+    heads, B, d = 20, 70, 64
+    hk = contexts(heads, d, "bf16", units=1400)
     g = torch.Generator(DEV).manual_seed(8)
     lens = np.array([1 + u * 31 % 150 for u in range(heads * B)])
     side = torch.cuda.Stream()
@@ -541,10 +541,11 @@ def test_a_schedule_over_a_packed_cache(contexts):
     hk.close()
 
 
-def test_graph_replays_and_eager_calls_in_turn(contexts):
+@pytest.mark.parametrize("B", [6, 20])
+def test_graph_replays_and_eager_calls_in_turn(contexts, B):
     """A serving step captured once: norms and rotation, the new row packed, attention; replayed with eager work and other inputs between."""
-    heads, B, d = 4, 6, 128
-    hk = contexts(heads, d, "bf16", units=24, queries=64)
+    heads, d = 4, 128
+    hk = contexts(heads, d, "bf16", units=4 * B, queries=64)
     g = torch.Generator(DEV).manual_seed(3)
     lens = np.array([1 + 97 * u for u in range(heads * B)])
     pc, _ = filled(hk, B, lens, d, g)
