@@ -68,6 +68,7 @@ struct hack_ctx {
   int score_capacity[hack::kScoreSizes] = {};   // bf16 path: score items one fused launch may hold (resident waves), by item size (kScoreItemKeys)
   int split_max_items = -1;      // launches with at most this many 32-query attention items use the key-split kernel (HACK_ATTN_SPLIT_ITEMS); -1 (default): see use_split_attention
   int attn_kernel = -1;          // bf16 kernel of the 128-query items (kAttnPlain ...); -1 (default): the deeper pipeline, keys in halves where use_key_halves says so
+  int packed_queries = 0;        // attention over packed caches: queries of a work-group (HACK_ATTN_PACKED_QUERIES: 16, 32 or 128); 0 (default): see queries_per_group
   // streamed form of that kernel: the launch is cut into equal runs of key blocks, one per resident work-group
   int attn_stream = -1;          // HACK_ATTN_STREAM; -1 (default): cut single work items where the pair model gains, 0: never, 1: equal runs
                                  // for every launch of the 128-query kernel, 2: A/B aid, 4: every cut the model likes (see use_stream_attention)

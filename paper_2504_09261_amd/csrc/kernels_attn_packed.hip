@@ -37,20 +37,6 @@ template <int D> struct PackedRows {   // a lane's share of a block of 64 rows
   __device__ __forceinline__ float scale(int t) const { return scale_of((exponents >> (8 * t)) & 255u); }
 };
 
-template <int N> struct AttnPackedArgs : AttnPackedHead { AttnPackedUnit unit[N]; };
-
-// Blocks [lo, hi) of chunk c of a unit of n blocks: as even as they can be.
-__device__ __forceinline__ int chunks_of(int n, int most) { return (n + most - 1) / most; }
-__device__ __forceinline__ int chunk_at(int n, int chunks, int c) { return (int)((unsigned)n / chunks * c + ((unsigned)n % chunks) * c / chunks); }
-
-// LDS layout of converted rows of V: groups of four, a group's 64-byte pieces row after row, the 16-byte chunks of a piece permuted by the group.
-// All operands of the PV product stand at constant distances from two addresses, a lane's share of a row at constant distances from two others, and
-// neither the writes (16 rows, one chunk) nor the transposing reads (8 rows, 32 bytes) meet a bank twice.
-__device__ __forceinline__ int v_flip(int row) { return 2 * ((row >> 2) & 1) | ((row >> 3) & 1); }
-template <int D> __device__ __forceinline__ int v_chunk(int row, int chunk) {   // element offset of a chunk
-  return (row >> 2) * 4 * D + (chunk >> 2) * 128 + (row & 3) * 32 + ((chunk & 3) ^ v_flip(row)) * 8;
-}
-
 template <int D, int NQ, int N>
 __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void attn_packed(const AttnPackedArgs<N> a) {
   constexpr int KC = D / 32, MT = D / 16, QROWS = 16 * NQ;
@@ -60,7 +46,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void at
   if (pair >= a.n_units * a.n_chunks) return;
   const int ui = pair % a.n_units, chunk = pair / a.n_units;
   const AttnPackedUnit u = a.unit[ui];
-  const int len = u.len, n_blocks = (len + kPackRows - 1) / kPackRows;
+  const int len = u.len, n_blocks = packed_blocks(len);
   const int chunks = chunks_of(n_blocks, a.chunk);
   if (chunk >= chunks) return;
   const int first = chunk_at(n_blocks, chunks, chunk), last = chunk_at(n_blocks, chunks, chunk + 1);
@@ -257,7 +243,7 @@ constexpr int kFactors = 1024;   // chunks whose factors are kept in LDS at a ti
 template <int D, int N>
 __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N> a, int q_rows) {
   constexpr int LPR = D / 4, SIDE = 256 / LPR;   // chunks at a time
-  const int ui = blockIdx.y, n = chunks_of((a.unit[ui].len + kPackRows - 1) / kPackRows, a.chunk);
+  const int ui = blockIdx.y, n = chunks_of(packed_blocks(a.unit[ui].len), a.chunk);
   if (n == 1) return;
   const int tid = threadIdx.x, qi = blockIdx.x, c0 = tid / LPR, lane = tid % LPR;
   const int64_t part0 = ((int64_t)ui * a.q_tiles + qi / q_rows) * a.n_chunks * q_rows + qi % q_rows;
@@ -319,7 +305,8 @@ void launch_some(hipStream_t s, int queries, const AttnPackedHead& h, const Attn
   for (int i = 0; i < h.n_units; ++i) a.unit[i] = units[i];
   const int pairs = h.n_units * h.n_chunks;
   const dim3 grid((pairs + 7) / 8 * 8 * h.q_tiles), block(64 * kWaves);
-  if (queries == 16) hipLaunchKernelGGL((attn_packed<D, 1, N>), grid, block, 0, s, a);
+  if (queries == kTileQueries) launch_attn_packed_tiles(s, D, h, units);
+  else if (queries == 16) hipLaunchKernelGGL((attn_packed<D, 1, N>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((attn_packed<D, 2, N>), grid, block, 0, s, a);
   if (h.n_chunks > 1) hipLaunchKernelGGL((attn_packed_merge<D, N>), dim3(h.N_k, h.n_units), dim3(256), 0, s, a, queries);
 }

@@ -91,6 +91,8 @@ struct AttnPackedHead {
 // Units of a launch.  They travel by value; a launch takes 2.5 us to issue and 0.3 to 0.5 more for every KiB of arguments up to 8 (a table in memory
 // would be another copy each time a length grows), so there is a short list too.
 constexpr int kFewUnits = 64, kPackUnits = 640, kAttnPackedUnits = 1024;
-// queries: of a work-group, 16 or 32
+// queries: of a work-group, 16, 32 or kTileQueries
+constexpr int kTileQueries = 128;
 void launch_attn_packed(hipStream_t s, int head_dim, int queries, const AttnPackedHead& h, const AttnPackedUnit* units);
+void launch_attn_packed_tiles(hipStream_t s, int head_dim, const AttnPackedHead& h, const AttnPackedUnit* units);   // without the merge
 }  // namespace hack

@@ -1,5 +1,7 @@
 """The operators around the cache (rotary positions, norms with rotation, packed caches, attention over them) against plain implementations in
 64 bits and more, through the C ABI.  Tolerances count roundings: half a step of a type is finfo.eps / 2 relative, H below is float32's."""
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -18,10 +20,14 @@ DEV = "cuda:0"
 def contexts():
     made = {}
 
-    def get(heads, d, dtype, units=64, queries=4096):
-        key = (heads, d, dtype, units, queries)
+    def get(heads, d, dtype, units=64, queries=4096, form=0):
+        key = (heads, d, dtype, units, queries, form)
         if key not in made:
-            made[key] = Hack(heads, d, dtype, units, 1024, queries)
+            os.environ["HACK_ATTN_PACKED_QUERIES"] = str(form)      # read when a context is created
+            try:
+                made[key] = Hack(heads, d, dtype, units, 1024, queries)
+            finally:
+                del os.environ["HACK_ATTN_PACKED_QUERIES"]
         return made[key]
     yield get
     for h in made.values():
@@ -369,7 +375,8 @@ def check_attention(q, rows, scale, out):
     """q, out [units, n, d]; rows: (K, V) of every unit.  Against softmax in float64.  Probabilities are rounded to bf16 where they are multiplied and
     where they are summed: 2 2^-8 of sum p |v|; a score of d products is summed in float32: (d + 4) 2^-24 of sum |q k|, and an error of s is a factor
     e^s on its probability and on the sum; exponentials and sums in float32: 1e-5; the output: half a step.
-    Probabilities below 2^-126 of the largest, float32's smallest normal number, may be zero: that much of each |v|."""
+    Probabilities are taken against a reference that lies up to 2^15 above the largest (many queries), and what is below 2^-126 then, float32's and bf16's
+    smallest normal number, may be zero: 2^-111 of each |v|."""
     q, o = to64(q), to64(out)
     d = q.shape[-1]
     for u, (k, v) in enumerate(rows):
@@ -378,7 +385,7 @@ def check_attention(q, rows, scale, out):
         p /= p.sum(-1, keepdims=True)
         want = p @ v
         slack = scale * (d + 4) * H * (np.abs(q[u]) @ np.abs(k).T).max(-1, keepdims=True)
-        tol = (2 * 2.0 ** -8 + 2 * slack + 1e-5) * (p @ np.abs(v)) * 1.01 + 2.0 ** -8 * 1.01 * np.abs(want) + 2.0 ** -126 * (1 + np.abs(v).sum(0))
+        tol = (2 * 2.0 ** -8 + 2 * slack + 1e-5) * (p @ np.abs(v)) * 1.01 + 2.0 ** -8 * 1.01 * np.abs(want) + 2.0 ** -111 * (1 + np.abs(v).sum(0))
         err = np.abs(o[u] - want)
         assert (err <= tol).all(), (u, k.shape, float((err / tol).max()))
 
@@ -388,9 +395,9 @@ LENGTHS = [[1, 2, 3, 15, 16, 17], [31, 32, 33, 63, 64, 65], [100, 511, 512, 513,
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("lens", LENGTHS, ids=lambda l: "-".join(map(str, l)))
-@pytest.mark.parametrize("n", [1, 4, 16, 17, 33, 129])
-def test_attention_over_a_packed_cache(contexts, d, lens, n):
-    hk = contexts(3, d, "bf16")
+@pytest.mark.parametrize("n, form", [(1, 0), (1, 128), (4, 0), (16, 0), (17, 0), (17, 16), (17, 128), (33, 0), (129, 16), (129, 32), (129, 128)])
+def test_attention_over_a_packed_cache(contexts, d, lens, n, form):
+    hk = contexts(3, d, "bf16", form=form)
     g = torch.Generator(DEV).manual_seed(n)
     pc, rows = filled(hk, 2, np.array(lens), d, g, order=[4, 2, 0, 1, 5, 3])
     q = (2 * torch.randn((2, 3, n, d), generator=g, device=DEV)).bfloat16()
@@ -403,11 +410,11 @@ def test_attention_over_a_packed_cache(contexts, d, lens, n):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("n", [300, 1000])
-def test_attention_of_many_queries_over_a_packed_cache(contexts, d, n):
-    hk = contexts(3, d, "bf16")
+@pytest.mark.parametrize("n, form", [(300, 0), (1000, 0), (1000, 32), (1000, 128)])
+def test_attention_of_many_queries_over_a_packed_cache(contexts, d, n, form):
+    hk = contexts(3, d, "bf16", form=form)
     g = torch.Generator(DEV).manual_seed(n)
-    for lens in ([1, 700, 33], [64, 4000, 129], [2500, 2500, 2500]):
+    for lens in ([1, 700, 33], [64, 4000, 129], [2500, 2500, 2500], [9000, 1, 260]):
         pc, rows = filled(hk, 1, np.array(lens), d, g)
         q = (3 * torch.randn((1, 3, n, d), generator=g, device=DEV)).bfloat16()
         out = torch.full_like(q, 9.0)
@@ -415,8 +422,9 @@ def test_attention_of_many_queries_over_a_packed_cache(contexts, d, n):
         check_attention(q[0], rows, float(np.float32(d ** -0.5)), out[0])
 
 
-def test_attention_where_the_largest_score_comes_late_or_alone(contexts):
-    hk = contexts(3, 128, "bf16")
+@pytest.mark.parametrize("form", [16, 32, 128])
+def test_attention_where_the_largest_score_comes_late_or_alone(contexts, form):
+    hk = contexts(3, 128, "bf16", form=form)
     g = torch.Generator(DEV).manual_seed(9)
     lens = np.array([700, 5000, 65])
     off, rows = offsets(lens, 8)
@@ -451,8 +459,9 @@ def test_heads_that_share_a_cache(contexts):
             check_attention(q[b, h][None], [rows[b * kv_heads + h // group]], 0.125, out[b, h][None])
 
 
-def test_attention_says_nan_where_a_row_holds_one(contexts):
-    hk = contexts(3, 64, "bf16")
+@pytest.mark.parametrize("form", [16, 32, 128])
+def test_attention_says_nan_where_a_row_holds_one(contexts, form):
+    hk = contexts(3, 64, "bf16", form=form)
     g = torch.Generator(DEV).manual_seed(6)
     lens = np.array([90, 90, 90])
     off, rows = offsets(lens, 8)
