@@ -430,7 +430,7 @@ hack_status hack_rope_freqs(int32_t rot_dim, int32_t axes, int32_t scaling, doub
 /* Rotates the rows of x.
  *   pos  DEVICE int32: row n of batch element b has position pos[b pos_stride_b + a N + n]
  *        on axis a (pos_stride_b 0: the same for every batch element); NULL: pos0 + n (one axis)
- * Errors: HACK_EINVAL (NULL/misaligned pointers, strides, layout, frequencies that are not finite, overlap, the current
+ * Errors: HACK_EINVAL (NULL/misaligned pointers, strides, layout, frequencies that are not numbers of at most 1e6, overlap, the current
  * device is not the context's), HACK_EUNSUPPORTED (rot_dim no multiple of 16 for each axis), HACK_ECAPACITY. */
 hack_status hack_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* x, const hack_rope* rope,
                         const int32_t* pos, int64_t pos_stride_b, int32_t pos0, hack_stream stream);

@@ -80,13 +80,13 @@ hack_status take_rope(hack_ctx* ctx, const hack_rope* rope, int32_t N, const int
     return fail(ctx, HACK_EINVAL, "pos_stride_b must be 0 or at least axes * N (got %lld)", (long long)pos_stride_b);
   if (!pos && (int64_t)pos0 + N - 1 > INT32_MAX) return fail(ctx, HACK_EINVAL, "positions from %d on leave 32 bits", pos0);
   for (int i = 0; i < rope->rot_dim / 2; ++i) {
-    if (!std::isfinite(rope->freq[i])) return fail(ctx, HACK_EINVAL, "freq[%d] is not finite", i);
-    // In 64 bits of mantissa.  Whole turns per position do not matter.
-    long double t = (long double)rope->freq[i] * 0.15915494309189533576888376337251436L;
-    if (fabsl(t) >= 9.0e18L) t = fmodl(t, 1.0L);
-    t -= (long double)(int64_t)t;
-    const uint64_t turn = (uint64_t)(fabsl(t) * 18446744073709551616.0L);
-    a->turns[i] = t < 0 ? 0 - turn : turn;
+    if (!(std::fabs(rope->freq[i]) <= 1e6)) return fail(ctx, HACK_EINVAL, "freq[%d] is not a number of at most 1e6", i);
+    // freq / 2 pi as the sum of two doubles, without its whole turns, which do not matter; then in units of 2^-64
+    constexpr double kInv = 0.15915494309189535, kInvLow = -9.839338337591243e-18;
+    const double t = rope->freq[i] * kInv, low = std::fma(rope->freq[i], kInv, -t) + rope->freq[i] * kInvLow;
+    double part = t - std::floor(t);   // exact, but for a tiny t below zero, where it may come out as one
+    if (part >= 1.0) part = 0.0;
+    a->turns[i] = (uint64_t)(part * 18446744073709551616.0) + (uint64_t)(int64_t)(low * 18446744073709551616.0);
   }
   a->pos = pos;
   a->pos_b = pos_stride_b;
@@ -114,9 +114,10 @@ hack_status rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, cons
   if (n == 2 && out[0].meets(out[1])) return fail(ctx, HACK_EINVAL, "the outputs overlap each other");
   a.n = N;
   a.eps = eps;
+  a.norm = norm;
   if (rope && (st = take_rope(ctx, rope, N, pos, pos_stride_b, pos0, &a)) != HACK_OK) return st;
   if ((st = check_device(ctx)) != HACK_OK) return st;
-  launch_rotate(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, !rope || rope->layout == HACK_ROPE_HALF, norm, B, n, a);
+  launch_rotate(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, !rope || rope->layout == HACK_ROPE_HALF, B, n, a);
   HIP_TRY(ctx, hipGetLastError());
   return HACK_OK;
 }

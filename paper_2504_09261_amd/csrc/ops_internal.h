@@ -33,14 +33,14 @@ struct RotateArgs {
   int32_t rot_dim;      // rotating elements of a head, 0: none
   int32_t section;      // of an axis
   float gain, eps;
+  int32_t norm;         // kNorm*
   // launch shape, set by launch_rotate
   int32_t tokens_log2;  // rows of one head a work-group takes (power of two)
   int32_t tiles;        // of rows
   int32_t steps;        // heads a thread takes, one after the other
-  int32_t pad;
   uint64_t turns[kMaxPairs];   // of a pair per position, in units of 2^-64 of a turn
 };
-void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout, int norm, int batch, int n_tensors, RotateArgs a);
+void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout, int batch, int n_tensors, RotateArgs a);
 
 // ---- rows in 4 bits ---------------------------------------------------------
 constexpr int kPackRows = 64;    // rows of a block

@@ -20,7 +20,7 @@ size_t calls() { return rotations.size() + packs.size() + unpacks.size() + atten
 extern "C" hipError_t hipGetDevice(int* d) { *d = stub::device; return hipSuccess; }
 
 namespace hack {
-void launch_rotate(hipStream_t, int, int, bool, int, int, int, RotateArgs a) { stub::Quiet q; stub::rotations.push_back(a); }
+void launch_rotate(hipStream_t, int, int, bool, int, int, RotateArgs a) { stub::Quiet q; stub::rotations.push_back(a); }
 void launch_pack(hipStream_t, int, int, PackHead h, const PackUnit* u, int n) { stub::Quiet q; stub::packs.push_back({h, {u, u + n}}); }
 void launch_unpack(hipStream_t, int, int, PackHead h, const PackUnit* u, int n) { stub::Quiet q; stub::unpacks.push_back({h, {u, u + n}}); }
 void launch_attn_packed(hipStream_t, int, int n, const AttnPackedHead& h, const AttnPackedUnit* u) {
@@ -121,6 +121,12 @@ int rotate_refusals() {
   REFUSED(HACK_EUNSUPPORTED, rot(x, p, at<int32_t>(kC)));
   freq[5] = NAN;
   REFUSED(HACK_EINVAL, rot(x, ok));
+  freq[5] = 1.5e6;
+  REFUSED(HACK_EINVAL, rot(x, ok));
+  freq[5] = -INFINITY;
+  REFUSED(HACK_EINVAL, rot(x, ok));
+  freq[5] = -1e-30;
+  CHECK(rot(x, ok) == HACK_OK && (stub::rotations.back().turns[5] == 0 || stub::rotations.back().turns[5] + 2 < 4));
   freq[5] = 0.1;
   REFUSED(HACK_EINVAL, rot(x, ok, at<int32_t>(kC + 2)));
   REFUSED(HACK_EINVAL, rot(x, ok, at<int32_t>(kC), 9));
