@@ -1,5 +1,5 @@
 """Thin binding over the C ABI of include/hack.h: ctypes, and for hack_step, which an image calls layers x scales
-times, a CPython entry of its own (csrc/py_step.cpp).
+times, and the operators around the cache, which a token calls for every layer, CPython entries (csrc/py_step.cpp, csrc/py_ops.cpp).
 
 Argument marshalling only: every step of the path runs in the HIP kernels of
 libhack_mi355x.so.  PyTorch is used for device memory and the current stream.
@@ -56,19 +56,15 @@ class hack_rope(C.Structure):
     _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("axes", C.c_int32), ("gain", C.c_float), ("freq", C.POINTER(C.c_double))]
 
 
-class hack_rows(C.Structure):
-    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("heads", C.c_int32), ("stride_b", C.c_int64), ("stride_h", C.c_int64),
-                ("stride_n", C.c_int64), ("weight", C.c_void_p), ("weight_stride_h", C.c_int64)]
-
-
 _lib = None
 _step_call = _step_addr = None    # CPython entry; addresses of hack_step and hack_step_final
+_ops_call = _ops_addr = None      # CPython entries; addresses of the functions they call
 
 
 def load_library() -> C.CDLL:
     """dlopen the in-tree library; torch is imported first so that both use the
     same HIP runtime."""
-    global _lib, _step_call, _step_addr
+    global _lib, _step_call, _step_addr, _ops_call, _ops_addr
     if _lib is not None:
         return _lib
     import torch  # noqa: F401  (loads libamdhip64 with the soname the library needs)
@@ -78,11 +74,13 @@ def load_library() -> C.CDLL:
             "(there is no fallback path)")
     try:
         from paper_2504_09261_amd._step_call import step as _step_call
+        from paper_2504_09261_amd import _ops_call
     except ImportError as e:
-        raise FileNotFoundError(f"the step entry beside {LIB_PATH} is missing: build it with "
+        raise FileNotFoundError(f"an entry beside {LIB_PATH} is missing: build it with "
                                 "`python -m paper_2504_09261_amd.build` (there is no fallback path)") from e
     lib = C.CDLL(LIB_PATH)
     _step_addr = tuple(C.cast(f, C.c_void_p).value for f in (lib.hack_step, lib.hack_step_final))
+    _ops_addr = {n: C.cast(getattr(lib, "hack_" + n), C.c_void_p).value for n in ("rotate", "norm_rotate", "pack", "unpack", "attn_packed")}
     vp, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
     pi32, pi64, pu8 = C.POINTER(C.c_int32), C.POINTER(C.c_int64), C.POINTER(C.c_uint8)
     pcache = C.POINTER(hack_cache)
@@ -118,14 +116,8 @@ def load_library() -> C.CDLL:
     lib.hack_kvcache_step_form.argtypes = [vp]
     lib.hack_kvcache_step_form.restype = i32
     lib.hack_step.argtypes = [vp, vp, i32, i32, vp, vp, vp, pu8, pi32, i32, f32, vp, vp, i64, vp]
-    pd, prows, prope = C.POINTER(C.c_double), C.POINTER(hack_rows), C.POINTER(hack_rope)
-    lib.hack_rope_freqs.argtypes = [i32, i32, i32, C.c_double, C.c_double, C.c_double, pd, C.POINTER(f32)]
-    lib.hack_rotate.argtypes = [vp, i32, i32, prows, prope, vp, i64, i32, vp]
-    lib.hack_norm_rotate.argtypes = [vp, i32, i32, prows, prows, i32, f32, prope, vp, i64, i32, vp]
+    lib.hack_rope_freqs.argtypes = [i32, i32, i32, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double), C.POINTER(f32)]
     lib.hack_packed_bytes.argtypes = [i32, i64, pi64]
-    lib.hack_pack.argtypes = [vp, i32, i32, pcache, vp, vp, i32, vp, i64, pi32, pcache, vp]
-    lib.hack_unpack.argtypes = [vp, i32, pcache, pi32, pcache, vp]
-    lib.hack_attn_packed.argtypes = [vp, i32, i32, vp, pcache, f32, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int and name not in ("hack_strerror", "hack_last_error"):
@@ -234,10 +226,6 @@ class PackedCache:
         pos = torch.empty((n * PACK_ROWS,), dtype=torch.int32, device=device) if with_pos else None
         return cls(k, v, PACK_ROWS * (np.cumsum(blocks) - blocks), np.zeros(len(blocks), np.int32), pos)
 
-    def struct(self) -> hack_cache:   # the two structures have the same members
-        return hack_cache.from_buffer(_raw_cache(_dev(self.k), _dev(self.v), _dev(self.pos), self.rows,
-                                                 _addr(self.off), _addr(self.len)))
-
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
@@ -252,6 +240,7 @@ class Rope:
         assert self.freq.shape == (rot_dim // 2,), "one frequency for every pair"
         self.rot_dim, self.axes, self.layout, self.gain = rot_dim, axes, layout, gain
         self._struct = hack_rope(ROPE_LAYOUTS[layout], rot_dim, axes, gain, self.freq.ctypes.data_as(C.POINTER(C.c_double)))
+        self.address = C.addressof(self._struct)
 
     @classmethod
     def scaled(cls, rot_dim: int, axes: int = 1, layout: str = "half", scaling: str = "plain", base: float = 10000.0, factor: float = 1.0,
@@ -333,6 +322,7 @@ class Hack:
         if st != 0:
             raise HackError(st, self.lib.hack_strerror(st).decode())
         self.ctx = ctx
+        self._info = (head_dim, heads, device, self.torch_dtype, torch.float32, torch.int32, torch.uint8)
 
     def close(self):
         if getattr(self, "ctx", None):
@@ -436,68 +426,47 @@ class Hack:
         self._check(self.lib.hack_head_variance(self.ctx, B, Nk, _dev(q), C.byref(cs), scale, _dev(sigma), _stream()))
 
     # ---- rotary positions, norms ----
-    def _rows(self, x, out, weight=None) -> hack_rows:
-        """x: [B, heads, N, head_dim] in any strides with the head's elements side by side; out: the same shape, contiguous."""
-        assert x.is_cuda and x.dim() == 4 and x.stride(3) == 1 and x.shape[3] == self.head_dim and x.dtype == self.torch_dtype, \
-            "rows: [B, heads, N, head_dim] of the context's element type, head_dim side by side"
-        assert out.shape == x.shape and out.dtype == x.dtype, "out: the shape and element type of x"
-        ws = 0
-        if weight is not None:
-            assert weight.is_cuda and weight.dtype.itemsize == 4 and weight.is_floating_point(), "weight: float32"
-            assert weight.shape[-1] == self.head_dim and weight.stride(-1) == 1 and (weight.dim() == 1 or weight.dim() == 2 and weight.shape[0] == x.shape[1])
-            ws = weight.stride(0) if weight.dim() == 2 else 0
-        # a dimension of one element may have any stride
-        s = [x.stride(i) if x.shape[i] > 1 else 0 for i in (0, 1, 2)]
-        return hack_rows(x.data_ptr(), _dev(out), x.shape[1], s[0], s[1], s[2], None if weight is None else weight.data_ptr(), ws)
-
-    @staticmethod
-    def _positions(pos, B: int, N: int, axes: int):
-        """(address, stride) of positions [axes, N], the same for all batch elements, or [B, axes, N]; with one axis also [N]."""
-        if pos is None:
-            return None, 0
-        assert pos.dtype.itemsize == 4 and not pos.is_floating_point(), "positions: int32"
-        shape = tuple(pos.shape)
-        assert shape in ((axes, N), (B, axes, N)) or axes == 1 and shape == (N,), "positions: [axes, N] or [B, axes, N]"
-        return _dev(pos), axes * N if len(shape) == 3 else 0
-
     def rotate(self, x, rope: Rope, out, pos=None, pos0: int = 0):
-        """out <- the rows of x rotated (x: [B, heads, N, head_dim], any strides; out may be x if that is contiguous)."""
-        B, _, N, _ = x.shape
-        p, stride = self._positions(pos, B, N, rope.axes)
-        self._check(self.lib.hack_rotate(self.ctx, B, N, C.byref(self._rows(x, out)), C.byref(rope._struct), p, stride, pos0, _stream()))
+        """out <- the rows of x rotated.  x: [B, heads, N, head_dim] in any strides with head_dim side by side; out: the same shape, contiguous (x itself if
+        that is).  pos: int32 [axes, N] for all batch elements or [B, axes, N], with one axis also [N]; None: pos0, pos0 + 1, ..."""
+        st = _ops_call.rotate(_ops_addr["rotate"], self.ctx and self.ctx.value, self._info, x, out, None, None, None, None, -1, 0.0, rope.address, rope.axes,
+                              pos, pos0, _stream())
+        if st != 0:
+            self._check(st)
 
     def norm_rotate(self, q, k, norm: str, eps: float, q_weight, k_weight, rope: Optional[Rope], q_out, k_out, pos=None, pos0: int = 0):
-        """Norms ("rms" or "l2") of the rows of q and k (or None), then their rotation (rope None: norms alone)."""
-        B, _, N, _ = q.shape
-        assert k is None or (k.shape[0], k.shape[2]) == (B, N)
-        p, stride = self._positions(pos, B, N, rope.axes) if rope is not None else (None, 0)
-        self._check(self.lib.hack_norm_rotate(self.ctx, B, N, C.byref(self._rows(q, q_out, q_weight)),
-                                              None if k is None else C.byref(self._rows(k, k_out, k_weight)), NORMS[norm], eps,
-                                              None if rope is None else C.byref(rope._struct), p, stride, pos0, _stream()))
+        """Norms ("rms" or "l2") of the rows of q and k (or None), then their rotation (rope None: norms alone).  Operands as in rotate; weights: float32
+        [head_dim] or [heads, head_dim], None: ones."""
+        st = _ops_call.rotate(_ops_addr["norm_rotate"], self.ctx and self.ctx.value, self._info, q, q_out, q_weight, k, k_out, k_weight, NORMS[norm], eps,
+                              None if rope is None else rope.address, 1 if rope is None else rope.axes, pos, pos0, _stream())
+        if st != 0:
+            self._check(st)
 
     # ---- caches in 4 bits ----
     def pack(self, B: int, Nk: int, packed: PackedCache, cache_in: Optional[Cache] = None, kept_idx=None, k_new=None, v_new=None,
              pos_new: int = 0, at=None):
-        """Rows of cache_in and new ones, all in order or those of kept_idx, become rows at[u] .. packed.len[u] of unit u."""
-        assert packed.head_dim == self.head_dim
-        ci, cp = None if cache_in is None else cache_in.struct(), packed.struct()
-        a = None if at is None else _i32(at)
-        self._check(self.lib.hack_pack(self.ctx, B, Nk, None if ci is None else C.byref(ci), _dev(k_new), _dev(v_new), pos_new, _dev(kept_idx),
-                                       0 if kept_idx is None else kept_idx.stride(0), _p(a, C.c_int32), C.byref(cp), _stream()))
+        """Rows of cache_in and new ones ([B, heads, Nk, head_dim]), all in order or those of kept_idx, become rows at[u] .. packed.len[u] of unit u."""
+        args = (_ops_addr["pack"], self.ctx and self.ctx.value, self._info, B, Nk, cache_in, k_new, v_new, pos_new, kept_idx)
+        st = _ops_call.pack(*args, at, packed, _stream())
+        if st is None:
+            st = _ops_call.pack(*args, _i32(at), packed, _stream())
+        if st != 0:
+            self._check(st)
 
     def unpack(self, B: int, packed: PackedCache, cache_out: Cache, first=None):
         """Rows first[u] .. first[u] + cache_out.len[u] of every unit, as rows of the context's element type."""
-        assert packed.head_dim == self.head_dim
-        cp, co = packed.struct(), cache_out.struct()
-        f = None if first is None else _i32(first)
-        self._check(self.lib.hack_unpack(self.ctx, B, C.byref(cp), _p(f, C.c_int32), C.byref(co), _stream()))
+        args = (_ops_addr["unpack"], self.ctx and self.ctx.value, self._info, B, packed)
+        st = _ops_call.unpack(*args, first, cache_out, _stream())
+        if st is None:
+            st = _ops_call.unpack(*args, _i32(first), cache_out, _stream())
+        if st != 0:
+            self._check(st)
 
     def attn_packed(self, q, packed: PackedCache, scale: float, out):
         """q: [B, G heads, N, head_dim], G query heads to each cache."""
-        B, H, N, d = q.shape
-        assert packed.head_dim == self.head_dim == d and H % self.heads == 0 and out.shape == q.shape
-        cp = packed.struct()
-        self._check(self.lib.hack_attn_packed(self.ctx, B, H // self.heads * N, _dev(q), C.byref(cp), scale, _dev(out), _stream()))
+        st = _ops_call.attn(_ops_addr["attn_packed"], self.ctx and self.ctx.value, self._info, q, packed, scale, out, _stream())
+        if st != 0:
+            self._check(st)
 
     # ---- a5 ----
     def managed_cache(self, cap, with_pos: bool = True) -> ManagedCache:

@@ -12,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_NAME = "libhack_mi355x.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
 STEP_CALL_PATH = os.path.join(HERE, "_step_call.so")   # CPython entry to hack_step
+OPS_CALL_PATH = os.path.join(HERE, "_ops_call.so")     # CPython entries to the operators around the cache
 SOURCES = ["hack_api.cpp", "kernels_move.hip", "kernels_select.hip", "kernels_score.hip", "kernels_attn.hip", "kernels_attn_split.hip", "kernels_attn_f32.hip", "kernels_step.hip",
            "kernels_headvar.hip", "kernels_merge.hip", "ops_api.cpp", "kernels_rotate.hip", "kernels_packed.hip", "kernels_attn_packed.hip", "kernels_attn_packed_tiles.hip"]
 
@@ -50,7 +51,7 @@ def _compile(src: str, objdir: str, extra) -> str:
 
 
 def build(verbose: bool = False, extra_flags=()) -> str:
-    """Compile every source for gfx950, link libhack_mi355x.so and the CPython step entry next to this file."""
+    """Compile every source for gfx950, link libhack_mi355x.so and the CPython entries next to this file."""
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
@@ -61,13 +62,13 @@ def build(verbose: bool = False, extra_flags=()) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB_PATH)
-    tmp = STEP_CALL_PATH + ".tmp"
-    cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"],
-           os.path.join(CSRC, "py_step.cpp"), "-o", tmp]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"g++ failed for py_step.cpp:\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, STEP_CALL_PATH)
+    for path, src in ((STEP_CALL_PATH, "py_step.cpp"), (OPS_CALL_PATH, "py_ops.cpp")):
+        tmp = path + ".tmp"
+        cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, src), "-o", tmp]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"g++ failed for {src}:\n{r.stdout}\n{r.stderr}")
+        os.replace(tmp, path)
     if verbose:
         print(f"built {LIB_PATH}")
     return LIB_PATH
