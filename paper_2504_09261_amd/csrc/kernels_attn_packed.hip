@@ -251,6 +251,12 @@ __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N>
   const float4* const po = reinterpret_cast<const float4*>(a.part_o + part0 * D) + lane;
   __shared__ float4 o_sh[SIDE][LPR];
   __shared__ float f_sh[kFactors], m_sh[4], l_sh[4];
+  // The first results are on their way while the factors are formed.
+  constexpr int kEarly = 8;
+  float4 early[kEarly];
+#pragma unroll
+  for (int i = 0; i < kEarly; ++i)
+    if (c0 + i * SIDE < n) early[i] = po[(int64_t)(c0 + i * SIDE) * q_rows * LPR];
   float M = -FLT_MAX, L = 0.f;
   for (int c = tid; c < n; c += 256) M = fmaxf(M, ml[(int64_t)c * q_rows].x);
 #pragma unroll
@@ -259,9 +265,15 @@ __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N>
   __syncthreads();
   M = fmaxf(fmaxf(m_sh[0], m_sh[1]), fmaxf(m_sh[2], m_sh[3]));
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float f, const float4& x) {
+    o.x = fmaf(f, x.x, o.x);
+    o.y = fmaf(f, x.y, o.y);
+    o.z = fmaf(f, x.z, o.z);
+    o.w = fmaf(f, x.w, o.w);
+  };
   for (int base = 0; base < n; base += kFactors) {
     const int here = min(kFactors, n - base);
-    __syncthreads();   // the last ones have been used
+    if (base > 0) __syncthreads();   // the last ones have been used
     for (int c = tid; c < here; c += 256) {
       const float2 x = ml[(int64_t)(base + c) * q_rows];
       const float f = __builtin_amdgcn_exp2f(x.x - M);
@@ -269,15 +281,15 @@ __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N>
       L = fmaf(f, x.y, L);
     }
     __syncthreads();
-#pragma unroll 4
-    for (int c = c0; c < here; c += SIDE) {
-      const float f = f_sh[c];
-      const float4 x = po[(int64_t)(base + c) * q_rows * LPR];
-      o.x = fmaf(f, x.x, o.x);
-      o.y = fmaf(f, x.y, o.y);
-      o.z = fmaf(f, x.z, o.z);
-      o.w = fmaf(f, x.w, o.w);
+    int c = c0;
+    if (base == 0) {
+#pragma unroll
+      for (int i = 0; i < kEarly; ++i)
+        if (c0 + i * SIDE < n) add(f_sh[c0 + i * SIDE], early[i]);
+      c = c0 + kEarly * SIDE;
     }
+#pragma unroll 4
+    for (; c < here; c += SIDE) add(f_sh[c], po[(int64_t)(base + c) * q_rows * LPR]);
   }
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) L += __shfl_xor(L, x, 64);

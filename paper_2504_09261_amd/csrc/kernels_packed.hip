@@ -14,6 +14,7 @@ namespace {
 using namespace dev;
 
 constexpr int kThreads = 256;
+constexpr int64_t kL2Bytes = 32 << 20;   // of eight XCDs: larger outputs pass the caches by
 
 template <typename T> __device__ __forceinline__ void load8(const T* p, float* v);
 template <> __device__ __forceinline__ void load8<float>(const float* p, float* v) {
@@ -86,15 +87,19 @@ __global__ __launch_bounds__(kThreads) void pack_rows(const PackArgs<N> a) {
     a.packed.pos[(int64_t)u.block * kPackRows + to] = cached ? a.plain.pos[row] : a.pos_new + (src - u.len_in);
 }
 
-__device__ __forceinline__ void store8(__bf16* p, unsigned w, float scale) { *reinterpret_cast<bf16x8*>(p) = codes_bf16(w, scale); }
-__device__ __forceinline__ void store8(float* p, unsigned w, float scale) {
+template <bool STREAM, typename V> __device__ __forceinline__ void put(V* p, const V& x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, p);
+  else *p = x;
+}
+template <bool STREAM> __device__ __forceinline__ void store8(__bf16* p, unsigned w, float scale) { put<STREAM>(reinterpret_cast<bf16x8*>(p), codes_bf16(w, scale)); }
+template <bool STREAM> __device__ __forceinline__ void store8(float* p, unsigned w, float scale) {
   const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1),
              c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-  reinterpret_cast<float4*>(p)[0] = make_float4(a[0], a[1], b[0], b[1]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(c[0], c[1], d[0], d[1]);
+  put<STREAM>(reinterpret_cast<floatx4*>(p), floatx4{a[0], a[1], b[0], b[1]});
+  put<STREAM>(reinterpret_cast<floatx4*>(p) + 1, floatx4{c[0], c[1], d[0], d[1]});
 }
 
-template <typename T, int D, int N>
+template <typename T, int D, int N, bool STREAM>
 __global__ __launch_bounds__(kThreads) void unpack_rows(const PackArgs<N> a) {
   constexpr int LPR = D / 8, RPG = kThreads / LPR;
   const PackUnit u = a.unit[blockIdx.y];
@@ -108,8 +113,8 @@ __global__ __launch_bounds__(kThreads) void unpack_rows(const PackArgs<N> a) {
   const unsigned wk = *reinterpret_cast<const unsigned*>(pk + at), wv = *reinterpret_cast<const unsigned*>(pv + at);
   const float sk = scale_of(pk[ex]), sv = scale_of(pv[ex]);
   const int64_t row = u.row0 + i;
-  store8(static_cast<T*>(a.plain.k) + row * D + 8 * c, wk, sk);
-  store8(static_cast<T*>(a.plain.v) + row * D + 8 * c, wv, sv);
+  store8<STREAM>(static_cast<T*>(a.plain.k) + row * D + 8 * c, wk, sk);
+  store8<STREAM>(static_cast<T*>(a.plain.v) + row * D + 8 * c, wv, sv);
   if (a.plain.pos != nullptr && a.packed.pos != nullptr && c == 0) a.plain.pos[row] = a.packed.pos[(int64_t)u.block * kPackRows + from];
 }
 
@@ -118,15 +123,18 @@ void launch_some(hipStream_t s, bool pack, const PackHead& h, const PackUnit* un
   PackArgs<N> a;
   static_cast<PackHead&>(a) = h;
   int rows = 0;
+  int64_t all = 0;
   for (int i = 0; i < n_units; ++i) {
     a.unit[i] = units[i];
     rows = std::max(rows, units[i].n);
+    all += units[i].n;
   }
   if (rows == 0) return;
   constexpr int per = kThreads / (D / 8);
   const dim3 grid((rows + per - 1) / per, n_units);
   if (pack) hipLaunchKernelGGL((pack_rows<T, D, N>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((unpack_rows<T, D, N>), grid, dim3(kThreads), 0, s, a);
+  else if (2 * all * D * (int64_t)sizeof(T) > kL2Bytes) hipLaunchKernelGGL((unpack_rows<T, D, N, true>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((unpack_rows<T, D, N, false>), grid, dim3(kThreads), 0, s, a);
 }
 
 template <typename T, int D>
