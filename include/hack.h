@@ -90,7 +90,8 @@ typedef struct {
  * merge workspace and the partial-result slots of cut attention work items:
  * 2 x resident work-groups x 128 x head_dim floats, 64 MiB at head_dim 128 on
  * MI355X; for fp32 contexts the logits of short units, 16 KiB per 64 keys and
- * unit, 10 MiB at most).  Returns HACK_EINVAL for an
+ * unit, 10 MiB at most, and the partial results of units that hack_attn_packed
+ * cuts, 16.25 MiB at head_dim 128).  Returns HACK_EINVAL for an
  * unsupported head_dim/dtype/n_obs or non-positive sizes, HACK_EHIP if the
  * device cannot be used. */
 hack_status hack_create(hack_ctx** out, const hack_config* cfg);
@@ -496,7 +497,7 @@ hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_cache* in, c
  * cache: queries [B, G H, N, d] of G heads to each of the H caches are [B, H, G N, d],
  * so N_k = G N.  The values that packing rounds to are bf16 numbers, so the accuracy is
  * hack_attn's over the rows that hack_unpack gives.  Results are reproducible bit for bit.
- * bf16 contexts only (HACK_EUNSUPPORTED).  Errors: HACK_EINVAL, HACK_ECAPACITY as above. */
+ * Errors: HACK_EINVAL, HACK_ECAPACITY as above. */
 hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, const void* q, const hack_packed_cache* kv,
                              float scale, void* out, hack_stream stream);
 

@@ -34,6 +34,7 @@ constexpr int kIotaRows = 32768;                 // rows a unit that keeps every
 // takes 0.16 us (launches that give up after 4096 and 16384 polls: 695 and 2662 us), so the wait lasts 96 ms; real ones last a few
 // microseconds, longer only where other work keeps the unit's other work-groups from running.
 constexpr int kScoreSpinLimit = 600000;
+constexpr int64_t kF32PartRows = 2048 * 16;      // partial results of units that attention over a packed cache cuts, fp32 contexts: 2048 work-groups of 16 queries
 
 }  // namespace
 
@@ -544,10 +545,16 @@ extern "C" hack_status hack_create(hack_ctx** out, const hack_config* cfg) {
     ctx->attn_slots = attn_stream_slots(cfg->head_dim);
     if (hipDeviceGetAttribute(&ctx->lds_bytes, hipDeviceAttributeMaxSharedMemoryPerBlock, cfg->device) != hipSuccess) ctx->lds_bytes = 0;
     const size_t n_part = 2 * (size_t)std::max(ctx->attn_slots, 1);
+    ctx->part_rows = (int64_t)n_part * 128;
     e = hipMalloc((void**)&ctx->part_o, n_part * 128 * cfg->head_dim * sizeof(float));
     if (e == hipSuccess) e = hipMalloc((void**)&ctx->part_ml, n_part * 256 * sizeof(float));
     if (e == hipSuccess) e = hipMalloc((void**)&ctx->part_count, (n_part / 2) * sizeof(unsigned));
     if (e == hipSuccess) e = hipMemset(ctx->part_count, 0, (n_part / 2) * sizeof(unsigned));
+  }
+  if (e == hipSuccess && cfg->dtype == HACK_F32) {   // attention over packed caches alone cuts units
+    ctx->part_rows = kF32PartRows;
+    e = hipMalloc((void**)&ctx->part_o, (size_t)ctx->part_rows * cfg->head_dim * sizeof(float));
+    if (e == hipSuccess) e = hipMalloc((void**)&ctx->part_ml, (size_t)ctx->part_rows * 2 * sizeof(float));
   }
   if (e == hipSuccess) e = hipHostMalloc((void**)&ctx->fault, 2 * sizeof(int), hipHostMallocDefault);
   if (e == hipSuccess) ctx->fault[0] = ctx->fault[1] = 0;
@@ -565,11 +572,11 @@ extern "C" hack_status hack_create(hack_ctx** out, const hack_config* cfg) {
   if (e == hipSuccess) e = hipEventCreateWithFlags(&ctx->ev_fork, hipEventDisableTiming);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&ctx->ev_join, hipEventDisableTiming);
   if (e == hipSuccess) e = score_static_setup(cfg->device);   // device address of the library's fixed scratch array
+  if (hipDeviceGetAttribute(&ctx->cus, hipDeviceAttributeMultiprocessorCount, cfg->device) != hipSuccess || ctx->cus < 1) ctx->cus = 1;
   if (e == hipSuccess && cfg->dtype == HACK_BF16) {
     // a unit's score items wait for each other inside one launch, so a launch may
     // hold at most as many items as the device keeps resident at once
     for (int i = 0; i < kScoreSizes; ++i) ctx->score_capacity[i] = score_fused_capacity(cfg->head_dim, kScoreItemKeys[i]);
-    if (hipDeviceGetAttribute(&ctx->cus, hipDeviceAttributeMultiprocessorCount, cfg->device) != hipSuccess || ctx->cus < 1) ctx->cus = 1;
     // the largest unit must fit one launch with the largest items
     const int per_unit = (cfg->max_cache_len + 255) / 256 + 3;
     if (ctx->score_capacity[kScoreSizes - 1] < per_unit || (per_unit + 3) / 4 > score_max_groups()) e = hipErrorInvalidConfiguration;

@@ -73,8 +73,9 @@ struct hack_ctx {
   int attn_stream = -1;          // HACK_ATTN_STREAM; -1 (default): cut single work items where the pair model gains, 0: never, 1: equal runs
                                  // for every launch of the 128-query kernel, 2: A/B aid, 4: every cut the model likes (see use_stream_attention)
   int attn_slots = 0;            // work-groups of the streamed kernel the device holds at once
-  float* part_o = nullptr;       // [2 * attn_slots, 128, head_dim] unnormalised partial outputs
-  float* part_ml = nullptr;      // [2 * attn_slots, 2, 128] their references and normalisers
+  float* part_o = nullptr;       // [2 * attn_slots, 128, head_dim] unnormalised partial outputs (fp32 contexts: [part_rows, head_dim])
+  float* part_ml = nullptr;      // [2 * attn_slots, 2, 128] their references and normalisers ([part_rows, 2])
+  int64_t part_rows = 0;         // rows of part_o
   unsigned* part_count = nullptr; // [attn_slots] ticket counters, zero between launches
   // hack_step overlap: the compression chain of one group of units runs beside the attention of the other group
   int lds_bytes = 0;             // of a work-group, as the device has it

@@ -2,7 +2,8 @@
 // the rows: packed_device.h).
 //
 // A code times its power of two is a bf16 number, so K and V enter the 16x16x32 bf16 matrix instructions exactly; what is rounded is what
-// attention over bf16 rows rounds, the probabilities and the output.
+// attention over bf16 rows rounds, the probabilities and the output.  In a float32 context queries and probabilities enter as three bf16 pieces each, which add up
+// to them exactly, so products and sums are those of float32.
 //
 // A work-group takes 16 NQ queries of a unit and a chunk of its keys, its four waves every fourth block of 64 keys.  K comes from
 // memory in the order of the A operand of S^T = K Q^T: conversion is all that stands between the load and the product.  V^T needs
@@ -37,9 +38,37 @@ template <int D> struct PackedRows {   // a lane's share of a block of 64 rows
   __device__ __forceinline__ float scale(int t) const { return scale_of((exponents >> (8 * t)) & 255u); }
 };
 
-template <int D, int NQ, int N>
-__global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void attn_packed(const AttnPackedArgs<N> a) {
-  constexpr int KC = D / 32, MT = D / 16, QROWS = 16 * NQ;
+// A number as a sum of bf16 pieces: itself, or three pieces of eight bits each, exactly.  (Cut, not rounded: a piece never passes the number.)
+template <typename T> struct Pieces;
+template <> struct Pieces<__bf16> {
+  static constexpr int kCount = 1;
+  static __device__ __forceinline__ void load(const __bf16* p, bf16x8 (&f)[1]) { f[0] = *reinterpret_cast<const bf16x8*>(p); }
+  static __device__ __forceinline__ void split(float x, int j, bf16x8 (&f)[1]) { f[0][j] = (__bf16)x; }
+};
+template <> struct Pieces<float> {
+  static constexpr int kCount = 3;
+  static __device__ __forceinline__ void split(float x, int j, bf16x8 (&f)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const unsigned top = __builtin_bit_cast(unsigned, x) & 0xFFFF0000u;
+      f[i][j] = __builtin_bit_cast(__bf16, (unsigned short)(top >> 16));
+      x -= __builtin_bit_cast(float, top);
+    }
+  }
+  static __device__ __forceinline__ void load(const float* p, bf16x8 (&f)[3]) {
+    const floatx4 a = reinterpret_cast<const floatx4*>(p)[0], b = reinterpret_cast<const floatx4*>(p)[1];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) split(j < 4 ? a[j] : b[j - 4], j, f);
+  }
+};
+__device__ __forceinline__ void store4(__bf16* p, const floatx4& x, float f) {
+  *reinterpret_cast<bf16x4*>(p) = bf16x4{(__bf16)(x[0] * f), (__bf16)(x[1] * f), (__bf16)(x[2] * f), (__bf16)(x[3] * f)};
+}
+__device__ __forceinline__ void store4(float* p, const floatx4& x, float f) { *reinterpret_cast<floatx4*>(p) = floatx4{x[0] * f, x[1] * f, x[2] * f, x[3] * f}; }
+
+template <typename T, int D, int NQ, int N>
+__global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 64 ? 4 : 3) void attn_packed(const AttnPackedArgs<N> a) {
+  constexpr int KC = D / 32, MT = D / 16, QROWS = 16 * NQ, NP = Pieces<T>::kCount;
   constexpr int SLOT = (NQ == 2 ? 64 : 32) * D;   // elements: 32 rows of V, then the wave's partial results
   // The query tiles of a unit and a chunk follow each other on an XCD (work-group id mod 8).
   const int local = blockIdx.x >> 3, pair = (local / a.q_tiles) * 8 + (blockIdx.x & 7), q_tile = local % a.q_tiles;
@@ -70,12 +99,12 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void at
     vr.load(vb, lane);
   }
   // Queries as the B operand, in the order in which the lane's quarter of a key comes: element 8 s + j of quarter g
-  bf16x8 qf[NQ][KC];
+  bf16x8 qf[NQ][KC][NP];
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
-    const __bf16* row = static_cast<const __bf16*>(a.q) + (row0 + min(q0 + 16 * qt + col, a.N_k - 1)) * D + g * (D / 4);
+    const T* row = static_cast<const T*>(a.q) + (row0 + min(q0 + 16 * qt + col, a.N_k - 1)) * D + g * (D / 4);
 #pragma unroll
-    for (int s = 0; s < KC; ++s) qf[qt][s] = *reinterpret_cast<const bf16x8*>(row + 8 * s);
+    for (int s = 0; s < KC; ++s) Pieces<T>::load(row + 8 * s, qf[qt][s]);
   }
   SplitStage<D, NQ> att;
   att.init(a.scale, lane);
@@ -98,7 +127,9 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void at
       for (int s = 0; s < KC; ++s) {
         const bf16x8 kf = codes_bf16(kr.slice(t, s), scale);
 #pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qt][s], sc[t][qt], 0, 0, 0);
+        for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+          for (int i = NP - 1; i >= 0; --i) sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qt][s][i], sc[t][qt], 0, 0, 0);
       }
     }
     const int left = len - b * kPackRows;   // rows of this block and behind it
@@ -158,23 +189,28 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void at
         vb += kWaves * kPackBytes<D>;
         if (more) vr.load(vb, lane);
       }
-      bf16x8 pf[NQ];
+      bf16x8 pf[NQ][NP];
 #pragma unroll
       for (int qt = 0; qt < NQ; ++qt)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) pf[qt][j] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[2 * h + (j >> 2)][qt][j & 3], att.c2, -att.mc[qt]));
+        for (int j = 0; j < 8; ++j) Pieces<T>::split(__builtin_amdgcn_exp2f(fmaf(sc[2 * h + (j >> 2)][qt][j & 3], att.c2, -att.mc[qt])), j, pf[qt]);
       if (h == 0) {
         kb += kWaves * kPackBytes<D>;
         if (more) kr.load(kb, lane);
       }
-      att.row_sums(pf);
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt)   // over the numbers that the PV product uses
+#pragma unroll
+        for (int i = NP - 1; i >= 0; --i) att.ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(att.ones, pf[qt][i], att.ls[qt], 0, 0, 0);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         const __bf16* const at = slot + 128 * (mt >> 1) + (mt & 1 ? v_odd : v_even);
         const bf16x4 v0 = lds_read_tr(at), v1 = lds_read_tr(at + 16 * D);
         const bf16x8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
 #pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) att.o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], att.o[mt][qt], 0, 0, 0);
+        for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+          for (int i = NP - 1; i >= 0; --i) att.o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt][i], att.o[mt][qt], 0, 0, 0);
       }
     }
   };
@@ -229,7 +265,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void at
       acc[3] = fmaf(f[x], p.w, acc[3]);
     }
     if (qi >= a.N_k) continue;
-    if (whole) att.store(static_cast<__bf16*>(a.out) + (row0 + qi) * D, mt, acc, inv);
+    if (whole) store4(static_cast<T*>(a.out) + (row0 + qi) * D + 16 * mt + 4 * g, acc, inv);
     else *reinterpret_cast<floatx4*>(a.part_o + part * D + 16 * mt + 4 * g) = acc;
   }
   if (!whole && w < NQ && g == 0 && qi < a.N_k) {
@@ -240,7 +276,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : D == 64 ? 4 : 3) void at
 
 // Rows of units that were cut: a work-group takes one query, D / 4 lanes a chunk.
 constexpr int kFactors = 1024;   // chunks whose factors are kept in LDS at a time
-template <int D, int N>
+template <typename T, int D, int N>
 __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N> a, int q_rows) {
   constexpr int LPR = D / 4, SIDE = 256 / LPR;   // chunks at a time
   const int ui = blockIdx.y, n = chunks_of(packed_blocks(a.unit[ui].len), a.chunk);
@@ -306,31 +342,40 @@ __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N>
     o.w += p.w;
   }
   const float inv = 1.f / (l_sh[0] + l_sh[1] + l_sh[2] + l_sh[3]);
-  __bf16* row = static_cast<__bf16*>(a.out) + ((int64_t)a.unit[ui].unit * a.N_k + qi) * D;
-  *reinterpret_cast<bf16x4*>(row + 4 * lane) = bf16x4{(__bf16)(o.x * inv), (__bf16)(o.y * inv), (__bf16)(o.z * inv), (__bf16)(o.w * inv)};
+  store4(static_cast<T*>(a.out) + ((int64_t)a.unit[ui].unit * a.N_k + qi) * D + 4 * lane, floatx4{o.x, o.y, o.z, o.w}, inv);
 }
 
-template <int D, int N>
+template <typename T, int D, int N>
 void launch_some(hipStream_t s, int queries, const AttnPackedHead& h, const AttnPackedUnit* units) {
   AttnPackedArgs<N> a;
   static_cast<AttnPackedHead&>(a) = h;
   for (int i = 0; i < h.n_units; ++i) a.unit[i] = units[i];
   const int pairs = h.n_units * h.n_chunks;
   const dim3 grid((pairs + 7) / 8 * 8 * h.q_tiles), block(64 * kWaves);
-  if (queries == kTileQueries) launch_attn_packed_tiles(s, D, h, units);
-  else if (queries == 16) hipLaunchKernelGGL((attn_packed<D, 1, N>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((attn_packed<D, 2, N>), grid, block, 0, s, a);
-  if (h.n_chunks > 1) hipLaunchKernelGGL((attn_packed_merge<D, N>), dim3(h.N_k, h.n_units), dim3(256), 0, s, a, queries);
+  if constexpr (sizeof(T) == 4) {
+    hipLaunchKernelGGL((attn_packed<T, D, 1, N>), grid, block, 0, s, a);
+  } else {
+    if (queries == kTileQueries) launch_attn_packed_tiles(s, D, h, units);
+    else if (queries == 16) hipLaunchKernelGGL((attn_packed<T, D, 1, N>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((attn_packed<T, D, 2, N>), grid, block, 0, s, a);
+  }
+  if (h.n_chunks > 1) hipLaunchKernelGGL((attn_packed_merge<T, D, N>), dim3(h.N_k, h.n_units), dim3(256), 0, s, a, queries);
+}
+
+template <typename T>
+void launch_typed(hipStream_t s, int head_dim, int queries, const AttnPackedHead& h, const AttnPackedUnit* units) {
+  const bool few = h.n_units <= kFewUnits;
+  if (head_dim == 64 && few) launch_some<T, 64, kFewUnits>(s, queries, h, units);
+  else if (head_dim == 64) launch_some<T, 64, kAttnPackedUnits>(s, queries, h, units);
+  else if (few) launch_some<T, 128, kFewUnits>(s, queries, h, units);
+  else launch_some<T, 128, kAttnPackedUnits>(s, queries, h, units);
 }
 
 }  // namespace
 
-void launch_attn_packed(hipStream_t s, int head_dim, int queries, const AttnPackedHead& h, const AttnPackedUnit* units) {
-  const bool few = h.n_units <= kFewUnits;
-  if (head_dim == 64 && few) launch_some<64, kFewUnits>(s, queries, h, units);
-  else if (head_dim == 64) launch_some<64, kAttnPackedUnits>(s, queries, h, units);
-  else if (few) launch_some<128, kFewUnits>(s, queries, h, units);
-  else launch_some<128, kAttnPackedUnits>(s, queries, h, units);
+void launch_attn_packed(hipStream_t s, int elem_bytes, int head_dim, int queries, const AttnPackedHead& h, const AttnPackedUnit* units) {
+  if (elem_bytes == 4) launch_typed<float>(s, head_dim, queries, h, units);
+  else launch_typed<__bf16>(s, head_dim, queries, h, units);
 }
 
 }  // namespace hack

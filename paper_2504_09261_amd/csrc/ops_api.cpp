@@ -160,7 +160,7 @@ bool units_overlap(int n_units, Lo lo, Hi hi) {
 int blocks_of(int len) { return (int)(((int64_t)len + kPackRows - 1) / kPackRows); }
 
 // Partial results of work-groups of so many queries that the workspace holds.
-int64_t partial_slots(const hack_ctx* ctx, int queries) { return 2 * (int64_t)std::max(ctx->attn_slots, 1) * 128 / queries; }
+int64_t partial_slots(const hack_ctx* ctx, int queries) { return ctx->part_rows / queries; }
 
 // How units are cut: into chunks that give each compute unit two work-groups (two are enough to read at the rate of the memory, and more start and end more
 // often: one token over 8 caches of 131071 rows, 512, 1024 and 2048 work-groups 31, 34 and 38 us), but not where cutting costs more than it gains: merging
@@ -207,6 +207,7 @@ double estimate_us(const hack_ctx* ctx, int queries, int n_units, int64_t blocks
 }
 
 int queries_per_group(const hack_ctx* ctx, const int32_t* len, int n_units, int N_k) {
+  if (ctx->cfg.dtype == HACK_F32) return 16;
   if (ctx->packed_queries != 0) return ctx->packed_queries;
   if (N_k <= 64) return N_k <= 16 ? 16 : 32;
   int64_t blocks, longest;
@@ -368,7 +369,6 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
                                         hack_stream stream) try {
   hack_status st = check_common(ctx, B, N_k, true);
   if (st != HACK_OK) return st;
-  if (ctx->cfg.dtype != HACK_BF16) return fail(ctx, HACK_EUNSUPPORTED, "attention over a packed cache is implemented for bf16 contexts");
   const int U = B * ctx->cfg.heads, d = ctx->cfg.head_dim;
   if (!q || !out) return fail(ctx, HACK_EINVAL, "q and out must not be NULL");
   if (!aligned16(q) || !aligned16(out)) return fail(ctx, HACK_EINVAL, "q/out must be 16-byte aligned");
@@ -376,7 +376,7 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
   if ((st = check_packed(ctx, kv, U, "kv")) != HACK_OK) return st;
   for (int u = 0; u < U; ++u)
     if (kv->len[u] < 1) return fail(ctx, HACK_EINVAL, "unit %d has an empty cache", u);
-  const int64_t bytes = (int64_t)U * N_k * d * 2;
+  const int64_t bytes = (int64_t)U * N_k * d * ctx->elem_bytes;
   const Range rq{(uintptr_t)q, (uintptr_t)q + (uintptr_t)bytes}, ro{(uintptr_t)out, (uintptr_t)out + (uintptr_t)bytes};
   if (rq.meets(ro)) return fail(ctx, HACK_EINVAL, "q and out overlap");
   if ((st = check_device(ctx)) != HACK_OK) return st;
@@ -402,7 +402,7 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
     plan_chunks(ctx, blocks, longest, slots, &a);
     order_units(ctx, len, a, &order, &count);
     for (int i = 0; i < a.n_units; ++i) units[i] = AttnPackedUnit{(int32_t)(kv->off[u0 + order[i]] / kPackRows), len[order[i]], u0 + order[i]};
-    launch_attn_packed(static_cast<hipStream_t>(stream), d, queries, a, units);
+    launch_attn_packed(static_cast<hipStream_t>(stream), ctx->elem_bytes, d, queries, a, units);
   }
   HIP_TRY(ctx, hipGetLastError());
   return HACK_OK;

@@ -68,7 +68,7 @@ struct PackHead {
 void launch_pack(hipStream_t s, int elem_bytes, int head_dim, PackHead h, const PackUnit* units, int n_units);
 void launch_unpack(hipStream_t s, int elem_bytes, int head_dim, PackHead h, const PackUnit* units, int n_units);
 
-// ---- attention over them (bf16 queries and outputs) -------------------------
+// ---- attention over them ----------------------------------------------------
 struct AttnPackedUnit {
   int32_t block;   // first block
   int32_t len;     // rows
@@ -77,7 +77,7 @@ struct AttnPackedUnit {
 struct AttnPackedHead {
   const uint8_t* k;
   const uint8_t* v;
-  const void* q;      // bf16
+  const void* q;
   void* out;
   float* part_o;      // [slot, queries of a work-group, head_dim] unnormalised partial outputs
   float* part_ml;     // [slot, queries of a work-group, 2] their references and normalisers
@@ -91,8 +91,8 @@ struct AttnPackedHead {
 // Units of a launch.  They travel by value; a launch takes 2.5 us to issue and 0.3 to 0.5 more for every KiB of arguments up to 8 (a table in memory
 // would be another copy each time a length grows), so there is a short list too.
 constexpr int kFewUnits = 64, kPackUnits = 640, kAttnPackedUnits = 1024;
-// queries: of a work-group, 16, 32 or kTileQueries
+// queries: of a work-group, 16, 32 or kTileQueries; float32 (elem_bytes 4): 16
 constexpr int kTileQueries = 128;
-void launch_attn_packed(hipStream_t s, int head_dim, int queries, const AttnPackedHead& h, const AttnPackedUnit* units);
+void launch_attn_packed(hipStream_t s, int elem_bytes, int head_dim, int queries, const AttnPackedHead& h, const AttnPackedUnit* units);
 void launch_attn_packed_tiles(hipStream_t s, int head_dim, const AttnPackedHead& h, const AttnPackedUnit* units);   // without the merge
 }  // namespace hack

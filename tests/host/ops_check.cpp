@@ -23,7 +23,7 @@ namespace hack {
 void launch_rotate(hipStream_t, int, int, bool, int, int, RotateArgs a) { stub::Quiet q; stub::rotations.push_back(a); }
 void launch_pack(hipStream_t, int, int, PackHead h, const PackUnit* u, int n) { stub::Quiet q; stub::packs.push_back({h, {u, u + n}}); }
 void launch_unpack(hipStream_t, int, int, PackHead h, const PackUnit* u, int n) { stub::Quiet q; stub::unpacks.push_back({h, {u, u + n}}); }
-void launch_attn_packed(hipStream_t, int, int n, const AttnPackedHead& h, const AttnPackedUnit* u) {
+void launch_attn_packed(hipStream_t, int, int, int n, const AttnPackedHead& h, const AttnPackedUnit* u) {
   stub::Quiet q;
   stub::attentions.push_back({h, {u, u + h.n_units}});
   stub::queries.push_back(n);
@@ -337,7 +337,8 @@ int attn_plan() {
   };
   hack_packed_cache kv = cache({100, 1, 5, 43});
   CHECK(attn(kv, 7) == HACK_OK);
-  REFUSED(HACK_EUNSUPPORTED, attn(kv, 7, 0.1f, nullptr, nullptr, f32.ctx));
+  CHECK(attn(kv, 7, 0.1f, nullptr, nullptr, f32.ctx) == HACK_OK && stub::queries.back() == 16);
+  REFUSED(HACK_EINVAL, attn(kv, 7, 0.1f, q, q + 4 * 7 * kD * 4 - 16, f32.ctx));
   REFUSED(HACK_EINVAL, hack_attn_packed(nullptr, 1, 7, q, &kv, 0.1f, out, kStream));
   REFUSED(HACK_EINVAL, hack_attn_packed(c.ctx, 1, 7, nullptr, &kv, 0.1f, out, kStream));
   REFUSED(HACK_EINVAL, hack_attn_packed(c.ctx, 1, 7, q, nullptr, 0.1f, out, kStream));
@@ -361,12 +362,12 @@ int attn_plan() {
   stub::device = 0;
   // Partial results fit the workspace, chunks cover the longest unit, and none is empty for it.
   const std::vector<std::vector<int32_t>> sets = {{1, 1, 1, 1}, {64, 65, 1, 3}, {100000, 1, 7, 700}, {2000000000, 1, 1, 1}, {511, 512, 513, 2}, {131071, 131071, 131071, 131071}};
-  for (const auto& s : sets)
+  for (hack_ctx* ctx : {c.ctx, f32.ctx}) for (const auto& s : sets)
     for (int N : {1, 16, 17, 33, 500}) {
       kv = cache(s);
       stub::attentions.clear();
       stub::queries.clear();
-      CHECK(attn(kv, N) == HACK_OK && stub::attentions.size() == 1);
+      CHECK(attn(kv, N, 0.1f, nullptr, nullptr, ctx) == HACK_OK && stub::attentions.size() == 1);
       const auto& a = stub::attentions[0];
       const int64_t queries = stub::queries[0], longest = (*std::max_element(s.begin(), s.end()) + 63LL) / 64;
       CHECK(a.q_tiles == (N + queries - 1) / queries && a.chunk >= 1 && a.n_chunks >= 1);

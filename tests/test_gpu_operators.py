@@ -362,13 +362,13 @@ def test_packed_sizes():
 
 
 # ---- attention ----------------------------------------------------------------
-def filled(hk, B, lens, d, g, order=None, scale=1.0):
+def filled(hk, B, lens, d, g, order=None):
     """A packed cache of random rows over memory that holds NaN everywhere else, and its rows."""
     pc = packed(lens, d, fill=0xFF, order=order, gap=64)
     off, rows = offsets(lens, 8)
-    k, v = (torch.randn((rows, d), generator=g, device=DEV) for _ in range(2))
-    hk.pack(B, 0, pc, cache_in=Cache((k * scale).bfloat16(), v.bfloat16(), off, lens))
-    return pc, [r[:2] for r in read_back(hk, B, pc, np.asarray(lens), "bf16")[0]]
+    k, v = (torch.randn((rows, d), generator=g, device=DEV).to(hk.torch_dtype) for _ in range(2))
+    hk.pack(B, 0, pc, cache_in=Cache(k, v, off, lens))
+    return pc, [r[:2] for r in read_back(hk, B, pc, np.asarray(lens), hk.dtype)[0]]
 
 
 def check_attention(q, rows, scale, out):
@@ -376,7 +376,10 @@ def check_attention(q, rows, scale, out):
     where they are summed: 2 2^-8 of sum p |v|; a score of d products is summed in float32: (d + 4) 2^-24 of sum |q k|, and an error of s is a factor
     e^s on its probability and on the sum; exponentials and sums in float32: 1e-5; the output: half a step.
     Probabilities are taken against a reference that lies up to 2^15 above the largest (many queries), and what is below 2^-126 then, float32's and bf16's
-    smallest normal number, may be zero: 2^-111 of each |v|."""
+    smallest normal number, may be zero: 2^-111 of each |v|.
+    float32: queries and probabilities are three exact pieces, so a score sums 3 d products, and the sums over T keys have 3 T / 32 steps of a matrix
+    instruction and 40 more of the merges, H each on the output and on the normaliser; the scale times log2 e is rounded twice: 2 H of a score on its exponent."""
+    exact = q.dtype == torch.float32
     q, o = to64(q), to64(out)
     d = q.shape[-1]
     for u, (k, v) in enumerate(rows):
@@ -384,13 +387,51 @@ def check_attention(q, rows, scale, out):
         p = np.exp(s - s.max(-1, keepdims=True))
         p /= p.sum(-1, keepdims=True)
         want = p @ v
-        slack = scale * (d + 4) * H * (np.abs(q[u]) @ np.abs(k).T).max(-1, keepdims=True)
-        tol = (2 * 2.0 ** -8 + 2 * slack + 1e-5) * (p @ np.abs(v)) * 1.01 + 2.0 ** -8 * 1.01 * np.abs(want) + 2.0 ** -111 * (1 + np.abs(v).sum(0))
+        slack = scale * ((3 * d if exact else d) + 4) * H * (np.abs(q[u]) @ np.abs(k).T).max(-1, keepdims=True)
+        rounding = 2 * (3 * len(k) / 32 + 40) * H + 4 * H * np.abs(s).max(-1, keepdims=True) if exact else 2 * 2.0 ** -8
+        half = HALF_STEP["f32" if exact else "bf16"]
+        tol = (rounding + 2 * slack + 1e-5) * (p @ np.abs(v)) * 1.01 + half * 1.01 * np.abs(want) + 2.0 ** -111 * (1 + np.abs(v).sum(0))
         err = np.abs(o[u] - want)
         assert (err <= tol).all(), (u, k.shape, float((err / tol).max()))
 
 
 LENGTHS = [[1, 2, 3, 15, 16, 17], [31, 32, 33, 63, 64, 65], [100, 511, 512, 513, 1, 64], [1000, 2000, 129, 900, 30, 4001], [20000, 1, 20001, 64, 7, 640]]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", LENGTHS, ids=lambda l: "-".join(map(str, l)))
+@pytest.mark.parametrize("n", [1, 16, 40])
+def test_float32_attention_over_a_packed_cache(contexts, d, lens, n):
+    hk = contexts(3, d, "f32")
+    g = torch.Generator(DEV).manual_seed(n)
+    pc, rows = filled(hk, 2, np.array(lens), d, g, order=[4, 2, 0, 1, 5, 3])
+    q = 2 * torch.randn((2, 3, n, d), generator=g, device=DEV)
+    out = torch.full_like(q, 9.0)
+    hk.attn_packed(q, pc, d ** -0.5, out)
+    check_attention(q.flatten(0, 1), rows, float(np.float32(d ** -0.5)), out.flatten(0, 1))
+    again = torch.full_like(q, -9.0)
+    hk.attn_packed(q, pc, d ** -0.5, again)
+    assert torch.equal(out, again)
+
+
+def test_float32_attention_of_odd_numbers(contexts):
+    """Queries that need all of their bits, are tiny, huge or no numbers: what is finite is right, the rest is NaN."""
+    hk = contexts(3, 64, "f32")
+    g = torch.Generator(DEV).manual_seed(2)
+    pc, rows = filled(hk, 1, np.array([70, 200, 33]), 64, g)
+    q = torch.randn((1, 3, 6, 64), generator=g, device=DEV)
+    q[0, :, 1] *= 1e-30
+    q[0, :, 2] = torch.nextafter(torch.ones(64, device=DEV), torch.full((64,), 2.0, device=DEV))
+    q[0, 0, 3, 5] = float("nan")
+    q[0, 1, 4, 6] = float("inf")
+    out = torch.empty_like(q)
+    hk.attn_packed(q, pc, 0.125, out)
+    bad = torch.zeros((3, 6), dtype=torch.bool, device=DEV)
+    bad[0, 3] = bad[1, 4] = True
+    assert torch.equal(torch.isnan(out[0]).all(-1), bad) and torch.isfinite(out[0][~bad]).all()
+    for u in range(3):
+        fine = ~bad[u].cpu()
+        check_attention(q[0, u][fine][None], [rows[u]], 0.125, out[0, u][fine][None])
 
 
 @pytest.mark.parametrize("d", [64, 128])
