@@ -5,16 +5,22 @@
 // attention over bf16 rows rounds, the probabilities and the output.  In a float32 context queries and probabilities enter as three bf16 pieces each, which add up
 // to them exactly, so products and sums are those of float32.
 //
-// A work-group takes 16 NQ queries of a unit and a chunk of its keys, its four waves every fourth block of 64 keys.  K comes from
+// A work-group takes 16 NQ queries of a unit and a chunk of its keys, its four waves every fourth block of 64 keys, each by itself.  K comes from
 // memory in the order of the A operand of S^T = K Q^T: conversion is all that stands between the load and the product.  V^T needs
-// keys side by side where memory has head-dim: each wave writes 32 converted rows to LDS and reads them with the transposing LDS read.  Scores,
-// probabilities and the PV product of 32 keys are those of SplitStage.  The partial results of the waves are merged through LDS, those of several chunks
-// of a unit in memory, by a launch of their own.
+// keys side by side where memory has head-dim: a wave writes the converted rows to LDS and reads them with the transposing LDS read, in the order of keys in
+// which the accumulators hold the probabilities.  One softmax update a block.  The next block's codes are loaded into the registers of this one's as soon as those have
+// been converted.  The partial results of the waves are merged through LDS, those of several chunks of a unit in memory, by a launch of their own.
+//
+// One token reads its cache once and is bound by that: 768 units of 4096 rows at head_dim 128 (428 MB) take 86 us, 5.0 TB/s, 512 units (285 MB, part of which the
+// last-level cache keeps from launch to launch) 46, and 58 and 44 where all units share one cache, so arithmetic is not far behind.  A block takes a wave 2.9 us with another work-group on the
+// compute unit and 1.6 alone.  Tried: four work-groups a compute unit (128 registers spill) 41 -> 56 us for 512 units of 900 to 4000 rows; V in two halves of
+// 32 rows, three work-groups a compute unit, equal within 3 %; the last work-group of a unit to end merges its chunks (tickets), 8.9 -> 9.6 us for 8 units of 4000 rows,
+// 13.6 -> 15.8 for 32.  K by the scaled matrix instruction, codes as they are and queries in two 8-bit or three 6-bit pieces: the sums keep 16 bits of the largest
+// product, or the pieces 14 of the largest query element, where bf16 operands lose nothing.
 #include <cfloat>
 #include <type_traits>
 
 #include "packed_device.h"
-#include "split_stage.h"
 
 namespace hack {
 
@@ -67,9 +73,9 @@ __device__ __forceinline__ void store4(__bf16* p, const floatx4& x, float f) {
 __device__ __forceinline__ void store4(float* p, const floatx4& x, float f) { *reinterpret_cast<floatx4*>(p) = floatx4{x[0] * f, x[1] * f, x[2] * f, x[3] * f}; }
 
 template <typename T, int D, int NQ, int N>
-__global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 64 ? 4 : 3) void attn_packed(const AttnPackedArgs<N> a) {
+__global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 64 ? 4 : 2) void attn_packed(const AttnPackedArgs<N> a) {
   constexpr int KC = D / 32, MT = D / 16, QROWS = 16 * NQ, NP = Pieces<T>::kCount;
-  constexpr int SLOT = (NQ == 2 ? 64 : 32) * D;   // elements: 32 rows of V, then the wave's partial results
+  constexpr int SLOT = 64 * D;   // elements: a block of V, then the wave's partial results
   // The query tiles of a unit and a chunk follow each other on an XCD (work-group id mod 8).
   const int local = blockIdx.x >> 3, pair = (local / a.q_tiles) * 8 + (blockIdx.x & 7), q_tile = local % a.q_tiles;
   if (pair >= a.n_units * a.n_chunks) return;
@@ -106,8 +112,20 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 6
 #pragma unroll
     for (int s = 0; s < KC; ++s) Pieces<T>::load(row + 8 * s, qf[qt][s]);
   }
-  SplitStage<D, NQ> att;
-  att.init(a.scale, lane);
+  floatx4 o[MT][NQ];   // O^T: head-dim 16 mt + 4 g + r, query 16 qt + col
+  floatx4 ls[NQ];      // row sums of P: all four rows hold the same
+  float mc[NQ];        // probabilities are 2^(c2 s - mc); finite from the start, so that keys whose score is -inf get 0
+  const float c2 = a.scale * kLog2eF;
+  bf16x8 ones;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) o[mt][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    ls[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    mc[qt] = -FLT_MAX;
+  }
   // V^T operand: rows 4 g + e and 16 + 4 g + e, head-dim 16 mt + 4 qd; even and odd mt
   const int qd = col & 3, v_even = v_chunk<D>(4 * g + (col >> 2), qd >> 1) + 4 * (qd & 1), v_odd = v_even ^ 16;
   __bf16* const slot = &ring[w][0];
@@ -133,20 +151,23 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 6
       }
     }
     const int left = len - b * kPackRows;   // rows of this block and behind it
-    auto v_rows = [&](int h) {   // rows 32 h ... of V, as bf16
-      wave_lds_order();   // the last reads of the slot
+    wave_lds_order();   // the last reads of the slot
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const int t = 2 * h + kt, r = 16 * kt + col;
-        const bool there = !RAGGED || 32 * h + r < left;
-        const float scale = there ? vr.scale(t) : 1.f;
+    for (int t = 0; t < 4; ++t) {   // V as bf16
+      const int r = 16 * t + col;
+      const bool there = !RAGGED || r < left;
+      const float scale = there ? vr.scale(t) : 1.f;
 #pragma unroll
-        for (int s = 0; s < KC; ++s)
-          *reinterpret_cast<bf16x8*>(&slot[v_chunk<D>(r, KC * g + s)]) = codes_bf16(there ? vr.slice(t, s) : 0u, scale);
-      }
-      wave_lds_order();
-    };
-    v_rows(0);
+      for (int s = 0; s < KC; ++s)
+        *reinterpret_cast<bf16x8*>(&slot[v_chunk<D>(r, KC * g + s)]) = codes_bf16(there ? vr.slice(t, s) : 0u, scale);
+    }
+    wave_lds_order();
+    kb += kWaves * kPackBytes<D>;
+    vb += kWaves * kPackBytes<D>;
+    if (more) {
+      kr.load(kb, lane);
+      vr.load(vb, lane);
+    }
     if constexpr (RAGGED) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -157,7 +178,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 6
             for (int qt = 0; qt < NQ; ++qt) sc[t][qt][r] = -INFINITY;
           }
     }
-    // The reference is the largest score so far (see SplitStage::follow).
+    // The reference is the largest score so far: the largest probabilities lie just below one, where bf16 rounds them finest.
     float m_new[NQ];
     bool moved = false;
 #pragma unroll
@@ -165,54 +186,46 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 6
       float mx = sc[0][qt][0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) mx = maximum(mx, sc[j >> 2][qt][j & 3]);
-      m_new[qt] = maximum(att.mc[qt], quad_maximum(mx) * att.c2);
-      moved |= m_new[qt] != att.mc[qt];
+      m_new[qt] = maximum(mc[qt], quad_maximum(mx) * c2);
+      moved |= m_new[qt] != mc[qt];
     }
     if (__any(moved)) {
 #pragma unroll
       for (int qt = 0; qt < NQ; ++qt) {
-        const float f = __builtin_amdgcn_exp2f(att.mc[qt] - m_new[qt]);
+        const float f = __builtin_amdgcn_exp2f(mc[qt] - m_new[qt]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          att.ls[qt][r] *= f;
+          ls[qt][r] *= f;
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) att.o[mt][qt][r] *= f;
+          for (int mt = 0; mt < MT; ++mt) o[mt][qt][r] *= f;
         }
-        att.mc[qt] = m_new[qt];
+        mc[qt] = m_new[qt];
       }
     }
+    bf16x8 pf[2][NQ][NP];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (h == 1) {
-        if (RAGGED && left <= 32) break;
-        v_rows(1);
-        vb += kWaves * kPackBytes<D>;
-        if (more) vr.load(vb, lane);
-      }
-      bf16x8 pf[NQ][NP];
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int qt = 0; qt < NQ; ++qt)
+      for (int qt = 0; qt < NQ; ++qt) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) Pieces<T>::split(__builtin_amdgcn_exp2f(fmaf(sc[2 * h + (j >> 2)][qt][j & 3], att.c2, -att.mc[qt])), j, pf[qt]);
-      if (h == 0) {
-        kb += kWaves * kPackBytes<D>;
-        if (more) kr.load(kb, lane);
+        for (int j = 0; j < 8; ++j)
+          Pieces<T>::split(__builtin_amdgcn_exp2f(fmaf(sc[2 * h + (j >> 2)][qt][j & 3], c2, -mc[qt])), j, pf[h][qt]);
+#pragma unroll
+        for (int i = NP - 1; i >= 0; --i)   // sums over the numbers that the PV product uses
+          ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[h][qt][i], ls[qt], 0, 0, 0);
       }
 #pragma unroll
-      for (int qt = 0; qt < NQ; ++qt)   // over the numbers that the PV product uses
-#pragma unroll
-        for (int i = NP - 1; i >= 0; --i) att.ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(att.ones, pf[qt][i], att.ls[qt], 0, 0, 0);
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        const __bf16* const at = slot + 128 * (mt >> 1) + (mt & 1 ? v_odd : v_even);
+        const __bf16* const at = slot + 32 * h * D + 128 * (mt >> 1) + (mt & 1 ? v_odd : v_even);
         const bf16x4 v0 = lds_read_tr(at), v1 = lds_read_tr(at + 16 * D);
         const bf16x8 vf = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
 #pragma unroll
         for (int qt = 0; qt < NQ; ++qt)
 #pragma unroll
-          for (int i = NP - 1; i >= 0; --i) att.o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt][i], att.o[mt][qt], 0, 0, 0);
+          for (int i = NP - 1; i >= 0; --i) o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[h][qt][i], o[mt][qt], 0, 0, 0);
       }
-    }
   };
   const int full = min(last, len / kPackRows);
   for (; b < full; b += kWaves) block(std::false_type{});
@@ -226,12 +239,12 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 6
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-    for (int qt = 0; qt < NQ; ++qt) mine[(mt * NQ + qt) * 64] = make_float4(att.o[mt][qt][0], att.o[mt][qt][1], att.o[mt][qt][2], att.o[mt][qt][3]);
+    for (int qt = 0; qt < NQ; ++qt) mine[(mt * NQ + qt) * 64] = make_float4(o[mt][qt][0], o[mt][qt][1], o[mt][qt][2], o[mt][qt][3]);
   if (g == 0) {
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
-      m_sh[w][16 * qt + col] = att.mc[qt];
-      l_sh[w][16 * qt + col] = att.ls[qt][0];
+      m_sh[w][16 * qt + col] = mc[qt];
+      l_sh[w][16 * qt + col] = ls[qt][0];
     }
   }
   __syncthreads();
