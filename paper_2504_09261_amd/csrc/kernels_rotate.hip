@@ -4,8 +4,8 @@
 // or (2i, 2i + 1) of a section of S elements; with two axes a head has two sections, each turned by a position of its own.  In front of it, RMS norm
 // x / sqrt(mean x^2 + eps) w or unit norm x / max(|x|, eps) w over the whole row.
 //
-// Memory-bound: a row is read and written once, whatever the strides it is read with.  A lane holds 16 elements of a row, two runs of eight chosen so
-// that its pairs are its own: no exchange but the sum of squares over the 8 (head_dim 128) or 4 lanes of a row.  Angles are formed
+// Memory-bound: a row is read and written once, whatever the strides it is read with.  A lane holds 16 elements of a row, pieces of 16 bytes chosen so
+// that its pairs are its own and the lanes of an access lie side by side: no exchange but the sum of squares over the 8 (head_dim 128) or 4 lanes of a row.  Angles are formed
 // once for a token and used for all heads that the thread walks over.  They are exact where it matters: the frequency is held in units of 2^-64
 // turns, so the product with a position wraps to its fraction of a turn in integers, however far the position.
 // Measured: 16384 rows of 32 + 8 heads of 128 out of a projection, normed and turned, 65 us (5.1 TB/s of the 6.2 that a plain elementwise
@@ -43,19 +43,20 @@ template <bool STREAM, typename V> __device__ __forceinline__ void put(V* p, con
   if constexpr (STREAM) __builtin_nontemporal_store(x, p);
   else *p = x;
 }
-template <typename T> struct Run;   // eight elements
-template <> struct Run<float> {
+template <typename T> struct Piece;   // 16 bytes
+template <> struct Piece<float> {
+  static constexpr int kElements = 4;
   static __device__ __forceinline__ void load(const float* p, float* v) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    const floatx4 a = *reinterpret_cast<const floatx4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i];
   }
   template <bool STREAM> static __device__ __forceinline__ void store(float* p, const float* v) {
-    const floatx4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
-    put<STREAM>(reinterpret_cast<floatx4*>(p), a);
-    put<STREAM>(reinterpret_cast<floatx4*>(p) + 1, b);
+    put<STREAM>(reinterpret_cast<floatx4*>(p), floatx4{v[0], v[1], v[2], v[3]});
   }
 };
-template <> struct Run<__bf16> {
+template <> struct Piece<__bf16> {
+  static constexpr int kElements = 8;
   static __device__ __forceinline__ void load(const __bf16* p, float* v) {
     const bf16x8 x = *reinterpret_cast<const bf16x8*>(p);
 #pragma unroll
@@ -71,6 +72,11 @@ template <> struct Run<__bf16> {
 
 template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
   return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+
+template <int E> __device__ __forceinline__ void load_weights(const float* p, float* v) {
+#pragma unroll
+  for (int i = 0; i < E; i += 4) Piece<float>::load(p + i, v + i);
 }
 
 template <typename T, int D, bool HALF, bool NORM, bool STREAM>
@@ -90,22 +96,24 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
   const int64_t n = (int64_t)(tile << a.tokens_log2) + (slot & ((1 << a.tokens_log2) - 1));
   if (n >= a.n) return;   // all lanes of a row
 
-  // this lane's two runs of eight elements, and the first of its eight pairs
+  // This lane's 16 elements: of its region of a row, an axis' section or what does not rotate, its piece of every part; in a rotating section they are
+  // whole pairs in either layout.
+  constexpr int E = Piece<T>::kElements, PIECES = 16 / E;
   const bool turns = 16 * j < a.rot_dim;
-  int lo = 16 * j, hi = 16 * j + 8, axis = 0, pair = 8 * j;
+  int base = a.rot_dim, size = D - a.rot_dim, axis = 0;
   if (turns) {
     axis = 16 * j >= a.section ? 1 : 0;
-    if (HALF) {
-      lo = axis * a.section + (16 * j - axis * a.section) / 2;
-      hi = lo + a.section / 2;
-    }
+    base = axis * a.section;
+    size = a.section;
   }
+  const int part = size / PIECES, in_part = (16 * j - base) / PIECES;   // elements of a part, and this lane's first one there
   float c[8], s[8];
   if (turns) {
     const int p = a.pos ? a.pos[b * a.pos_b + (int64_t)axis * a.n + n] : a.pos0 + (int)n;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint64_t f = a.turns[pair + i];
+    for (int i = 0; i < 8; ++i) {   // pair i: elements i and 8 + i, or 2 i and 2 i + 1
+      const int number = HALF ? i / E * part + in_part + i % E : (2 * i / E * part + in_part + 2 * i % E) / 2;
+      const uint64_t f = a.turns[base / 2 + number];
       // upper half of the low 64 bits of p f; the low half of f makes up for p < 0 standing for p + 2^32
       const unsigned u = __umulhi((unsigned)p, (unsigned)f) + (unsigned)p * (unsigned)(f >> 32) - (p < 0 ? (unsigned)f : 0u);
       cos_sin(u, c[i], s[i]);
@@ -113,6 +121,7 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
       s[i] *= a.gain;
     }
   }
+  const int at = base + in_part;
   const T* src = static_cast<const T*>(t.x) + b * t.sb + n * t.sn;
   T* dst = static_cast<T*>(t.out) + (b * t.heads * a.n + n) * D;
   const int across = SLOTS >> a.tokens_log2;   // heads at a time
@@ -120,17 +129,17 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
   const int h1 = min(t.heads, (chunk + 1) * across * a.steps);
   float w[16];
   if (NORM && t.w != nullptr && t.w_stride == 0) {
-    Run<float>::load(t.w + lo, w);
-    Run<float>::load(t.w + hi, w + 8);
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) load_weights<E>(t.w + at + k * part, w + k * E);
   }
   for (int h = h0; h < h1; h += across) {
     float v[16];
-    Run<T>::load(src + h * t.sh + lo, v);
-    Run<T>::load(src + h * t.sh + hi, v + 8);
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) Piece<T>::load(src + h * t.sh + at + k * part, v + k * E);
     if (NORM) {
       if (t.w != nullptr && t.w_stride != 0) {
-        Run<float>::load(t.w + (int64_t)h * t.w_stride + lo, w);
-        Run<float>::load(t.w + (int64_t)h * t.w_stride + hi, w + 8);
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) load_weights<E>(t.w + (int64_t)h * t.w_stride + at + k * part, w + k * E);
       }
       float ss = 0.f;
 #pragma unroll
@@ -155,8 +164,8 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
       }
     }
     T* o = dst + (int64_t)h * a.n * D;
-    Run<T>::template store<STREAM>(o + lo, v);
-    Run<T>::template store<STREAM>(o + hi, v + 8);
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) Piece<T>::template store<STREAM>(o + at + k * part, v + k * E);
   }
 }
 
@@ -196,8 +205,10 @@ void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout
   a.tokens_log2 = log2;
   a.tiles = (a.n + (1 << log2) - 1) >> log2;
   // Outputs that the L2 caches cannot hold pass them by (16384 rows of 32 + 8 heads 71.7 -> 65.3 us, 32 x 256 of 30 + 30 heads 30.2 -> 26.6); smaller ones
-  // are for the next launch to find there.
-  const bool stream = rows * head_dim * elem_bytes > kL2Bytes;
+  // are for the next launch to find there, and where a row's pieces of an access make up less than 32 bytes (as many as its region has elements) they
+  // need the caches to become lines (8 x 8192 float32 rows of 16 heads of 64, of which 16 elements rotate: 129 us, past the caches 326; 32 elements of bf16 rows 61, 51).
+  const auto wide = [](int region) { return region == 0 || region >= 32; };
+  const bool stream = rows * head_dim * elem_bytes > kL2Bytes && wide(a.section) && wide(head_dim - a.rot_dim);
   const int across = slots >> log2;
   // A thread walks over as many heads as leave enough work-groups: it forms its angles once for all of them.
   int64_t groups = 0;

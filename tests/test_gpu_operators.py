@@ -142,6 +142,27 @@ def test_rotate_keeps_what_does_not_rotate_and_spreads_nan_to_its_pair_only(cont
     assert out[0, 1, 2, 50] == float("inf") and torch.equal(out[..., 32:50], x[..., 32:50])
 
 
+@pytest.mark.parametrize("dtype, d, rot, layout", [("bf16", 128, 128, "half"), ("bf16", 64, 32, "interleaved"), ("f32", 64, 64, "half"), ("f32", 128, 32, "interleaved"), ("f32", 64, 16, "half")])
+def test_large_outputs_are_those_of_their_parts(contexts, dtype, d, rot, layout):
+    """Beyond 32 MB of output stores take another way."""
+    hk = contexts(1, d, dtype)
+    g = torch.Generator(DEV).manual_seed(8)
+    heads, N = 10, 4001
+    B = (40 << 20) // (heads * N * d * TYPES[dtype].itemsize) + 1
+    x, k = rows_in((B, heads, N, d), "projection", dtype, g), rows_in((B, 3, N, d), "plain", dtype, g)
+    rope, pos = Rope.scaled(rot, 1, layout), torch.arange(N, dtype=torch.int32, device=DEV) * 77
+    out, part = torch.empty((B, heads, N, d), dtype=x.dtype, device=DEV), torch.empty((1, heads, N, d), dtype=x.dtype, device=DEV)
+    hk.rotate(x, rope, out, pos=pos)
+    for b in range(B):
+        hk.rotate(x[b:b + 1], rope, part, pos=pos)
+        assert torch.equal(part[0], out[b])
+    ko, kp = torch.empty_like(k), torch.empty_like(k[:1])
+    hk.norm_rotate(x, k, "rms", 1e-6, None, None, rope, out, ko, pos=pos)
+    for b in range(B):
+        hk.norm_rotate(x[b:b + 1], k[b:b + 1], "rms", 1e-6, None, None, rope, part, kp, pos=pos)
+        assert torch.equal(part[0], out[b]) and torch.equal(kp[0], ko[b])
+
+
 # The sum of squares: chains of 16 and three more sums, half of it in the root, 10 H; root, reciprocal, mean and eps 4 H; the two products 2 H.
 NORM = 17.0
 
@@ -351,6 +372,30 @@ def test_pack_through_kept_lists(contexts):
     got, _ = read_back(hk, B, pc, n_kept, "bf16", first=first)
     for u, i in enumerate(lists):
         assert np.array_equal(got[u][2], np.where(i < cached[u], -3, 77 + i - cached[u]))
+
+
+@pytest.mark.parametrize("dtype, d", [("bf16", 128), ("f32", 64)])
+def test_many_rows_read_back_as_their_parts(contexts, dtype, d):
+    """Beyond 32 MB of output stores take another way."""
+    hk = contexts(1, d, dtype, units=8)
+    g = torch.Generator(DEV).manual_seed(1)
+    lens = np.array([30001, 1, 17000, 20003, 64, 9999, 22222, 5000])
+    off, rows = offsets(lens, 8)
+    assert 2 * rows * d * TYPES[dtype].itemsize > 50 << 20
+    k, v = (torch.randn((rows, d), generator=g, device=DEV).to(TYPES[dtype]) for _ in range(2))
+    pc = packed(lens, d)
+    hk.pack(8, 0, pc, cache_in=Cache(k, v, off, lens))
+    out, part = (Cache(torch.zeros_like(k), torch.zeros_like(v), off, lens) for _ in range(2))
+    hk.unpack(8, pc, out)
+    for a in range(0, 30001, 9000):     # rows a .. of every unit
+        n = np.minimum(np.maximum(lens - a, 0), 9000)
+        some, at = Cache(torch.zeros_like(k), torch.zeros_like(v), off, n), np.minimum(lens, a)
+        hk.unpack(8, pc, some, first=at)
+        for u in range(8):
+            part.k[off[u] + at[u]:off[u] + at[u] + n[u]] = some.k[off[u]:off[u] + n[u]]
+            part.v[off[u] + at[u]:off[u] + at[u] + n[u]] = some.v[off[u]:off[u] + n[u]]
+    assert torch.equal(out.k, part.k) and torch.equal(out.v, part.v)
+    assert same(to64(out.k[off[3]:off[3] + 200]), nearest(to64(k[off[3]:off[3] + 200])))
 
 
 def test_packed_sizes():
