@@ -84,16 +84,13 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
   constexpr int LPR = D / 16;             // lanes of a row
   constexpr int SLOTS = kThreads / LPR;   // rows of a work-group at a time
   const int j = threadIdx.x % LPR, slot = threadIdx.x / LPR;
-  unsigned x = blockIdx.x;
-  const int tile = x % (unsigned)a.tiles;
-  x /= (unsigned)a.tiles;
-  const unsigned chunks = a.t[0].chunks + a.t[1].chunks;
-  int chunk = x % chunks;
-  const int64_t b = x / chunks;
-  const bool second = chunk >= a.t[0].chunks;
-  if (second) chunk -= a.t[0].chunks;
+  const int64_t b = blockIdx.x / a.groups[1];
+  unsigned x = blockIdx.x - (unsigned)b * a.groups[1];
+  const bool second = x >= a.groups[0];
   const RotateTensor& t = a.t[second ? 1 : 0];
-  const int64_t n = (int64_t)(tile << a.tokens_log2) + (slot & ((1 << a.tokens_log2) - 1));
+  if (second) x -= a.groups[0];
+  const int chunk = x / (unsigned)t.tiles, tile = x - (unsigned)chunk * t.tiles;
+  const int64_t n = (int64_t)(tile << t.tokens_log2) + (slot & ((1 << t.tokens_log2) - 1));
   if (n >= a.n) return;   // all lanes of a row
 
   // This lane's 16 elements: of its region of a row, an axis' section or what does not rotate, its piece of every part; in a rotating section they are
@@ -124,8 +121,8 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
   const int at = base + in_part;
   const T* src = static_cast<const T*>(t.x) + b * t.sb + n * t.sn;
   T* dst = static_cast<T*>(t.out) + (b * t.heads * a.n + n) * D;
-  const int across = SLOTS >> a.tokens_log2;   // heads at a time
-  const int h0 = chunk * across * a.steps + (slot >> a.tokens_log2);
+  const int across = SLOTS >> t.tokens_log2;   // heads at a time
+  const int h0 = chunk * across * a.steps + (slot >> t.tokens_log2);
   const int h1 = min(t.heads, (chunk + 1) * across * a.steps);
   float w[16];
   if (NORM && t.w != nullptr && t.w_stride == 0) {
@@ -192,32 +189,40 @@ void launch_typed(hipStream_t s, bool half_layout, bool stream, unsigned groups,
 
 void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout, int batch, int n_tensors, RotateArgs a) {
   const int slots = kThreads / (head_dim / 16);
-  int heads = 0;
   int64_t rows = 0;
   for (int i = 0; i < n_tensors; ++i) {
-    heads = std::max(heads, a.t[i].heads);
-    rows += (int64_t)batch * a.n * a.t[i].heads;
+    RotateTensor& t = a.t[i];
+    rows += (int64_t)batch * a.n * t.heads;
+    // Rows of one head side by side: few, so that the rest of the work-group takes the heads beside it, which lie behind each other in a projection
+    // (4, 8, 32 rows: 16384 rows of 32 + 8 heads 64.8, 66.7, 65.4 us, 32 x 256 of 30 + 30 heads 26.0, 29.0, 28.5, 2 x 4096 of 16 heads 15.4, 14.0, 14.6),
+    // but as many as leave no more than a quarter of the lanes without a head (2 x 11844 rows of 10 + 2 heads of 64: 22.7 us with as few as fit the heads of
+    // the larger tensor, 15.8 so; 8 x 10948 of 2 + 1 heads 21.1, 18.6; 50 x 900 float32 rows of 8 + 1 heads, the one of 71 drawn shapes that loses much, 58, 69).
+    const auto idle = [&](int log2) {
+      const int across = slots >> log2, taken = (t.heads + across - 1) / across * across;
+      return 4 * (taken - t.heads) > taken;
+    };
+    int log2 = 0;
+    while ((1 << log2) < slots && (1 << log2) < a.n && (log2 < 2 || idle(log2))) ++log2;
+    t.tokens_log2 = log2;
+    t.tiles = (a.n + (1 << log2) - 1) >> log2;
   }
-  // Rows of one head side by side: few, so that the rest of the work-group takes the heads beside it, which lie behind each other in a projection
-  // (4, 8, 32 rows: 16384 rows of 32 + 8 heads 64.8, 66.7, 65.4 us, 32 x 256 of 30 + 30 heads 26.0, 29.0, 28.5, 2 x 4096 of 16 heads 15.4, 14.0, 14.6).
-  int log2 = 0;
-  while ((1 << log2) < slots && (1 << log2) < a.n && (log2 < 2 || (slots >> log2) > heads)) ++log2;
-  a.tokens_log2 = log2;
-  a.tiles = (a.n + (1 << log2) - 1) >> log2;
   // Outputs that the L2 caches cannot hold pass them by (16384 rows of 32 + 8 heads 71.7 -> 65.3 us, 32 x 256 of 30 + 30 heads 30.2 -> 26.6); smaller ones
   // are for the next launch to find there, and where a row's pieces of an access make up less than 32 bytes (as many as its region has elements) they
   // need the caches to become lines (8 x 8192 float32 rows of 16 heads of 64, of which 16 elements rotate: 129 us, past the caches 326; 32 elements of bf16 rows 61, 51).
   const auto wide = [](int region) { return region == 0 || region >= 32; };
   const bool stream = rows * head_dim * elem_bytes > kL2Bytes && wide(a.section) && wide(head_dim - a.rot_dim);
-  const int across = slots >> log2;
   // A thread walks over as many heads as leave enough work-groups: it forms its angles once for all of them.
   int64_t groups = 0;
   for (a.steps = kMaxSteps;; a.steps /= 2) {
     groups = 0;
     for (int i = 0; i < n_tensors; ++i) {
-      a.t[i].chunks = (a.t[i].heads + across * a.steps - 1) / (across * a.steps);
-      groups += (int64_t)a.t[i].chunks * a.tiles * batch;
+      RotateTensor& t = a.t[i];
+      const int each = (slots >> t.tokens_log2) * a.steps;
+      groups += (int64_t)((t.heads + each - 1) / each) * t.tiles;
+      a.groups[i] = (uint32_t)groups;
     }
+    a.groups[1] = (uint32_t)groups;
+    groups *= batch;
     if (a.steps == 1 || groups >= kWantGroups) break;
   }
   if (elem_bytes == 4) {

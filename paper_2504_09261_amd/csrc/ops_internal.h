@@ -21,8 +21,9 @@ struct RotateTensor {
   int64_t sb, sh, sn;
   int32_t heads;
   int32_t w_stride;
-  int32_t chunks;       // work-groups that share a tile's heads
-  int32_t pad;
+  // launch shape, set by launch_rotate
+  int32_t tokens_log2;  // rows of one head a work-group takes (power of two)
+  int32_t tiles;        // of rows: work-groups take one of them and a part of the heads
 };
 struct RotateArgs {
   RotateTensor t[2];
@@ -35,8 +36,7 @@ struct RotateArgs {
   float gain, eps;
   int32_t norm;         // kNorm*
   // launch shape, set by launch_rotate
-  int32_t tokens_log2;  // rows of one head a work-group takes (power of two)
-  int32_t tiles;        // of rows
+  uint32_t groups[2];   // work-groups of a batch element: of t[0], of both
   int32_t steps;        // heads a thread takes, one after the other
   uint64_t turns[kMaxPairs];   // of a pair per position, in units of 2^-64 of a turn
 };
