@@ -287,7 +287,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 6
   }
 }
 
-// Rows of units that were cut: a work-group takes one query, D / 4 lanes a chunk.
+// Rows of units that were cut, where these are few and the chunks many: a work-group takes one query, D / 4 lanes a chunk.
 constexpr int kFactors = 1024;   // chunks whose factors are kept in LDS at a time
 template <typename T, int D, int N>
 __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N> a, int q_rows) {
@@ -358,6 +358,49 @@ __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N>
   store4(static_cast<T*>(a.out) + ((int64_t)a.unit[ui].unit * a.N_k + qi) * D + 4 * lane, floatx4{o.x, o.y, o.z, o.w}, inv);
 }
 
+// The same for many rows or few chunks: a query to D / 4 lanes, which walk over its chunks.
+template <typename T, int D, int N>
+__global__ __launch_bounds__(256) void attn_packed_merge_rows(const AttnPackedArgs<N> a, int q_rows) {
+  constexpr int LPR = D / 4, ROWS = 256 / LPR;
+  const int ui = blockIdx.y, n = chunks_of(packed_blocks(a.unit[ui].len), a.chunk);
+  const int tid = threadIdx.x, qi = blockIdx.x * ROWS + tid / LPR, lane = tid % LPR;
+  if (n == 1 || qi >= a.N_k) return;
+  const int64_t part0 = ((int64_t)ui * a.q_tiles + qi / q_rows) * a.n_chunks * q_rows + qi % q_rows;
+  const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + part0;
+  const float4* const po = reinterpret_cast<const float4*>(a.part_o + part0 * D) + lane;
+  float M = -FLT_MAX, L = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kAhead = 8;   // chunks whose loads are under way together
+  for (int c0 = 0; c0 < n; c0 += kAhead) {
+    float2 x[kAhead];
+    float4 p[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t at = (int64_t)min(c0 + i, n - 1) * q_rows;
+      x[i] = ml[at];
+      p[i] = po[at * LPR];
+    }
+    float m = M;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) m = fmaxf(m, x[i].x);
+    const float old = __builtin_amdgcn_exp2f(M - m);
+    M = m;
+    L *= old;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] *= old;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float f = c0 + i < n ? __builtin_amdgcn_exp2f(x[i].x - M) : 0.f;
+      L = fmaf(f, x[i].y, L);
+      o[0] = fmaf(f, p[i].x, o[0]);
+      o[1] = fmaf(f, p[i].y, o[1]);
+      o[2] = fmaf(f, p[i].z, o[2]);
+      o[3] = fmaf(f, p[i].w, o[3]);
+    }
+  }
+  store4(static_cast<T*>(a.out) + ((int64_t)a.unit[ui].unit * a.N_k + qi) * D + 4 * lane, o, 1.f / L);
+}
+
 template <typename T, int D, int N>
 void launch_some(hipStream_t s, int queries, const AttnPackedHead& h, const AttnPackedUnit* units) {
   AttnPackedArgs<N> a;
@@ -372,7 +415,15 @@ void launch_some(hipStream_t s, int queries, const AttnPackedHead& h, const Attn
     else if (queries == 16) hipLaunchKernelGGL((attn_packed<T, D, 1, N>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((attn_packed<T, D, 2, N>), grid, block, 0, s, a);
   }
-  if (h.n_chunks > 1) hipLaunchKernelGGL((attn_packed_merge<T, D, N>), dim3(h.N_k, h.n_units), dim3(256), 0, s, a, queries);
+  if (h.n_chunks == 1) return;
+  // One query to a work-group reads many chunks at a time; where a query has few or the queries fill the chip, D / 4 lanes each are as fast and more of them
+  // run (launch and merge, us, a work-group / D / 4 lanes a query, head_dim 128: 4 chunks, 64 units, 1 query 9.6 / 8.5, 472 queries 111 / 73; 16 chunks, 64
+  // units, 1 query 12.3 / 12.0, 4 units 7.8 / 8.1, 64 units, 100 queries 59 / 54).
+  constexpr int kRows = 1024 / D;
+  if (h.n_chunks <= 8 || (int64_t)h.N_k * h.n_units >= 2048)
+    hipLaunchKernelGGL((attn_packed_merge_rows<T, D, N>), dim3((h.N_k + kRows - 1) / kRows, h.n_units), dim3(256), 0, s, a, queries);
+  else
+    hipLaunchKernelGGL((attn_packed_merge<T, D, N>), dim3(h.N_k, h.n_units), dim3(256), 0, s, a, queries);
 }
 
 template <typename T>
