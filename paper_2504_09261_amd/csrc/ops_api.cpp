@@ -162,20 +162,6 @@ int blocks_of(int len) { return (int)(((int64_t)len + kPackRows - 1) / kPackRows
 // Partial results of work-groups of so many queries that the workspace holds.
 int64_t partial_slots(const hack_ctx* ctx, int queries) { return ctx->part_rows / queries; }
 
-// How units are cut: into chunks that give each compute unit two work-groups (two are enough to read at the rate of the memory, and more start and end more
-// often: one token over 8 caches of 131071 rows, 512, 1024 and 2048 work-groups 31, 34 and 38 us), but not where cutting costs more than it gains: merging
-// the parts is a launch of its own, 5 us, which is what a work-group alone on its compute unit takes for 16 blocks, and a work-group whose neighbour has finished
-// runs 1.7 times as fast, so that units of up to twice the mean need no cut (512 units of 900 to 4000 rows: whole 41 us, in chunks of 16 or 32 blocks 45).
-void plan_chunks(const hack_ctx* ctx, int64_t blocks, int64_t longest, int64_t slots, AttnPackedHead* a) {
-  const int64_t fill = 2 * (int64_t)ctx->cus;
-  int64_t chunk = std::max<int64_t>(8, (blocks * a->q_tiles + fill - 1) / fill);
-  if (longest <= std::max(2 * chunk, chunk + 16)) chunk = longest;
-  const int64_t most = std::max<int64_t>(1, slots / ((int64_t)a->n_units * a->q_tiles));   // chunks whose partial results the workspace holds
-  chunk = std::max(chunk, (longest + most - 1) / most);
-  a->chunk = (int32_t)std::min<int64_t>(chunk, longest);
-  a->n_chunks = (int32_t)((longest + a->chunk - 1) / a->chunk);
-}
-
 void measure(const int32_t* len, int n, int64_t* blocks, int64_t* longest) {
   *blocks = *longest = 0;
   for (int i = 0; i < n; ++i) {
@@ -185,20 +171,83 @@ void measure(const int32_t* len, int n, int64_t* blocks, int64_t* longest) {
   }
 }
 
+// How units are cut, if at all.  Work-groups of less to do fill the chip and end together, but each leaves a part, and merging the parts is a launch of its
+// own: neither the most nor the fewest work-groups are best.  Tried by an estimate of the time are: no cut; chunks that give each compute unit one work-group,
+// and two (by the mean, by the mean and half a chunk left over in every unit, by the longest); chunks that balance their own time with that of their parts.
+// Fitted to 250 launches of 4 to 600 units, even and ragged, 500 to 32000 keys, 1 to 1500 queries, each cut into 1 to 32 chunks: what it picks takes
+// 1.03 times the best of them on average, 1.38 at most (always two work-groups to a compute unit: 1.06, 2.1).  Us a launch, always two / so: 14 units
+// of 21747 to 27815 keys, 472 queries 132 / 103, 12 of 1009 to 1591, 5 queries 9.1 / 6.9; head_dim 64, 10 of 13694 to 22356, 176 queries 30 / 35.
+void plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t blocks, int64_t longest, AttnPackedHead* a) {
+  struct Rates { double block, merge, part; };   // us of 64 keys to a work-group alone, of the merge, of a work-group's part
+  static constexpr Rates kRates[2][3] = {{{.16, 2.7, .003}, {.28, 2.5, .005}, {.80, 5.5, .011}}, {{.23, 3.0, .006}, {.45, 4.0, .022}, {1.45, 4.8, .036}}};
+  constexpr int kXcds = 8, kLeast = 4;   // blocks of a chunk: one for each wave of the smaller forms
+  const Rates& r = kRates[ctx->cfg.head_dim == 128][queries == 16 ? 0 : queries == 32 ? 1 : 2];
+  const int64_t n = a->n_units, tiles = a->q_tiles, cus = std::max(ctx->cus / kXcds, 1);
+  const int64_t most = std::max<int64_t>(1, partial_slots(ctx, queries) / (n * tiles));   // chunks whose partial results the workspace holds
+  constexpr int kRows = 256;
+  int32_t ends[kRows + 1];   // units of so many chunks
+  const auto us = [&](int64_t chunk) {
+    const int64_t rows = (longest + chunk - 1) / chunk;
+    const bool exact = tiles > 1 && rows <= kRows;
+    if (exact) std::fill(ends, ends + rows + 1, 0);
+    int64_t parts = 0;
+    for (int i = 0; i < n; ++i) {
+      const int64_t chunks = ((len[i] - 1) / kPackRows + chunk) / chunk;
+      parts += chunks;
+      if (exact) ++ends[chunks];
+    }
+    // Chunks on one XCD: chunk c of the i-th unit, by length, is on (c n + i) mod 8.  Its query tiles share it, so that one chunk more may be many work-groups.
+    int64_t on = (parts + kXcds - 1) / kXcds;
+    if (exact) {
+      int64_t left = n, even = 0, more[kXcds] = {};
+      for (int64_t c = 0; c < rows; ++c) {
+        left -= ends[c];
+        even += left / kXcds;
+        for (int64_t i = 0; i < left % kXcds; ++i) ++more[(c * n + i) % kXcds];
+      }
+      on = even + *std::max_element(more, more + kXcds);
+    }
+    const double fill = (double)(on * tiles) / cus;   // work-groups of a compute unit
+    const double slower = queries == 16 ? std::max(1.0 + 0.6 * fill, 1.1 * fill) : std::max(1.0, 0.76 * std::ceil(fill));
+    const double t = r.block * std::max((double)chunk, (double)blocks / parts * slower);
+    return parts == n ? t : t + r.merge + r.part * parts * tiles + 3e-4 * (rows * n * tiles);   // the last: empty work-groups
+  };
+  int64_t best = longest;
+  if (most > 1 && longest > kLeast) {
+    double best_us = us(longest);
+    const auto consider = [&](int64_t chunk) {
+      chunk = std::max<int64_t>({chunk, kLeast, (longest + most - 1) / most});
+      if (chunk >= longest) return;
+      const double t = us(chunk);
+      if (t < best_us) best = chunk, best_us = t;
+    };
+    for (int each = 1; each <= 2; ++each) {
+      const int64_t groups = kXcds * (each * cus / tiles);   // a query tile's
+      if (groups < 1) continue;
+      consider((blocks + groups - 1) / groups);
+      if (2 * groups > n) consider((2 * blocks + 2 * groups - n - 1) / (2 * groups - n));
+      if (groups > n) consider((longest + groups / n - 1) / (groups / n));
+    }
+    consider((int64_t)std::ceil(std::sqrt(r.part * tiles * blocks / r.block)));
+  }
+  a->chunk = (int32_t)best;
+  a->n_chunks = (int32_t)((longest + best - 1) / best);
+}
+
 // Queries of a work-group.  Sixteen and 32 have every wave convert the keys it takes, 128 (kTileQueries) share every converted block, which is what a large
 // launch wants, but give a quarter of the work-groups.  Which is faster for more than 64 queries goes by an estimate in rounds of the work-groups that start at
 // once, at what a block of 64 keys takes a work-group (two to a compute unit, or three of 32 queries at head_dim 64, and alone), its start and end, and a
 // merge.  Fitted to 192 launches of 8 to 480 units, 300 to 6000 keys, 33 to 1024 queries; there it picks a form 0.5 % slower than the better one on average,
 // 17 % at most but for one (42 %; always 32 queries: 3.4 % on average, 68 % at most, always 128: 38 and 170 %).  Us a launch, 32 / 128 queries, head_dim 128: 64 units of 6000 keys, 1024 queries 247 /
 // 189, of 1500, 200 22.6 / 37.1; 128 units of 300, 576 38.0 / 28.0; head_dim 64: 480 units of 300, 1024 104 / 83, 240 of 6000, 128 77 / 115.
-double estimate_us(const hack_ctx* ctx, int queries, int n_units, int64_t blocks, int64_t longest, int N_k) {
+double estimate_us(const hack_ctx* ctx, int queries, const int32_t* len, int n_units, int64_t blocks, int64_t longest, int N_k) {
   struct Rates { int at_once; double pair, alone, fixed; };   // work-groups a compute unit holds, us a block of 64 keys with neighbours and alone, start and end
   static constexpr Rates kRates[2][2] = {{{3, .62, .28, 3.5}, {2, 1.45, 1.02, 4.0}}, {{2, .70, .43, 4.0}, {2, 1.94, 1.40, 5.0}}};
   const Rates& r = kRates[ctx->cfg.head_dim == 128][queries == kTileQueries];
   AttnPackedHead a{};
   a.n_units = n_units;
   a.q_tiles = (N_k + queries - 1) / queries;
-  plan_chunks(ctx, blocks, longest, partial_slots(ctx, queries), &a);
+  plan_chunks(ctx, queries, len, blocks, longest, &a);
   const double each = (double)blocks / n_units, cut = std::max(1.0, std::ceil(each / a.chunk));
   const int64_t groups = (int64_t)(n_units * cut) * a.q_tiles, slots = (int64_t)r.at_once * ctx->cus, full = groups / slots, rest = groups % slots;
   double us = each / cut * (full * r.pair + (rest == 0 ? 0.0 : rest <= ctx->cus ? r.alone : r.pair)) + r.fixed * (1.0 + 0.6 * (double)(full + (rest > 0) - 1));
@@ -212,7 +261,7 @@ int queries_per_group(const hack_ctx* ctx, const int32_t* len, int n_units, int 
   if (N_k <= 64) return N_k <= 16 ? 16 : 32;
   int64_t blocks, longest;
   measure(len, n_units, &blocks, &longest);
-  return 1.06 * estimate_us(ctx, kTileQueries, n_units, blocks, longest, N_k) < estimate_us(ctx, 32, n_units, blocks, longest, N_k) ? kTileQueries : 32;
+  return 1.06 * estimate_us(ctx, kTileQueries, len, n_units, blocks, longest, N_k) < estimate_us(ctx, 32, len, n_units, blocks, longest, N_k) ? kTileQueries : 32;
 }
 
 // In what order units start: the longest first, except that where all work-groups start at once, two to a compute unit (one on each first, then a second
@@ -392,14 +441,13 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
   a.scale = scale;
   const int queries = queries_per_group(ctx, kv->len, U, N_k);
   a.q_tiles = (N_k + queries - 1) / queries;
-  const int64_t slots = partial_slots(ctx, queries);
   std::vector<int32_t> order(std::min(U, kAttnPackedUnits)), count;
   for (int u0 = 0; u0 < U; u0 += kAttnPackedUnits) {
     a.n_units = std::min(kAttnPackedUnits, U - u0);
     const int32_t* len = kv->len + u0;
     int64_t blocks, longest;
     measure(len, a.n_units, &blocks, &longest);
-    plan_chunks(ctx, blocks, longest, slots, &a);
+    plan_chunks(ctx, queries, len, blocks, longest, &a);
     order_units(ctx, len, a, &order, &count);
     for (int i = 0; i < a.n_units; ++i) units[i] = AttnPackedUnit{(int32_t)(kv->off[u0 + order[i]] / kPackRows), len[order[i]], u0 + order[i]};
     launch_attn_packed(static_cast<hipStream_t>(stream), ctx->elem_bytes, d, queries, a, units);
