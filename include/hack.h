@@ -478,8 +478,8 @@ hack_status hack_packed_bytes(int32_t head_dim, int64_t rows, int64_t* bytes);
  *   kept_idx  DEVICE int32 [B*H, idx_stride], entries in [0, in->len[u] + N_k) (clamped to it), or NULL
  *   first     HOST [B*H], NULL = 0 for all
  * `pos` is written for rows from k_new (pos_new + row number), and for cached rows
- * if `in` carries it too.  bf16 and fp32 contexts.
- * Errors: HACK_EINVAL (NULL/misaligned pointers, more rows than there are, units outside out or overlapping in it, the
+ * if `in` carries it too.  `out` shares no memory with what is read.  bf16 and fp32 contexts.
+ * Errors: HACK_EINVAL (NULL/misaligned pointers, more rows than there are, units outside out or overlapping in it, shared memory, the
  * current device is not the context's), HACK_ECAPACITY. */
 hack_status hack_pack(hack_ctx* ctx, int32_t B, int32_t N_k, const hack_cache* in, const void* k_new, const void* v_new,
                       int32_t pos_new, const int32_t* kept_idx, int64_t idx_stride, const int32_t* first,
@@ -493,7 +493,7 @@ hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_cache* in, c
 
 /* hack_attn over a packed cache: O = Softmax(scale * Q K^T) V for every unit over its
  * own kv->len[u] rows, no mask.  Every unit must have at least one row; out must not
- * share memory with q.  Units are not limited by max_cache_len.  Heads that share a
+ * share memory with q (refused) or kv.  Units are not limited by max_cache_len.  Heads that share a
  * cache: queries [B, G H, N, d] of G heads to each of the H caches are [B, H, G N, d],
  * so N_k = G N.  The values that packing rounds to are bf16 numbers, so the accuracy is
  * hack_attn's over the rows that hack_unpack gives.  Results are reproducible bit for bit.

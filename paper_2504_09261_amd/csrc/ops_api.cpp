@@ -2,6 +2,7 @@
 // packed into 4 bits and read back, attention over them.  Arguments are checked here, launches take everything by value.
 #include <algorithm>
 #include <climits>
+#include <initializer_list>
 #include <utility>
 #include <vector>
 
@@ -26,6 +27,21 @@ struct Range {   // bytes
   uintptr_t lo, hi;
   bool meets(const Range& o) const { return lo < o.hi && o.lo < hi; }
 };
+
+Range range_of(const void* p, int64_t n, int64_t bytes) {   // n elements; none for NULL
+  const uintptr_t lo = (uintptr_t)p;
+  return p ? Range{lo, lo + (uintptr_t)(std::min<int64_t>(n, (int64_t)1 << 44) * bytes)} : Range{0, 0};
+}
+// Whether an output shares memory with an input or with another output.
+bool share(std::initializer_list<Range> out, std::initializer_list<Range> in) {
+  for (const Range* o = out.begin(); o != out.end(); ++o) {
+    for (const Range& i : in)
+      if (o->meets(i)) return true;
+    for (const Range* p = o + 1; p != out.end(); ++p)
+      if (o->meets(*p)) return true;
+  }
+  return false;
+}
 
 // Checks one operand and fills in its part of the launch.
 hack_status take_rows(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* r, const char* name, RotateTensor* t, Range* in, Range* out) {
@@ -371,6 +387,12 @@ extern "C" hack_status hack_pack(hack_ctx* ctx, int32_t B, int32_t N_k, const ha
   if (!any) return HACK_OK;
   if (units_overlap(U, [&](int u) { return out->off[u] + units[u].first; }, [&](int u) { return out->off[u] + out->len[u]; }))
     return fail(ctx, HACK_EINVAL, "units of out overlap");
+  const int64_t row = (int64_t)ctx->cfg.head_dim * ctx->elem_bytes, block = packed_block_bytes(ctx->cfg.head_dim), blocks = out->rows / kPackRows;
+  const int64_t rows = in ? in->rows : 0, fresh = (int64_t)U * n_new;
+  if (share({range_of(out->k, blocks, block), range_of(out->v, blocks, block), range_of(out->pos, out->rows, 4)},
+            {range_of(in ? in->k : nullptr, rows, row), range_of(in ? in->v : nullptr, rows, row), range_of(in ? in->pos : nullptr, rows, 4),
+             range_of(k_new, fresh, row), range_of(v_new, fresh, row), range_of(kept_idx, U * idx_stride, 4)}))
+    return fail(ctx, HACK_EINVAL, "out shares memory with what is read, or K with V");
   if ((st = check_device(ctx)) != HACK_OK) return st;
   PackHead a{};
   if (in) a.plain = CachePtrs{in->k, in->v, in->pos};
@@ -405,6 +427,10 @@ extern "C" hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_c
   if (!any) return HACK_OK;
   if (units_overlap(U, [&](int u) { return out->off[u]; }, [&](int u) { return out->off[u] + out->len[u]; }))
     return fail(ctx, HACK_EINVAL, "units of out overlap");
+  const int64_t row = (int64_t)ctx->cfg.head_dim * ctx->elem_bytes, block = packed_block_bytes(ctx->cfg.head_dim), blocks = in->rows / kPackRows;
+  if (share({range_of(out->k, out->rows, row), range_of(out->v, out->rows, row), range_of(out->pos, out->rows, 4)},
+            {range_of(in->k, blocks, block), range_of(in->v, blocks, block), range_of(in->pos, in->rows, 4)}))
+    return fail(ctx, HACK_EINVAL, "out shares memory with what is read, or K with V");
   if ((st = check_device(ctx)) != HACK_OK) return st;
   PackHead a{};
   a.plain = CachePtrs{out->k, out->v, out->pos};
@@ -425,9 +451,8 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
   if ((st = check_packed(ctx, kv, U, "kv")) != HACK_OK) return st;
   for (int u = 0; u < U; ++u)
     if (kv->len[u] < 1) return fail(ctx, HACK_EINVAL, "unit %d has an empty cache", u);
-  const int64_t bytes = (int64_t)U * N_k * d * ctx->elem_bytes;
-  const Range rq{(uintptr_t)q, (uintptr_t)q + (uintptr_t)bytes}, ro{(uintptr_t)out, (uintptr_t)out + (uintptr_t)bytes};
-  if (rq.meets(ro)) return fail(ctx, HACK_EINVAL, "q and out overlap");
+  const int64_t rows = (int64_t)U * N_k, row = (int64_t)d * ctx->elem_bytes;
+  if (range_of(q, rows, row).meets(range_of(out, rows, row))) return fail(ctx, HACK_EINVAL, "q and out overlap");
   if ((st = check_device(ctx)) != HACK_OK) return st;
   AttnPackedHead a{};
   AttnPackedUnit units[kAttnPackedUnits];

@@ -150,8 +150,11 @@ bool read_packed(Packed& a, PyObject* o, const Info& i, int64_t units) { return 
 
 void* address(PyObject* o) { return o == Py_None ? nullptr : PyLong_AsVoidPtr(o); }
 bool int32_arg(PyObject* o, int32_t* v) {
-  *v = (int32_t)PyLong_AsUnsignedLongMask(o);
-  return !PyErr_Occurred();
+  const long x = PyLong_AsLong(o);
+  *v = (int32_t)x;
+  if (PyErr_Occurred()) return false;
+  if (x < INT32_MIN || x > INT32_MAX) PyErr_SetString(PyExc_OverflowError, "a number of more than 32 bits");
+  return x >= INT32_MIN && x <= INT32_MAX;
 }
 bool arity(Py_ssize_t n, Py_ssize_t want) {
   if (n == want) return true;

@@ -283,6 +283,41 @@ int pack_refusals() {
   return 0;
 }
 
+// Outputs that share memory with inputs, or K with V.
+int shared_memory() {
+  Context c;
+  const int64_t off[kH] = {0, 64, 128, 192};
+  const int32_t len[kH] = {40, 40, 40, 40};
+  uint8_t *const k = at(0x50000000), *const v = at(0x60000000), *const q = at(0x70000000);
+  constexpr int64_t kPlain = 256 * kD * 2, kPacked = 4 * 34 * kD, kNew = kH * 40 * kD * 2;   // bytes
+  const auto plain = [&](uint8_t* a, uint8_t* b, int32_t* pos = nullptr) { return hack_cache{a, b, pos, 256, off, len}; };
+  const auto packed = [&](uint8_t* a, uint8_t* b, int32_t* pos = nullptr) { return hack_packed_cache{a, b, pos, 256, off, len}; };
+  const auto pack = [&](const hack_cache& i, const hack_packed_cache& p, const int32_t* kept = nullptr) {
+    return hack_pack(c.ctx, 1, 40, &i, k, v, 0, kept, 40, nullptr, &p, kStream);
+  };
+  const auto unpack = [&](const hack_packed_cache& p, const hack_cache& r) { return hack_unpack(c.ctx, 1, &p, nullptr, &r, kStream); };
+  const auto attn = [&](uint8_t* x, const hack_packed_cache& p, uint8_t* out) { return hack_attn_packed(c.ctx, 1, 40, x, &p, 0.5f, out, kStream); };
+  int32_t *const pos = at<int32_t>(0x40000000), *const kept = at<int32_t>(0x48000000);
+  // side by side is apart
+  CHECK(pack(plain(at(kA), at(kA + kPlain)), packed(at(kC), at(kC + kPacked)), kept) == HACK_OK);
+  CHECK(pack(plain(at(kC + 2 * kPacked), at(kA)), packed(at(kC), at(kC + kPacked))) == HACK_OK);
+  CHECK(unpack(packed(at(kC), at(kC + kPacked), pos), plain(at(kA), at(kA + kPlain), pos + 256)) == HACK_OK);
+  CHECK(attn(q, packed(at(kC), at(kE)), q + kNew) == HACK_OK);
+  CHECK(pack(plain(at(kC), at(kA)), packed(at(kC + kPlain - 16), at(kE))) == HACK_EINVAL);
+  CHECK(pack(plain(at(kB), at(kA)), packed(at(kE), at(kA + kPlain - 16))) == HACK_EINVAL);
+  CHECK(pack(plain(at(kA), at(kB)), packed(at(kC), at(kC + kPacked - 16))) == HACK_EINVAL);
+  CHECK(pack(plain(at(kA), at(kB)), packed(k + kNew - 16, at(kE))) == HACK_EINVAL);
+  CHECK(pack(plain(at(kA), at(kB)), packed(at(kE), v)) == HACK_EINVAL);
+  CHECK(pack(plain(at(kA), at(kB), pos), packed(at(kC), at(kE), pos + 255)) == HACK_EINVAL);
+  CHECK(pack(plain(at(kA), at(kB)), packed(at(kC), at(kE), kept + 159), kept) == HACK_EINVAL);
+  CHECK(unpack(packed(at(kC), at(kE)), plain(at(kA), at(kA + kPlain - 16))) == HACK_EINVAL);
+  CHECK(unpack(packed(at(kC), at(kE)), plain(at(kC + kPacked - 16), at(kA))) == HACK_EINVAL);
+  CHECK(unpack(packed(at(kC), at(kE), pos), plain(at(kB), at(kA), pos + 255)) == HACK_EINVAL);
+  CHECK(attn(q, packed(at(kC), at(kE)), q + kNew - 16) == HACK_EINVAL);
+  CHECK(stub::packs.size() == 2 && stub::unpacks.size() == 1);
+  return 0;
+}
+
 // Every unit once, whatever their number.
 int many_units() {
   constexpr int n = 3000;
@@ -400,7 +435,7 @@ int no_exceptions() {
 
 int main(int argc, char** argv) {
   const std::map<std::string, int (*)()> checks = {{"rotate_refusals", rotate_refusals}, {"rope_freqs", rope_freqs}, {"pack_refusals", pack_refusals},
-                                                   {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions}};
+                                                   {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions}};
   const auto it = argc > 1 ? checks.find(argv[1]) : checks.end();
   if (it == checks.end()) return 2;
   const int rc = it->second();

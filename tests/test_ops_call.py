@@ -190,3 +190,14 @@ def test_wrong_calls():
         rotate(eps="x")
     with pytest.raises(AttributeError):
         pack(cache_in=7)
+
+
+@pytest.mark.parametrize("number", [2**31, -2**31 - 1, 2**64])
+def test_numbers_of_more_than_32_bits_are_refused(number):
+    assert rotate(pos0=-2**31) == -4 and rotate(pos0=2**31 - 1) == -4
+    assert [x[7] for x in SEEN] == [-2**31, 2**31 - 1]
+    SEEN.clear()
+    for f in (lambda: rotate(pos0=number), lambda: pack(N=number), lambda: pack(B=number)):
+        with pytest.raises(OverflowError):
+            f()
+    assert not SEEN

@@ -18,7 +18,7 @@ def program(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("name", ["rotate_refusals", "rope_freqs", "pack_refusals", "many_units", "attn_plan", "no_exceptions"])
+@pytest.mark.parametrize("name", ["rotate_refusals", "rope_freqs", "pack_refusals", "shared_memory", "many_units", "attn_plan", "no_exceptions"])
 def test_host_side(program, name):
     r = subprocess.run([str(program), name], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip().endswith("ok"), r.stdout + r.stderr[-2000:]
