@@ -204,14 +204,15 @@ void plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t b
   int32_t ends[kRows + 1];   // units of so many chunks
   const auto us = [&](int64_t chunk) {
     const int64_t rows = (longest + chunk - 1) / chunk;
-    const bool exact = tiles > 1 && rows <= kRows;
+    const bool exact = tiles > 1 && rows > 1 && rows <= kRows;
     if (exact) std::fill(ends, ends + rows + 1, 0);
     int64_t parts = 0;
-    for (int i = 0; i < n; ++i) {
-      const int64_t chunks = ((len[i] - 1) / kPackRows + chunk) / chunk;
+    for (int i = 0; i < n && rows > 1; ++i) {
+      const uint32_t chunks = ((uint32_t)(len[i] - 1) / kPackRows + (uint32_t)chunk) / (uint32_t)chunk;
       parts += chunks;
       if (exact) ++ends[chunks];
     }
+    if (rows == 1) parts = n;
     // Chunks on one XCD: chunk c of the i-th unit, by length, is on (c n + i) mod 8.  Its query tiles share it, so that one chunk more may be many work-groups.
     int64_t on = (parts + kXcds - 1) / kXcds;
     if (exact) {
@@ -231,20 +232,22 @@ void plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t b
   int64_t best = longest;
   if (most > 1 && longest > kLeast) {
     double best_us = us(longest);
+    // no cut can be faster than the merge and the blocks spread evenly: most launches of short units end here
+    const double least = r.merge + r.part * n * tiles + r.block * std::max((double)kLeast, 0.76 * blocks * tiles / (kXcds * cus));
     const auto consider = [&](int64_t chunk) {
       chunk = std::max<int64_t>({chunk, kLeast, (longest + most - 1) / most});
       if (chunk >= longest) return;
       const double t = us(chunk);
       if (t < best_us) best = chunk, best_us = t;
     };
-    for (int each = 1; each <= 2; ++each) {
+    for (int each = 1; each <= 2 && best_us > least; ++each) {
       const int64_t groups = kXcds * (each * cus / tiles);   // a query tile's
       if (groups < 1) continue;
       consider((blocks + groups - 1) / groups);
       if (2 * groups > n) consider((2 * blocks + 2 * groups - n - 1) / (2 * groups - n));
       if (groups > n) consider((longest + groups / n - 1) / (groups / n));
     }
-    consider((int64_t)std::ceil(std::sqrt(r.part * tiles * blocks / r.block)));
+    if (best_us > least) consider((int64_t)std::ceil(std::sqrt(r.part * tiles * blocks / r.block)));
   }
   a->chunk = (int32_t)best;
   a->n_chunks = (int32_t)((longest + best - 1) / best);
