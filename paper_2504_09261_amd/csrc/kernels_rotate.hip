@@ -8,8 +8,8 @@
 // that its pairs are its own and the lanes of an access lie side by side: no exchange but the sum of squares over the 8 (head_dim 128) or 4 lanes of a row.  Angles are formed
 // once for a token and used for all heads that the thread walks over.  They are exact where it matters: the frequency is held in units of 2^-64
 // turns, so the product with a position wraps to its fraction of a turn in integers, however far the position.
-// Measured: 16384 rows of 32 + 8 heads of 128 out of a projection, normed and turned, 65 us (5.1 TB/s of the 6.2 that a plain elementwise
-// kernel reaches), 2 x 4096 rows of 16 heads in two axes 14 us (4.8).
+// Measured: 16384 rows of 32 + 8 heads of 128 out of a projection, normed and turned, 66 us (5.1 TB/s of the 6.2 that a plain elementwise
+// kernel reaches), 2 x 4096 rows of 16 heads in two axes 13 us (5.1).
 #include <algorithm>
 
 #include "device_util.h"
