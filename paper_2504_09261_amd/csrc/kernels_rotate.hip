@@ -93,32 +93,44 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
   const int64_t n = (int64_t)(tile << t.tokens_log2) + (slot & ((1 << t.tokens_log2) - 1));
   if (n >= a.n) return;   // all lanes of a row
 
-  // This lane's 16 elements: of its region of a row, an axis' section or what does not rotate, its piece of every part; in a rotating section they are
-  // whole pairs in either layout.
+  // This lane's 16 elements: a piece of every part of its region of a row.  Pairs side by side lie in one piece, so that the region is the whole row and
+  // pieces turn or not; pairs (i, i + S/2) need a region each for an axis' section and for what does not rotate, and lanes turn or not.  (Regions for the
+  // former too: 3 x 1369 float32 rows of 20 heads of 64, of which 16 elements rotate, 11.8 us, so 9.6; 50 x 900 of 8 + 1 heads 70, 37.)
   constexpr int E = Piece<T>::kElements, PIECES = 16 / E;
-  const bool turns = 16 * j < a.rot_dim;
-  int base = a.rot_dim, size = D - a.rot_dim, axis = 0;
-  if (turns) {
-    axis = 16 * j >= a.section ? 1 : 0;
-    base = axis * a.section;
-    size = a.section;
+  const bool lane_turns = 16 * j < a.rot_dim;
+  int base = 0, size = D;
+  if (HALF) {
+    base = lane_turns ? (16 * j >= a.section ? a.section : 0) : a.rot_dim;
+    size = lane_turns ? a.section : D - a.rot_dim;
   }
-  const int part = size / PIECES, in_part = (16 * j - base) / PIECES;   // elements of a part, and this lane's first one there
-  float c[8], s[8];
-  if (turns) {
-    const int p = a.pos ? a.pos[b * a.pos_b + (int64_t)axis * a.n + n] : a.pos0 + (int)n;
+  const int part = size / PIECES, in_part = (16 * j - base) / PIECES, at = base + in_part;   // elements of a part, and this lane's first one
+  const auto turns = [&](int piece) { return HALF ? lane_turns : at + piece * part < a.rot_dim; };
+  constexpr int STEP = HALF ? 8 : E / 2;   // pairs that turn or not together
+  const int* const pos = a.pos ? a.pos + b * a.pos_b + n : nullptr;
+  const bool two = HALF ? lane_turns && base > 0 : a.section < a.rot_dim;   // the second axis' position is needed
+  int p0 = a.pos0 + (int)n, p1 = p0;   // on the two axes
+  if (pos) {
+    p0 = pos[0];
+    if (two) p1 = pos[a.n];
+  }
+  uint64_t f[8];   // loaded in front of the branches; numbers of pairs that do not turn are below D / 2 too
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {   // pair i: elements i and 8 + i, or 2 i and 2 i + 1
-      const int number = HALF ? i / E * part + in_part + i % E : (2 * i / E * part + in_part + 2 * i % E) / 2;
-      const uint64_t f = a.turns[base / 2 + number];
+  for (int i = 0; i < 8; ++i) f[i] = a.turns[HALF ? base / 2 + i / E * part + in_part + i % E : (at + 2 * i / E * part + 2 * i % E) / 2];
+  float c[8], s[8];
+#pragma unroll
+  for (int i0 = 0; i0 < 8; i0 += STEP) {   // pair i: elements i and 8 + i, or 2 i and 2 i + 1
+    const int piece = 2 * i0 / E;
+    if (!turns(piece)) continue;
+    const int p = (HALF ? base > 0 : at + piece * part >= a.section) ? p1 : p0;
+#pragma unroll
+    for (int i = i0; i < i0 + STEP; ++i) {
       // upper half of the low 64 bits of p f; the low half of f makes up for p < 0 standing for p + 2^32
-      const unsigned u = __umulhi((unsigned)p, (unsigned)f) + (unsigned)p * (unsigned)(f >> 32) - (p < 0 ? (unsigned)f : 0u);
+      const unsigned u = __umulhi((unsigned)p, (unsigned)f[i]) + (unsigned)p * (unsigned)(f[i] >> 32) - (p < 0 ? (unsigned)f[i] : 0u);
       cos_sin(u, c[i], s[i]);
       c[i] *= a.gain;
       s[i] *= a.gain;
     }
   }
-  const int at = base + in_part;
   const T* src = static_cast<const T*>(t.x) + b * t.sb + n * t.sn;
   T* dst = static_cast<T*>(t.out) + (b * t.heads * a.n + n) * D;
   const int across = SLOTS >> t.tokens_log2;   // heads at a time
@@ -151,9 +163,11 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
         if (t.w != nullptr) v[i] *= w[i];
       }
     }
-    if (turns) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+    for (int i0 = 0; i0 < 8; i0 += STEP) {
+      if (!turns(2 * i0 / E)) continue;
+#pragma unroll
+      for (int i = i0; i < i0 + STEP; ++i) {
         const int ia = HALF ? i : 2 * i, ib = HALF ? 8 + i : 2 * i + 1;
         const float p = v[ia], q = v[ib];
         v[ia] = fmaf(p, c[i], -(q * s[i]));
@@ -196,7 +210,7 @@ void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout
     // Rows of one head side by side: few, so that the rest of the work-group takes the heads beside it, which lie behind each other in a projection
     // (4, 8, 32 rows: 16384 rows of 32 + 8 heads 64.8, 66.7, 65.4 us, 32 x 256 of 30 + 30 heads 26.0, 29.0, 28.5, 2 x 4096 of 16 heads 15.4, 14.0, 14.6),
     // but as many as leave no more than a quarter of the lanes without a head (2 x 11844 rows of 10 + 2 heads of 64: 22.7 us with as few as fit the heads of
-    // the larger tensor, 15.8 so; 8 x 10948 of 2 + 1 heads 21.1, 18.6; 50 x 900 float32 rows of 8 + 1 heads, the one of 71 drawn shapes that loses much, 58, 69).
+    // the larger tensor, 15.8 so; 8 x 10948 of 2 + 1 heads 21.1, 18.6).
     const auto idle = [&](int log2) {
       const int across = slots >> log2, taken = (t.heads + across - 1) / across * across;
       return 4 * (taken - t.heads) > taken;
@@ -209,7 +223,7 @@ void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout
   // Outputs that the L2 caches cannot hold pass them by (16384 rows of 32 + 8 heads 71.7 -> 65.3 us, 32 x 256 of 30 + 30 heads 30.2 -> 26.6); smaller ones
   // are for the next launch to find there, and where a row's pieces of an access make up less than 32 bytes (as many as its region has elements) they
   // need the caches to become lines (8 x 8192 float32 rows of 16 heads of 64, of which 16 elements rotate: 129 us, past the caches 326; 32 elements of bf16 rows 61, 51).
-  const auto wide = [](int region) { return region == 0 || region >= 32; };
+  const auto wide = [&](int region) { return !half_layout || region == 0 || region >= 32; };
   const bool stream = rows * head_dim * elem_bytes > kL2Bytes && wide(a.section) && wide(head_dim - a.rot_dim);
   // A thread walks over as many heads as leave enough work-groups: it forms its angles once for all of them.
   int64_t groups = 0;
