@@ -192,8 +192,8 @@ void measure(const int32_t* len, int n, int64_t* blocks, int64_t* longest) {
 // and two (by the mean, by the mean and half a chunk left over in every unit, by the longest); chunks that balance their own time with that of their parts.
 // Fitted to 250 launches of 4 to 600 units, even and ragged, 500 to 32000 keys, 1 to 1500 queries, each cut into 1 to 32 chunks: what it picks takes
 // 1.03 times the best of them on average, 1.38 at most (always two work-groups to a compute unit: 1.06, 2.1).  Us a launch, always two / so: 14 units
-// of 21747 to 27815 keys, 472 queries 132 / 103, 12 of 1009 to 1591, 5 queries 9.1 / 6.9; head_dim 64, 10 of 13694 to 22356, 176 queries 30 / 35.
-void plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t blocks, int64_t longest, AttnPackedHead* a) {
+// of 21747 to 27815 keys, 472 queries 132 / 103, 12 of 1009 to 1591, 5 queries 9.1 / 6.9.
+double plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t blocks, int64_t longest, AttnPackedHead* a) {
   struct Rates { double block, merge, part; };   // us of 64 keys to a work-group alone, of the merge, of a work-group's part
   static constexpr Rates kRates[2][3] = {{{.16, 2.7, .003}, {.28, 2.5, .005}, {.80, 5.5, .011}}, {{.23, 3.0, .006}, {.45, 4.0, .022}, {1.45, 4.8, .036}}};
   constexpr int kXcds = 8, kLeast = 4;   // blocks of a chunk: one for each wave of the smaller forms
@@ -207,12 +207,19 @@ void plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t b
     const bool exact = tiles > 1 && rows > 1 && rows <= kRows;
     if (exact) std::fill(ends, ends + rows + 1, 0);
     int64_t parts = 0;
-    for (int i = 0; i < n && rows > 1; ++i) {
-      const uint32_t chunks = ((uint32_t)(len[i] - 1) / kPackRows + (uint32_t)chunk) / (uint32_t)chunk;
-      parts += chunks;
-      if (exact) ++ends[chunks];
+    const float inv = 1.f / chunk;
+    const auto chunks_of = [&](int i) { return (int)(((len[i] - 1) / kPackRows + 0.5f) * inv) + 1; };
+    if (rows == 1) {
+      parts = n;
+    } else if (exact) {
+      for (int i = 0; i < n; ++i) {
+        const int chunks = std::min<int>(chunks_of(i), rows);
+        parts += chunks;
+        ++ends[chunks];
+      }
+    } else {
+      for (int i = 0; i < n; ++i) parts += chunks_of(i);
     }
-    if (rows == 1) parts = n;
     // Chunks on one XCD: chunk c of the i-th unit, by length, is on (c n + i) mod 8.  Its query tiles share it, so that one chunk more may be many work-groups.
     int64_t on = (parts + kXcds - 1) / kXcds;
     if (exact) {
@@ -230,8 +237,8 @@ void plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t b
     return parts == n ? t : t + r.merge + r.part * parts * tiles + 3e-4 * (rows * n * tiles);   // the last: empty work-groups
   };
   int64_t best = longest;
+  double best_us = us(longest);
   if (most > 1 && longest > kLeast) {
-    double best_us = us(longest);
     // no cut can be faster than the merge and the blocks spread evenly: most launches of short units end here
     const double least = r.merge + r.part * n * tiles + r.block * std::max((double)kLeast, 0.76 * blocks * tiles / (kXcds * cus));
     const auto consider = [&](int64_t chunk) {
@@ -251,36 +258,33 @@ void plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t b
   }
   a->chunk = (int32_t)best;
   a->n_chunks = (int32_t)((longest + best - 1) / best);
+  return best_us;
 }
 
 // Queries of a work-group.  Sixteen and 32 have every wave convert the keys it takes, 128 (kTileQueries) share every converted block, which is what a large
-// launch wants, but give a quarter of the work-groups.  Which is faster for more than 64 queries goes by an estimate in rounds of the work-groups that start at
-// once, at what a block of 64 keys takes a work-group (two to a compute unit, or three of 32 queries at head_dim 64, and alone), its start and end, and a
-// merge.  Fitted to 192 launches of 8 to 480 units, 300 to 6000 keys, 33 to 1024 queries; there it picks a form 0.5 % slower than the better one on average,
-// 17 % at most but for one (42 %; always 32 queries: 3.4 % on average, 68 % at most, always 128: 38 and 170 %).  Us a launch, 32 / 128 queries, head_dim 128: 64 units of 6000 keys, 1024 queries 247 /
-// 189, of 1500, 200 22.6 / 37.1; 128 units of 300, 576 38.0 / 28.0; head_dim 64: 480 units of 300, 1024 104 / 83, 240 of 6000, 128 77 / 115.
-double estimate_us(const hack_ctx* ctx, int queries, const int32_t* len, int n_units, int64_t blocks, int64_t longest, int N_k) {
-  struct Rates { int at_once; double pair, alone, fixed; };   // work-groups a compute unit holds, us a block of 64 keys with neighbours and alone, start and end
-  static constexpr Rates kRates[2][2] = {{{3, .62, .28, 3.5}, {2, 1.45, 1.02, 4.0}}, {{2, .70, .43, 4.0}, {2, 1.94, 1.40, 5.0}}};
-  const Rates& r = kRates[ctx->cfg.head_dim == 128][queries == kTileQueries];
-  AttnPackedHead a{};
-  a.n_units = n_units;
-  a.q_tiles = (N_k + queries - 1) / queries;
-  plan_chunks(ctx, queries, len, blocks, longest, &a);
-  const double each = (double)blocks / n_units, cut = std::max(1.0, std::ceil(each / a.chunk));
-  const int64_t groups = (int64_t)(n_units * cut) * a.q_tiles, slots = (int64_t)r.at_once * ctx->cus, full = groups / slots, rest = groups % slots;
-  double us = each / cut * (full * r.pair + (rest == 0 ? 0.0 : rest <= ctx->cus ? r.alone : r.pair)) + r.fixed * (1.0 + 0.6 * (double)(full + (rest > 0) - 1));
-  if (cut > 1.0) us += 4.0 + n_units * cut * N_k * ctx->cfg.head_dim * 8.0 / 4e6;
-  return us;
-}
-
+// launch wants, but give an eighth of the work-groups.  Which is fastest goes by the plan's estimate, scaled and with the start of the work-groups added as
+// fitted to 257 drawn launches of 1 to 500 units, even and ragged, 100 to 60000 keys, 17 to 2000 queries: what it picks takes 1.014 times the best on
+// average, 1.30 at most (114 others: 1.02, 1.32; always 16: 1.16, 2.4; always 32: 1.08, 1.6; always 128: 1.33, 2.6).  Us a launch, 16 / 32 / 128 queries,
+// head_dim 128: 9 units of 1440 keys, 207 queries 10.6 / 13.2 / 15.6, 46 of 12401, 187 88.8 / 70.7 / 85.3, 14 of 20679, 378 108 / 77 / 64.
 int queries_per_group(const hack_ctx* ctx, const int32_t* len, int n_units, int N_k) {
   if (ctx->cfg.dtype == HACK_F32) return 16;
   if (ctx->packed_queries != 0) return ctx->packed_queries;
-  if (N_k <= 64) return N_k <= 16 ? 16 : 32;
+  if (N_k <= 16) return 16;
+  struct Form { int queries; double scale, start, groups; };   // us of a launch's start, of 256 work-groups'
+  static constexpr Form kForms[2][3] = {{{16, .81, 4.0, .36}, {32, .85, 4.1, .75}, {kTileQueries, 1.10, 4.6, 2.2}},
+                                        {{16, 1.00, 4.2, 1.1}, {32, .83, 4.5, 2.0}, {kTileQueries, .86, 4.3, 3.35}}};
   int64_t blocks, longest;
   measure(len, n_units, &blocks, &longest);
-  return 1.06 * estimate_us(ctx, kTileQueries, len, n_units, blocks, longest, N_k) < estimate_us(ctx, 32, len, n_units, blocks, longest, N_k) ? kTileQueries : 32;
+  int queries = 0;
+  double best = 0.0;
+  for (const Form& f : kForms[ctx->cfg.head_dim == 128]) {
+    AttnPackedHead a{};
+    a.n_units = n_units;
+    a.q_tiles = (N_k + f.queries - 1) / f.queries;
+    const double us = f.scale * plan_chunks(ctx, f.queries, len, blocks, longest, &a) + f.start + f.groups * n_units * a.q_tiles / 256.0;
+    if (queries == 0 || us < best) queries = f.queries, best = us;
+  }
+  return queries;
 }
 
 // In what order units start: the longest first, except that where all work-groups start at once, two to a compute unit (one on each first, then a second
