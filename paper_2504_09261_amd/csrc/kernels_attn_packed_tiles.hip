@@ -104,10 +104,10 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_packed_tiles(const AttnPacke
     }
     c.exponent = p[exp_off + (b & 1) * 2];
   };
-  // Rows in groups of four, a group's 64-byte pieces row after row, 16-byte chunks permuted by the group.  Written 16 rows at one chunk, K read 16 rows
-  // at one chunk, V^T 8 rows x 32 bytes.
+  // Rows in groups of four, a group's 64-byte pieces row after row, 16-byte chunks permuted by two bits of the row (packed_device.h).  Written 8 rows at one
+  // chunk at a time, K read 16 rows at one chunk, V^T 8 rows x 32 bytes.
   const int row = 16 * (w >> 1) + col, chunk0 = D == 128 ? 4 * g + 2 * (w & 1) : 2 * g + (w & 1);
-  auto k_chunk = [](int r, int c) { return (r >> 2) * 4 * D + (c >> 2) * 128 + (r & 3) * 32 + ((c & 3) ^ ((r >> 2) & 3)) * 8; };
+  auto k_chunk = [](int r, int c) { return (r >> 2) * 4 * D + (c >> 2) * 128 + (r & 3) * 32 + ((c & 3) ^ v_flip(r)) * 8; };
   int k_to[CW], v_to[CW];
 #pragma unroll
   for (int i = 0; i < CW; ++i) {
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_packed_tiles(const AttnPacke
   float mc[2] = {-FLT_MAX, -FLT_MAX};   // probabilities are 2^(c2 s - mc); finite from the start, so that keys whose score is -inf get 0
 
   const int e = col >> 2, qd = col & 3;
-  const int k_off = e * 4 * D + (col & 3) * 32 + (g ^ e) * 8;                          // K operand: row 16 kt + col, chunk 4 c + g
+  const int k_off = e * 4 * D + (col & 3) * 32 + (g ^ v_flip(col)) * 8;                          // K operand: row 16 kt + col, chunk 4 c + g
   const int v_even = v_chunk<D>(4 * g + e, qd >> 1) + 4 * (qd & 1), v_odd = v_even ^ 16;   // V^T operand: rows 4 g + e and 16 + 4 g + e
   bf16x8 ones;
 #pragma unroll
