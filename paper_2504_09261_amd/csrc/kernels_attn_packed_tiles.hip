@@ -6,7 +6,7 @@
 // rows to LDS, here every thread loads 16 codes of K and 16 of V (8 at head_dim 64) stages ahead, and in the first half of a stage
 // turns them into bf16 and writes them: K(j + 2) and V(j), which the barrier in the middle of the stage publishes and the next stage reads.
 //
-// Bound by the matrix cores and the vector work beside them.  Measured, head_dim 128: 32 units of 1943 and 3885 keys, 4096 queries 182 to 186 us (1.05 to 1.07
+// Bound by the matrix cores and the vector work beside them.  Measured, head_dim 128: 32 units of 1943 and 3885 keys, 4096 queries 179 to 186 us (1.05 to 1.09
 // PFLOP/s; a large library product reaches 1.2), over 10521 keys 605 to 617 us (1.14 to 1.17), where the kernel over bf16 rows, which converts nothing,
 // takes 568.  Conversions earlier in the stage 1 % slower, explicit waits equal.
 #include <cfloat>
