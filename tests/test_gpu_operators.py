@@ -201,6 +201,27 @@ def test_norm_rotate(contexts, dtype, d, rot, axes, layout, norm):
         assert torch.equal(alone, qo)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d, rot, axes, layout", [(128, 128, 1, "half"), (64, 32, 2, "half"), (64, 16, 1, "interleaved"), (128, 96, 2, "interleaved")])
+@pytest.mark.parametrize("hq, hk_", [(1, 1), (3, 1), (10, 2), (1, 5), (17, 33)])
+def test_any_number_of_heads_gives_what_each_gives_alone(contexts, dtype, d, rot, axes, layout, hq, hk_):
+    """How many rows of a head a work-group takes follows from the heads of each tensor; what becomes of a row does not."""
+    hk = contexts(1, d, dtype)
+    g = torch.Generator(DEV).manual_seed(hq)
+    B, N = 2, 67
+    q, k = rows_in((B, hq, N, d), "projection", dtype, g), rows_in((B, hk_, N, d), "part", dtype, g)
+    w = [1 + torch.randn((h, d), generator=g, device=DEV) / 3 for h in (hq, hk_)]
+    rope = Rope.scaled(rot, axes, layout)
+    pos = torch.randint(0, 9000, (B, axes, N), generator=g, device=DEV, dtype=torch.int32)
+    out = [torch.full((B, h, N, d), 7.0, dtype=q.dtype, device=DEV) for h in (hq, hk_)]
+    hk.norm_rotate(q, k, "rms", 1e-6, *w, rope, *out, pos=pos)
+    alone = torch.empty((B, 1, N, d), dtype=q.dtype, device=DEV)
+    for x, weight, o in zip((q, k), w, out):
+        for h in range(x.shape[1]):
+            hk.norm_rotate(x[:, h:h + 1], None, "rms", 1e-6, weight[h].contiguous(), None, rope, alone, None, pos=pos)
+            assert torch.equal(alone[:, 0], o[:, h])
+
+
 # ---- packed caches -----------------------------------------------------------
 GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
