@@ -232,21 +232,42 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
-// A host array of a row number for every unit; None: NULL.  Sets *convert for another object, which the caller makes one of.
-bool read_first(PyObject* o, int64_t units, HostArray* a, const int32_t** p, bool* convert) {
-  *p = nullptr;
-  *convert = false;
-  if (o == Py_None) return true;
-  if (!a->is(o, 'i', 'i')) {
-    *convert = true;
-    return true;
+// A host array of a row number for every unit, int32 or int64; None: NULL.  Sets convert for another object, which the caller makes one of.
+struct First {
+  HostArray a;
+  int32_t* own = nullptr;
+  const int32_t* p = nullptr;
+  bool convert = false;
+  ~First() { PyMem_Free(own); }
+  bool read(PyObject* o, int64_t units) {
+    if (o == Py_None) return true;
+    const bool narrow = a.is(o, 'i', 'i');
+    if (!narrow && !(a.held && a.b.format && (a.b.format[0] == 'l' || a.b.format[0] == 'q') && a.b.format[1] == 0 && a.b.itemsize == 8)) {
+      convert = true;
+      return true;
+    }
+    if (a.count() != units) return refuse("a row number for every unit");
+    if (narrow) {
+      p = static_cast<const int32_t*>(a.b.buf);
+      return true;
+    }
+    p = own = static_cast<int32_t*>(PyMem_Malloc(units * sizeof(int32_t) + 1));
+    if (!own) {
+      PyErr_NoMemory();
+      return false;
+    }
+    const int64_t* from = static_cast<const int64_t*>(a.b.buf);
+    bool fits = true;
+    for (int64_t i = 0; i < units; ++i) {
+      own[i] = (int32_t)from[i];
+      fits &= own[i] == from[i];
+    }
+    if (!fits) PyErr_SetString(PyExc_OverflowError, "a number of more than 32 bits");
+    return fits;
   }
-  if (a->count() != units) return refuse("a row number for every unit");
-  *p = static_cast<const int32_t*>(a->b.buf);
-  return true;
-}
+};
 
-// pack(fn, ctx, info, B, N_k, cache_in, k_new, v_new, pos_new, kept, first, packed, stream) -> status, None unless first is an array of int32
+// pack(fn, ctx, info, B, N_k, cache_in, k_new, v_new, pos_new, kept, first, packed, stream) -> status, None where first is no array of integers
 PyObject* pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!arity(n, 13)) return nullptr;
   Info info;
@@ -255,11 +276,9 @@ PyObject* pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t B, N_k, pos_new;
   if (!int32_arg(a[3], &B) || !int32_arg(a[4], &N_k) || !int32_arg(a[8], &pos_new)) return nullptr;
   const int64_t units = (int64_t)B * info.heads;
-  HostArray fa;
-  const int32_t* first;
-  bool convert;
-  if (!read_first(a[10], units, &fa, &first, &convert)) return nullptr;
-  if (convert) Py_RETURN_NONE;
+  First first;
+  if (!first.read(a[10], units)) return nullptr;
+  if (first.convert) Py_RETURN_NONE;
   RowCache in;
   Packed out;
   if (a[5] != Py_None && !read_rows(in, a[5], info, units)) return nullptr;
@@ -284,12 +303,12 @@ PyObject* pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int status;
   Py_BEGIN_ALLOW_THREADS
   status = reinterpret_cast<decltype(&hack_pack)>(fn)((hack_ctx*)ctx, B, N_k, a[5] == Py_None ? nullptr : &in.c, k.p, v.p, pos_new, (const int32_t*)kept.p,
-                                                     kept.p ? kept.shape[1] : 0, first, &out.c, stream);
+                                                     kept.p ? kept.shape[1] : 0, first.p, &out.c, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(status);
 }
 
-// unpack(fn, ctx, info, B, packed, first, out, stream) -> status, None unless first is an array of int32
+// unpack(fn, ctx, info, B, packed, first, out, stream) -> status, None where first is no array of integers
 PyObject* unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!arity(n, 8)) return nullptr;
   Info info;
@@ -298,17 +317,15 @@ PyObject* unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t B;
   if (!int32_arg(a[3], &B)) return nullptr;
   const int64_t units = (int64_t)B * info.heads;
-  HostArray fa;
-  const int32_t* first;
-  bool convert;
-  if (!read_first(a[5], units, &fa, &first, &convert)) return nullptr;
-  if (convert) Py_RETURN_NONE;
+  First first;
+  if (!first.read(a[5], units)) return nullptr;
+  if (first.convert) Py_RETURN_NONE;
   Packed in;
   RowCache out;
   if (!read_packed(in, a[4], info, units) || !read_rows(out, a[6], info, units)) return nullptr;
   int status;
   Py_BEGIN_ALLOW_THREADS
-  status = reinterpret_cast<decltype(&hack_unpack)>(fn)((hack_ctx*)ctx, B, &in.c, first, &out.c, stream);
+  status = reinterpret_cast<decltype(&hack_unpack)>(fn)((hack_ctx*)ctx, B, &in.c, first.p, &out.c, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(status);
 }

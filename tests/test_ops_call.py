@@ -148,11 +148,13 @@ def test_packed_calls_arrive_as_given():
     assert SEEN.pop() == (2**47, 2, 4, None, 16, 32, 5, None, 0, None, (1024, 2048, None, 2560, OFF, LEN), 77)
     assert pack(cache(pos=True), None, None, Tensor(8, (6, 33), I32), np.arange(6, dtype=np.int32), cache(packed=True, pos=True)) == 0
     assert SEEN.pop() == (2**47, 2, 4, (1024, 2048, 4096, 40, OFF, LEN), None, None, 5, 8, 33, LEN, (1024, 2048, 4096, 2560, OFF, LEN), 77)
-    assert pack(first=np.arange(6)) is None and pack(first=list(range(6))) is None and not SEEN     # the caller converts them
+    assert pack(first=np.arange(6)) == 0 and SEEN.pop()[9] == LEN                                     # int64 arrays as well
+    assert pack(first=list(range(6))) is None and pack(first=np.arange(6.0)) is None and pack(first=np.arange(12)[::2]) is None and not SEEN     # the caller converts them
     un = lambda **kw: binding._ops_call.unpack(addr(unpack_fn), 2**47, INFO, 2, kw.get("packed") or cache(packed=True), kw.get("first"), kw.get("out") or cache(), 77)  # noqa: E731
     assert un(first=np.arange(6, dtype=np.int32)) == 0
     assert SEEN.pop() == (2**47, 2, (1024, 2048, None, 2560, OFF, LEN), LEN, (1024, 2048, None, 40, OFF, LEN), 77)
-    assert un(first=np.arange(6)) is None and not SEEN
+    assert un(first=np.arange(6)) == 0 and SEEN.pop()[3] == LEN
+    assert un(first=list(range(6))) is None and not SEEN
     at = lambda q, kv=None: binding._ops_call.attn(addr(attn_fn), 2**47, INFO, q, kv or cache(packed=True), 0.25, Tensor(48, q.shape), 77)  # noqa: E731
     assert at(Tensor(16, (2, 12, 5, 64))) == 0
     assert SEEN.pop() == (2**47, 2, 20, 16, (1024, 2048, None, 2560, OFF, LEN), 0.25, 48, 77)
@@ -197,7 +199,7 @@ def test_numbers_of_more_than_32_bits_are_refused(number):
     assert rotate(pos0=-2**31) == -4 and rotate(pos0=2**31 - 1) == -4
     assert [x[7] for x in SEEN] == [-2**31, 2**31 - 1]
     SEEN.clear()
-    for f in (lambda: rotate(pos0=number), lambda: pack(N=number), lambda: pack(B=number)):
+    for f in (lambda: rotate(pos0=number), lambda: pack(N=number), lambda: pack(B=number)) + ((lambda: pack(first=np.full(6, number)),) if number < 2**63 else ()):
         with pytest.raises(OverflowError):
             f()
     assert not SEEN
