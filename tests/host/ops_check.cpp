@@ -199,6 +199,22 @@ int rope_freqs() {
   return 0;
 }
 
+// Frequencies below zero turn exactly the other way.
+int backward_frequencies() {
+  Context c;
+  double w[64], back[64];
+  for (int i = 0; i < 64; ++i) {
+    w[i] = i == 0 ? 1e6 : i == 1 ? 1e-30 : std::pow(10000.0, -i / 64.0);
+    back[i] = -w[i];
+  }
+  const hack_rope forth{HACK_ROPE_HALF, 128, 1, 1.f, w}, p{HACK_ROPE_HALF, 128, 1, 1.f, back};
+  const hack_rows x{at(kA), at(kB), 1, 0, 0, kD, nullptr, 0};
+  CHECK(hack_rotate(c.ctx, 1, 1, &x, &forth, nullptr, 0, 0, kStream) == HACK_OK && hack_rotate(c.ctx, 1, 1, &x, &p, nullptr, 0, 0, kStream) == HACK_OK);
+  const RotateArgs &a = stub::rotations[0], &b = stub::rotations[1];
+  for (int i = 0; i < 64; ++i) CHECK(a.turns[i] + b.turns[i] == 0);
+  return 0;
+}
+
 int pack_refusals() {
   Context c;
   CHECK(hack_packed_bytes(96, 64, nullptr) == HACK_EINVAL);
@@ -435,7 +451,8 @@ int no_exceptions() {
 
 int main(int argc, char** argv) {
   const std::map<std::string, int (*)()> checks = {{"rotate_refusals", rotate_refusals}, {"rope_freqs", rope_freqs}, {"pack_refusals", pack_refusals},
-                                                   {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions}};
+                                                   {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions},
+                                                   {"backward_frequencies", backward_frequencies}};
   const auto it = argc > 1 ? checks.find(argv[1]) : checks.end();
   if (it == checks.end()) return 2;
   const int rc = it->second();

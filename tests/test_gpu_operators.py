@@ -114,6 +114,23 @@ def test_rotate(contexts, dtype, d, rot, axes, layout):
         assert torch.equal(y, out)
 
 
+@pytest.mark.parametrize("d, axes, layout", [(128, 1, "half"), (64, 1, "interleaved"), (128, 2, "half")])
+def test_rotate_backwards_at_far_positions(contexts, d, axes, layout):
+    """Small frequencies below zero are as exact as those above, and undo them."""
+    hk = contexts(1, d, "f32")
+    g = torch.Generator(DEV).manual_seed(d)
+    S = d // axes
+    x = torch.randn((1, 3, 6, d), generator=g, device=DEV)
+    pos = np.repeat(np.array([2 ** 31 - 1, -2 ** 31, 2 ** 31 - 12345, 2 ** 30 + 1, -2 ** 31 + 7, 1])[None, None], axes, 1).astype(np.int32)
+    freq = -np.tile(10000.0 ** (-2 * np.arange(S // 2) / S), axes)
+    out, back = torch.empty_like(x), torch.empty_like(x)
+    hk.rotate(x, Rope(freq, d, axes, layout), out, pos=torch.from_numpy(pos).to(DEV))
+    want, mag = turned(to64(x), pos, freq, 1.0, d, axes, layout)
+    check_rows(out, want, mag, "f32", ROTATION)
+    hk.rotate(out, Rope(-freq, d, axes, layout), back, pos=torch.from_numpy(pos).to(DEV))
+    check_rows(back, to64(x), 2 * np.abs(to64(x)).max() * np.ones(x.shape), "f32", ROTATION * 2.5)
+
+
 def test_rotate_numbers_rows_without_positions_and_turns_back(contexts):
     hk = contexts(1, 128, "f32")
     g = torch.Generator(DEV).manual_seed(3)

@@ -22,3 +22,8 @@ def program(tmp_path_factory):
 def test_host_side(program, name):
     r = subprocess.run([str(program), name], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip().endswith("ok"), r.stdout + r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("name", ["backward_frequencies"])
+def test_ranges(program, name):
+    test_host_side(program, name)
