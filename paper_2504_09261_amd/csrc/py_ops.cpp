@@ -299,6 +299,9 @@ PyObject* pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
       refuse("kept_idx: a row for every unit");
       return nullptr;
     }
+    // without columns the tensor has no address; NULL would say that there is no list, and the rows come in order
+    static int32_t nothing;
+    if (!kept.p) kept.p = &nothing;
   }
   int status;
   Py_BEGIN_ALLOW_THREADS

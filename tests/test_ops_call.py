@@ -203,3 +203,13 @@ def test_numbers_of_more_than_32_bits_are_refused(number):
         with pytest.raises(OverflowError):
             f()
     assert not SEEN
+
+
+def test_a_kept_list_of_no_columns_is_still_one():
+    """torch gives tensors without elements the address 0, which the C function takes for no list: all rows in order."""
+    assert pack(kept=Tensor(0, (6, 0), I32)) == 0
+    call = SEEN.pop()
+    assert call[7] and call[7] % 4 == 0 and call[8] == 0
+    with pytest.raises(AssertionError):
+        pack(kept=Tensor(0, (5, 0), I32))
+    assert not SEEN
