@@ -134,6 +134,18 @@ def _i64(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int64)
 
 
+def _exact(a, dtype) -> np.ndarray:
+    """A host array of an integer type; numbers that it does not hold are refused, not cut."""
+    x = np.asarray(a)
+    if x.dtype == dtype:
+        return np.ascontiguousarray(x)
+    with np.errstate(invalid="ignore"):
+        y = x.astype(dtype)
+    if not np.array_equal(x, y):
+        raise OverflowError(f"not all of the numbers are {np.dtype(dtype).name}")
+    return np.ascontiguousarray(y)
+
+
 def _u8(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.uint8)
 
@@ -210,7 +222,7 @@ class PackedCache:
     def __init__(self, k, v, off, length, pos=None):
         import torch
         self.k, self.v, self.pos = k, v, pos
-        self.off, self.len = _i64(off), _i32(length)
+        self.off, self.len = _exact(off, np.int64), _exact(length, np.int32)
         assert k.dtype == v.dtype == torch.uint8 and k.shape == v.shape and k.dim() == 2, "K and V: byte tensors [rows / 64, bytes of 64 rows]"
         assert k.shape[1] in (34 * 64, 34 * 128), "a block of 64 rows has 34 bytes an element of the head"
         assert pos is None or pos.dtype == torch.int32 and pos.numel() >= PACK_ROWS * k.shape[0], "pos: an int32 for every row"
@@ -220,7 +232,7 @@ class PackedCache:
     def empty(cls, head_dim: int, cap, device="cuda", with_pos: bool = False) -> "PackedCache":
         """Room for units of up to cap[u] rows, all of them empty."""
         import torch
-        blocks = -(-_i64(cap) // PACK_ROWS)
+        blocks = -(-_exact(cap, np.int64) // PACK_ROWS)
         n = int(blocks.sum())
         k, v = (torch.empty((n, packed_bytes(head_dim, PACK_ROWS)), dtype=torch.uint8, device=device) for _ in range(2))
         pos = torch.empty((n * PACK_ROWS,), dtype=torch.int32, device=device) if with_pos else None
@@ -449,7 +461,7 @@ class Hack:
         args = (_ops_addr["pack"], self.ctx and self.ctx.value, self._info, B, Nk, cache_in, k_new, v_new, pos_new, kept_idx)
         st = _ops_call.pack(*args, at, packed, _stream())
         if st is None:
-            st = _ops_call.pack(*args, _i32(at), packed, _stream())
+            st = _ops_call.pack(*args, _exact(at, np.int32), packed, _stream())
         if st != 0:
             self._check(st)
 
@@ -458,7 +470,7 @@ class Hack:
         args = (_ops_addr["unpack"], self.ctx and self.ctx.value, self._info, B, packed)
         st = _ops_call.unpack(*args, first, cache_out, _stream())
         if st is None:
-            st = _ops_call.unpack(*args, _i32(first), cache_out, _stream())
+            st = _ops_call.unpack(*args, _exact(first, np.int32), cache_out, _stream())
         if st != 0:
             self._check(st)
 

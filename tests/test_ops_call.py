@@ -213,3 +213,33 @@ def test_a_kept_list_of_no_columns_is_still_one():
     with pytest.raises(AssertionError):
         pack(kept=Tensor(0, (5, 0), I32))
     assert not SEEN
+
+
+@pytest.mark.parametrize("rows", [np.full(12, 2**32 + 5)[::2], [2**32 + 5] * 6, np.full(6, 2.0**32 + 5), np.full(6, 5.5), np.full(6, np.nan), np.full(6, 2**31, np.uint32),
+                                  [2**70] * 6, np.full(6, 2**64 - 1, np.uint64)],
+                         ids=["strided", "list", "far float", "half", "nan", "uint32", "far list", "uint64"])
+def test_row_numbers_that_32_bits_do_not_hold_are_refused(monkeypatch, rows):
+    """Those that the entries leave to the caller, and lengths of a packed cache."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(binding, "_stream", lambda: 77)
+    hk = object.__new__(binding.Hack)
+    hk.ctx, hk._info, hk.lib = C.c_void_p(2**47), INFO, None
+    monkeypatch.setitem(binding._ops_addr, "pack", addr(pack_fn))
+    monkeypatch.setitem(binding._ops_addr, "unpack", addr(unpack_fn))
+    new = dict(k_new=Tensor(16, (2, 3, 4, 64)), v_new=Tensor(32, (2, 3, 4, 64)))
+    mem = torch.zeros((100, 34 * 64), dtype=torch.uint8)
+    with pytest.raises(OverflowError):
+        hk.pack(2, 4, cache(packed=True), at=rows, **new)
+    with pytest.raises(OverflowError):
+        hk.unpack(2, cache(packed=True), cache(), first=rows)
+    with pytest.raises(OverflowError):
+        binding.PackedCache(mem, mem, np.zeros(6), rows)
+    assert not SEEN
+    hk.pack(2, 4, cache(packed=True), at=np.arange(12)[::2], **new)
+    hk.pack(2, 4, cache(packed=True), at=[0, 2, 4, 6, 8, 10], **new)
+    hk.unpack(2, cache(packed=True), cache(), first=torch.arange(0, 12, 2))
+    assert [c[9] for c in SEEN[:2]] == [[0, 2, 4, 6, 8, 10]] * 2 and SEEN[2][3] == [0, 2, 4, 6, 8, 10]
+    assert list(binding.PackedCache(mem, mem, [0, 64], np.array([3.0, 4.0])).len) == [3, 4]
+    for off in ([0.5, 64.0], np.array([2**64 - 64, 64], np.uint64)):
+        with pytest.raises(OverflowError):
+            binding.PackedCache(mem, mem, off, [1, 2])
