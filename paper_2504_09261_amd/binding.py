@@ -245,14 +245,20 @@ NORMS = {"rms": 0, "l2": 1}
 
 
 class Rope:
-    """A hack_rope: frequencies (radians per position, axis after axis), which elements rotate and how they pair."""
+    """A hack_rope: frequencies (radians per position, axis after axis), which elements rotate and how they pair.  Its parts are not replaced, since the library
+    reads the structure that they were put into; frequencies may be changed in place."""
 
     def __init__(self, freq, rot_dim: int, axes: int = 1, layout: str = "half", gain: float = 1.0):
-        self.freq = np.ascontiguousarray(freq, np.float64)
-        assert self.freq.shape == (rot_dim // 2,), "one frequency for every pair"
-        self.rot_dim, self.axes, self.layout, self.gain = rot_dim, axes, layout, gain
-        self._struct = hack_rope(ROPE_LAYOUTS[layout], rot_dim, axes, gain, self.freq.ctypes.data_as(C.POINTER(C.c_double)))
-        self.address = C.addressof(self._struct)
+        freq = np.ascontiguousarray(freq, np.float64)
+        assert freq.shape == (rot_dim // 2,), "one frequency for every pair"
+        struct = hack_rope(ROPE_LAYOUTS[layout], rot_dim, axes, gain, freq.ctypes.data_as(C.POINTER(C.c_double)))
+        self.__dict__.update(freq=freq, rot_dim=rot_dim, axes=axes, layout=layout, gain=gain, _struct=struct, address=C.addressof(struct))
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"a Rope's {name} is not replaced: make another one")
+
+    def __reduce__(self):   # a copy has a structure of its own, which points to its own frequencies
+        return Rope, (self.freq.copy(), self.rot_dim, self.axes, self.layout, self.gain)
 
     @classmethod
     def scaled(cls, rot_dim: int, axes: int = 1, layout: str = "half", scaling: str = "plain", base: float = 10000.0, factor: float = 1.0,

@@ -243,3 +243,27 @@ def test_row_numbers_that_32_bits_do_not_hold_are_refused(monkeypatch, rows):
     for off in ([0.5, 64.0], np.array([2**64 - 64, 64], np.uint64)):
         with pytest.raises(OverflowError):
             binding.PackedCache(mem, mem, off, [1, 2])
+
+
+def _freq_address(rope):
+    s = C.cast(rope.address, C.POINTER(binding.hack_rope)).contents
+    return C.cast(s.freq, C.c_void_p).value
+
+
+def test_a_rope_keeps_what_its_structure_points_to():
+    """The library reads frequencies, sizes and axes from the structure: they stay what the checks have seen, and alive, whatever becomes of the parts."""
+    import copy
+    import pickle
+    freq = np.linspace(0.5, 2, 16)
+    rope = binding.Rope(freq, 32, axes=2, layout="interleaved", gain=1.5)
+    for r in (rope, copy.copy(rope), copy.deepcopy(rope), pickle.loads(pickle.dumps(rope))):
+        s = C.cast(r.address, C.POINTER(binding.hack_rope)).contents
+        assert (s.layout, s.rot_dim, s.axes, s.gain) == (1, 32, 2, 1.5) == (binding.ROPE_LAYOUTS[r.layout], r.rot_dim, r.axes, r.gain)
+        assert s.freq[:16] == list(np.linspace(0.5, 2, 16)) == list(r.freq)
+        assert _freq_address(r) == r.freq.ctypes.data
+        assert r is rope or (r.address != rope.address and _freq_address(r) != _freq_address(rope))
+    for name, value in (("freq", np.zeros(16)), ("axes", 1), ("rot_dim", 16), ("layout", "half"), ("gain", 1.0), ("address", 0)):
+        with pytest.raises(AttributeError):
+            setattr(rope, name, value)
+    rope.freq[3] = 7.0     # in place: the structure points there
+    assert C.cast(rope.address, C.POINTER(binding.hack_rope)).contents.freq[3] == 7.0
