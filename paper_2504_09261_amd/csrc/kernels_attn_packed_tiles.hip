@@ -74,8 +74,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_packed_tiles(const AttnPacke
   const int all = packed_blocks(u.len), chunks = chunks_of(all, a.chunk);
   if (chunk >= chunks) return;
   const int first = chunk_at(all, chunks, chunk), last = chunk_at(all, chunks, chunk + 1);
-  const int len = min(last * kPackRows, u.len) - first * kPackRows;   // keys of this work-group
-  const int n_blocks = (len + kKB - 1) / kKB;
+  const int len = rows_in(u.len, first, last), n_blocks = stages_of(len, kKB);   // keys of this work-group
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, col = lane & 15, g = lane >> 4;

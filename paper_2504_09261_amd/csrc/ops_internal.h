@@ -88,6 +88,16 @@ struct AttnPackedHead {
   int32_t n_chunks;   // most chunks that a unit's keys are cut into
   int32_t chunk;      // most blocks of kPackRows keys of one
 };
+// Chunks of a unit's blocks: how many of at most `most` blocks, where chunk c begins (as even as they can be), and the rows of a unit of len rows in blocks
+// [lo, hi).  Unsigned: the last block of a unit may end at row 2^31.
+__host__ __device__ inline int packed_blocks(int len) { return (int)(((unsigned)len + kPackRows - 1) / kPackRows); }
+__host__ __device__ inline int chunks_of(int n, int most) { return (n + most - 1) / most; }
+__host__ __device__ inline int chunk_at(int n, int chunks, int c) { return (int)((unsigned)n / chunks * c + ((unsigned)n % chunks) * c / chunks); }
+__host__ __device__ inline int rows_in(int len, int lo, int hi) {
+  const unsigned end = (unsigned)hi * kPackRows;
+  return (int)((end < (unsigned)len ? end : (unsigned)len) - (unsigned)lo * kPackRows);
+}
+__host__ __device__ inline int stages_of(int rows, int each) { return (int)(((unsigned)rows + each - 1) / each); }
 // Units of a launch.  They travel by value; a launch takes 2.5 us to issue and 0.3 to 0.5 more for every KiB of arguments up to 8 (a table in memory
 // would be another copy each time a length grows), so there is a short list too.
 constexpr int kFewUnits = 64, kPackUnits = 640, kAttnPackedUnits = 1024;

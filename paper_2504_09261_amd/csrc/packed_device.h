@@ -36,13 +36,8 @@ __device__ __forceinline__ bf16x8 codes_bf16(unsigned w, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// ---- attention: arguments, chunks of a unit's blocks, V in LDS ---------------
+// ---- attention: arguments, V in LDS -------------------------------------------
 template <int N> struct AttnPackedArgs : AttnPackedHead { AttnPackedUnit unit[N]; };
-
-__device__ __forceinline__ int packed_blocks(int len) { return (int)(((unsigned)len + kPackRows - 1) / kPackRows); }
-// Blocks [lo, hi) of chunk c of a unit of n blocks: as even as they can be.
-__device__ __forceinline__ int chunks_of(int n, int most) { return (n + most - 1) / most; }
-__device__ __forceinline__ int chunk_at(int n, int chunks, int c) { return (int)((unsigned)n / chunks * c + ((unsigned)n % chunks) * c / chunks); }
 
 // LDS layout of converted rows of V: groups of four, a group's 64-byte pieces row after row, the 16-byte chunks of a piece permuted by two bits of the row.
 // All operands of the PV product stand at constant distances from two addresses, a lane's share of a row at constant distances from two others, and

@@ -215,6 +215,28 @@ int backward_frequencies() {
   return 0;
 }
 
+// The chunks of a unit cover its rows once, whatever its length.
+int chunk_rows() {
+  for (int64_t len : {1LL, 63LL, 64LL, 65LL, 1000LL, 131071LL, 2147483520LL, 2147483583LL, 2147483584LL, 2147483585LL, 2147483646LL, 2147483647LL}) {
+    const int n = packed_blocks((int)len);
+    CHECK(n == (len + 63) / 64);
+    for (int64_t most : {1LL << 30, (long long)n, n / 2 + 1LL, n / 7 + 1LL, n / 1023 + 1LL}) {
+      const int chunks = chunks_of(n, (int)std::min<int64_t>(most, n));
+      int64_t end = 0;
+      for (int c = 0; c < chunks; ++c) {
+        const int lo = chunk_at(n, chunks, c), hi = chunk_at(n, chunks, c + 1);
+        CHECK(lo < hi && hi - lo <= most && (int64_t)lo * 64 == end);
+        const int64_t rows = rows_in((int)len, lo, hi);
+        CHECK(rows >= 1 && rows <= (int64_t)(hi - lo) * 64);
+        for (int each : {32, 64}) CHECK(stages_of((int)rows, each) == (rows + each - 1) / each);
+        end += rows;
+      }
+      CHECK(end == len);
+    }
+  }
+  return 0;
+}
+
 int pack_refusals() {
   Context c;
   CHECK(hack_packed_bytes(96, 64, nullptr) == HACK_EINVAL);
@@ -452,7 +474,7 @@ int no_exceptions() {
 int main(int argc, char** argv) {
   const std::map<std::string, int (*)()> checks = {{"rotate_refusals", rotate_refusals}, {"rope_freqs", rope_freqs}, {"pack_refusals", pack_refusals},
                                                    {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions},
-                                                   {"backward_frequencies", backward_frequencies}};
+                                                   {"backward_frequencies", backward_frequencies}, {"chunk_rows", chunk_rows}};
   const auto it = argc > 1 ? checks.find(argv[1]) : checks.end();
   if (it == checks.end()) return 2;
   const int rc = it->second();
