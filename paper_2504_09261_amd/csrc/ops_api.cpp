@@ -175,6 +175,8 @@ bool units_overlap(int n_units, Lo lo, Hi hi) {
 
 int blocks_of(int len) { return (int)(((int64_t)len + kPackRows - 1) / kPackRows); }
 
+int tiles_of(int N_k, int queries) { return (int)(((int64_t)N_k + queries - 1) / queries); }
+
 // Partial results of work-groups of so many queries that the workspace holds.
 int64_t partial_slots(const hack_ctx* ctx, int queries) { return ctx->part_rows / queries; }
 
@@ -280,7 +282,7 @@ int queries_per_group(const hack_ctx* ctx, const int32_t* len, int n_units, int 
   for (const Form& f : kForms[ctx->cfg.head_dim == 128]) {
     AttnPackedHead a{};
     a.n_units = n_units;
-    a.q_tiles = (N_k + f.queries - 1) / f.queries;
+    a.q_tiles = tiles_of(N_k, f.queries);
     const double us = f.scale * plan_chunks(ctx, f.queries, len, blocks, longest, &a) + f.start + f.groups * n_units * a.q_tiles / 256.0;
     if (queries == 0 || us < best) queries = f.queries, best = us;
   }
@@ -472,10 +474,14 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
   a.N_k = N_k;
   a.scale = scale;
   const int queries = queries_per_group(ctx, kv->len, U, N_k);
-  a.q_tiles = (N_k + queries - 1) / queries;
-  std::vector<int32_t> order(std::min(U, kAttnPackedUnits)), count;
-  for (int u0 = 0; u0 < U; u0 += kAttnPackedUnits) {
-    a.n_units = std::min(kAttnPackedUnits, U - u0);
+  a.q_tiles = tiles_of(N_k, queries);
+  // Units of a launch: its work-groups, a multiple of eight times the tiles, are of 256 threads, which a launch counts in 32 bits.  (Units that are cut have few.)
+  constexpr int kMostGroups = (1 << 24) - 1;
+  const int most = std::min(kAttnPackedUnits, kMostGroups / a.q_tiles / 8 * 8);
+  if (most < 1) return fail(ctx, HACK_ECAPACITY, "%d queries are more than a launch takes", N_k);
+  std::vector<int32_t> order(std::min(U, most)), count;
+  for (int u0 = 0; u0 < U; u0 += most) {
+    a.n_units = std::min(most, U - u0);
     const int32_t* len = kv->len + u0;
     int64_t blocks, longest;
     measure(len, a.n_units, &blocks, &longest);

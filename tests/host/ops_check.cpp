@@ -237,6 +237,31 @@ int chunk_rows() {
   return 0;
 }
 
+// Launches stay below 2^32 threads, 256 a work-group: units of many queries in several ones, and one unit of too many queries refused.
+int large_launches() {
+  constexpr int n = 1024;
+  hack_ctx* ctx = nullptr;
+  hack_config cfg{0, 1, kD, HACK_F32, n, 64, INT32_MAX, 32};
+  CHECK(hack_create(&ctx, &cfg) == HACK_OK);
+  std::vector<int64_t> off(n, 0);
+  std::vector<int32_t> len(n, 64);
+  const hack_packed_cache kv{at(kA), at(kA + 0x100000), nullptr, 64, off.data(), len.data()};
+  for (int N : {1, 1 << 17, (1 << 18) - 15, (1 << 18) + 1, 3000001, 1 << 24, (1 << 25) - 16}) {
+    stub::attentions.clear();
+    CHECK(hack_attn_packed(ctx, n, N, at(0x100000000000), &kv, 0.1f, at(0x600000000000), kStream) == HACK_OK);
+    std::vector<int> seen(n, 0);
+    for (const auto& a : stub::attentions) {
+      CHECK(((int64_t)a.n_units * a.n_chunks + 7) / 8 * 8 * a.q_tiles < (1 << 24) && a.n_units >= 1);
+      for (const auto& u : a.unit) ++seen[u.unit];
+    }
+    for (int u = 0; u < n; ++u) CHECK(seen[u] == 1);
+    if (N <= (1 << 18) - 16) CHECK(stub::attentions.size() == 1);
+  }
+  for (int N : {(1 << 25) - 15, INT32_MAX}) REFUSED(HACK_ECAPACITY, hack_attn_packed(ctx, 1, N, at(0x100000000000), &kv, 0.1f, at(0x600000000000), kStream));
+  hack_destroy(ctx);
+  return 0;
+}
+
 int pack_refusals() {
   Context c;
   CHECK(hack_packed_bytes(96, 64, nullptr) == HACK_EINVAL);
@@ -474,7 +499,7 @@ int no_exceptions() {
 int main(int argc, char** argv) {
   const std::map<std::string, int (*)()> checks = {{"rotate_refusals", rotate_refusals}, {"rope_freqs", rope_freqs}, {"pack_refusals", pack_refusals},
                                                    {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions},
-                                                   {"backward_frequencies", backward_frequencies}, {"chunk_rows", chunk_rows}};
+                                                   {"backward_frequencies", backward_frequencies}, {"chunk_rows", chunk_rows}, {"large_launches", large_launches}};
   const auto it = argc > 1 ? checks.find(argv[1]) : checks.end();
   if (it == checks.end()) return 2;
   const int rc = it->second();
