@@ -63,7 +63,7 @@ template <typename T, int D, int N>
 __global__ __launch_bounds__(kThreads) void pack_rows(const PackArgs<N> a) {
   constexpr int LPR = D / 8, RPG = kThreads / LPR;   // lanes of a row, rows of a work-group
   const PackUnit u = a.unit[blockIdx.y];
-  const int i = blockIdx.x * RPG + threadIdx.x / LPR, c = threadIdx.x % LPR;
+  const int i = a.row_at + (int)(blockIdx.x * RPG + threadIdx.x / LPR), c = threadIdx.x % LPR;
   if (i >= u.n) return;   // all lanes of a row
   const int64_t unit = a.unit0 + blockIdx.y;
   int src = a.kept ? a.kept[unit * a.kept_stride + i] : i;
@@ -106,7 +106,7 @@ template <typename T, int D, int N, bool STREAM>
 __global__ __launch_bounds__(kThreads) void unpack_rows(const PackArgs<N> a) {
   constexpr int LPR = D / 8, RPG = kThreads / LPR;
   const PackUnit u = a.unit[blockIdx.y];
-  const int i = blockIdx.x * RPG + threadIdx.x / LPR, c = threadIdx.x % LPR;
+  const int i = a.row_at + (int)(blockIdx.x * RPG + threadIdx.x / LPR), c = threadIdx.x % LPR;
   if (i >= u.n) return;
   const int from = u.first + i, r = from & (kPackRows - 1);
   const int64_t block = (int64_t)(u.block + (from >> 6)) * kPackBytes<D>;
@@ -132,12 +132,15 @@ void launch_some(hipStream_t s, bool pack, const PackHead& h, const PackUnit* un
     rows = std::max(rows, units[i].n);
     all += units[i].n;
   }
-  if (rows == 0) return;
   constexpr int per = kThreads / (D / 8);
-  const dim3 grid((rows + per - 1) / per, n_units);
-  if (pack) hipLaunchKernelGGL((pack_rows<T, D, N>), grid, dim3(kThreads), 0, s, a);
-  else if (2 * all * D * (int64_t)sizeof(T) > kL2Bytes) hipLaunchKernelGGL((unpack_rows<T, D, N, true>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((unpack_rows<T, D, N, false>), grid, dim3(kThreads), 0, s, a);
+  constexpr int kMostRows = 1 << 27;   // of a unit and a launch, which counts its threads in 32 bits; a row's number and what a work-group adds fit them too
+  for (int64_t at = 0; at < rows; at += kMostRows) {
+    a.row_at = (int)at;
+    const dim3 grid((unsigned)((std::min<int64_t>(rows - at, kMostRows) + per - 1) / per), n_units);
+    if (pack) hipLaunchKernelGGL((pack_rows<T, D, N>), grid, dim3(kThreads), 0, s, a);
+    else if (2 * all * D * (int64_t)sizeof(T) > kL2Bytes) hipLaunchKernelGGL((unpack_rows<T, D, N, true>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((unpack_rows<T, D, N, false>), grid, dim3(kThreads), 0, s, a);
+  }
 }
 
 template <typename T, int D>

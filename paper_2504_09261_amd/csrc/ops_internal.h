@@ -63,7 +63,7 @@ struct PackHead {
   int32_t n_new;         // rows of k_new / v_new of a unit
   int32_t pos_new;
   int32_t unit0;         // of the launch, set by the launchers
-  int32_t pad;
+  int32_t row_at;        // row of each unit that the launch begins with, set by the launchers
 };
 void launch_pack(hipStream_t s, int elem_bytes, int head_dim, PackHead h, const PackUnit* units, int n_units);
 void launch_unpack(hipStream_t s, int elem_bytes, int head_dim, PackHead h, const PackUnit* units, int n_units);

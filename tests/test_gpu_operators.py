@@ -436,6 +436,27 @@ def test_many_rows_read_back_as_their_parts(contexts, dtype, d):
     assert same(to64(out.k[off[3]:off[3] + 200]), nearest(to64(k[off[3]:off[3] + 200])))
 
 
+def test_a_unit_of_more_rows_than_a_launch_takes(contexts):
+    """More than 2^28 rows of 128, read back at both ends and where launches of 2^27 rows meet; K and V are the same 69 GB."""
+    hk = contexts(1, 128, "bf16", units=8)
+    g = torch.Generator(DEV).manual_seed(28)
+    n, period = 2 ** 28 + 1000, 1 << 16
+    some = torch.randn((period, 128), generator=g, device=DEV).bfloat16()
+    k = torch.empty((n, 128), dtype=torch.bfloat16, device=DEV)
+    k[:2 ** 28].view(-1, period, 128).copy_(some)
+    k[2 ** 28:].copy_(some[:1000])
+    pc = PackedCache(*(torch.empty(((n + 63) // 64, 34 * 128), dtype=torch.uint8, device=DEV) for _ in range(2)), [0], [n])
+    hk.pack(1, 0, pc, cache_in=Cache(k, k, [0], [n]))
+    want = nearest(to64(some))
+    for at in (0, 2 ** 27 - 500, 2 ** 28 - 500, n - 1000):
+        out = Cache(torch.zeros((1000, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((1000, 128), dtype=torch.bfloat16, device=DEV), [0], [1000])
+        hk.unpack(1, pc, out, first=np.array([at], np.int32))
+        i = (at + np.arange(1000)) % period
+        assert same(to64(out.k), want[i]) and same(to64(out.v), want[i])
+    del k, pc
+    torch.cuda.empty_cache()
+
+
 def test_packed_sizes():
     assert packed_bytes(128, 64) == 34 * 128 and packed_bytes(64, 1) == 34 * 64
     with pytest.raises(HackError):
