@@ -408,7 +408,7 @@ typedef struct {
 typedef struct {
   const void* x;        /* DEVICE element (b, h, n, i) at b stride_b + h stride_h + n stride_n + i */
   void* out;            /* DEVICE [B, heads, N, head_dim]; may be x if x lies in that layout, must not share memory with
-                           rows that are read otherwise */
+                           rows that are read otherwise, weights or positions */
   int32_t heads;
   int64_t stride_b, stride_h, stride_n;   /* elements, not negative, multiples of 16 bytes */
   const float* weight;  /* DEVICE [head_dim] or [heads, weight_stride_h], NULL = ones (hack_norm_rotate only) */

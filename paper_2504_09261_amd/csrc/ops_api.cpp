@@ -32,6 +32,8 @@ Range range_of(const void* p, int64_t n, int64_t bytes) {   // n elements; none 
   const uintptr_t lo = (uintptr_t)p;
   return p ? Range{lo, lo + (uintptr_t)(std::min<int64_t>(n, (int64_t)1 << 44) * bytes)} : Range{0, 0};
 }
+// A stride whose product with a count fits 64 bits.
+int64_t apart(int64_t stride) { return std::min<int64_t>(stride, (int64_t)1 << 32); }
 // Whether an output shares memory with an input or with another output.
 bool share(std::initializer_list<Range> out, std::initializer_list<Range> in) {
   for (const Range* o = out.begin(); o != out.end(); ++o) {
@@ -132,6 +134,12 @@ hack_status rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, cons
   a.eps = eps;
   a.norm = norm;
   if (rope && (st = take_rope(ctx, rope, N, pos, pos_stride_b, pos0, &a)) != HACK_OK) return st;
+  for (int i = 0; i < n; ++i) {   // work-groups that store would change what others still have to read
+    if (rope && out[i].meets(range_of(pos, apart(pos_stride_b) * (B - 1) + (int64_t)rope->axes * N, 4))) return fail(ctx, HACK_EINVAL, "an output overlaps the positions");
+    for (int j = 0; j < n; ++j)
+      if (out[i].meets(range_of(r[j]->weight, r[j]->weight_stride_h * (r[j]->heads - 1) + ctx->cfg.head_dim, 4)))
+        return fail(ctx, HACK_EINVAL, "an output overlaps the weights");
+  }
   if ((st = check_device(ctx)) != HACK_OK) return st;
   launch_rotate(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, !rope || rope->layout == HACK_ROPE_HALF, B, n, a);
   HIP_TRY(ctx, hipGetLastError());

@@ -262,6 +262,42 @@ int large_launches() {
   return 0;
 }
 
+// Outputs of rotations over weights or positions, which other work-groups still read.
+int rotation_shared_memory() {
+  Context c;
+  double freq[64];
+  CHECK(hack_rope_freqs(128, 2, HACK_ROPE_PLAIN, 10000.0, 1.0, 0.0, freq, nullptr) == HACK_OK);
+  const hack_rope rope{HACK_ROPE_HALF, 128, 2, 1.f, freq};
+  constexpr int N = 10, B = 2;
+  constexpr int64_t kBytes = (int64_t)B * 4 * N * kD * 2;
+  const hack_rows x{at(kA), at(kB), 4, 4 * N * kD, N * kD, kD, nullptr, 0};
+  const auto pos = [&](uintptr_t p, int64_t sb) { return hack_rotate(c.ctx, B, N, &x, &rope, at<int32_t>(p), sb, 0, kStream); };
+  CHECK(pos(kB - 2 * N * 4, 0) == HACK_OK && pos(kB + kBytes, 0) == HACK_OK);
+  REFUSED(HACK_EINVAL, pos(kB, 0));
+  REFUSED(HACK_EINVAL, pos(kB + kBytes - 4, 0));
+  REFUSED(HACK_EINVAL, pos(kB - 2 * N * 4 + 4, 0));
+  CHECK(pos(kB - (50 + 2 * N) * 4, 50) == HACK_OK);
+  REFUSED(HACK_EINVAL, pos(kB - (50 + 2 * N) * 4 + 4, 50));
+  CHECK(pos(kB + kBytes, INT64_MAX) == HACK_OK);
+  hack_rows k = x;
+  k.x = at(kC); k.out = at(kE);
+  const auto norm = [&](uintptr_t qw, int64_t qs, uintptr_t kw, int64_t ks, const hack_rope* r, uintptr_t p) {
+    hack_rows a = x, b = k;
+    a.weight = at<float>(qw);
+    a.weight_stride_h = qs;
+    b.weight = at<float>(kw);
+    b.weight_stride_h = ks;
+    return hack_norm_rotate(c.ctx, B, N, &a, &b, HACK_NORM_RMS, 1e-6f, r, at<int32_t>(p), 0, 0, kStream);
+  };
+  CHECK(norm(kB - kD * 4, 0, kE - (3 * 256 + kD) * 4, 256, &rope, kE + kBytes) == HACK_OK);
+  REFUSED(HACK_EINVAL, norm(kB, 0, 0, 0, &rope, 0x50000000));
+  REFUSED(HACK_EINVAL, norm(kE + kBytes - 16, 0, 0, 0, &rope, 0x50000000));   // the other tensor's output
+  REFUSED(HACK_EINVAL, norm(0, 0, kB - (3 * 256 + kD) * 4 + 16, 256, &rope, 0x50000000));
+  REFUSED(HACK_EINVAL, norm(0, 0, 0, 0, &rope, kE + 64));
+  CHECK(norm(0, 0, 0, 0, nullptr, kE + 64) == HACK_OK);                       // positions are not read without a rotation
+  return 0;
+}
+
 int pack_refusals() {
   Context c;
   CHECK(hack_packed_bytes(96, 64, nullptr) == HACK_EINVAL);
@@ -499,7 +535,8 @@ int no_exceptions() {
 int main(int argc, char** argv) {
   const std::map<std::string, int (*)()> checks = {{"rotate_refusals", rotate_refusals}, {"rope_freqs", rope_freqs}, {"pack_refusals", pack_refusals},
                                                    {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions},
-                                                   {"backward_frequencies", backward_frequencies}, {"chunk_rows", chunk_rows}, {"large_launches", large_launches}};
+                                                   {"backward_frequencies", backward_frequencies}, {"chunk_rows", chunk_rows}, {"large_launches", large_launches},
+                                                   {"rotation_shared_memory", rotation_shared_memory}};
   const auto it = argc > 1 ? checks.find(argv[1]) : checks.end();
   if (it == checks.end()) return 2;
   const int rc = it->second();

@@ -24,6 +24,6 @@ def test_host_side(program, name):
     assert r.returncode == 0 and r.stdout.strip().endswith("ok"), r.stdout + r.stderr[-2000:]
 
 
-@pytest.mark.parametrize("name", ["backward_frequencies", "chunk_rows", "large_launches"])
+@pytest.mark.parametrize("name", ["backward_frequencies", "chunk_rows", "large_launches", "rotation_shared_memory"])
 def test_ranges(program, name):
     test_host_side(program, name)
