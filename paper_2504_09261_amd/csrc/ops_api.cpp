@@ -408,7 +408,7 @@ extern "C" hack_status hack_pack(hack_ctx* ctx, int32_t B, int32_t N_k, const ha
   const int64_t rows = in ? in->rows : 0, fresh = (int64_t)U * n_new;
   if (share({range_of(out->k, blocks, block), range_of(out->v, blocks, block), range_of(out->pos, out->rows, 4)},
             {range_of(in ? in->k : nullptr, rows, row), range_of(in ? in->v : nullptr, rows, row), range_of(in ? in->pos : nullptr, rows, 4),
-             range_of(k_new, fresh, row), range_of(v_new, fresh, row), range_of(kept_idx, U * idx_stride, 4)}))
+             range_of(k_new, fresh, row), range_of(v_new, fresh, row), range_of(kept_idx, U * apart(idx_stride), 4)}))
     return fail(ctx, HACK_EINVAL, "out shares memory with what is read, or K with V");
   if ((st = check_device(ctx)) != HACK_OK) return st;
   PackHead a{};

@@ -298,6 +298,41 @@ int rotation_shared_memory() {
   return 0;
 }
 
+// Lists with strides whose product with the units passes 64 bits (one unit: nothing lies a stride away).
+int far_lists() {
+  for (int heads : {1, kH}) {
+    Context c(HACK_BF16, heads);
+    const int64_t off[kH] = {0, 64, 128, 192};
+    const int32_t len[kH] = {40, 40, 40, 40};
+    const hack_cache in{at(kA), at(kB), nullptr, 256, off, len};
+    const hack_packed_cache out{at(0x7f0000000000), at(0x7f1000000000), nullptr, 256, off, len};
+    for (int64_t stride : {(int64_t)40, (int64_t)1 << 33, INT64_MAX / 2, INT64_MAX}) {
+      const int32_t* const kept = at<int32_t>(0x70000000);
+      CHECK(hack_pack(c.ctx, 1, 0, &in, nullptr, nullptr, 0, kept, stride, nullptr, &out, kStream) == HACK_OK);
+    }
+  }
+  return 0;
+}
+
+// Frequencies by parts at the ends of what is accepted: pairs that turn less than once over the trained length are divided, even the fastest.
+int rope_parts_ends() {
+  double f[64];
+  for (double length : {1.0, 3.0, 6.28, 6.29, 30.0, 1e3, 1e9, 1e300})
+    for (double base : {1.0001, 10.0, 1e4, 1e30}) {
+      CHECK(hack_rope_freqs(64, 1, HACK_ROPE_PARTS, base, 8.0, length, f, nullptr) == HACK_OK);
+      double last = 0.0;
+      for (int i = 0; i < 32; ++i) {
+        const double plain = std::pow(base, -i / 32.0), ratio = plain / f[i], turns = length * plain / 6.283185307179586;
+        CHECK(ratio > 1 - 1e-12 && ratio < 8 + 1e-9 && ratio >= last - 1e-9);
+        last = ratio;
+        const double one_pair = std::pow(base, 1 / 32.0);          // the ramp begins and ends at whole pairs
+        if (turns > 32.0 * one_pair) CHECK(std::fabs(ratio - 1) < 1e-12);
+        if (turns * one_pair < 1.0 || (i == 0 && turns < 1.0)) CHECK(std::fabs(ratio - 8) < 1e-9);
+      }
+    }
+  return 0;
+}
+
 int pack_refusals() {
   Context c;
   CHECK(hack_packed_bytes(96, 64, nullptr) == HACK_EINVAL);
@@ -536,7 +571,7 @@ int main(int argc, char** argv) {
   const std::map<std::string, int (*)()> checks = {{"rotate_refusals", rotate_refusals}, {"rope_freqs", rope_freqs}, {"pack_refusals", pack_refusals},
                                                    {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions},
                                                    {"backward_frequencies", backward_frequencies}, {"chunk_rows", chunk_rows}, {"large_launches", large_launches},
-                                                   {"rotation_shared_memory", rotation_shared_memory}};
+                                                   {"rotation_shared_memory", rotation_shared_memory}, {"far_lists", far_lists}, {"rope_parts_ends", rope_parts_ends}};
   const auto it = argc > 1 ? checks.find(argv[1]) : checks.end();
   if (it == checks.end()) return 2;
   const int rc = it->second();
