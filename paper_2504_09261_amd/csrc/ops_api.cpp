@@ -344,7 +344,8 @@ extern "C" hack_status hack_rope_freqs(int32_t rot_dim, int32_t axes, int32_t sc
     double f = std::pow(base, -2.0 * i / size);
     if (scaling == HACK_ROPE_LINEAR) f /= factor;
     if (scaling == HACK_ROPE_PARTS) {
-      const double ramp = std::min(std::max((i - low) / std::max(high - low, 0.001), 0.0), 1.0);
+      // no pair between where the fastest turns less than once (all are slow) or the slowest more than 32 times (all are fast)
+      const double ramp = high > low ? std::min(std::max((i - low) / (high - low), 0.0), 1.0) : i >= low ? 1.0 : 0.0;
       f = f * (1.0 - ramp) + f / factor * ramp;
     }
     for (int a = 0; a < axes; ++a) freq[a * n + i] = f;
