@@ -288,7 +288,6 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 || sizeof(T) == 4 ? 2 : D == 6
 }
 
 // Rows of units that were cut, where these are few and the chunks many: a work-group takes one query, D / 4 lanes a chunk.
-constexpr int kFactors = 1024;   // chunks whose factors are kept in LDS at a time
 template <typename T, int D, int N>
 __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N> a, int q_rows) {
   constexpr int LPR = D / 4, SIDE = 256 / LPR;   // chunks at a time
@@ -299,7 +298,7 @@ __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N>
   const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + part0;
   const float4* const po = reinterpret_cast<const float4*>(a.part_o + part0 * D) + lane;
   __shared__ float4 o_sh[SIDE][LPR];
-  __shared__ float f_sh[kFactors], m_sh[4], l_sh[4];
+  __shared__ float f_sh[kMostChunks], m_sh[4], l_sh[4];
   // The first results are on their way while the factors are formed.
   constexpr int kEarly = 8;
   float4 early[kEarly];
@@ -320,26 +319,18 @@ __global__ __launch_bounds__(256) void attn_packed_merge(const AttnPackedArgs<N>
     o.z = fmaf(f, x.z, o.z);
     o.w = fmaf(f, x.w, o.w);
   };
-  for (int base = 0; base < n; base += kFactors) {
-    const int here = min(kFactors, n - base);
-    if (base > 0) __syncthreads();   // the last ones have been used
-    for (int c = tid; c < here; c += 256) {
-      const float2 x = ml[(int64_t)(base + c) * q_rows];
-      const float f = __builtin_amdgcn_exp2f(x.x - M);
-      f_sh[c] = f;
-      L = fmaf(f, x.y, L);
-    }
-    __syncthreads();
-    int c = c0;
-    if (base == 0) {
-#pragma unroll
-      for (int i = 0; i < kEarly; ++i)
-        if (c0 + i * SIDE < n) add(f_sh[c0 + i * SIDE], early[i]);
-      c = c0 + kEarly * SIDE;
-    }
-#pragma unroll 4
-    for (; c < here; c += SIDE) add(f_sh[c], po[(int64_t)(base + c) * q_rows * LPR]);
+  for (int c = tid; c < n; c += 256) {
+    const float2 x = ml[(int64_t)c * q_rows];
+    const float f = __builtin_amdgcn_exp2f(x.x - M);
+    f_sh[c] = f;
+    L = fmaf(f, x.y, L);
   }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kEarly; ++i)
+    if (c0 + i * SIDE < n) add(f_sh[c0 + i * SIDE], early[i]);
+#pragma unroll 4
+  for (int c = c0 + kEarly * SIDE; c < n; c += SIDE) add(f_sh[c], po[(int64_t)c * q_rows * LPR]);
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) L += __shfl_xor(L, x, 64);
   if ((tid & 63) == 0) l_sh[tid >> 6] = L;

@@ -209,7 +209,7 @@ double plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t
   constexpr int kXcds = 8, kLeast = 4;   // blocks of a chunk: one for each wave of the smaller forms
   const Rates& r = kRates[ctx->cfg.head_dim == 128][queries == 16 ? 0 : queries == 32 ? 1 : 2];
   const int64_t n = a->n_units, tiles = a->q_tiles, cus = std::max(ctx->cus / kXcds, 1);
-  const int64_t most = std::max<int64_t>(1, partial_slots(ctx, queries) / (n * tiles));   // chunks whose partial results the workspace holds
+  const int64_t most = std::min<int64_t>(kMostChunks, std::max<int64_t>(1, partial_slots(ctx, queries) / (n * tiles)));   // ... whose partial results the workspace holds
   constexpr int kRows = 256;
   int32_t ends[kRows + 1];   // units of so many chunks
   const auto us = [&](int64_t chunk) {

@@ -98,6 +98,8 @@ __host__ __device__ inline int rows_in(int len, int lo, int hi) {
   return (int)((end < (unsigned)len ? end : (unsigned)len) - (unsigned)lo * kPackRows);
 }
 __host__ __device__ inline int stages_of(int rows, int each) { return (int)(((unsigned)rows + each - 1) / each); }
+// Chunks of a unit at most: the merge keeps their factors in LDS.  (Two work-groups to each of 256 compute units make 512.)
+constexpr int kMostChunks = 1024;
 // Units of a launch.  They travel by value; a launch takes 2.5 us to issue and 0.3 to 0.5 more for every KiB of arguments up to 8 (a table in memory
 // would be another copy each time a length grows), so there is a short list too.
 constexpr int kFewUnits = 64, kPackUnits = 640, kAttnPackedUnits = 1024;

@@ -333,6 +333,25 @@ int rope_parts_ends() {
   return 0;
 }
 
+// Chunks of very long units: what the merge's LDS holds, and as many as a case of tests/test_gpu_operators.py wants.
+int many_chunks() {
+  for (int dtype : {HACK_BF16, HACK_F32})
+    for (int units : {1, 2, kH})
+      for (int64_t len : {140001LL, 1000000LL, 16000000LL, 200000000LL, 2147483647LL})
+        for (int N : {1, 5, 16, 40}) {
+          Context c(dtype, units, units);
+          std::vector<int64_t> off(units, 0);
+          std::vector<int32_t> l(units, (int32_t)len);
+          const hack_packed_cache kv{at(0x100000000000), at(0x200000000000), nullptr, (len + 63) / 64 * 64, off.data(), l.data()};
+          stub::attentions.clear();
+          CHECK(hack_attn_packed(c.ctx, 1, N, at(0x50000000), &kv, 0.1f, at(0x60000000), kStream) == HACK_OK && stub::attentions.size() == 1);
+          const auto& a = stub::attentions[0];
+          CHECK(a.n_chunks <= kMostChunks && (int64_t)a.chunk * a.n_chunks >= (len + 63) / 64);
+          if (units == 1 && N <= 16) CHECK(a.n_chunks >= 200);
+        }
+  return 0;
+}
+
 int pack_refusals() {
   Context c;
   CHECK(hack_packed_bytes(96, 64, nullptr) == HACK_EINVAL);
@@ -571,7 +590,8 @@ int main(int argc, char** argv) {
   const std::map<std::string, int (*)()> checks = {{"rotate_refusals", rotate_refusals}, {"rope_freqs", rope_freqs}, {"pack_refusals", pack_refusals},
                                                    {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions},
                                                    {"backward_frequencies", backward_frequencies}, {"chunk_rows", chunk_rows}, {"large_launches", large_launches},
-                                                   {"rotation_shared_memory", rotation_shared_memory}, {"far_lists", far_lists}, {"rope_parts_ends", rope_parts_ends}};
+                                                   {"rotation_shared_memory", rotation_shared_memory}, {"far_lists", far_lists}, {"rope_parts_ends", rope_parts_ends},
+                                                   {"many_chunks", many_chunks}};
   const auto it = argc > 1 ? checks.find(argv[1]) : checks.end();
   if (it == checks.end()) return 2;
   const int rc = it->second();

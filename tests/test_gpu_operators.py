@@ -554,6 +554,20 @@ def test_attention_over_a_packed_cache(contexts, d, lens, n, form):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_few_queries_over_one_long_cache(contexts, dtype, d):
+    """One unit in hundreds of chunks: the merge has more of them than it loads ahead."""
+    hk = contexts(1, d, dtype)
+    g = torch.Generator(DEV).manual_seed(d)
+    pc, rows = filled(hk, 1, np.array([140001]), d, g)
+    for n in (1, 5):
+        q = (2 * torch.randn((1, 1, n, d), generator=g, device=DEV)).to(TYPES[dtype])
+        out = torch.full_like(q, 9.0)
+        hk.attn_packed(q, pc, d ** -0.5, out)
+        check_attention(q[0], rows, float(np.float32(d ** -0.5)), out[0])
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n, form", [(300, 0), (1000, 0), (1000, 32), (1000, 128)])
 def test_attention_of_many_queries_over_a_packed_cache(contexts, d, n, form):
