@@ -439,7 +439,8 @@ hack_status hack_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* x,
 /* Norms of the rows of q and k, head by head, and their rotation, in one launch.
  *   HACK_NORM_RMS   x / sqrt(mean(x^2) + eps) * weight
  *   HACK_NORM_UNIT  x / max(|x|, eps) * weight (a weight per head: unit rows times a learned scale)
- * over all head_dim elements, sums of squares in float32.  k may be NULL, rope may be
+ * over all head_dim elements, sums of squares in float32 (of a row scaled by a power of two
+ * where its squares leave float32: rows of any finite magnitude have their norm).  k may be NULL, rope may be
  * NULL (norms alone; pos is not read then).  eps > 0.  Errors as hack_rotate. */
 enum { HACK_NORM_RMS = 0, HACK_NORM_UNIT = 1 };
 hack_status hack_norm_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, int32_t norm,

@@ -11,6 +11,7 @@
 // Measured: 16384 rows of 32 + 8 heads of 128 out of a projection, normed and turned, 66 us (5.1 TB/s of the 6.2 that a plain elementwise
 // kernel reaches), 2 x 4096 rows of 16 heads in two axes 13 us (5.1).
 #include <algorithm>
+#include <cfloat>
 
 #include "device_util.h"
 #include "ops_internal.h"
@@ -72,6 +73,27 @@ template <> struct Piece<__bf16> {
 
 template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
   return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+
+// Of the lanes of a row, in all of them.
+template <int LPR> __device__ __forceinline__ float row_sum(float v) {
+  v = dpp_add<0xB1>(v);    // lane ^ 1
+  v = dpp_add<0x4E>(v);    // lane ^ 2
+  return LPR == 8 ? dpp_add<0x141>(v) : v;   // mirrored within eight lanes
+}
+template <int CTRL> __device__ __forceinline__ unsigned dpp_max(unsigned v) {
+  return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true));
+}
+template <int LPR> __device__ __forceinline__ unsigned row_max(unsigned v) {
+  v = dpp_max<0xB1>(v);
+  v = dpp_max<0x4E>(v);
+  return LPR == 8 ? dpp_max<0x141>(v) : v;
+}
+__device__ __forceinline__ float sum_of_squares(const float* v) {
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) ss = fmaf(v[i], v[i], ss);
+  return ss;
 }
 
 template <int E> __device__ __forceinline__ void load_weights(const float* p, float* v) {
@@ -150,13 +172,27 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(const RotateArgs a) {
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) load_weights<E>(t.w + (int64_t)h * t.w_stride + at + k * part, w + k * E);
       }
-      float ss = 0.f;
+      float ss = row_sum<LPR>(sum_of_squares(v)), eps = a.eps, eps2 = a.eps;
+      // Squares that float32 does not hold, and do matter: the row is scaled by a power of two (eps with it, for the mean of squares twice) that brings its largest
+      // element to about one.  The RMS norm leaves a tiny row where eps, 2^-149 at least, still fits scaled by 2^120, and decides.
+      if (__builtin_expect(!(ss >= a.low && ss <= FLT_MAX), 0)) {
+        unsigned top = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ss = fmaf(v[i], v[i], ss);
-      ss = dpp_add<0xB1>(ss);    // lane ^ 1
-      ss = dpp_add<0x4E>(ss);    // lane ^ 2
-      if (LPR == 8) ss = dpp_add<0x141>(ss);   // mirrored within eight lanes
-      const float r = 1.f / (a.norm == kNormRms ? sqrtf(ss * (1.f / D) + a.eps) : fmaxf(sqrtf(ss), a.eps));
+        for (int i = 0; i < 16; ++i) top = max(top, __builtin_bit_cast(unsigned, v[i]) & 0x7FFFFFFFu);
+        top = row_max<LPR>(top);
+        if (top == 0) {
+          eps = eps2 = 1.f;   // a row of zeros stays one, whatever 1 / eps is
+        } else if (top < 0x7F800000u) {
+          const int e = 253 - (int)(top >> 23);
+          const float scale = __builtin_bit_cast(float, (unsigned)min(max(e, 1), a.norm == kNormRms ? 187 : 253) << 23);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] *= scale;
+          ss = row_sum<LPR>(sum_of_squares(v));
+          eps *= scale;
+          eps2 = eps * scale;
+        }
+      }
+      const float r = 1.f / (a.norm == kNormRms ? sqrtf(ss * (1.f / D) + eps2) : fmaxf(sqrtf(ss), eps));
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         v[i] *= r;
@@ -220,6 +256,8 @@ void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout
     t.tokens_log2 = log2;
     t.tiles = (a.n + (1 << log2) - 1) >> log2;
   }
+  // With an eps from 2^-50 on, what a sum of squares below 2^-100 is off by does not reach the result.
+  a.low = a.eps < 0x1p-50f ? 0x1p-100f : 0.f;
   // Outputs that the L2 caches cannot hold pass them by (16384 rows of 32 + 8 heads 71.7 -> 65.3 us, 32 x 256 of 30 + 30 heads 30.2 -> 26.6); smaller ones
   // are for the next launch to find there, and where a row's pieces of an access make up less than 32 bytes (as many as its region has elements) they
   // need the caches to become lines (8 x 8192 float32 rows of 16 heads of 64, of which 16 elements rotate: 129 us, past the caches 326; 32 elements of bf16 rows 61, 51).

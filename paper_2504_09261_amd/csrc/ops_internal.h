@@ -35,6 +35,7 @@ struct RotateArgs {
   int32_t section;      // of an axis
   float gain, eps;
   int32_t norm;         // kNorm*
+  float low;            // sums of squares below it, or not finite, are formed again from scaled rows; set by launch_rotate
   // launch shape, set by launch_rotate
   uint32_t groups[2];   // work-groups of a batch element: of t[0], of both
   int32_t steps;        // heads a thread takes, one after the other

@@ -219,6 +219,34 @@ def test_norm_rotate(contexts, dtype, d, rot, axes, layout, norm):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("norm", ["rms", "l2"])
+@pytest.mark.parametrize("eps", [2.0 ** -149, 2.0 ** -127, 1e-30, 2.0 ** -51, 2.0 ** -49, 1e-6, 1e30])
+def test_norms_of_rows_whose_squares_leave_float32(contexts, dtype, d, norm, eps):
+    """Rows of any finite magnitude, zero ones too, for every eps above zero.  Scaling by a power of two adds no rounding to NORM's; elements below 2^-149 of a row's
+    largest, and results below the smallest normal number, may lose what falls off there: half of float32's smallest step in either place (bf16: its own)."""
+    hk = contexts(1, d, dtype)
+    g = torch.Generator(DEV).manual_seed(d)
+    exps = [-149, -140, -133, -126, -120, -101, -76, -75, -74, -64, -63, -62, -51, -50, -49, -30, 0, 40, 59, 60, 61, 62, 63, 64, 65, 100, 124]
+    x = torch.randn((1, 2, len(exps) + 1, d), generator=g, device=DEV, dtype=torch.float64).clamp_(-4, 4)
+    x[:, :, :-1] *= torch.exp2(torch.tensor(exps, dtype=torch.float64, device=DEV))[:, None]
+    x[:, :, -1] = 0
+    x[:, 1, :, 1:] *= 0.0                     # the second head: one element alone
+    x = x.to(TYPES[dtype])
+    out = torch.empty_like(x)
+    hk.norm_rotate(x, None, norm, eps, None, None, None, out, None)
+    y = to64(x)
+    e = float(np.float32(eps))
+    ss = (y * y).sum(-1, keepdims=True)
+    want = y / np.sqrt(ss / d + e) if norm == "rms" else y / np.maximum(np.sqrt(ss), e)
+    tiny = 2.0 ** -149 + (2.0 ** -134 if dtype == "bf16" else 0.0)
+    err = np.abs(to64(out) - want)
+    tol = HALF_STEP[dtype] * 1.01 * np.abs(want) + NORM * H * np.abs(want) + tiny
+    assert (err <= tol).all(), (float((err / tol).max()), np.unravel_index(np.argmax(err / tol), err.shape))
+    assert not to64(out)[:, :, -1].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d, rot, axes, layout", [(128, 128, 1, "half"), (64, 32, 2, "half"), (64, 16, 1, "interleaved"), (128, 96, 2, "interleaved")])
 @pytest.mark.parametrize("hq, hk_", [(1, 1), (3, 1), (10, 2), (1, 5), (17, 33)])
 def test_any_number_of_heads_gives_what_each_gives_alone(contexts, dtype, d, rot, axes, layout, hq, hk_):
