@@ -106,13 +106,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_packed_tiles(const AttnPacke
   // Rows in groups of four, a group's 64-byte pieces row after row, 16-byte chunks permuted by two bits of the row (packed_device.h).  Written 8 rows at one
   // chunk at a time, K read 16 rows at one chunk, V^T 8 rows x 32 bytes.
   const int row = 16 * (w >> 1) + col, chunk0 = D == 128 ? 4 * g + 2 * (w & 1) : 2 * g + (w & 1);
-  auto k_chunk = [](int r, int c) { return (r >> 2) * 4 * D + (c >> 2) * 128 + (r & 3) * 32 + ((c & 3) ^ v_flip(r)) * 8; };
-  int k_to[CW], v_to[CW];
+  int to[CW];   // the same place for K and V
 #pragma unroll
-  for (int i = 0; i < CW; ++i) {
-    k_to[i] = k_chunk(row, chunk0 + i);
-    v_to[i] = v_chunk<D>(row, chunk0 + i);
-  }
+  for (int i = 0; i < CW; ++i) to[i] = v_chunk<D>(row, chunk0 + i);
 
   // Block 0 is the last one, ragged or not, blocks 1 .. n_blocks - 1 are the full ones in front of it: what is particular about a ragged block stays in front
   // of the main loop.  Past the last block the one before is loaded and converted again, into slots that nobody reads any more.
@@ -133,10 +129,10 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_packed_tiles(const AttnPacke
     const bool there = (n_blocks - 1) * kKB + row < len;
 #pragma unroll
     for (int i = 0; i < CW; ++i) {
-      *reinterpret_cast<bf16x8*>(&Ks[0][k_to[i]]) = codes_bf16(k0.w[i], scale_of(k0.exponent));
-      *reinterpret_cast<bf16x8*>(&Vs[0][v_to[i]]) = codes_bf16(there ? v0.w[i] : 0u, there ? scale_of(v0.exponent) : 1.f);
-      *reinterpret_cast<bf16x8*>(&Ks[1][k_to[i]]) = codes_bf16(k1.w[i], scale_of(k1.exponent));
-      *reinterpret_cast<bf16x8*>(&Ks[2][k_to[i]]) = codes_bf16(k2.w[i], scale_of(k2.exponent));
+      *reinterpret_cast<bf16x8*>(&Ks[0][to[i]]) = codes_bf16(k0.w[i], scale_of(k0.exponent));
+      *reinterpret_cast<bf16x8*>(&Vs[0][to[i]]) = codes_bf16(there ? v0.w[i] : 0u, there ? scale_of(v0.exponent) : 1.f);
+      *reinterpret_cast<bf16x8*>(&Ks[1][to[i]]) = codes_bf16(k1.w[i], scale_of(k1.exponent));
+      *reinterpret_cast<bf16x8*>(&Ks[2][to[i]]) = codes_bf16(k2.w[i], scale_of(k2.exponent));
     }
   }
   int k_at = min(kAhead + 2, last_full), v_at = min(kAhead, last_full);   // the next blocks to load
@@ -249,7 +245,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_packed_tiles(const AttnPacke
       const bf16x2 y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(is_k ? ck.w[d] : cv.w[d], is_k ? k_scale : v_scale, p);
       conv[2 * p] = y[0];
       conv[2 * p + 1] = y[1];
-      if constexpr (p == 3) *reinterpret_cast<bf16x8*>(is_k ? &Ks[(S + 2) % kNS][k_to[d]] : &Vs[S][v_to[d]]) = conv;
+      if constexpr (p == 3) *reinterpret_cast<bf16x8*>(is_k ? &Ks[(S + 2) % kNS][to[d]] : &Vs[S][to[d]]) = conv;
     };
     constexpr int SLOTS = 8 * KC + 2, END = SLOTS - 3 * KC / 4, MIDDLE = 4 * KC;
     constexpr int CONV_SLOTS = MIDDLE - KC / 2, FIRST_CYCLES = kSoftmaxCycles * 2 / 5;
@@ -339,7 +335,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_packed_tiles(const AttnPacke
       if ((n_blocks - 1) % kAhead == j) cv = vc[j];
 #pragma unroll
     for (int i = 0; i < CW; ++i)
-      *reinterpret_cast<bf16x8*>(&Vs[(n_blocks - 1) % kNS][v_to[i]]) = codes_bf16(cv.w[i], scale_of(cv.exponent));
+      *reinterpret_cast<bf16x8*>(&Vs[(n_blocks - 1) % kNS][to[i]]) = codes_bf16(cv.w[i], scale_of(cv.exponent));
     const bf16x8 pl[2] = {odd ? P[1][0] : P[0][0], odd ? P[1][1] : P[0][1]};
     pv_block(&Vs[(n_blocks - 2) % kNS][0], pl);
     __syncthreads();
