@@ -22,10 +22,8 @@ namespace {
 
 using namespace dev;
 
-constexpr int kThreads = 256;
-constexpr int kMaxSteps = 8;
+constexpr int kThreads = kRotateThreads;
 constexpr int64_t kL2Bytes = 32 << 20;   // of eight XCDs
-constexpr int kWantGroups = 2048;   // work-groups that fill the chip: eight a compute unit
 
 // 2^32 u turns -> cosine and sine.  The nearest quarter turn, then the Taylor series of the rest (at most pi / 4: the first terms
 // left out are 2e-9 and 2e-11).
@@ -238,24 +236,8 @@ void launch_typed(hipStream_t s, bool half_layout, bool stream, unsigned groups,
 }  // namespace
 
 void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout, int batch, int n_tensors, RotateArgs a) {
-  const int slots = kThreads / (head_dim / 16);
   int64_t rows = 0;
-  for (int i = 0; i < n_tensors; ++i) {
-    RotateTensor& t = a.t[i];
-    rows += (int64_t)batch * a.n * t.heads;
-    // Rows of one head side by side: few, so that the rest of the work-group takes the heads beside it, which lie behind each other in a projection
-    // (4, 8, 32 rows: 16384 rows of 32 + 8 heads 64.8, 66.7, 65.4 us, 32 x 256 of 30 + 30 heads 26.0, 29.0, 28.5, 2 x 4096 of 16 heads 15.4, 14.0, 14.6),
-    // but as many as leave no more than a quarter of the lanes without a head (2 x 11844 rows of 10 + 2 heads of 64: 22.7 us with as few as fit the heads of
-    // the larger tensor, 15.8 so; 8 x 10948 of 2 + 1 heads 21.1, 18.6).
-    const auto idle = [&](int log2) {
-      const int across = slots >> log2, taken = (t.heads + across - 1) / across * across;
-      return 4 * (taken - t.heads) > taken;
-    };
-    int log2 = 0;
-    while ((1 << log2) < slots && (1 << log2) < a.n && (log2 < 2 || idle(log2))) ++log2;
-    t.tokens_log2 = log2;
-    t.tiles = (a.n + (1 << log2) - 1) >> log2;
-  }
+  for (int i = 0; i < n_tensors; ++i) rows += (int64_t)batch * a.n * a.t[i].heads;
   // With an eps from 2^-50 on, what a sum of squares below 2^-100 is off by does not reach the result.
   a.low = a.eps < 0x1p-50f ? 0x1p-100f : 0.f;
   // Outputs that the L2 caches cannot hold pass them by (16384 rows of 32 + 8 heads 71.7 -> 65.3 us, 32 x 256 of 30 + 30 heads 30.2 -> 26.6); smaller ones
@@ -263,26 +245,13 @@ void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout
   // need the caches to become lines (8 x 8192 float32 rows of 16 heads of 64, of which 16 elements rotate: 129 us, past the caches 326; 32 elements of bf16 rows 61, 51).
   const auto wide = [&](int region) { return !half_layout || region == 0 || region >= 32; };
   const bool stream = rows * head_dim * elem_bytes > kL2Bytes && wide(a.section) && wide(head_dim - a.rot_dim);
-  // A thread walks over as many heads as leave enough work-groups: it forms its angles once for all of them.
-  int64_t groups = 0;
-  for (a.steps = kMaxSteps;; a.steps /= 2) {
-    groups = 0;
-    for (int i = 0; i < n_tensors; ++i) {
-      RotateTensor& t = a.t[i];
-      const int each = (slots >> t.tokens_log2) * a.steps;
-      groups += (int64_t)((t.heads + each - 1) / each) * t.tiles;
-      a.groups[i] = (uint32_t)groups;
-    }
-    a.groups[1] = (uint32_t)groups;
-    groups *= batch;
-    if (a.steps == 1 || groups >= kWantGroups) break;
-  }
+  const unsigned groups = a.groups[1] * (unsigned)batch;
   if (elem_bytes == 4) {
-    if (head_dim == 64) launch_typed<float, 64>(s, half_layout, stream, (unsigned)groups, a);
-    else launch_typed<float, 128>(s, half_layout, stream, (unsigned)groups, a);
+    if (head_dim == 64) launch_typed<float, 64>(s, half_layout, stream, groups, a);
+    else launch_typed<float, 128>(s, half_layout, stream, groups, a);
   } else {
-    if (head_dim == 64) launch_typed<__bf16, 64>(s, half_layout, stream, (unsigned)groups, a);
-    else launch_typed<__bf16, 128>(s, half_layout, stream, (unsigned)groups, a);
+    if (head_dim == 64) launch_typed<__bf16, 64>(s, half_layout, stream, groups, a);
+    else launch_typed<__bf16, 128>(s, half_layout, stream, groups, a);
   }
 }
 

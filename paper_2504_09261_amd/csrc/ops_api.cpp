@@ -13,6 +13,8 @@ using namespace hack;
 
 namespace {
 
+constexpr int kMostGroups = (1 << 24) - 1;   // of 256 threads, which a launch counts in 32 bits
+
 // Kernels run on the device that is current when they are launched; the context's memory lies on its own.
 hack_status check_device(hack_ctx* ctx) {
   int dev = -1;
@@ -72,7 +74,7 @@ hack_status take_rows(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* r, c
   t->sn = r->stride_n;
   t->heads = r->heads;
   const int64_t rows = (int64_t)B * r->heads * N;
-  if (rows > (int64_t)1 << 34) return fail(ctx, HACK_ECAPACITY, "%s has %lld rows, more than a launch takes", name, (long long)rows);
+  if (rows > (int64_t)1 << 34 || r->heads > 1 << 30) return fail(ctx, HACK_ECAPACITY, "%s has %lld rows, more than a launch takes", name, (long long)rows);
   *in = Range{(uintptr_t)r->x, (uintptr_t)r->x + (uintptr_t)span * e};
   *out = Range{(uintptr_t)r->out, (uintptr_t)r->out + (uintptr_t)(rows * d) * e};
   return HACK_OK;
@@ -115,6 +117,41 @@ hack_status take_rope(hack_ctx* ctx, const hack_rope* rope, int32_t N, const int
   return HACK_OK;
 }
 
+// The launch shape of a rotation, and its number of work-groups.
+int64_t shape_rotation(int head_dim, int batch, int n_tensors, RotateArgs* a) {
+  constexpr int kMaxSteps = 8;
+  constexpr int kWantGroups = 2048;   // work-groups that fill the chip: eight a compute unit
+  const int slots = kRotateThreads / (head_dim / 16);
+  for (int i = 0; i < n_tensors; ++i) {
+    RotateTensor& t = a->t[i];
+    // Rows of one head side by side: few, so that the rest of the work-group takes the heads beside it, which lie behind each other in a projection
+    // (4, 8, 32 rows: 16384 rows of 32 + 8 heads 64.8, 66.7, 65.4 us, 32 x 256 of 30 + 30 heads 26.0, 29.0, 28.5, 2 x 4096 of 16 heads 15.4, 14.0, 14.6),
+    // but as many as leave no more than a quarter of the lanes without a head (2 x 11844 rows of 10 + 2 heads of 64: 22.7 us with as few as fit the heads of
+    // the larger tensor, 15.8 so; 8 x 10948 of 2 + 1 heads 21.1, 18.6).
+    const auto idle = [&](int log2) {
+      const int64_t across = slots >> log2, taken = (t.heads + across - 1) / across * across;
+      return 4 * (taken - t.heads) > taken;
+    };
+    int log2 = 0;
+    while ((1 << log2) < slots && (1 << log2) < a->n && (log2 < 2 || idle(log2))) ++log2;
+    t.tokens_log2 = log2;
+    t.tiles = (int32_t)(((int64_t)a->n + (1 << log2) - 1) >> log2);
+  }
+  // A thread walks over as many heads as leave enough work-groups: it forms its angles once for all of them.
+  for (a->steps = kMaxSteps;; a->steps /= 2) {
+    int64_t groups = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+      const RotateTensor& t = a->t[i];
+      const int64_t each = (slots >> t.tokens_log2) * a->steps;
+      groups += (t.heads + each - 1) / each * t.tiles;
+      a->groups[i] = (uint32_t)groups;
+    }
+    a->groups[1] = (uint32_t)groups;
+    groups *= batch;
+    if (a->steps == 1 || groups >= kWantGroups) return groups;
+  }
+}
+
 hack_status rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, int norm, float eps, const hack_rope* rope,
                    const int32_t* pos, int64_t pos_stride_b, int32_t pos0, hack_stream stream) {
   hack_status st = check_common(ctx, B, N, true);
@@ -141,6 +178,8 @@ hack_status rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, cons
         return fail(ctx, HACK_EINVAL, "an output overlaps the weights");
   }
   if ((st = check_device(ctx)) != HACK_OK) return st;
+  const int64_t groups = shape_rotation(ctx->cfg.head_dim, B, n, &a);
+  if (groups > kMostGroups) return fail(ctx, HACK_ECAPACITY, "%lld work-groups are more than a launch takes", (long long)groups);
   launch_rotate(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, !rope || rope->layout == HACK_ROPE_HALF, B, n, a);
   HIP_TRY(ctx, hipGetLastError());
   return HACK_OK;
@@ -484,8 +523,7 @@ extern "C" hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, c
   a.scale = scale;
   const int queries = queries_per_group(ctx, kv->len, U, N_k);
   a.q_tiles = tiles_of(N_k, queries);
-  // Units of a launch: its work-groups, a multiple of eight times the tiles, are of 256 threads, which a launch counts in 32 bits.  (Units that are cut have few.)
-  constexpr int kMostGroups = (1 << 24) - 1;
+  // Units of a launch: its work-groups are a multiple of eight times the tiles.  (Units that are cut have few.)
   const int most = std::min(kAttnPackedUnits, kMostGroups / a.q_tiles / 8 * 8);
   if (most < 1) return fail(ctx, HACK_ECAPACITY, "%d queries are more than a launch takes", N_k);
   std::vector<int32_t> order(std::min(U, most)), count;

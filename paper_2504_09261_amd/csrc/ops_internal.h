@@ -21,7 +21,7 @@ struct RotateTensor {
   int64_t sb, sh, sn;
   int32_t heads;
   int32_t w_stride;
-  // launch shape, set by launch_rotate
+  // launch shape, set by shape_rotation
   int32_t tokens_log2;  // rows of one head a work-group takes (power of two)
   int32_t tiles;        // of rows: work-groups take one of them and a part of the heads
 };
@@ -36,11 +36,12 @@ struct RotateArgs {
   float gain, eps;
   int32_t norm;         // kNorm*
   float low;            // sums of squares below it, or not finite, are formed again from scaled rows; set by launch_rotate
-  // launch shape, set by launch_rotate
+  // launch shape, set by shape_rotation
   uint32_t groups[2];   // work-groups of a batch element: of t[0], of both
   int32_t steps;        // heads a thread takes, one after the other
   uint64_t turns[kMaxPairs];   // of a pair per position, in units of 2^-64 of a turn
 };
+constexpr int kRotateThreads = 256;   // of a work-group, 16 elements each
 void launch_rotate(hipStream_t s, int elem_bytes, int head_dim, bool half_layout, int batch, int n_tensors, RotateArgs a);
 
 // ---- rows in 4 bits ---------------------------------------------------------

@@ -352,6 +352,31 @@ int many_chunks() {
   return 0;
 }
 
+// Rotations: every row once in fewer than 2^32 threads, or a refusal.
+int large_rotations() {
+  double freq[64];
+  CHECK(hack_rope_freqs(16, 1, HACK_ROPE_PLAIN, 10000.0, 1.0, 0.0, freq, nullptr) == HACK_OK);
+  const hack_rope rope{HACK_ROPE_HALF, 16, 1, 1.f, freq};
+  struct Call { int B, heads, N; bool fits; };
+  for (const Call& x : {Call{1, 1, 1, true}, Call{64, 40, 1, true}, Call{2, 16, 4096, true}, Call{1, 1, 32 * ((1 << 24) - 1), true}, Call{1, 1, 32 * ((1 << 24) - 1) + 1, false},
+                        Call{1, 1, INT32_MAX, false}, Call{1, 3, INT32_MAX, false}, Call{(1 << 24) - 1, 1, 1, true}, Call{1 << 24, 1, 1, false}, Call{1, 1 << 30, 1, true}, Call{1, (1 << 30) + 1, 1, false},
+                        Call{8, INT32_MAX, 1, false}, Call{INT32_MAX, 1, 1, false}}) {
+    hack_ctx ctx;   // no workspace is used
+    ctx.cfg = hack_config{0, 1, kD, HACK_BF16, INT32_MAX, 64, INT32_MAX, 32};
+    const hack_rows r{at(0x100000000000), at(0x600000000000), x.heads, (int64_t)x.heads * x.N * kD, (int64_t)x.N * kD, kD, nullptr, 0};
+    stub::rotations.clear();
+    const hack_status st = hack_rotate(&ctx, x.B, x.N, &r, &rope, nullptr, 0, 0, kStream);
+    CHECK(st == (x.fits ? HACK_OK : HACK_ECAPACITY) && stub::rotations.size() == (x.fits ? 1 : 0));
+    if (!x.fits) continue;
+    const RotateArgs& a = stub::rotations[0];
+    CHECK((int64_t)a.groups[1] * x.B < (1 << 24) && a.groups[0] == a.groups[1]);
+    const int64_t across = (kRotateThreads / 8) >> a.t[0].tokens_log2, rows = 1 << a.t[0].tokens_log2, parts = a.groups[0] / a.t[0].tiles;
+    CHECK(parts * a.t[0].tiles == a.groups[0] && a.t[0].tiles * rows >= x.N && (a.t[0].tiles - 1) * rows < x.N);
+    CHECK(parts * across * a.steps >= x.heads && (parts - 1) * across * a.steps < x.heads);
+  }
+  return 0;
+}
+
 int pack_refusals() {
   Context c;
   CHECK(hack_packed_bytes(96, 64, nullptr) == HACK_EINVAL);
@@ -591,7 +616,7 @@ int main(int argc, char** argv) {
                                                    {"shared_memory", shared_memory}, {"many_units", many_units}, {"attn_plan", attn_plan}, {"no_exceptions", no_exceptions},
                                                    {"backward_frequencies", backward_frequencies}, {"chunk_rows", chunk_rows}, {"large_launches", large_launches},
                                                    {"rotation_shared_memory", rotation_shared_memory}, {"far_lists", far_lists}, {"rope_parts_ends", rope_parts_ends},
-                                                   {"many_chunks", many_chunks}};
+                                                   {"many_chunks", many_chunks}, {"large_rotations", large_rotations}};
   const auto it = argc > 1 ? checks.find(argv[1]) : checks.end();
   if (it == checks.end()) return 2;
   const int rc = it->second();

@@ -24,7 +24,7 @@ def test_host_side(program, name):
     assert r.returncode == 0 and r.stdout.strip().endswith("ok"), r.stdout + r.stderr[-2000:]
 
 
-@pytest.mark.parametrize("name", ["backward_frequencies", "chunk_rows", "large_launches", "rotation_shared_memory", "far_lists", "rope_parts_ends", "many_chunks"])
+@pytest.mark.parametrize("name", ["backward_frequencies", "chunk_rows", "large_launches", "rotation_shared_memory", "far_lists", "rope_parts_ends", "many_chunks", "large_rotations"])
 def test_ranges(program, name):
     r = subprocess.run([str(program), name], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip().endswith("ok") and not r.stderr, r.stdout + r.stderr[-2000:]
