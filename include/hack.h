@@ -392,9 +392,10 @@ hack_status hack_step_final(hack_ctx* ctx, hack_kvcache* cache, int32_t B,
  *
  * A pair (a, b) of a head's row at position p becomes
  *   (gain (a cos(p f) - b sin(p f)), gain (a sin(p f) + b cos(p f))),
- * f its frequency in radians per position.  Angles are exact to 1e-8 for every
- * 32-bit position, negative ones too: -p undoes p where gain is 1.  Elements from
- * rot_dim on pass through.  Everything is formed in float32 and rounded once. */
+ * f its frequency in radians per position, of either sign.  p f is known to 1e-8 within
+ * its turn for every 32-bit position, negative ones too (-p undoes p where gain is 1); from there on everything
+ * is formed in float32 (off by at most 10.1 2^-24 gain (|a| + |b|)) and rounded once.  Elements from
+ * rot_dim on pass through. */
 enum { HACK_ROPE_HALF = 0, HACK_ROPE_INTERLEAVED = 1 };
 
 typedef struct {
@@ -432,7 +433,8 @@ hack_status hack_rope_freqs(int32_t rot_dim, int32_t axes, int32_t scaling, doub
  *   pos  DEVICE int32: row n of batch element b has position pos[b pos_stride_b + a N + n]
  *        on axis a (pos_stride_b 0: the same for every batch element); NULL: pos0 + n (one axis)
  * Errors: HACK_EINVAL (NULL/misaligned pointers, strides, layout, frequencies that are not numbers of at most 1e6, overlap, the current
- * device is not the context's), HACK_EUNSUPPORTED (rot_dim no multiple of 16 for each axis), HACK_ECAPACITY. */
+ * device is not the context's), HACK_EUNSUPPORTED (rot_dim no multiple of 16 for each axis), HACK_ECAPACITY (B or N beyond what the context was made
+ * for: max_units / H, max_queries). */
 hack_status hack_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* x, const hack_rope* rope,
                         const int32_t* pos, int64_t pos_stride_b, int32_t pos0, hack_stream stream);
 
@@ -481,7 +483,7 @@ hack_status hack_packed_bytes(int32_t head_dim, int64_t rows, int64_t* bytes);
  * `pos` is written for rows from k_new (pos_new + row number), and for cached rows
  * if `in` carries it too.  `out` shares no memory with what is read.  bf16 and fp32 contexts.
  * Errors: HACK_EINVAL (NULL/misaligned pointers, more rows than there are, units outside out or overlapping in it, shared memory, the
- * current device is not the context's), HACK_ECAPACITY. */
+ * current device is not the context's), HACK_ECAPACITY (kept_idx rows shorter than a unit takes, B or N_k beyond max_units / H, max_queries). */
 hack_status hack_pack(hack_ctx* ctx, int32_t B, int32_t N_k, const hack_cache* in, const void* k_new, const void* v_new,
                       int32_t pos_new, const int32_t* kept_idx, int64_t idx_stride, const int32_t* first,
                       const hack_packed_cache* out, hack_stream stream);
@@ -493,8 +495,9 @@ hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_cache* in, c
                         const hack_cache* out, hack_stream stream);
 
 /* hack_attn over a packed cache: O = Softmax(scale * Q K^T) V for every unit over its
- * own kv->len[u] rows, no mask.  Every unit must have at least one row; out must not
- * share memory with q (refused) or kv.  Units are not limited by max_cache_len.  Heads that share a
+ * own kv->len[u] rows, no mask: the rows that a call packed for its own queries are seen by all of them, as
+ * those of a scale are (a text prompt whose tokens must not see later ones is not this call's).  Every unit must have at least one row; out must not
+ * share memory with q (refused) or kv (not looked for).  Units are not limited by max_cache_len.  Heads that share a
  * cache: queries [B, G H, N, d] of G heads to each of the H caches are [B, H, G N, d],
  * so N_k = G N.  The values that packing rounds to are bf16 numbers, so the accuracy is
  * hack_attn's over the rows that hack_unpack gives.  Results are reproducible bit for bit.

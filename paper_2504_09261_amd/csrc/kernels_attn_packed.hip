@@ -15,7 +15,8 @@
 // last-level cache keeps from launch to launch) 46, and 58 and 44 where all units share one cache, so arithmetic is not far behind.  A block takes a wave 2.9 us with another work-group on the
 // compute unit and 1.6 alone.  Tried: four work-groups a compute unit (128 registers spill) 41 -> 56 us for 512 units of 900 to 4000 rows; V in two halves of
 // 32 rows, three work-groups a compute unit, equal within 3 %; the last work-group of a unit to end merges its chunks (tickets), 8.9 -> 9.6 us for 8 units of 4000 rows,
-// 13.6 -> 15.8 for 32.  K by the scaled matrix instruction, codes as they are and queries in two 8-bit or three 6-bit pieces: the sums keep 16 bits of the largest
+// 13.6 -> 15.8 for 32.  In float32 contexts there are three matrix instructions for every bf16 one: 512 units of 900 to 4000 rows, 4 queries 45 us (bf16 37), 32 units of
+// 3000 rows, 1000 queries 136 us (362 TFLOP/s; bf16 in its form of 128 queries 66).  K by the scaled matrix instruction, codes as they are and queries in two 8-bit or three 6-bit pieces: the sums keep 16 bits of the largest
 // product, or the pieces 14 of the largest query element, where bf16 operands lose nothing.
 #include <cfloat>
 #include <type_traits>

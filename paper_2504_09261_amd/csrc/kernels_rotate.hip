@@ -7,7 +7,7 @@
 // Memory-bound: a row is read and written once, whatever the strides it is read with.  A lane holds 16 elements of a row, pieces of 16 bytes chosen so
 // that its pairs are its own and the lanes of an access lie side by side: no exchange but the sum of squares over the 8 (head_dim 128) or 4 lanes of a row.  Angles are formed
 // once for a token and used for all heads that the thread walks over.  They are exact where it matters: the frequency is held in units of 2^-64
-// turns, so the product with a position wraps to its fraction of a turn in integers, however far the position.
+// turns, so the product with a position wraps to its fraction of a turn in integers, however far the position (cut at 2^-32 turns, 1.5e-9 rad).
 // Measured: 16384 rows of 32 + 8 heads of 128 out of a projection, normed and turned, 66 us (5.1 TB/s of the 6.2 that a plain elementwise
 // kernel reaches), 2 x 4096 rows of 16 heads in two axes 13 us (5.1).
 #include <algorithm>
@@ -26,7 +26,7 @@ constexpr int kThreads = kRotateThreads;
 constexpr int64_t kL2Bytes = 32 << 20;   // of eight XCDs
 
 // 2^32 u turns -> cosine and sine.  The nearest quarter turn, then the Taylor series of the rest (at most pi / 4: the first terms
-// left out are 2e-9 and 2e-11).
+// left out are 1.8e-9 of the sine, 1.2e-10 of the cosine).  The rest is a float32 number of radians: rounded twice, up to 7.5e-8 off.
 __device__ __forceinline__ void cos_sin(unsigned u, float& c, float& s) {
   const unsigned q = (u + 0x20000000u) >> 30;
   const float x = (float)(int)(u - (q << 30)) * 1.4629180792671596e-9f;   // 2 pi 2^-32

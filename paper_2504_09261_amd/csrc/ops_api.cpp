@@ -239,7 +239,8 @@ void measure(const int32_t* len, int n, int64_t* blocks, int64_t* longest) {
 // How units are cut, if at all.  Work-groups of less to do fill the chip and end together, but each leaves a part, and merging the parts is a launch of its
 // own: neither the most nor the fewest work-groups are best.  Tried by an estimate of the time are: no cut; chunks that give each compute unit one work-group,
 // and two (by the mean, by the mean and half a chunk left over in every unit, by the longest); chunks that balance their own time with that of their parts.
-// Fitted to 250 launches of 4 to 600 units, even and ragged, 500 to 32000 keys, 1 to 1500 queries, each cut into 1 to 32 chunks: what it picks takes
+// Fitted to 250 bf16 launches of 4 to 600 units, even and ragged, 500 to 32000 keys, 1 to 1500 queries, each cut into 1 to 32 chunks (float32 contexts are cut by the
+// rates of the 16-query bf16 form as they are; no fit was made for them): what it picks takes
 // 1.03 times the best of them on average, 1.38 at most (always two work-groups to a compute unit: 1.06, 2.1).  Us a launch, always two / so: 14 units
 // of 21747 to 27815 keys, 472 queries 132 / 103, 12 of 1009 to 1591, 5 queries 9.1 / 6.9.
 double plan_chunks(const hack_ctx* ctx, int queries, const int32_t* len, int64_t blocks, int64_t longest, AttnPackedHead* a) {
