@@ -496,7 +496,7 @@ hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_cache* in, c
 
 /* hack_attn over a packed cache: O = Softmax(scale * Q K^T) V for every unit over its
  * own kv->len[u] rows, no mask: the rows that a call packed for its own queries are seen by all of them, as
- * those of a scale are (a text prompt whose tokens must not see later ones is not this call's).  Every unit must have at least one row; out must not
+ * those of a scale are (there is no form for a text prompt, whose tokens must not see later ones).  Every unit must have at least one row; out must not
  * share memory with q (refused) or kv (not looked for).  Units are not limited by max_cache_len.  Heads that share a
  * cache: queries [B, G H, N, d] of G heads to each of the H caches are [B, H, G N, d],
  * so N_k = G N.  The values that packing rounds to are bf16 numbers, so the accuracy is
