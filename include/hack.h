@@ -444,7 +444,7 @@ hack_status hack_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* x,
  * over all head_dim elements, sums of squares in float32 (of a row scaled by a power of two
  * where its squares leave float32: rows of any finite magnitude have their norm).  k may be NULL, rope may be
  * NULL (norms alone; pos is not read then).  eps > 0.  Errors as hack_rotate. */
-enum { HACK_NORM_RMS = 0, HACK_NORM_UNIT = 1 };
+enum { HACK_NORM_NONE = -1 /* hack_append_pages only */, HACK_NORM_RMS = 0, HACK_NORM_UNIT = 1 };
 hack_status hack_norm_rotate(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, int32_t norm,
                              float eps, const hack_rope* rope, const int32_t* pos, int64_t pos_stride_b, int32_t pos0,
                              hack_stream stream);
@@ -504,6 +504,74 @@ hack_status hack_unpack(hack_ctx* ctx, int32_t B, const hack_packed_cache* in, c
  * Errors: HACK_EINVAL, HACK_ECAPACITY as above. */
 hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, const void* q, const hack_packed_cache* kv,
                              float scale, void* out, hack_stream stream);
+
+/* ---- caches in pages ------------------------------------------------------------
+ * The rows of a sequence lie in pages of a pool, in the order of a table of page
+ * numbers, so that sequences grow without moving and share pages.  Tables, lengths and
+ * numbers of new rows are DEVICE memory, read when the kernels run: a captured graph goes
+ * on as a sequence grows.  Row r of a sequence is row r % page_rows of page
+ * table[r / page_rows].
+ *
+ * What only a running kernel can see is reported as HACK_EINVAL by hack_check and the next
+ * call, once: a page number outside [0, pages) (rows there are left out: not stored, not
+ * seen), a length outside [0, max_len] or a number of new rows outside [0, N] (brought to
+ * the nearest of these).  Entries of a table behind a sequence's last row are not read. */
+typedef struct {
+  void* k;              /* DEVICE element (page p, row r, head h, i) at p stride_page + r stride_row + h stride_head + i */
+  void* v;              /* DEVICE the same; rows of K and V may lie in turn in one allocation */
+  int64_t pages;        /* 1 .. 2^31 - 1 */
+  int32_t page_rows;    /* a power of two, 16 .. 65536 */
+  int64_t stride_page, stride_row, stride_head;   /* elements, multiples of 16 bytes; rows do not overlap.  stride_head 0: a page holds one head
+                           (tables by head, or one head) */
+  const int32_t* table; /* DEVICE [B, table_stride], by_head: [B*H, table_stride] */
+  int32_t table_pages;  /* entries of a row of the table */
+  int64_t table_stride; /* elements, at least table_pages */
+  const int32_t* len;   /* DEVICE [B], by_head: [B*H]: rows with those that the call brings */
+  int32_t by_head;      /* nonzero: every (batch, head) has a row of the table and a length of its own, as compression leaves them */
+  int32_t max_len;      /* no length is greater; 0: table_pages * page_rows.  Launches are laid out for it */
+} hack_pages;
+
+/* New rows of k and v into the pages of their sequences, k normed and rotated on the way, and, q
+ * not NULL, the queries normed and rotated in the same launch.  Row i < fresh[b] of batch
+ * element b becomes row len[b] - fresh[b] + i of its sequence (dropped if that is
+ * negative); rows of q from fresh[b] on are left as they are in q->out, and pages are
+ * written nowhere else.  A page row must not be the target of two rows of a call.
+ *   q      as in hack_norm_rotate, any number of heads; NULL: none
+ *   k, v   H heads, out NULL; v has no weight
+ *   norm   HACK_NORM_*, over k and q (HACK_NORM_NONE: no weights either)
+ *   rope   NULL: no rotation
+ *   pos    as in hack_rotate; NULL: the rows' numbers in the cache (one axis, not by_head)
+ *   fresh  DEVICE int32 [B], NULL: N new rows for all
+ * Arithmetic as in hack_rotate and hack_norm_rotate, v is copied.  The new rows' keys are the ones that
+ * hack_attn_pages reads; rows must not be read by another call while they are written.
+ * Errors: HACK_EINVAL (NULL/misaligned pointers, strides, layout, frequencies, rows that overlap each other or what is read, the current
+ * device is not the context's), HACK_EUNSUPPORTED (rot_dim no multiple of 16 for each axis), HACK_ECAPACITY (B or N beyond
+ * max_units / H, max_queries). */
+hack_status hack_append_pages(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, const hack_rows* v,
+                              int32_t norm, float eps, const hack_rope* rope, const int32_t* pos, int64_t pos_stride_b,
+                              const int32_t* fresh, const hack_pages* cache, hack_stream stream);
+
+/* Batch elements first .. first + count - 1 have the same rows 0 .. rows - 1: those of element `first` (its heads, by_head). */
+typedef struct {
+  int32_t first, count, rows;
+} hack_shared;
+
+/* Attention over caches in pages: O = Softmax(scale * Q K^T) V over the rows that a query sees.
+ * Query n < fresh[b] sees the len[b] rows of its sequence, or, causal, the first
+ * len[b] - fresh[b] + n + 1 of them (the last fresh[b] rows are the queries' own).  A query
+ * that sees no row gives zeros; queries from fresh[b] on are not computed and `out` is left
+ * as it is there.  What rows hold that a query does not see (infinities and NaN too) does not reach it.
+ *   heads   of q, a multiple G of H: query heads G h .. G h + G - 1 read cache h
+ *   q, out  DEVICE [B, heads, N, head_dim]
+ *   shared  HOST n_shared groups in ascending order, none in two of them; NULL: none.  Rows that a group shares are read
+ *           once for all of it where that is faster, from the first element's pages.  Lengths count them: an element whose length is smaller sees that many.
+ * Sums are in float32, softmax in one pass; results are reproducible bit for bit from call to call with the same
+ * lengths, groups and max_len.  out must not share memory with q or the cache.
+ * Errors: HACK_EINVAL, HACK_ECAPACITY (B or N beyond max_units / H, max_queries, more than 256 groups, more queries than a
+ * launch takes). */
+hack_status hack_attn_pages(hack_ctx* ctx, int32_t B, int32_t N, int32_t heads, const void* q, const hack_pages* cache,
+                            const int32_t* fresh, int32_t causal, const hack_shared* shared, int32_t n_shared, float scale,
+                            void* out, hack_stream stream);
 
 #ifdef __cplusplus
 }

@@ -25,7 +25,8 @@ EXPORTS = [
     "hack_kvcache_rows_required", "hack_kvcache_create", "hack_kvcache_destroy",
     "hack_kvcache_reset", "hack_kvcache_view", "hack_kvcache_step_form", "hack_step", "hack_head_variance",
     "hack_set_score_mode", "hack_get_score_mode", "hack_score_static", "hack_score_item_keys", "hack_merge", "hack_step_final",
-    "hack_rope_freqs", "hack_rotate", "hack_norm_rotate", "hack_packed_bytes", "hack_pack", "hack_unpack", "hack_attn_packed",
+    "hack_rope_freqs", "hack_rotate", "hack_norm_rotate", "hack_packed_bytes", "hack_pack", "hack_unpack", "hack_attn_packed", "hack_append_pages",
+    "hack_attn_pages",
 ]
 
 
@@ -56,6 +57,12 @@ class hack_rope(C.Structure):
     _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("axes", C.c_int32), ("gain", C.c_float), ("freq", C.POINTER(C.c_double))]
 
 
+class hack_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_int64), ("page_rows", C.c_int32), ("stride_page", C.c_int64), ("stride_row", C.c_int64),
+                ("stride_head", C.c_int64), ("table", C.c_void_p), ("table_pages", C.c_int32), ("table_stride", C.c_int64), ("len", C.c_void_p),
+                ("by_head", C.c_int32), ("max_len", C.c_int32)]
+
+
 _lib = None
 _step_call = _step_addr = None    # CPython entry; addresses of hack_step and hack_step_final
 _ops_call = _ops_addr = None      # CPython entries; addresses of the functions they call
@@ -80,7 +87,7 @@ def load_library() -> C.CDLL:
                                 "`python -m paper_2504_09261_amd.build` (there is no fallback path)") from e
     lib = C.CDLL(LIB_PATH)
     _step_addr = tuple(C.cast(f, C.c_void_p).value for f in (lib.hack_step, lib.hack_step_final))
-    _ops_addr = {n: C.cast(getattr(lib, "hack_" + n), C.c_void_p).value for n in ("rotate", "norm_rotate", "pack", "unpack", "attn_packed")}
+    _ops_addr = {n: C.cast(getattr(lib, "hack_" + n), C.c_void_p).value for n in ("rotate", "norm_rotate", "pack", "unpack", "attn_packed", "append_pages", "attn_pages")}
     vp, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
     pi32, pi64, pu8 = C.POINTER(C.c_int32), C.POINTER(C.c_int64), C.POINTER(C.c_uint8)
     pcache = C.POINTER(hack_cache)
@@ -237,6 +244,34 @@ class PackedCache:
         k, v = (torch.empty((n, packed_bytes(head_dim, PACK_ROWS)), dtype=torch.uint8, device=device) for _ in range(2))
         pos = torch.empty((n * PACK_ROWS,), dtype=torch.int32, device=device) if with_pos else None
         return cls(k, v, PACK_ROWS * (np.cumsum(blocks) - blocks), np.zeros(len(blocks), np.int32), pos)
+
+
+class PagedCache:
+    """A hack_pages view.  k, v: [pages, rows of a page, heads, head_dim] in the same strides, any with head_dim side by side (so a pool that keeps a head's rows
+    together is given transposed).  table: int32 [B, pages of a sequence], length: int32 [B], with the rows that a call brings; where pages hold one head and the context has
+    more, both go by head, [B heads, ...]; max_len: the most that a length will be (default: what a row of the table holds), which launches are laid out for.  Its
+    tensors are not replaced, since the library reads the structure that they were put into; what they hold may change at any time, in captured graphs too."""
+
+    def __init__(self, k, v, table, length, max_len: int = 0):
+        import torch
+        assert k.is_cuda and all(t.device == k.device for t in (v, table, length)), "device tensors, on one device"
+        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.stride() == v.stride() and k.stride(3) == 1, \
+            "K and V: [pages, rows, heads, head_dim] in the same strides"
+        assert table.dtype == length.dtype == torch.int32 and table.dim() == 2 and length.shape == table.shape[:1], "table: int32 rows of pages; length: an int32 for each"
+        assert length.is_contiguous() and (table.stride(1) == 1 or table.shape[1] <= 1), "lengths, and the entries of a table's row, side by side"
+        assert 0 <= max_len < 1 << 31, "max_len: an int32"
+        pages, rows, heads, head_dim = k.shape
+        across = table.stride(0) if table.shape[0] > 1 else table.shape[1]
+        struct = hack_pages(k.data_ptr(), v.data_ptr(), pages, rows, k.stride(0) if pages > 1 else 0, k.stride(1), k.stride(2) if heads > 1 else 0, table.data_ptr(),
+                            table.shape[1], across, length.data_ptr(), 0, max_len)
+        self.__dict__.update(k=k, v=v, table=table, len=length, max_len=max_len, _struct=struct,
+                             _info=(C.addressof(struct), k.get_device(), k.dtype, head_dim, heads, int(table.shape[0])))
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"a PagedCache's {name} is not replaced: make another one")
+
+    def __reduce__(self):   # a copy has a structure of its own
+        return PagedCache, (self.k, self.v, self.table, self.len, self.max_len)
 
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
@@ -483,6 +518,24 @@ class Hack:
     def attn_packed(self, q, packed: PackedCache, scale: float, out):
         """q: [B, G heads, N, head_dim], G query heads to each cache."""
         st = _ops_call.attn(_ops_addr["attn_packed"], self.ctx and self.ctx.value, self._info, q, packed, scale, out, _stream())
+        if st != 0:
+            self._check(st)
+
+    # ---- caches in pages ----
+    def append_pages(self, k, v, cache: PagedCache, rope: Optional[Rope] = None, pos=None, fresh=None, q=None, q_out=None, norm: Optional[str] = None,
+                     eps: float = 1e-6, q_weight=None, k_weight=None):
+        """The first fresh[b] (int32 [B]; None: all) rows of k and v ([B, heads, N, head_dim] in any strides) become the last ones of their sequences, k normed and
+        rotated (rope None: not); q: normed and rotated into q_out.  pos as in rotate; None: the rows' numbers in the cache."""
+        st = _ops_call.append_pages(_ops_addr["append_pages"], self.ctx and self.ctx.value, self._info, q, q_out, q_weight, k, k_weight, v,
+                                    -1 if norm is None else NORMS[norm], eps, None if rope is None else rope.address, 1 if rope is None else rope.axes, pos, fresh,
+                                    cache._info, _stream())
+        if st != 0:
+            self._check(st)
+
+    def attn_pages(self, q, cache: PagedCache, scale: float, out, causal: bool = False, fresh=None, shared=None):
+        """q: [B, G heads, N, head_dim], G query heads to each cache; the first fresh[b] queries (None: all) see their sequence's rows, causal: those up to their own.
+        shared: (first, count, rows) of batch elements that have the same first rows."""
+        st = _ops_call.attn_pages(_ops_addr["attn_pages"], self.ctx and self.ctx.value, self._info, q, cache._info, fresh, causal, shared, scale, out, _stream())
         if st != 0:
             self._check(st)
 

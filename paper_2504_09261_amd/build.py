@@ -14,7 +14,8 @@ LIB_PATH = os.path.join(HERE, LIB_NAME)
 STEP_CALL_PATH = os.path.join(HERE, "_step_call.so")   # CPython entry to hack_step
 OPS_CALL_PATH = os.path.join(HERE, "_ops_call.so")     # CPython entries to the operators around the cache
 SOURCES = ["hack_api.cpp", "kernels_move.hip", "kernels_select.hip", "kernels_score.hip", "kernels_attn.hip", "kernels_attn_split.hip", "kernels_attn_f32.hip", "kernels_step.hip",
-           "kernels_headvar.hip", "kernels_merge.hip", "ops_api.cpp", "kernels_rotate.hip", "kernels_packed.hip", "kernels_attn_packed.hip", "kernels_attn_packed_tiles.hip"]
+           "kernels_headvar.hip", "kernels_merge.hip", "ops_api.cpp", "kernels_rotate.hip", "kernels_packed.hip", "kernels_attn_packed.hip", "kernels_attn_packed_tiles.hip",
+           "pages_api.cpp", "kernels_pages.hip", "kernels_attn_pages.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms are switched off for all device code.

@@ -18,6 +18,7 @@
 #include "../../include/hack.h"
 #include "hack_ctx.h"
 #include "hack_internal.h"
+#include "pages_internal.h"
 #include "table_cache.h"
 
 using namespace hack;
@@ -556,8 +557,9 @@ extern "C" hack_status hack_create(hack_ctx** out, const hack_config* cfg) {
     e = hipMalloc((void**)&ctx->part_o, (size_t)ctx->part_rows * cfg->head_dim * sizeof(float));
     if (e == hipSuccess) e = hipMalloc((void**)&ctx->part_ml, (size_t)ctx->part_rows * 2 * sizeof(float));
   }
-  if (e == hipSuccess) e = hipHostMalloc((void**)&ctx->fault, 2 * sizeof(int), hipHostMallocDefault);
-  if (e == hipSuccess) ctx->fault[0] = ctx->fault[1] = 0;
+  if (e == hipSuccess) e = hipMalloc((void**)&ctx->page_plan, ((size_t)cfg->max_units + kMostShared) * sizeof(int2));
+  if (e == hipSuccess) e = hipHostMalloc((void**)&ctx->fault, 3 * sizeof(int), hipHostMallocDefault);
+  if (e == hipSuccess) ctx->fault[0] = ctx->fault[1] = ctx->fault[2] = 0;
   if (e == hipSuccess) e = hipMemset(ctx->rowstat, 0xFF, n_slots * sizeof(unsigned long long));   // every slot empty
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e == hipSuccess) {
@@ -608,6 +610,7 @@ extern "C" void hack_destroy(hack_ctx* ctx) {
   if (ctx->part_o) (void)hipFree(ctx->part_o);
   if (ctx->part_ml) (void)hipFree(ctx->part_ml);
   if (ctx->part_count) (void)hipFree(ctx->part_count);
+  if (ctx->page_plan) (void)hipFree(ctx->page_plan);
   if (ctx->ev_fork) (void)hipEventDestroy(ctx->ev_fork);
   if (ctx->ev_join) (void)hipEventDestroy(ctx->ev_join);
   if (ctx->aux_stream) (void)hipStreamDestroy(ctx->aux_stream);

@@ -62,8 +62,9 @@ struct hack_ctx {
   int32_t* merge_nn = nullptr;   // final-step merge (bf16): [max_units, ws_stride] nearest kept row of every cache row
   float* merge_w = nullptr;      //   ... its weight
   float* merge_inv = nullptr;    //   ... inverse key norms of the kept rows
-  int* fault = nullptr;          // pinned, device-visible int[2]: [0] a score wave's bounded wait gave up (fatal),
-                                 // [1] a logit exceeded the range the bf16 score kernel supports
+  int* fault = nullptr;          // pinned, device-visible int[3]: [0] a score wave's bounded wait gave up (fatal),
+                                 // [1] a logit exceeded the range the bf16 score kernel supports,
+                                 // [2] a page number or a length of a cache in pages was out of range
   int cus = 1;                   // compute units of the device
   int score_capacity[hack::kScoreSizes] = {};   // bf16 path: score items one fused launch may hold (resident waves), by item size (kScoreItemKeys)
   int split_max_items = -1;      // launches with at most this many 32-query attention items use the key-split kernel (HACK_ATTN_SPLIT_ITEMS); -1 (default): see use_split_attention
@@ -76,6 +77,7 @@ struct hack_ctx {
   float* part_o = nullptr;       // [2 * attn_slots, 128, head_dim] unnormalised partial outputs (fp32 contexts: [part_rows, head_dim])
   float* part_ml = nullptr;      // [2 * attn_slots, 2, 128] their references and normalisers ([part_rows, 2])
   int64_t part_rows = 0;         // rows of part_o
+  int2* page_plan = nullptr;     // attention over caches in pages: [groups, then batch elements or units] how each is cut
   unsigned* part_count = nullptr; // [attn_slots] ticket counters, zero between launches
   // hack_step overlap: the compression chain of one group of units runs beside the attention of the other group
   int lds_bytes = 0;             // of a work-group, as the device has it
@@ -151,6 +153,11 @@ inline hack_status device_report(hack_ctx* ctx) {
     f[1] = 0;
     return fail(ctx, HACK_EUNSUPPORTED, "an earlier bf16 score launch met a logit beyond +-354 (scale * q.k); such logits "
                                         "are clamped, so its importance may differ from the definition");
+  }
+  if (f && f[2]) {
+    f[2] = 0;
+    return fail(ctx, HACK_EINVAL, "an earlier call over a cache in pages met a page number outside the cache (rows there were left out), or a "
+                                  "length or a number of new rows out of range (taken as the nearest that is not)");
   }
   return HACK_OK;
 }

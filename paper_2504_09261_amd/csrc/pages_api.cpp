@@ -1,0 +1,195 @@
+// Host side of the caches in pages that include/hack.h declares: appending to them and attention over them.  Arguments are checked here and launches laid
+// out for the longest caches they may meet; tables and lengths are device memory that only the kernels read.
+#include "ops_host.h"
+#include "pages_internal.h"
+
+using namespace hack;
+
+namespace {
+
+struct Dim { int64_t stride, count; };
+
+// Whether rows of `width` bytes at the multiples of nested dimensions (the widest first), and the same ones delta bytes on, keep clear of each other.
+bool clear_of(int64_t delta, const Dim* dim, int n, int64_t width) {
+  if (n == 0) return delta >= width || -delta >= width;
+  const int64_t s = dim->stride, below = delta / s - (delta % s < 0);   // numbers differ by this, or one more
+  for (int64_t k = below; k <= below + 1; ++k)
+    if (k > -dim->count && k < dim->count && !clear_of(delta - k * s, dim + 1, n - 1, width)) return false;
+  return true;
+}
+
+struct PageMemory {
+  Range k, v, table, len, fresh;
+};
+
+// Checks a cache and fills in what kernels take of it.
+hack_status take_pages(hack_ctx* ctx, int32_t B, int32_t N, const hack_pages* c, const int32_t* fresh, Pages* p, PageMemory* mem) {
+  if (!c) return fail(ctx, HACK_EINVAL, "cache is NULL");
+  if (!c->k || !c->v || !c->table || !c->len) return fail(ctx, HACK_EINVAL, "cache has a NULL member");
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(ctx, HACK_EINVAL, "cache k/v must be 16-byte aligned");
+  if (((uintptr_t)c->table & 3) || ((uintptr_t)c->len & 3) || ((uintptr_t)fresh & 3)) return fail(ctx, HACK_EINVAL, "table, len and fresh must be 4-byte aligned");
+  if (c->pages < 1 || c->pages > INT32_MAX) return fail(ctx, HACK_EINVAL, "cache pages %lld outside [1, 2^31)", (long long)c->pages);
+  if (c->page_rows < 16 || c->page_rows > 65536 || (c->page_rows & (c->page_rows - 1)))
+    return fail(ctx, HACK_EINVAL, "page_rows %d is no power of two in [16, 65536]", c->page_rows);
+  if (c->table_pages < 1 || c->table_stride < c->table_pages) return fail(ctx, HACK_EINVAL, "a table has at least an entry and table_stride covers its entries");
+  const int64_t H = ctx->cfg.heads, d = ctx->cfg.head_dim, e = ctx->elem_bytes, piece = 16 / e;
+  const int64_t strides[3] = {c->stride_page, c->stride_row, c->stride_head};
+  for (int64_t s : strides)
+    if (s < 0 || s % piece != 0) return fail(ctx, HACK_EINVAL, "cache strides must be non-negative multiples of 16 bytes (got %lld elements)", (long long)s);
+  if (c->stride_row * e > 1 << 26) return fail(ctx, HACK_EINVAL, "cache stride_row is beyond 64 MiB");
+  const bool one = c->stride_head == 0;   // a page holds the rows of one head
+  if (one && H > 1 && !c->by_head) return fail(ctx, HACK_EINVAL, "stride_head 0 needs tables by head");
+  Dim dims[3] = {{c->stride_page, c->pages}, {c->stride_row, c->page_rows}, {one ? 0 : c->stride_head, one ? 1 : H}};
+  std::sort(dims, dims + 3, [](const Dim& a, const Dim& b) { return a.stride > b.stride; });
+  int64_t span = d;   // elements from a row's first to behind the last of the dimensions so far
+  for (int i = 2; i >= 0; --i) {
+    if (dims[i].count == 1) continue;
+    if (dims[i].stride < span) return fail(ctx, HACK_EINVAL, "rows of the cache overlap");
+    if (dims[i].stride > (INT64_MAX >> 4) / dims[i].count) return fail(ctx, HACK_EINVAL, "cache strides are too large");
+    span += dims[i].stride * (dims[i].count - 1);
+  }
+  mem->k = range_of(c->k, span, e);
+  mem->v = range_of(c->v, span, e);
+  if (mem->k.meets(mem->v)) {
+    int n = 0;
+    for (const Dim& x : dims)
+      if (x.count > 1) dims[n++] = Dim{x.stride * e, x.count};
+    if (!clear_of((int64_t)((uintptr_t)c->v - (uintptr_t)c->k), dims, n, d * e)) return fail(ctx, HACK_EINVAL, "rows of K and V overlap");
+  }
+  const int64_t rows = c->by_head ? B * H : B, most = std::min<int64_t>((int64_t)c->table_pages * c->page_rows, INT32_MAX - 2 * kKeys);
+  if (c->table_stride > (INT64_MAX >> 4) / rows) return fail(ctx, HACK_EINVAL, "table_stride is too large");
+  if (c->max_len < 0 || c->max_len > most) return fail(ctx, HACK_EINVAL, "max_len %d outside [0, %lld]", c->max_len, (long long)most);
+  mem->table = range_of(c->table, apart(c->table_stride) * (rows - 1) + c->table_pages, 4);
+  mem->len = range_of(c->len, rows, 4);
+  mem->fresh = range_of(fresh, B, 4);
+  *p = Pages{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->stride_page * e, c->stride_row * e, one ? 0 : c->stride_head * e, c->table, c->table_stride,
+             c->len, fresh, ctx->fault + 2, (int32_t)c->pages, __builtin_ctz((unsigned)c->page_rows), c->max_len ? c->max_len : (int32_t)most, (int32_t)H,
+             c->by_head != 0, N};
+  return HACK_OK;
+}
+
+}  // namespace
+
+extern "C" hack_status hack_append_pages(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, const hack_rows* v, int32_t norm,
+                                         float eps, const hack_rope* rope, const int32_t* pos, int64_t pos_stride_b, const int32_t* fresh,
+                                         const hack_pages* cache, hack_stream stream) {
+  hack_status st = check_common(ctx, B, N, true);
+  if (st != HACK_OK) return st;
+  if (norm != HACK_NORM_NONE && norm != HACK_NORM_RMS && norm != HACK_NORM_UNIT) return fail(ctx, HACK_EINVAL, "bad norm %d", norm);
+  if (norm != HACK_NORM_NONE && (!std::isfinite(eps) || eps <= 0.f)) return fail(ctx, HACK_EINVAL, "eps must be finite and > 0");
+  AppendArgs a{};
+  Range in[3] = {}, out[3] = {};
+  if (q && (st = take_rows(ctx, B, N, q, "q", &a.t[0], &in[0], &out[0])) != HACK_OK) return st;
+  if ((st = take_rows(ctx, B, N, k, "k", &a.t[1], &in[1], &out[1], true)) != HACK_OK) return st;
+  if ((st = take_rows(ctx, B, N, v, "v", &a.v, &in[2], &out[2], true)) != HACK_OK) return st;
+  if (k->heads != ctx->cfg.heads || v->heads != ctx->cfg.heads) return fail(ctx, HACK_EINVAL, "k and v have the context's %d heads", ctx->cfg.heads);
+  if (v->weight || (norm == HACK_NORM_NONE && (k->weight || (q && q->weight)))) return fail(ctx, HACK_EINVAL, "rows without a norm take no weight");
+  PageMemory mem;
+  if ((st = take_pages(ctx, B, N, cache, fresh, &a.c, &mem)) != HACK_OK) return st;
+  a.n = N;
+  a.eps = eps;
+  a.norm = norm == HACK_NORM_NONE ? kNormNone : norm == HACK_NORM_RMS ? kNormRms : kNormL2;
+  if (rope) {
+    if (!pos && cache->by_head) return fail(ctx, HACK_EINVAL, "lengths by head need positions");
+    if ((st = take_rope(ctx, rope, N, pos, pos_stride_b, 0, &a)) != HACK_OK) return st;
+    a.own_rows = !pos;
+  }
+  // what is read, and what is written: the pages and the queries
+  Range read[12];
+  int n_read = 0;
+  for (const Range& r : in) read[n_read++] = r;
+  read[n_read++] = mem.table;
+  read[n_read++] = mem.len;
+  read[n_read++] = mem.fresh;
+  if (rope) read[n_read++] = range_of(pos, apart(pos_stride_b) * (B - 1) + (int64_t)rope->axes * N, 4);
+  for (const hack_rows* r : {q, k})
+    if (r) read[n_read++] = range_of(r->weight, r->weight_stride_h * (r->heads - 1) + ctx->cfg.head_dim, 4);
+  for (int i = 0; i < n_read; ++i) {
+    if (mem.k.meets(read[i]) || mem.v.meets(read[i])) return fail(ctx, HACK_EINVAL, "the cache shares memory with what is read");
+    if (q && out[0].meets(read[i]) && !(i == 0 && in_place(ctx, B, N, q)))
+      return fail(ctx, HACK_EINVAL, "the queries' output shares memory with what is read (in place: x in the layout of out, from the same address)");
+  }
+  if (q && (out[0].meets(mem.k) || out[0].meets(mem.v))) return fail(ctx, HACK_EINVAL, "the queries' output shares memory with the cache");
+  if ((st = check_device(ctx)) != HACK_OK) return st;
+  // v takes the launch shape of k
+  if (!q) std::swap(a.t[0], a.t[1]);
+  shape_rotation(ctx->cfg.head_dim, B, q ? 2 : 1, &a);
+  uint32_t k_groups = a.groups[1] - (q ? a.groups[0] : 0);
+  if (!q) {
+    std::swap(a.t[0], a.t[1]);
+    a.groups[0] = 0;
+  }
+  a.v.tokens_log2 = a.t[1].tokens_log2;
+  a.v.tiles = a.t[1].tiles;
+  const int64_t all = (int64_t)a.groups[1] + k_groups;
+  if (all * B > kMostGroups) return fail(ctx, HACK_ECAPACITY, "%lld work-groups are more than a launch takes", (long long)all * B);
+  a.all_groups = (uint32_t)all;
+  launch_append(static_cast<hipStream_t>(stream), ctx->elem_bytes, ctx->cfg.head_dim, !rope || rope->layout == HACK_ROPE_HALF, B, a);
+  HIP_TRY(ctx, hipGetLastError());
+  return HACK_OK;
+}
+
+extern "C" hack_status hack_attn_pages(hack_ctx* ctx, int32_t B, int32_t N, int32_t heads, const void* q, const hack_pages* cache, const int32_t* fresh,
+                                       int32_t causal, const hack_shared* shared, int32_t n_shared, float scale, void* out, hack_stream stream) {
+  hack_status st = check_common(ctx, B, N, true);
+  if (st != HACK_OK) return st;
+  const int H = ctx->cfg.heads, d = ctx->cfg.head_dim;
+  if (heads < 1 || heads % H != 0) return fail(ctx, HACK_EINVAL, "heads %d are no multiple of the context's %d", heads, H);
+  if (!q || !out) return fail(ctx, HACK_EINVAL, "q and out must not be NULL");
+  if (!aligned16(q) || !aligned16(out)) return fail(ctx, HACK_EINVAL, "q/out must be 16-byte aligned");
+  if (!scale_ok(scale)) return fail(ctx, HACK_EINVAL, "scale must be finite and > 0");
+  if (n_shared < 0 || (n_shared > 0 && !shared)) return fail(ctx, HACK_EINVAL, "shared is NULL or n_shared negative");
+  if (n_shared > kMostShared) return fail(ctx, HACK_ECAPACITY, "%d groups are more than %d", n_shared, kMostShared);
+  AttnPagesArgs a;
+  PageMemory mem;
+  if ((st = take_pages(ctx, B, N, cache, fresh, &a.c, &mem)) != HACK_OK) return st;
+  const int64_t GN = (int64_t)(heads / H) * N, rows = (int64_t)B * H * GN;
+  if (rows > ((int64_t)1 << 31) - 64) return fail(ctx, HACK_ECAPACITY, "%lld queries are more than a launch takes", (long long)rows);
+  const Range from = range_of(q, rows, (int64_t)d * ctx->elem_bytes), to = range_of(out, rows, (int64_t)d * ctx->elem_bytes);
+  for (const Range& r : {from, mem.k, mem.v, mem.table, mem.len, mem.fresh})
+    if (to.meets(r)) return fail(ctx, HACK_EINVAL, "out shares memory with what is read");
+  a.n_shared = 0;
+  for (int i = 0, end = 0; i < n_shared; ++i) {
+    const hack_shared& s = shared[i];
+    if (s.first < end || s.count < 1 || s.count > B - s.first || s.rows < 0 || s.rows > a.c.max_len)
+      return fail(ctx, HACK_EINVAL, "group %d: batch elements %d + %d outside [%d, %d) or %d rows outside [0, %d]", i, s.first, s.count, end, B, s.rows, a.c.max_len);
+    end = s.first + s.count;
+    if (s.count > 1 && s.rows > 0) a.shared[a.n_shared++] = Shared{s.first, s.count, s.rows};
+  }
+  if ((st = check_device(ctx)) != HACK_OK) return st;
+  a.q = q;
+  a.out = out;
+  a.part_o = ctx->part_o;
+  a.part_ml = ctx->part_ml;
+  a.plan = ctx->page_plan;
+  a.batch = B;
+  a.G = heads / H;
+  a.causal = causal != 0;
+  a.scale = scale;
+  a.least = 8;
+  const int queries = GN <= 16 ? 16 : 32;
+  const int64_t slots = ctx->part_rows / queries, units = (int64_t)B * H;
+  const auto blocks = [](int64_t rows) { return (rows + kKeys - 1) / kKeys; };
+  const int64_t cuts = (blocks(a.c.max_len) + 1 + a.least - 1) / a.least;   // chunks of an entry at most
+  const int64_t want = 3 * (int64_t)ctx->cus;
+  a.part[1].tiles = (int32_t)((GN + queries - 1) / queries);
+  a.part[0].tiles = 1;
+  int64_t items[2] = {0, units * a.part[1].tiles};
+  for (int i = 0; i < a.n_shared; ++i) {
+    a.part[0].tiles = std::max<int32_t>(a.part[0].tiles, (int32_t)((a.shared[i].count * GN + queries - 1) / queries));
+  }
+  items[0] = (int64_t)a.n_shared * H * a.part[0].tiles;
+  if (items[0] + items[1] > slots) a.n_shared = 0, items[0] = 0;   // the joined rows' partial results do not fit: every element reads all of its rows
+  const int64_t spare = std::min(want, (slots - items[0] - items[1]) / 2);   // each part may be cut into so many more
+  a.share = spare > 0 && cuts > 1 ? (float)spare : 0.f;
+  const int64_t more = a.share > 0 ? spare : 0;
+  a.part[0].pairs = a.n_shared ? (int32_t)std::min<int64_t>((more + items[0]) / a.part[0].tiles, (int64_t)a.n_shared * H * cuts) : 0;
+  a.part[1].pairs = (int32_t)std::min<int64_t>((more + items[1]) / a.part[1].tiles, units * cuts);
+  a.part[0].slot0 = 0;
+  a.part[1].slot0 = a.part[0].pairs * a.part[0].tiles;
+  if (pairs_grid(a.part[0].pairs, a.part[0].tiles) + pairs_grid(a.part[1].pairs, a.part[1].tiles) > kMostGroups)
+    return fail(ctx, HACK_ECAPACITY, "%lld queries are more than a launch takes", (long long)rows);
+  launch_attn_pages(static_cast<hipStream_t>(stream), ctx->elem_bytes, d, queries, a.share > 0 || a.n_shared > 0, a);
+  HIP_TRY(ctx, hipGetLastError());
+  return HACK_OK;
+}

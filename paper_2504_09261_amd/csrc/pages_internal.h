@@ -1,0 +1,79 @@
+// Internal declarations of the caches in pages: appending to them and attention over them (pages_api.cpp and the kernels behind it).  Nothing here is part
+// of the C ABI.  Tables and lengths are device memory that the host never reads; everything else travels by value.
+#pragma once
+
+#include "ops_internal.h"
+
+namespace hack {
+
+struct Pages {
+  uint8_t* k;
+  uint8_t* v;
+  int64_t stride_page, stride_row, stride_head;   // bytes
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* len;
+  const int32_t* fresh;    // NULL: n for all
+  int* fault;              // host-visible word that kernels raise
+  int32_t pages;
+  int32_t log2_rows;       // of a page
+  int32_t max_len;
+  int32_t heads;           // H
+  int32_t by_head;
+  int32_t n;               // N
+};
+
+// ---- appending --------------------------------------------------------------
+// t[0]: q (no work-groups where there are none), t[1]: k, v beside them.
+struct AppendArgs : RotateArgs {
+  RotateTensor v;
+  uint32_t all_groups;   // work-groups of a batch element
+  int32_t own_rows;      // positions are the rows' numbers in the cache
+  Pages c;
+};
+void launch_append(hipStream_t s, int elem_bytes, int head_dim, bool half_layout, int batch, AppendArgs a);
+
+// ---- attention --------------------------------------------------------------
+constexpr int kMostShared = 256;   // groups of a call
+constexpr int kKeys = 32;          // of a block, in which work is counted and cut
+struct Shared {
+  int32_t first, count, rows;
+};
+// The shared rows of groups (0) and the rows that every batch element, or head of it, has alone (1).
+struct AttnPart {
+  int32_t tiles;      // of an entry's queries
+  int32_t pairs;      // (entry, head, chunk) at most
+  int32_t slot0;      // first slot of its partial results
+};
+struct AttnPagesHead {
+  Pages c;
+  const void* q;
+  void* out;
+  float* part_o;      // [slot, queries of a tile, head_dim] unnormalised partial outputs
+  float* part_ml;     // [slot, queries of a tile, 2] their references and normalisers
+  int2* plan;         // [groups, then batch elements or units]: first pair and chunks of an entry
+  AttnPart part[2];
+  int32_t batch;
+  int32_t G;          // query heads of a cache
+  int32_t n_shared;
+  int32_t causal;
+  float scale;
+  int32_t least;      // blocks of a chunk at least
+  float share;        // work-groups that all blocks are cut for; 0: no cuts
+};
+struct AttnPagesArgs : AttnPagesHead {
+  Shared shared[kMostShared];
+};
+// How the kernels cut: blocks that hold rows lo to hi, blocks of a chunk where all entries have `total` (times heads and tiles of queries), chunks of an entry.
+__host__ __device__ inline int blocks_between(int lo, int hi) { return hi > lo ? (hi + kKeys - 1) / kKeys - lo / kKeys : 0; }
+__host__ __device__ inline int chunk_blocks(float total, float share, int least) {
+  const float each = share > 0.f ? total / share : 1e9f;
+  const int whole = (int)(each < 1e9f ? each : 1e9f);
+  return whole < least ? least : whole + 1;
+}
+__host__ __device__ inline int entry_chunks(int blocks, int chunk) { return blocks > chunk ? chunks_of(blocks, chunk) : 1; }
+constexpr int64_t pairs_grid(int64_t pairs, int64_t tiles) { return (pairs + 7) / 8 * 8 * tiles; }
+// queries: of a tile.  merge: partial results may have to be joined.
+void launch_attn_pages(hipStream_t s, int elem_bytes, int head_dim, int queries, bool merge, const AttnPagesArgs& a);
+
+}  // namespace hack

@@ -162,14 +162,14 @@ bool arity(Py_ssize_t n, Py_ssize_t want) {
   return false;
 }
 
-// One operand of a rotation: x [B, heads, N, head_dim] in any strides with the head's elements side by side, out contiguous.
+// One operand of a rotation: x [B, heads, N, head_dim] in any strides with the head's elements side by side, out contiguous (a null pointer: none).
 bool read_operand(PyObject* x, PyObject* out, PyObject* weight, const Info& info, hack_rows* r, int64_t* B, int64_t* N) {
   View a, o, w;
-  if (!read_tensor(x, info, info.type, true, &a) || !read_tensor(out, info, info.type, false, &o)) return false;
+  if (!read_tensor(x, info, info.type, true, &a) || (out && !read_tensor(out, info, info.type, false, &o))) return false;
   if (a.dim != 4 || a.shape[3] != info.head_dim || a.stride[3] != 1) return refuse("rows: [B, heads, N, head_dim], head_dim side by side");
-  if (!o.is(a.shape[0], a.shape[1], a.shape[2], a.shape[3])) return refuse("out: the shape of x");
+  if (out && !o.is(a.shape[0], a.shape[1], a.shape[2], a.shape[3])) return refuse("out: the shape of x");
   if (a.shape[1] > INT32_MAX || a.shape[0] > INT32_MAX || a.shape[2] > INT32_MAX) return refuse("rows: too many of them");
-  *r = hack_rows{a.p, o.p, (int32_t)a.shape[1], 0, 0, 0, nullptr, 0};
+  *r = hack_rows{a.p, out ? o.p : nullptr, (int32_t)a.shape[1], 0, 0, 0, nullptr, 0};
   // a dimension of one element may have any stride
   if (a.shape[0] > 1) r->stride_b = a.stride[0];
   if (a.shape[1] > 1) r->stride_h = a.stride[1];
@@ -183,6 +183,21 @@ bool read_operand(PyObject* x, PyObject* out, PyObject* weight, const Info& info
   }
   *B = a.shape[0];
   *N = a.shape[2];
+  return true;
+}
+
+// Positions [axes, N], the same for all batch elements, or [B, axes, N]; with one axis also [N]; None: NULL.
+bool read_positions(PyObject* t, const Info& info, int64_t B, long axes, int64_t N, const int32_t** pos, int64_t* stride) {
+  *pos = nullptr;
+  *stride = 0;
+  if (t == Py_None) return true;
+  View p;
+  if (!read_tensor(t, info, info.i32, false, &p)) return false;
+  const bool each = p.dim == 3 && p.shape[0] == B && p.shape[1] == axes && p.shape[2] == N;
+  if (!each && !(p.dim == 2 && p.shape[0] == axes && p.shape[1] == N) && !(p.dim == 1 && axes == 1 && p.shape[0] == N))
+    return refuse("positions: [axes, N] or [B, axes, N]");
+  *pos = static_cast<const int32_t*>(p.p);
+  if (each) *stride = axes * N;
   return true;
 }
 
@@ -208,19 +223,9 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
       return nullptr;
     }
   }
-  const int32_t* pos = nullptr;
-  int64_t stride = 0;
-  if (rope && a[13] != Py_None) {   // [axes, N], the same for all batch elements, or [B, axes, N]; with one axis also [N]
-    View p;
-    if (!read_tensor(a[13], info, info.i32, false, &p)) return nullptr;
-    const bool each = p.dim == 3 && p.shape[0] == B && p.shape[1] == axes && p.shape[2] == N;
-    if (!each && !(p.dim == 2 && p.shape[0] == axes && p.shape[1] == N) && !(p.dim == 1 && axes == 1 && p.shape[0] == N)) {
-      refuse("positions: [axes, N] or [B, axes, N]");
-      return nullptr;
-    }
-    pos = static_cast<const int32_t*>(p.p);
-    stride = each ? axes * N : 0;
-  }
+  const int32_t* pos;
+  int64_t stride;
+  if (!read_positions(rope ? a[13] : Py_None, info, B, axes, N, &pos, &stride)) return nullptr;
   int status;
   Py_BEGIN_ALLOW_THREADS
   if (norm < 0)
@@ -361,8 +366,118 @@ PyObject* attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
+// ---- caches in pages ----
+// A PagedCache's structure, (address, device, element type, head_dim, heads of a page, rows of the table).  Tables go by head where a page holds
+// one and the context has more.
+bool read_pages(PyObject* t, const Info& info, int64_t B, hack_pages* c) {
+  if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 6) return refuse("cache is a PagedCache");
+  const void* p = PyLong_AsVoidPtr(PyTuple_GET_ITEM(t, 0));
+  const long device = PyLong_AsLong(PyTuple_GET_ITEM(t, 1)), head_dim = PyLong_AsLong(PyTuple_GET_ITEM(t, 3)), heads = PyLong_AsLong(PyTuple_GET_ITEM(t, 4));
+  const int64_t rows = PyLong_AsLongLong(PyTuple_GET_ITEM(t, 5));
+  if (PyErr_Occurred()) return false;
+  if (device != info.device) return refuse("device tensors must lie on the context's device");
+  if (PyTuple_GET_ITEM(t, 2) != info.type || head_dim != info.head_dim) return refuse("a cache has another element type or head_dim");
+  *c = *static_cast<const hack_pages*>(p);
+  if (heads != info.heads && heads != 1) return refuse("pages hold the rows of the context's heads, or of one head");
+  c->by_head = heads != info.heads;
+  if (rows != (c->by_head ? B * info.heads : B)) return refuse("a cache has a table and a length for every batch element, or, a head to a page, for every head of it");
+  return true;
+}
+bool read_fresh(PyObject* t, const Info& info, int64_t B, const int32_t** p) {
+  *p = nullptr;
+  if (t == Py_None) return true;
+  View v;
+  if (!read_tensor(t, info, info.i32, false, &v)) return false;
+  if (v.dim != 1 || v.shape[0] != B) return refuse("fresh: a number for every batch element");
+  *p = static_cast<const int32_t*>(v.p);
+  return true;
+}
+
+// append(fn, ctx, info, q, q_out, q_weight, k, k_weight, v, norm, eps, rope, axes, pos, fresh, cache, stream) -> status
+PyObject* append_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arity(n, 17)) return nullptr;
+  Info info;
+  if (!read_info(a[2], &info)) return nullptr;
+  void *fn = address(a[0]), *ctx = address(a[1]), *rope = address(a[11]), *stream = address(a[16]);
+  const long norm = PyLong_AsLong(a[9]), axes = PyLong_AsLong(a[12]);
+  const double eps = PyFloat_AsDouble(a[10]);
+  if (PyErr_Occurred()) return nullptr;
+  hack_rows q, k, v;
+  int64_t B, N, B2, N2;
+  if (!read_operand(a[6], nullptr, a[7], info, &k, &B, &N) || !read_operand(a[8], nullptr, Py_None, info, &v, &B2, &N2)) return nullptr;
+  bool same = B2 == B && N2 == N;
+  const bool queries = a[3] != Py_None;
+  if (queries) {
+    if (!read_operand(a[3], a[4], a[5], info, &q, &B2, &N2)) return nullptr;
+    same &= B2 == B && N2 == N;
+  }
+  if (!same) {
+    refuse("q, k and v: the same batch and rows");
+    return nullptr;
+  }
+  const int32_t *pos, *fresh;
+  int64_t stride;
+  hack_pages cache;
+  if (!read_positions(rope ? a[13] : Py_None, info, B, axes, N, &pos, &stride) || !read_fresh(a[14], info, B, &fresh) || !read_pages(a[15], info, B, &cache)) return nullptr;
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = reinterpret_cast<decltype(&hack_append_pages)>(fn)((hack_ctx*)ctx, (int32_t)B, (int32_t)N, queries ? &q : nullptr, &k, &v, (int32_t)norm, (float)eps,
+                                                             (const hack_rope*)rope, pos, stride, fresh, &cache, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// attn_pages(fn, ctx, info, q, cache, fresh, causal, shared, scale, out, stream) -> status
+PyObject* attn_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arity(n, 11)) return nullptr;
+  Info info;
+  if (!read_info(a[2], &info)) return nullptr;
+  void *fn = address(a[0]), *ctx = address(a[1]), *stream = address(a[10]);
+  const int causal = PyObject_IsTrue(a[6]);
+  const double scale = PyFloat_AsDouble(a[8]);
+  if (causal < 0 || PyErr_Occurred()) return nullptr;
+  View q, out;
+  if (!read_tensor(a[3], info, info.type, false, &q) || !read_tensor(a[9], info, info.type, false, &out)) return nullptr;
+  if (q.dim != 4 || q.shape[3] != info.head_dim || q.shape[1] % info.heads != 0 || !out.is(q.shape[0], q.shape[1], q.shape[2], q.shape[3])) {
+    refuse("q and out: [B, G heads, N, head_dim]");
+    return nullptr;
+  }
+  if (q.shape[0] > INT32_MAX || q.shape[1] > INT32_MAX || q.shape[2] > INT32_MAX) {
+    refuse("q: too many rows");
+    return nullptr;
+  }
+  const int32_t* fresh;
+  hack_pages cache;
+  if (!read_fresh(a[5], info, q.shape[0], &fresh) || !read_pages(a[4], info, q.shape[0], &cache)) return nullptr;
+  constexpr Py_ssize_t kMost = 256;
+  hack_shared groups[kMost];
+  Py_ssize_t n_groups = 0;
+  if (a[7] != Py_None) {
+    PyObject* f = PySequence_Fast(a[7], "shared: a list of (first, count, rows)");
+    if (!f) return nullptr;
+    n_groups = PySequence_Fast_GET_SIZE(f);
+    bool ok = n_groups <= kMost || refuse("shared: too many groups");
+    for (Py_ssize_t i = 0; ok && i < n_groups; ++i) {
+      PyObject* g = PySequence_Fast(PySequence_Fast_GET_ITEM(f, i), "shared: a list of (first, count, rows)");
+      ok = g && (PySequence_Fast_GET_SIZE(g) == 3 || refuse("shared: a list of (first, count, rows)"));
+      if (ok)
+        ok = int32_arg(PySequence_Fast_GET_ITEM(g, 0), &groups[i].first) && int32_arg(PySequence_Fast_GET_ITEM(g, 1), &groups[i].count) &&
+             int32_arg(PySequence_Fast_GET_ITEM(g, 2), &groups[i].rows);
+      Py_XDECREF(g);
+    }
+    Py_DECREF(f);
+    if (!ok) return nullptr;
+  }
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = reinterpret_cast<decltype(&hack_attn_pages)>(fn)((hack_ctx*)ctx, (int32_t)q.shape[0], (int32_t)q.shape[2], (int32_t)q.shape[1], q.p, &cache, fresh, causal,
+                                                           groups, (int32_t)n_groups, (float)scale, out.p, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
 #define ENTRY(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ENTRY(rotate), ENTRY(pack), ENTRY(unpack), ENTRY(attn), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {ENTRY(rotate), ENTRY(pack), ENTRY(unpack), ENTRY(attn), ENTRY(append_pages), ENTRY(attn_pages), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
