@@ -15,7 +15,7 @@ STEP_CALL_PATH = os.path.join(HERE, "_step_call.so")   # CPython entry to hack_s
 OPS_CALL_PATH = os.path.join(HERE, "_ops_call.so")     # CPython entries to the operators around the cache
 SOURCES = ["hack_api.cpp", "kernels_move.hip", "kernels_select.hip", "kernels_score.hip", "kernels_attn.hip", "kernels_attn_split.hip", "kernels_attn_f32.hip", "kernels_step.hip",
            "kernels_headvar.hip", "kernels_merge.hip", "ops_api.cpp", "kernels_rotate.hip", "kernels_packed.hip", "kernels_attn_packed.hip", "kernels_attn_packed_tiles.hip",
-           "pages_api.cpp", "kernels_pages.hip", "kernels_attn_pages.hip"]
+           "pages_api.cpp", "kernels_pages.hip", "kernels_attn_pages.hip", "kernels_attn_pages_tiles.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms are switched off for all device code.
@@ -32,6 +32,7 @@ DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang"
 # registers (a launch of 568 us takes 8840).
 PER_SOURCE = {"kernels_attn.hip": ["-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"],
               "kernels_attn_packed_tiles.hip": ["-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"],
+              "kernels_attn_pages_tiles.hip": ["-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"],
               "kernels_step.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
               "kernels_score.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-mllvm", "-amdgpu-atomic-optimizer-strategy=None"]}
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-unknown-warning-option", "-Wno-inline-asm",

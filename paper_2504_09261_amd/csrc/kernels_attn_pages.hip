@@ -12,89 +12,13 @@
 #include <cfloat>
 #include <type_traits>
 
-#include "pages_device.h"
+#include "attn_pages_device.h"
 
 namespace hack {
 
 namespace {
 
 using namespace dev;
-
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
-
-// ---- which work a work-group has ---------------------------------------------
-struct Work {
-  int entry, base, chunks, local;   // base: first pair of the entry; local: pair within it
-};
-__device__ __forceinline__ int group_of(const AttnPagesArgs& a, int b) {   // whose shared rows batch element b has; -1: none
-  int lo = 0, hi = a.n_shared;
-  while (lo < hi) {   // the first group behind b
-    const int mid = (lo + hi) >> 1;
-    if (a.shared[mid].first <= b) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo > 0 && b < a.shared[lo - 1].first + a.shared[lo - 1].count ? lo - 1 : -1;
-}
-__device__ __forceinline__ int shared_rows(const AttnPagesArgs& a, int g) { return g < 0 ? 0 : min(a.shared[g].rows, a.c.max_len); }
-// Blocks of an entry, and its heads.
-__device__ __forceinline__ int entry_blocks(const AttnPagesArgs& a, int part, int e) {
-  if (part == 0) return blocks_between(0, shared_rows(a, e));
-  return blocks_between(shared_rows(a, group_of(a, a.c.by_head ? e / a.c.heads : e)), rows_of(a.c, e));
-}
-__device__ __forceinline__ int entries_of(const AttnPagesArgs& a, int part) { return part == 0 ? a.n_shared : a.c.by_head ? a.batch * a.c.heads : a.batch; }
-__device__ __forceinline__ int entry_heads(const AttnPagesArgs& a, int part) { return part == 1 && a.c.by_head ? 1 : a.c.heads; }
-
-__device__ __forceinline__ bool find_work(const AttnPagesArgs& a, int part, int pair, Work& w) {
-  __shared__ float total_sh[kWaves];
-  __shared__ int scan_sh[kWaves];
-  __shared__ Work work_sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float sum = 0.f;
-  if (a.share > 0.f) {
-    for (int p = 0; p < 2; ++p) {
-      const float each = (float)entry_heads(a, p) * a.part[p].tiles;
-      for (int e = tid; e < entries_of(a, p); e += kThreads) sum += each * entry_blocks(a, p, e);
-    }
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x, 64);
-    if (lane == 0) total_sh[wave] = sum;
-    __syncthreads();
-    sum = total_sh[0] + total_sh[1] + total_sh[2] + total_sh[3];
-  }
-  const int chunk = chunk_blocks(sum, a.share, a.least);
-  const int n = entries_of(a, part), heads = entry_heads(a, part);
-  if (tid == 0) work_sh.entry = -1;
-  int carry = 0;
-  for (int e0 = 0; e0 < n && carry <= pair; e0 += kThreads) {
-    const int e = e0 + tid;
-    const int chunks = e < n ? entry_chunks(entry_blocks(a, part, e), chunk) : 0;
-    int incl = chunks * heads;
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) {
-      const int y = __shfl_up(incl, x, 64);
-      if (lane >= x) incl += y;
-    }
-    __syncthreads();   // the sums of the round before have been read
-    if (lane == 63) scan_sh[wave] = incl;
-    __syncthreads();
-    int all = 0, before = 0;
-#pragma unroll
-    for (int x = 0; x < kWaves; ++x) {
-      if (x < wave) before += scan_sh[x];
-      all += scan_sh[x];
-    }
-    const int base = carry + before + incl - chunks * heads;
-    if (pair >= base && pair < base + chunks * heads) work_sh = Work{e, base, chunks, pair - base};
-    carry += all;
-  }
-  __syncthreads();
-  w = work_sh;
-  w.entry = __builtin_amdgcn_readfirstlane(w.entry);
-  w.base = __builtin_amdgcn_readfirstlane(w.base);
-  w.chunks = __builtin_amdgcn_readfirstlane(w.chunks);
-  w.local = __builtin_amdgcn_readfirstlane(w.local);
-  return w.entry >= 0;
-}
 
 // ---- rows in registers ---------------------------------------------------------
 template <typename T, int D> struct Rows;
@@ -190,7 +114,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_pages(const AttnPagesArgs a)
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int MT = D / 16, QROWS = 16 * NQ, SIDE = kBf16 ? MT : 4;   // head-dims of a lane that lie side by side
   const Pages& c = a.c;
-  const int grid0 = (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles;
+  const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0;
   const int part = (int)blockIdx.x >= grid0 ? 1 : 0, id = blockIdx.x - (part ? grid0 : 0), tiles = a.part[part].tiles;
   // The tiles of an entry, head and chunk follow each other on an XCD (work-group id mod 8).
   const int along = id >> 3, pair = (along / tiles) * 8 + (id & 7), tile = along % tiles;
@@ -252,8 +176,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_pages(const AttnPagesArgs a)
   const int first = (begin + chunk_at(n_blocks, work.chunks, chunk)) * PER, last = (begin + chunk_at(n_blocks, work.chunks, chunk + 1)) * PER;
   const ConstInts table = as_const(c.table) + entry0 * c.table_stride;
   const int in_page = (1 << c.log2_rows) - 1;
-  // Tiles of 16 rows lie in one page.  Tiles behind the last row that is seen are the last one again (their scores are masked).
-  const auto tile_row = [&](int blk, int t) { return min(blk * R::kRows + 16 * t, (most - 1) & ~15); };
+  // Tiles of 16 rows lie in one page.  Tiles behind the last row that is seen, or in front of the first one, are the nearest again (their scores are masked).
+  const auto tile_row = [&](int blk, int t) { return max(min(blk * R::kRows + 16 * t, (most - 1) & ~15), lo & ~15); };
   const auto pages_of = [&](int blk, int (&p)[R::kTiles]) {
 #pragma unroll
     for (int t = 0; t < R::kTiles; ++t) p[t] = table[tile_row(blk, t) >> c.log2_rows];
@@ -475,7 +399,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_pages(const AttnPagesArgs a)
   }
   __syncthreads();
   const bool whole = part == 1 && work.chunks == 1 && group < 0;
-  const int64_t slot = (int64_t)a.part[part].slot0 + (int64_t)pair * tiles + tile;
+  const int64_t slot = (int64_t)pair * tiles + tile;
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
     float M = -FLT_MAX;
@@ -503,7 +427,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_pages(const AttnPagesArgs a)
     }
     if (row[qt] < 0) continue;
     const float inv = sees[qt] > 0 ? 1.f / L : 0.f;
-    const int64_t prow = slot * QROWS + 16 * qt + col;
+    const int64_t prow = a.part[part].row0 + slot * QROWS + 16 * qt + col;
 #pragma unroll
     for (int mt = 0; mt < MT; mt += SIDE) {
       const int d = R::dim(mt, 4 * g + w);
@@ -516,7 +440,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_pages(const AttnPagesArgs a)
 
 // Rows with partial results: ROWS of them a work-group, each by 256 / ROWS threads, D / 4 lanes a slot, which walk over its slots.
 template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a, int q_rows) {
+__global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a) {
   constexpr int LPR = D / 4, SIDE = 256 / LPR / ROWS;   // slots of a row at a time
   const Pages& c = a.c;
   const int tid = threadIdx.x, lane = tid % LPR, side = tid / LPR % SIDE;
@@ -534,10 +458,10 @@ __global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a, i
   mine = mine && n < fresh && (group >= 0 || own.y > 1);
   const int slots = mine ? common.y + own.y : 0;
   const int64_t j = group >= 0 ? (int64_t)(b - a.shared[group].first) * GN + r : 0;   // the row among its group's
-  const int64_t at0 = ((int64_t)a.part[0].slot0 + ((int64_t)common.x + h) * a.part[0].tiles + j / q_rows) * q_rows + j % q_rows;
-  const int64_t step0 = (int64_t)c.heads * a.part[0].tiles * q_rows;
-  const int64_t at1 = ((int64_t)a.part[1].slot0 + ((int64_t)own.x + (c.by_head ? 0 : h)) * a.part[1].tiles + r / q_rows) * q_rows + r % q_rows;
-  const int64_t step1 = (int64_t)(c.by_head ? 1 : c.heads) * a.part[1].tiles * q_rows;
+  // a part's slots are tiles of whole rows, one tile behind the other: query x of an entry is row x of its pair
+  const int64_t rows0 = (int64_t)a.part[0].tiles * a.part[0].queries, rows1 = (int64_t)a.part[1].tiles * a.part[1].queries;
+  const int64_t at0 = a.part[0].row0 + ((int64_t)common.x + h) * rows0 + j, step0 = c.heads * rows0;
+  const int64_t at1 = a.part[1].row0 + ((int64_t)own.x + (c.by_head ? 0 : h)) * rows1 + r, step1 = (c.by_head ? 1 : c.heads) * rows1;
   const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
   const float4* const po = reinterpret_cast<const float4*>(a.part_o) + lane;
   float M = -FLT_MAX, L = 0.f;
@@ -606,26 +530,35 @@ __global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a, i
 }
 
 template <typename T, int D>
-void launch_some(hipStream_t s, int queries, bool merge, const AttnPagesArgs& a) {
-  const dim3 grid((unsigned)(pairs_grid(a.part[0].pairs, a.part[0].tiles) + pairs_grid(a.part[1].pairs, a.part[1].tiles)));
-  if (queries == 16) hipLaunchKernelGGL((attn_pages<T, D, 1>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((attn_pages<T, D, 2>), grid, dim3(kThreads), 0, s, a);
+void launch_some(hipStream_t s, bool merge, AttnPagesArgs& a) {
+  // parts of equal tiles go together
+  const int both = a.n_shared > 0 ? 3 : 2;
+  for (int left = both; left != 0; left &= ~a.parts) {
+    const int queries = a.part[left & 1 ? 0 : 1].queries;
+    a.parts = 0;
+    for (int p = 0; p < 2; ++p)
+      if ((left >> p & 1) && a.part[p].queries == queries) a.parts |= 1 << p;
+    const dim3 grid((unsigned)(part_grid(a, 0) + part_grid(a, 1)));
+    if (queries == 16) hipLaunchKernelGGL((attn_pages<T, D, 1>), grid, dim3(kThreads), 0, s, a);
+    else if (queries == 32) hipLaunchKernelGGL((attn_pages<T, D, 2>), grid, dim3(kThreads), 0, s, a);
+    else launch_attn_pages_tiles(s, D, a);
+  }
   if (!merge) return;
   const int64_t rows = (int64_t)a.batch * a.c.heads * a.G * a.c.n;
   constexpr int kRows = 1024 / D;
-  if (rows >= 4096) hipLaunchKernelGGL((attn_pages_merge<T, D, kRows>), dim3((unsigned)((rows + kRows - 1) / kRows)), dim3(256), 0, s, a, queries);
-  else hipLaunchKernelGGL((attn_pages_merge<T, D, 1>), dim3((unsigned)rows), dim3(256), 0, s, a, queries);
+  if (rows >= 4096) hipLaunchKernelGGL((attn_pages_merge<T, D, kRows>), dim3((unsigned)((rows + kRows - 1) / kRows)), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attn_pages_merge<T, D, 1>), dim3((unsigned)rows), dim3(256), 0, s, a);
 }
 
 }  // namespace
 
-void launch_attn_pages(hipStream_t s, int elem_bytes, int head_dim, int queries, bool merge, const AttnPagesArgs& a) {
+void launch_attn_pages(hipStream_t s, int elem_bytes, int head_dim, bool merge, AttnPagesArgs a) {
   if (elem_bytes == 4) {
-    if (head_dim == 64) launch_some<float, 64>(s, queries, merge, a);
-    else launch_some<float, 128>(s, queries, merge, a);
+    if (head_dim == 64) launch_some<float, 64>(s, merge, a);
+    else launch_some<float, 128>(s, merge, a);
   } else {
-    if (head_dim == 64) launch_some<__bf16, 64>(s, queries, merge, a);
-    else launch_some<__bf16, 128>(s, queries, merge, a);
+    if (head_dim == 64) launch_some<__bf16, 64>(s, merge, a);
+    else launch_some<__bf16, 128>(s, merge, a);
   }
 }
 

@@ -1,0 +1,536 @@
+// Attention over caches in pages for many queries, bf16: work items of 128 queries, four waves of 32, which share every block of 32 keys through LDS (few
+// queries, float32 contexts and the merge of partial results: kernels_attn_pages.hip).
+//
+// The stage is that of the 128-query kernel over contiguous rows: scores of block j + 1, probabilities of block j and PV product of block j - 1 side by
+// side, in slots of one matrix instruction, an LDS read and a share of the vector work.  What pages add: a copy instruction takes rows of one
+// 16-row tile, which lie in one page, so it has a base of its own, from an entry of the table that is read a stage ahead out of LDS, where a work-group
+// brings its part of the table first.  Blocks with rows that some query of the item does not see (the last ones, causal; a first one that
+// begins inside the shared rows) come first, their scores are masked, and rows that nobody sees are not copied: the nearest row that is seen stands in for them.
+// A masked row's probability is zero, which keeps it out of the sums unless its value is an infinity or NaN: an item whose results are no numbers, or
+// that met a page that is none, does these queries again row by row, and numbers among their results stand.
+#include <type_traits>
+
+#include "attn_pages_device.h"
+
+namespace hack {
+
+namespace {
+
+using namespace dev;
+
+constexpr int kNW = 4;            // waves
+constexpr int kNS = 4;            // LDS slots per tensor
+constexpr int kTableEntries = 2048;   // of a work-group's part of the table that LDS holds
+constexpr float kHeadroom = 15.f; // the reference lies 2^15 above the running maximum: the exponent's top bit says that a probability reached 2
+
+template <int I, int N, typename F>
+__device__ __forceinline__ void for_each(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    for_each<I + 1, N>(f);
+  }
+}
+
+// Vector work of a stage in the order of issue: 16 scores a lane become probabilities, dependent operations two elements apart.
+struct Step {
+  int kind, index;   // 0 multiply-add, 1 exponential, 2 conversion of elements index and index + 1
+};
+constexpr int kSteps = 40, kStepCycles = 16 * 4 + 16 * 8 + 8 * 4;
+constexpr Step softmax_step(int t) {
+  int n = 0;
+  for (int j = -2; j < 18; ++j) {
+    if (j >= 0 && j < 16 && n++ == t) return Step{1, j};
+    if (j + 2 < 16 && n++ == t) return Step{0, j + 2};
+    if (j >= 2 && j % 2 == 0 && n++ == t) return Step{2, j - 2};
+  }
+  return Step{-1, 0};
+}
+constexpr int steps_before(int s, int slots) {   // in front of slot s
+  if (s >= slots) return kSteps;
+  int c = 0, t = 0;
+  while (t < kSteps) {
+    c += softmax_step(t).kind == 1 ? 8 : 4;
+    if (c * slots > kStepCycles * s) break;
+    ++t;
+  }
+  return t;
+}
+
+__device__ __forceinline__ const void* uniform(const void* p) {
+  const uint64_t x = (uint64_t)(uintptr_t)p;
+  const uint64_t lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)x), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (const void*)(uintptr_t)(hi << 32 | lo);
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesArgs a) {
+  constexpr int KC = D / 32;        // MFMA steps over head_dim for S^T
+  constexpr int MT = D / 16;        // 16-row tiles of O^T
+  constexpr int IPW = D / 64;       // copy instructions per wave, block and tensor
+  constexpr int BLK = kKeys * D;    // elements per block and tensor
+  constexpr int QROWS = kPageTileQueries;
+  const Pages& c = a.c;
+  const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0;
+  const int part = (int)blockIdx.x >= grid0 ? 1 : 0, id = blockIdx.x - (part ? grid0 : 0), tiles = a.part[part].tiles;
+  // The tiles of an entry, head and chunk follow each other on an XCD (work-group id mod 8), the last ones, which see the most rows, first.
+  const int along = id >> 3, pair = (along / tiles) * 8 + (id & 7), tile = tiles - 1 - along % tiles;
+  Work work;
+  if (!find_work(a, part, pair, work)) return;
+  const int heads = entry_heads(a, part), chunk = work.local / heads;
+  if (work.local == 0 && tile == 0 && threadIdx.x == 0) a.plan[(part ? a.n_shared : 0) + work.entry] = make_int2(work.base, work.chunks);
+  const int b0 = part == 0 ? a.shared[work.entry].first : c.by_head ? work.entry / c.heads : work.entry;
+  const int h = part == 1 && c.by_head ? work.entry % c.heads : work.local % heads;
+  const int group = part == 0 ? work.entry : group_of(a, b0), common = shared_rows(a, group);
+  const int entry0 = c.by_head ? b0 * c.heads + h : b0;     // of the table
+  const int lo = part ? common : 0;
+  const int GN = a.G * c.n, n_rows = part ? GN : a.shared[work.entry].count * GN;
+  if (tile * QROWS >= n_rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  __shared__ __attribute__((aligned(1024))) __bf16 Ks[kNS][BLK];
+  __shared__ __attribute__((aligned(1024))) __bf16 Vs[kNS][BLK];
+  __shared__ int table_sh[kTableEntries];
+  __shared__ int most_sh[kNW], fewest_sh[kNW], bad_sh;
+
+  // ---- queries and the rows that they see ----
+  struct Query {
+    int64_t row;    // of q and out
+    int sees;
+    bool there;
+  };
+  const auto query = [&](int x) {
+    const int j = tile * QROWS + x, jj = min(j, n_rows - 1), m = jj / GN, r = jj - m * GN, n = r % c.n, b = b0 + m;
+    const int fresh = fresh_of(c, b), len = rows_of(c, c.by_head ? b * c.heads + h : b);
+    Query q{((int64_t)b * c.heads + h) * GN + r, max(0, a.causal ? len - fresh + n + 1 : len), j < n_rows && n < fresh};
+    if (part == 0) q.sees = min(q.sees, common);
+    if (!q.there) q.sees = 0;
+    return q;
+  };
+  int sees[2];
+  int most = 0, fewest = c.max_len;
+  const __bf16* qrow[2];
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const Query q = query(w * 32 + 16 * qt + col);
+    sees[qt] = q.sees;
+    if (q.there) {
+      most = max(most, q.sees);
+      fewest = min(fewest, q.sees);
+    }
+    qrow[qt] = static_cast<const __bf16*>(a.q) + q.row * D + 8 * g;
+  }
+#pragma unroll
+  for (int x = 1; x < 16; x *= 2) {
+    most = max(most, __shfl_xor(most, x, 64));
+    fewest = min(fewest, __shfl_xor(fewest, x, 64));
+  }
+  if (lane == 0) {
+    most_sh[w] = most;
+    fewest_sh[w] = fewest;
+  }
+  if (tid == 0) bad_sh = 0;
+  __syncthreads();
+  most = __builtin_amdgcn_readfirstlane(max(max(most_sh[0], most_sh[1]), max(most_sh[2], most_sh[3])));
+  fewest = __builtin_amdgcn_readfirstlane(min(min(fewest_sh[0], fewest_sh[1]), min(fewest_sh[2], fewest_sh[3])));
+
+  // ---- blocks of this chunk: [first, first + n_blocks), taken in the order of block_of ----
+  const int all = blocks_between(lo, most), begin = lo / kKeys;
+  const int first = begin + chunk_at(all, work.chunks, chunk), n_blocks = begin + chunk_at(all, work.chunks, chunk + 1) - first;
+  const int end = first + n_blocks;
+  const int full_end = max(first, min(end, fewest / kKeys));      // blocks from here on have rows that some query does not see
+  const int n_tail = end - full_end, n_head = first < full_end && first * kKeys < lo ? 1 : 0, n_masked = n_tail + n_head;
+  const auto block_of = [&](int j) { return j < n_tail ? end - 1 - j : j < n_masked ? first : first + j - n_tail; };
+
+  floatx4 o[MT][2];        // O^T: head-dim 16mt + 4g + r, query 16qt + col
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) o[mt][0] = o[mt][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+  floatx4 ls[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};   // row sums of P (equal in all four rows)
+  float mc[2] = {-FLT_MAX, -FLT_MAX};   // probabilities are 2^(c2 s - mc); finite from the start, so that keys whose score is -inf get 0
+
+  if (n_blocks > 0) {
+    // ---- the part of the table that these blocks need ----
+    const int row_lo = lo & ~15, row_hi = (most - 1) & ~15;   // first rows of the tiles that hold rows somebody sees
+    const int first_page = max(first * kKeys, row_lo) >> c.log2_rows, n_pages = (min(end * kKeys - 1, row_hi) >> c.log2_rows) - first_page + 1;
+    const int32_t* const table = c.table + entry0 * c.table_stride + first_page;
+    const bool in_lds = n_pages <= kTableEntries;
+    if (in_lds) {
+      bool bad = false;
+      for (int i = tid; i < n_pages; i += 64 * kNW) {
+        int p = table[i];
+        if ((unsigned)p >= (unsigned)c.pages) {
+          bad = true;
+          p = 0;
+        }
+        table_sh[i] = p;
+      }
+      if (bad) {
+        report(c);
+        bad_sh = 1;
+      }
+    }
+    __syncthreads();
+
+    // LDS layout of a block: rows in groups of four, a group's 64-byte pieces row after row (piece x of row r at (r / 4) 8D + 256 x + 64 (r % 4)), the 16-byte
+    // chunks of a piece permuted by the group: chunk y holds y ^ (group & 3) in K and y ^ 2 (group & 1) in V.  A copy instruction fills 1 KiB:
+    // one group of rows at head_dim 128, two at 64; instruction i of a wave takes rows of tile i (128), or of tile w / 2 (64).
+    constexpr int GPI = 2 / IPW;
+    const int group_row = (GPI == 1 ? 4 * w : 4 * ((2 * w + (lane >> 5)) & 3)) + ((lane >> 2) & 3);   // row of this lane's piece within its tile
+    const int cg = GPI == 1 ? w : 2 * w + (lane >> 5), piece = 4 * ((lane >> 4) & (KC - 1));
+    const unsigned k_chunk = (piece + ((lane & 3) ^ (cg & 3))) * 16, v_chunk = (piece + ((lane & 3) ^ (2 * (cg & 1)))) * 16;
+    const unsigned k_src = group_row * (unsigned)c.stride_row + k_chunk, v_src = group_row * (unsigned)c.stride_row + v_chunk;
+    const unsigned ks_lds = lds_addr_of(&Ks[0][0]), vs_lds = lds_addr_of(&Vs[0][0]);
+    const int in_page = (1 << c.log2_rows) - 1;
+    const auto tile_of = [&](int i) { return IPW == 2 ? i : w >> 1; };
+    const auto tile_row = [&](int blk, int i) { return min(max(blk * kKeys + 16 * tile_of(i), row_lo), row_hi); };
+    struct Entries { int p[IPW]; };
+    const auto entries = [&](int blk) {   // as they come out of memory, the same in all lanes
+      Entries e;
+#pragma unroll
+      for (int i = 0; i < IPW; ++i) {
+        const int x = (tile_row(blk, i) >> c.log2_rows) - first_page;
+        e.p[i] = in_lds ? table_sh[x] : table[x];
+      }
+      return e;
+    };
+    int64_t at[kNS][IPW];   // where the tiles of the block that goes to a slot begin in k and v
+    const auto place = [&](int slot, int blk, const Entries& e) {
+#pragma unroll
+      for (int i = 0; i < IPW; ++i) {
+        int p = __builtin_amdgcn_readfirstlane(e.p[i]);
+        if (!in_lds && (unsigned)p >= (unsigned)c.pages) {
+          report(c);
+          bad_sh = 1;
+          p = 0;
+        }
+        at[slot][i] = p * c.stride_page + (tile_row(blk, i) & in_page) * c.stride_row + h * c.stride_head;
+      }
+    };
+    const auto copy = [&](const uint8_t* mem, int slot, int blk, bool masked, unsigned src, unsigned chunk_off, unsigned lds) {
+#pragma unroll
+      for (int i = 0; i < IPW; ++i) {
+        unsigned off = src;
+        if (masked) {
+          const int r0 = tile_row(blk, i);
+          off = min(max(r0 + group_row, lo), most - 1) - r0;
+          off = off * (unsigned)c.stride_row + chunk_off;
+        }
+        load_to_lds(uniform(mem + at[slot][i]), off, lds + (unsigned)((slot * BLK + (w + i * kNW) * 512) * 2));
+      }
+    };
+    const auto issue_k = [&](int slot, int j) {   // block number j in the order of processing
+      const int x = min(j, n_blocks - 1);
+      copy(c.k, slot, block_of(x), x < n_masked, k_src, k_chunk, ks_lds);
+    };
+    const auto issue_v = [&](int slot, int j) {
+      const int x = min(j, n_blocks - 1);
+      copy(c.v, slot, block_of(x), x < n_masked, v_src, v_chunk, vs_lds);
+    };
+    // Copies past the last block repeat it into slots that nobody reads any more, so that every stage issues and awaits as many.
+    const auto where = [&](int j) { return block_of(min(j, n_blocks - 1)); };
+#pragma unroll
+    for (int j = 0; j < kNS; ++j) place(j, where(j), entries(where(j)));
+    issue_k(0, 0);
+    issue_v(0, 0);
+    if (n_blocks > 1) {
+      issue_k(1, 1);
+      issue_k(2, 2);
+      issue_k(3, 3);
+      issue_v(1, 1);
+    }
+    Entries next = entries(where(kNS));
+
+    // Q fragments (B operand of S^T = K Q^T): query 16 qt + col, head-dim slice [32kc + 8g, +8); consumed here, so that a wait for them does not drain the
+    // copies that are meant to stay in flight later.
+    bf16x8 qf[2][KC];
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) qf[qt][kc] = *reinterpret_cast<const bf16x8*>(qrow[qt] + 32 * kc);
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) asm volatile("" ::"v"(qf[0][kc]), "v"(qf[1][kc]));
+
+    const float c2 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.scale * kLog2eF)));
+    const int e = col >> 2, qd = col & 3;
+    const int k_off = e * 4 * D + (col & 3) * 32 + (g ^ e) * 8;   // K operand: row 16kt + col, chunk 4kc + g
+    // V^T operand: rows 4g + e and 16 + 4g + e, head-dim 16mt + 4qd; even and odd mt
+    const int v_even = g * 4 * D + e * 32 + (2 * (g & 1) + (qd >> 1)) * 8 + 4 * (qd & 1), v_odd = v_even ^ 16;
+    bf16x8 ones;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
+    asm volatile("" : "+v"(ones));   // stays in registers
+
+    struct Scores { floatx4 t[2][2]; };   // keys 16kt + 4g + r, query 16qt + col
+    const auto mask = [&](Scores& sc, int blk) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int key = blk * kKeys + 16 * kt + 4 * g + r;
+#pragma unroll
+          for (int qt = 0; qt < 2; ++qt)
+            if (key < lo || key >= sees[qt]) sc.t[kt][qt][r] = -INFINITY;
+        }
+    };
+    const auto probs = [&](const Scores& sc, int qt, bf16x8& pf) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pf[j] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc.t[j >> 2][qt][j & 3], c2, -mc[qt]));
+    };
+    const auto too_large = [&](const bf16x8 (&pf)[2]) -> bool {
+      const uintx4 x = __builtin_bit_cast(uintx4, pf[0]), y = __builtin_bit_cast(uintx4, pf[1]);
+      return (((x[0] | x[1] | x[2]) | x[3] | y[0]) | y[1] | y[2] | y[3]) & 0x40004000u;
+    };
+    const auto rescale = [&](const Scores& sc, bf16x8 (&pf)[2]) {
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+        float mx = sc.t[0][qt][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc.t[j >> 2][qt][j & 3]);
+        const float m_new = fmaxf(mc[qt], fmaf(quad_max(mx), c2, kHeadroom));
+        const float f = __builtin_amdgcn_exp2f(mc[qt] - m_new);
+        mc[qt] = m_new;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          ls[qt][r] *= f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) o[mt][qt][r] *= f;
+        }
+        probs(sc, qt, pf[qt]);
+      }
+    };
+    // Operands of step i of a stage: head-dim slice i of S^T and two head-dim tiles of O^T.
+    struct Frags {
+      bf16x8 k[2];
+      bf16x4 v[2][2];
+    };
+    const auto load_frag = [&](Frags& f, const __bf16* Kt, const __bf16* Vt, int i, int p) {   // one LDS read, p 0 .. 5
+      if (p < 2) f.k[p] = *reinterpret_cast<const bf16x8*>(&Kt[16 * p * D + 128 * i + k_off]);
+      else f.v[(p >> 1) - 1][p & 1] = lds_read_tr(&Vt[16 * (p & 1) * D + 128 * i + ((p >> 1) - 1 ? v_odd : v_even)]);
+    };
+    const auto joined = [](const bf16x4 (&v)[2]) { return bf16x8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]}; };
+    const auto qk = [&](Scores& sn, const Frags& f, int kc, int n) {
+      const int kt = n >> 1, qt = kt ^ (n & 1);
+      sn.t[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.k[kt], qf[qt][kc], sn.t[kt][qt], 0, 0, 0);
+    };
+    const auto pv = [&](const Frags& f, const bf16x8 (&p)[2], int i, int n) {
+      const int m = n >> 1, qt = m ^ (n & 1);
+      o[2 * i + m][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(joined(f.v[m]), p[qt], o[2 * i + m][qt], 0, 0, 0);
+    };
+    const auto row_sums = [&](const bf16x8 (&p)[2], int qt) { ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[qt], ls[qt], 0, 0, 0); };
+
+    bf16x8 P[2][2];   // probabilities of block j in P[j & 1]: those of the previous block wait for their PV product
+    Frags pre;        // operands of the next stage's first step
+
+    // Stage j, slot S = j % 4 (compile time).  On entry sc = scores of block j, on exit those of block j + 1.  FIRST: j = 0 (no previous block).
+    auto stage = [&](auto slot_tag, auto first_tag, int j, Scores& sc) {
+      constexpr int S = decltype(slot_tag)::value;
+      constexpr bool FIRST = decltype(first_tag)::value;
+      const __bf16* const Kt = &Ks[(S + 1) % kNS][0];
+      const __bf16* const Vt = &Vs[(S + 3) % kNS][0];
+      Scores sn;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sn.t[i >> 1][i & 1] = floatx4{0.f, 0.f, 0.f, 0.f};
+      bf16x8 (&pp)[2] = P[(S + 1) & 1], (&pf)[2] = P[S & 1];
+      Frags f = pre, nx;
+      float x[16];
+      auto vec_op = [&](auto t_tag) {
+        constexpr Step op = softmax_step(decltype(t_tag)::value);
+        constexpr int i = op.index, qt = (i >> 3) & 1, jj = i & 7;
+        if constexpr (op.kind == 0) x[i] = fmaf(sc.t[jj >> 2][qt][jj & 3], c2, -mc[qt]);
+        else if constexpr (op.kind == 1) x[i] = __builtin_amdgcn_exp2f(x[i]);
+        else { pf[qt][jj] = (__bf16)x[i]; pf[qt][jj + 1] = (__bf16)x[i + 1]; }
+      };
+      constexpr int SLOTS = 8 * KC + 2, VEC_SLOTS = SLOTS - 3 * KC / 4;   // the vector work ends early: its test travels beside the last MFMAs
+      bool large = false;
+      auto slot = [&](auto s_tag) {
+        constexpr int T = decltype(s_tag)::value, I = T / 8 < KC ? T / 8 : KC - 1, N = T - 8 * I;   // the last step has two more
+        if constexpr (N < 4) qk(sn, f, I, N);
+        else if constexpr (N < 8) { if (!FIRST) pv(f, pp, I, N - 4); }
+        else { if (!FIRST) row_sums(pp, N - 8); }
+        for_each<steps_before(T, VEC_SLOTS), steps_before(T + 1, VEC_SLOTS)>(vec_op);
+        if constexpr (T == VEC_SLOTS) large = __any(too_large(pf));
+        if constexpr (N < 2 || (N >= 4 && N < 8)) {
+          constexpr int p = N < 2 ? N : N - 2;
+          if constexpr (I + 1 < KC) load_frag(nx, Kt, Vt, I + 1, p);
+          else load_frag(nx, &Ks[(S + 2) % kNS][0], &Vs[S][0], 0, p);
+        }
+        if constexpr (N == 7 && I + 1 < KC) f = nx;
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      for_each<0, 4 * KC>(slot);
+      place(S, where(j + kNS), next);
+      wait_and_sync<2 * IPW>();   // K(j + 2) and V(j) have landed: everything but what the previous stage issued
+      issue_k(S, j + kNS);
+      issue_v((S + 2) % kNS, j + 2);
+      next = entries(where(j + kNS + 1));
+      __builtin_amdgcn_sched_barrier(0);
+      for_each<4 * KC, SLOTS>(slot);
+      pre = nx;
+      const bool masked = j + 1 < n_masked;
+      if (__builtin_expect(large || masked, 0)) {
+        if (large) rescale(sc, pf);
+        if (masked) mask(sn, block_of(j + 1));
+      }
+      sc = sn;
+    };
+
+    dma_wait_but<0>();
+    __syncthreads();
+    Scores sc;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sc.t[i >> 1][i & 1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      Frags f;
+      for (int n = 0; n < 2; ++n) load_frag(f, &Ks[0][0], nullptr, kc, n);
+      for (int n = 0; n < 4; ++n) qk(sc, f, kc, n);
+    }
+    for (int n = 0; n < 2; ++n) load_frag(pre, &Ks[1][0], nullptr, 0, n);
+    for (int n = 2; n < 6; ++n) load_frag(pre, nullptr, &Vs[0][0], 0, n);
+    if (n_masked > 0) mask(sc, block_of(0));
+
+    using No = std::false_type;
+    using Yes = std::true_type;
+    if (n_blocks > 1) {
+      stage(std::integral_constant<int, 0>{}, Yes{}, 0, sc);
+      for (int j = 1;; j += 4) {
+        if (j >= n_blocks - 1) break;
+        stage(std::integral_constant<int, 1>{}, No{}, j, sc);
+        if (j + 1 >= n_blocks - 1) break;
+        stage(std::integral_constant<int, 2>{}, No{}, j + 1, sc);
+        if (j + 2 >= n_blocks - 1) break;
+        stage(std::integral_constant<int, 3>{}, No{}, j + 2, sc);
+        if (j + 3 >= n_blocks - 1) break;
+        stage(std::integral_constant<int, 0>{}, No{}, j + 3, sc);
+      }
+    }
+    // the last block: its probabilities, its PV product and the one of the block before
+    const auto pv_block = [&](const __bf16* Vt, const bf16x8 (&p)[2]) {
+#pragma unroll
+      for (int i = 0; i < KC; ++i) {
+        Frags f;
+        for (int n = 2; n < 6; ++n) load_frag(f, nullptr, Vt, i, n);
+        for (int n = 0; n < 4; ++n) pv(f, p, i, n);
+      }
+      row_sums(p, 0);
+      row_sums(p, 1);
+    };
+    if (n_blocks > 1) {
+      const bool odd = n_blocks & 1;   // the block before the last has an odd number
+      const bf16x8 pl[2] = {odd ? P[1][0] : P[0][0], odd ? P[1][1] : P[0][1]};
+      pv_block(&Vs[(n_blocks - 2) % kNS][0], pl);
+    }
+    wait_and_sync<0>();
+    probs(sc, 0, P[0][0]);
+    probs(sc, 1, P[0][1]);
+    if (__any(too_large(P[0]))) rescale(sc, P[0]);
+    pv_block(&Vs[(n_blocks - 1) % kNS][0], P[0]);
+  }
+
+  // ---- normalise and store: a lane holds head-dim 16mt + 4g .. +4 of queries 16qt + col ----
+  const bool whole = part == 1 && work.chunks == 1 && group < 0;
+  const int64_t row0 = a.part[part].row0 + ((int64_t)pair * tiles + tile) * QROWS;   // of partial results
+  const bool mixed = fewest < min(most, end * kKeys);   // rows that some query does not see and another does
+  unsigned odd[2] = {0, 0};   // queries whose results are no numbers
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const Query q = query(w * 32 + 16 * qt + col);
+    if (mixed) {
+      float x = ls[qt][0] * 0.f;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x = fmaf(o[mt][qt][r], 0.f, x);
+      const uint64_t b = __ballot(q.there && x != 0.f);   // NaN
+      odd[qt] = (unsigned)((b | b >> 16 | b >> 32 | b >> 48) & 0xFFFFu);
+    }
+    if (!q.there) continue;
+    const float inv = q.sees > 0 ? 1.f / ls[qt][0] : 0.f;
+    __bf16* const orow = static_cast<__bf16*>(a.out) + q.row * D;
+    const int64_t prow = row0 + w * 32 + 16 * qt + col;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      if (whole) {
+        bf16x4 pk;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) pk[r] = (__bf16)(o[mt][qt][r] * inv);
+        *reinterpret_cast<bf16x4*>(orow + 16 * mt + 4 * g) = pk;
+      } else {
+        *reinterpret_cast<floatx4*>(a.part_o + prow * D + 16 * mt + 4 * g) = o[mt][qt];
+      }
+    }
+    if (!whole && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(mc[qt], ls[qt][0]);
+  }
+  __syncthreads();
+  unsigned again = bad_sh ? ~0u : odd[0] | odd[1] << 16;   // of the wave's queries
+  if (__builtin_expect(again == 0 || n_blocks <= 0, 1)) return;
+
+  // ---- row by row: a query of the wave after the other, D / 64 elements of the head a lane ----
+  constexpr int E = D / 64;
+  typedef std::conditional_t<E == 2, unsigned, unsigned short> Piece;
+  const auto unpack = [](Piece p, float (&x)[E]) {
+    x[0] = __builtin_bit_cast(float, (unsigned)p << 16);
+    if constexpr (E == 2) x[1] = __builtin_bit_cast(float, (unsigned)p & 0xFFFF0000u);
+  };
+  const int32_t* const table = c.table + entry0 * c.table_stride;
+#pragma unroll 1
+  for (; again != 0; again &= again - 1) {
+    const int x = w * 32 + __builtin_ctz(again);
+    const Query q = query(x);
+    if (!q.there) continue;
+    float qv[E], acc[E] = {}, M = -FLT_MAX, L = 0.f;
+    unpack(*reinterpret_cast<const Piece*>(static_cast<const __bf16*>(a.q) + q.row * D + E * lane), qv);
+    const int key1 = min(q.sees, end * kKeys);
+#pragma unroll 1
+    for (int key = max(lo, first * kKeys); key < key1; ++key) {
+      const int p = table[key >> c.log2_rows];
+      if ((unsigned)p >= (unsigned)c.pages) continue;
+      const int64_t off = p * c.stride_page + (key & ((1 << c.log2_rows) - 1)) * c.stride_row + h * c.stride_head + E * 2 * lane;
+      float kv[E], vv[E], s = 0.f;
+      unpack(*reinterpret_cast<const Piece*>(c.k + off), kv);
+      unpack(*reinterpret_cast<const Piece*>(c.v + off), vv);
+#pragma unroll
+      for (int i = 0; i < E; ++i) s = fmaf(qv[i], kv[i], s);
+#pragma unroll
+      for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i, 64);
+      s *= a.scale * kLog2eF;
+      const float m = maximum(M, s), f = __builtin_amdgcn_exp2f(M - m), pr = __builtin_amdgcn_exp2f(s - m);
+      M = m;
+      L = fmaf(L, f, pr);
+#pragma unroll
+      for (int i = 0; i < E; ++i) acc[i] = fmaf(pr, vv[i], acc[i] * f);
+    }
+    // Numbers among the results stand, unless a page was none or the sum of probabilities is no number.
+    const int64_t prow = row0 + x;
+    __bf16* const orow = static_cast<__bf16*>(a.out) + q.row * D + E * lane;
+    float* const po = a.part_o + prow * D + E * lane;
+    float* const ml = a.part_ml + 2 * prow;
+    if (whole) {
+      const float inv = q.sees > 0 ? 1.f / L : 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (bad_sh || (float)orow[i] * 0.f != 0.f) orow[i] = (__bf16)(acc[i] * inv);
+    } else {
+      const float m = ml[0], l = ml[1];
+      const bool all_of_it = bad_sh || l * 0.f != 0.f;
+      const float f = all_of_it ? 1.f : __builtin_amdgcn_exp2f(M - m);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (all_of_it || po[i] * 0.f != 0.f) po[i] = acc[i] * f;
+      if (all_of_it && lane == 0) {
+        ml[0] = M;
+        ml[1] = L;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+void launch_attn_pages_tiles(hipStream_t s, int head_dim, const AttnPagesArgs& a) {
+  const dim3 grid((unsigned)(part_grid(a, 0) + part_grid(a, 1)));
+  if (head_dim == 64) hipLaunchKernelGGL((attn_pages_tiles<64>), grid, dim3(64 * kNW), 0, s, a);
+  else hipLaunchKernelGGL((attn_pages_tiles<128>), grid, dim3(64 * kNW), 0, s, a);
+}
+
+}  // namespace hack

@@ -68,6 +68,46 @@ hack_status take_pages(hack_ctx* ctx, int32_t B, int32_t N, const hack_pages* c,
   return HACK_OK;
 }
 
+// Queries of a tile for so many queries of a cache.
+int tile_queries(const hack_ctx* ctx, int64_t queries) {
+  if (queries <= 16) return 16;
+  return ctx->cfg.dtype == HACK_F32 || queries <= 48 ? 32 : kPageTileQueries;
+}
+
+// How the parts of a call are laid out: tiles of queries, at most how many (entry, head, chunk) there may be, and where their partial results go.  Lengths are
+// not known here, so all bounds hold for any up to max_len.  false: more work-groups than a launch takes.
+bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
+  const int64_t H = a->c.heads, GN = (int64_t)a->G * a->c.n, units = (int64_t)a->batch * H;
+  const int64_t cuts = (((int64_t)a->c.max_len + kKeys - 1) / kKeys + a->least) / a->least;   // chunks of an entry at most
+  const auto lay_out = [&](AttnPart* p, int64_t queries, int64_t entries) -> int64_t {   // rows of partial results without a cut
+    p->queries = tile_queries(ctx, queries);
+    p->tiles = (int32_t)((queries + p->queries - 1) / p->queries);
+    return entries * p->tiles * p->queries;
+  };
+  int64_t most = 0, shared_rows = 0;
+  for (int i = 0; i < a->n_shared; ++i) most = std::max(most, a->shared[i].count * GN);
+  const int64_t own_rows = lay_out(&a->part[1], GN, units);
+  if (a->n_shared) shared_rows = lay_out(&a->part[0], most, a->n_shared * H);
+  if (shared_rows + own_rows > ctx->part_rows) a->n_shared = 0, shared_rows = 0;   // no room to join the parts: every element reads all of its rows
+  const int64_t spare = (ctx->part_rows - shared_rows - own_rows) / (a->n_shared ? 2 : 1);   // rows that the chunks of a part may take beyond
+  int64_t rows = 0, groups = 0;
+  for (int i = 0; i < 2; ++i) {
+    AttnPart& p = a->part[i];
+    const int64_t pairs = i ? units : a->n_shared * H;
+    if (pairs == 0) {
+      p = AttnPart{0, 1, 0, 0.f, 0};
+      continue;
+    }
+    const int64_t each = p.queries == 16 ? 3 : 2, more = std::min(each * ctx->cus, spare / p.queries);
+    p.share = more > 0 && cuts > 1 ? (float)more : 0.f;
+    p.pairs = (int32_t)std::min(pairs * cuts, p.share > 0.f ? (more + pairs * p.tiles) / p.tiles : pairs);
+    p.row0 = rows;
+    rows += (int64_t)p.pairs * p.tiles * p.queries;
+    groups += pairs_grid(p.pairs, p.tiles);
+  }
+  return groups <= kMostGroups;
+}
+
 }  // namespace
 
 extern "C" hack_status hack_append_pages(hack_ctx* ctx, int32_t B, int32_t N, const hack_rows* q, const hack_rows* k, const hack_rows* v, int32_t norm,
@@ -167,29 +207,8 @@ extern "C" hack_status hack_attn_pages(hack_ctx* ctx, int32_t B, int32_t N, int3
   a.causal = causal != 0;
   a.scale = scale;
   a.least = 8;
-  const int queries = GN <= 16 ? 16 : 32;
-  const int64_t slots = ctx->part_rows / queries, units = (int64_t)B * H;
-  const auto blocks = [](int64_t rows) { return (rows + kKeys - 1) / kKeys; };
-  const int64_t cuts = (blocks(a.c.max_len) + 1 + a.least - 1) / a.least;   // chunks of an entry at most
-  const int64_t want = 3 * (int64_t)ctx->cus;
-  a.part[1].tiles = (int32_t)((GN + queries - 1) / queries);
-  a.part[0].tiles = 1;
-  int64_t items[2] = {0, units * a.part[1].tiles};
-  for (int i = 0; i < a.n_shared; ++i) {
-    a.part[0].tiles = std::max<int32_t>(a.part[0].tiles, (int32_t)((a.shared[i].count * GN + queries - 1) / queries));
-  }
-  items[0] = (int64_t)a.n_shared * H * a.part[0].tiles;
-  if (items[0] + items[1] > slots) a.n_shared = 0, items[0] = 0;   // the joined rows' partial results do not fit: every element reads all of its rows
-  const int64_t spare = std::min(want, (slots - items[0] - items[1]) / 2);   // each part may be cut into so many more
-  a.share = spare > 0 && cuts > 1 ? (float)spare : 0.f;
-  const int64_t more = a.share > 0 ? spare : 0;
-  a.part[0].pairs = a.n_shared ? (int32_t)std::min<int64_t>((more + items[0]) / a.part[0].tiles, (int64_t)a.n_shared * H * cuts) : 0;
-  a.part[1].pairs = (int32_t)std::min<int64_t>((more + items[1]) / a.part[1].tiles, units * cuts);
-  a.part[0].slot0 = 0;
-  a.part[1].slot0 = a.part[0].pairs * a.part[0].tiles;
-  if (pairs_grid(a.part[0].pairs, a.part[0].tiles) + pairs_grid(a.part[1].pairs, a.part[1].tiles) > kMostGroups)
-    return fail(ctx, HACK_ECAPACITY, "%lld queries are more than a launch takes", (long long)rows);
-  launch_attn_pages(static_cast<hipStream_t>(stream), ctx->elem_bytes, d, queries, a.share > 0 || a.n_shared > 0, a);
+  if (!plan_parts(ctx, &a)) return fail(ctx, HACK_ECAPACITY, "%lld queries are more than a launch takes", (long long)rows);
+  launch_attn_pages(static_cast<hipStream_t>(stream), ctx->elem_bytes, d, a.part[1].share > 0.f || a.n_shared > 0, a);
   HIP_TRY(ctx, hipGetLastError());
   return HACK_OK;
 }

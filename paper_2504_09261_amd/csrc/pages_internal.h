@@ -41,16 +41,19 @@ struct Shared {
 };
 // The shared rows of groups (0) and the rows that every batch element, or head of it, has alone (1).
 struct AttnPart {
+  int32_t queries;    // of a tile: 16, 32 or kPageTileQueries
   int32_t tiles;      // of an entry's queries
   int32_t pairs;      // (entry, head, chunk) at most
-  int32_t slot0;      // first slot of its partial results
+  float share;        // work-groups that the blocks of its launch are cut for; 0: no cuts
+  int64_t row0;       // first row of its partial results
 };
+constexpr int kPageTileQueries = 128;
 struct AttnPagesHead {
   Pages c;
   const void* q;
   void* out;
-  float* part_o;      // [slot, queries of a tile, head_dim] unnormalised partial outputs
-  float* part_ml;     // [slot, queries of a tile, 2] their references and normalisers
+  float* part_o;      // [row0 of the part + (pair, tile, query of the tile), head_dim] unnormalised partial outputs
+  float* part_ml;     // [.., 2] their references and normalisers
   int2* plan;         // [groups, then batch elements or units]: first pair and chunks of an entry
   AttnPart part[2];
   int32_t batch;
@@ -59,7 +62,7 @@ struct AttnPagesHead {
   int32_t causal;
   float scale;
   int32_t least;      // blocks of a chunk at least
-  float share;        // work-groups that all blocks are cut for; 0: no cuts
+  int32_t parts;      // of the launch, a bit each; set by launch_attn_pages
 };
 struct AttnPagesArgs : AttnPagesHead {
   Shared shared[kMostShared];
@@ -73,7 +76,10 @@ __host__ __device__ inline int chunk_blocks(float total, float share, int least)
 }
 __host__ __device__ inline int entry_chunks(int blocks, int chunk) { return blocks > chunk ? chunks_of(blocks, chunk) : 1; }
 constexpr int64_t pairs_grid(int64_t pairs, int64_t tiles) { return (pairs + 7) / 8 * 8 * tiles; }
-// queries: of a tile.  merge: partial results may have to be joined.
-void launch_attn_pages(hipStream_t s, int elem_bytes, int head_dim, int queries, bool merge, const AttnPagesArgs& a);
+// merge: partial results may have to be joined.
+void launch_attn_pages(hipStream_t s, int elem_bytes, int head_dim, bool merge, AttnPagesArgs a);
+void launch_attn_pages_tiles(hipStream_t s, int head_dim, const AttnPagesArgs& a);   // a launch of tiles of kPageTileQueries queries, bf16
+// Work-groups of part p in the launch.
+inline int64_t part_grid(const AttnPagesArgs& a, int p) { return a.parts >> p & 1 ? pairs_grid(a.part[p].pairs, a.part[p].tiles) : 0; }
 
 }  // namespace hack

@@ -9,7 +9,7 @@
 namespace stub {
 int device = 0;
 std::vector<AppendArgs> appends;
-struct Attention { AttnPagesArgs a; int queries; bool merge; };
+struct Attention { AttnPagesArgs a; bool merge; };
 std::vector<Attention> attentions;
 size_t calls() { return appends.size() + attentions.size(); }
 }  // namespace stub
@@ -18,7 +18,7 @@ extern "C" hipError_t hipGetDevice(int* d) { *d = stub::device; return hipSucces
 
 namespace hack {
 void launch_append(hipStream_t, int, int, bool, int, AppendArgs a) { stub::appends.push_back(a); }
-void launch_attn_pages(hipStream_t, int, int, int queries, bool merge, const AttnPagesArgs& a) { stub::attentions.push_back({a, queries, merge}); }
+void launch_attn_pages(hipStream_t, int, int, bool merge, AttnPagesArgs a) { stub::attentions.push_back({a, merge}); }
 }  // namespace hack
 
 #define CHECK(c)                                    \
@@ -295,7 +295,6 @@ int plans() {
     if (groups.size() > 256) groups.resize(256);
     CHECK(hack_attn_pages(c.ctx, batch, rows, heads * std::max(G, 1), at(kE << 8), &p, nullptr, 0, groups.data(), (int)groups.size(), 0.1f, at(kF << 8), kStream) == HACK_OK);
     const AttnPagesArgs& a = stub::attentions.back().a;
-    const int queries = stub::attentions.back().queries;
     const int64_t GN = (int64_t)a.G * rows;
     for (int tries = 0; tries < 4; ++tries) {
       std::vector<int> len(p.by_head ? batch * heads : batch);
@@ -310,26 +309,28 @@ int plans() {
           if (b >= a.shared[g].first && b < a.shared[g].first + a.shared[g].count) lo = a.shared[g].rows;
         blocks[1].push_back(blocks_between(lo, len[e]));
       }
-      float total = 0.f;
+      const bool together = a.n_shared > 0 && a.part[0].queries == a.part[1].queries;   // parts of equal tiles are one launch
+      float total[2] = {};
       for (int part = 0; part < 2; ++part)
-        for (int n : blocks[part]) total += (float)mult[part] * a.part[part].tiles * n;
-      const int chunk = chunk_blocks(total, a.share, a.least);
-      int64_t slots = 0, pairs[2] = {};
+        for (int n : blocks[part]) total[part] += (float)mult[part] * a.part[part].tiles * n;
+      if (together) total[0] = total[1] = total[0] + total[1];
+      int64_t pairs[2] = {}, rows = 0;
       bool joined = a.n_shared > 0;
       for (int part = 0; part < 2; ++part) {
+        const int chunk = chunk_blocks(total[part], a.part[part].share, a.least);
         for (int n : blocks[part]) {
           pairs[part] += (int64_t)mult[part] * entry_chunks(n, chunk);
           joined |= entry_chunks(n, chunk) > 1;
         }
         CHECK(pairs[part] <= a.part[part].pairs);
-        slots = a.part[part].slot0 + pairs[part] * a.part[part].tiles;
-        if (part == 0) CHECK(slots <= a.part[1].slot0);
+        CHECK(rows <= a.part[part].row0);
+        rows = a.part[part].row0 + pairs[part] * a.part[part].tiles * a.part[part].queries;
       }
       CHECK(!joined || stub::attentions.back().merge);
-      CHECK(!joined || slots * queries <= c.ctx->part_rows);
+      CHECK(!joined || rows <= c.ctx->part_rows);
     }
-    CHECK((int64_t)a.part[1].tiles * queries >= GN);
-    for (int g = 0; g < a.n_shared; ++g) CHECK((int64_t)a.part[0].tiles * queries >= a.shared[g].count * GN);
+    CHECK((int64_t)a.part[1].tiles * a.part[1].queries >= GN);
+    for (int g = 0; g < a.n_shared; ++g) CHECK((int64_t)a.part[0].tiles * a.part[0].queries >= a.shared[g].count * GN);
     CHECK(pairs_grid(a.part[0].pairs, a.part[0].tiles) + pairs_grid(a.part[1].pairs, a.part[1].tiles) <= kMostGroups);
     stub::attentions.clear();
   }

@@ -249,13 +249,16 @@ def test_what_is_not_seen_does_not_matter(contexts, dtype, d, n, value):
     out = torch.full_like(clean, 9.0)
     hk.attn_pages(clean, pool.cache, 0.1, out, causal=True)
     same = torch.ones_like(out, dtype=torch.bool)
-    same[1, 1, at:, 5] = False
+    same[1, 1, :, 5] = False
     assert torch.equal(out[same], fine[same]), (out[same] != fine[same]).sum()
-    hit = out[1, 1, at:, 5]
+    hit = out[1, 1, at:, 5].clone()
     assert torch.isnan(hit).all() if np.isnan(value) else (hit == value).all(), hit
     pool.v[page, row, head] = old
+    out[1, 1, at:, 5] = fine[1, 1, at:, 5]
+    check_attention(pool, clean, out, float(np.float32(0.1)), True)
     pool.k[page, row, head, 5] = value            # a score that is no number, or infinite
     hk.attn_pages(clean, pool.cache, 0.1, out, causal=True)
+    same[1, 1, :, 5] = True
     same[1, 1, at:] = False
     assert torch.equal(out[same], fine[same])
 
