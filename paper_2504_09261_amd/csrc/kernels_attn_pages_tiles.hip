@@ -3,8 +3,8 @@
 //
 // The stage is that of the 128-query kernel over contiguous rows: scores of block j + 1, probabilities of block j and PV product of block j - 1 side by
 // side, in slots of one matrix instruction, an LDS read and a share of the vector work.  What pages add: a copy instruction takes rows of one
-// 16-row tile, which lie in one page, so it has a base of its own, from an entry of the table that is read a stage ahead out of LDS, where a work-group
-// brings its part of the table first.  Blocks with rows that some query of the item does not see (the last ones, causal; a first one that
+// 16-row tile, which lie in one page, so it has a base of its own, which is read a stage ahead out of a ring in LDS that the
+// threads fill from the table, 256 blocks at a time.  Blocks with rows that some query of the item does not see (the last ones, causal; a first one that
 // begins inside the shared rows) come first, their scores are masked, and rows that nobody sees are not copied: the nearest row that is seen stands in for them.
 // A masked row's probability is zero, which keeps it out of the sums unless its value is an infinity or NaN: an item whose results are no numbers, or
 // that met a page that is none, does these queries again row by row, and numbers among their results stand.
@@ -20,7 +20,7 @@ using namespace dev;
 
 constexpr int kNW = 4;            // waves
 constexpr int kNS = 4;            // LDS slots per tensor
-constexpr int kTableEntries = 2048;   // of a work-group's part of the table that LDS holds
+constexpr int kRing = 512;        // blocks whose places LDS holds, filled by halves
 constexpr float kHeadroom = 15.f; // the reference lies 2^15 above the running maximum: the exponent's top bit says that a probability reached 2
 
 template <int I, int N, typename F>
@@ -56,12 +56,6 @@ constexpr int steps_before(int s, int slots) {   // in front of slot s
   return t;
 }
 
-__device__ __forceinline__ const void* uniform(const void* p) {
-  const uint64_t x = (uint64_t)(uintptr_t)p;
-  const uint64_t lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)x), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32));
-  return (const void*)(uintptr_t)(hi << 32 | lo);
-}
-
 template <int D>
 __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesArgs a) {
   constexpr int KC = D / 32;        // MFMA steps over head_dim for S^T
@@ -90,7 +84,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
 
   __shared__ __attribute__((aligned(1024))) __bf16 Ks[kNS][BLK];
   __shared__ __attribute__((aligned(1024))) __bf16 Vs[kNS][BLK];
-  __shared__ int table_sh[kTableEntries];
+  __shared__ __attribute__((aligned(16))) int64_t place_sh[kRing][2];   // where the two tiles of a block begin in k and v, bytes
   __shared__ int most_sh[kNW], fewest_sh[kNW], bad_sh;
 
   // ---- queries and the rows that they see ----
@@ -99,7 +93,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
     int sees;
     bool there;
   };
-  const auto query = [&](int x) {
+  const auto query = [&](int x) __attribute__((always_inline)) {
     const int j = tile * QROWS + x, jj = min(j, n_rows - 1), m = jj / GN, r = jj - m * GN, n = r % c.n, b = b0 + m;
     const int fresh = fresh_of(c, b), len = rows_of(c, c.by_head ? b * c.heads + h : b);
     Query q{((int64_t)b * c.heads + h) * GN + r, max(0, a.causal ? len - fresh + n + 1 : len), j < n_rows && n < fresh};
@@ -140,7 +134,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
   const int end = first + n_blocks;
   const int full_end = max(first, min(end, fewest / kKeys));      // blocks from here on have rows that some query does not see
   const int n_tail = end - full_end, n_head = first < full_end && first * kKeys < lo ? 1 : 0, n_masked = n_tail + n_head;
-  const auto block_of = [&](int j) { return j < n_tail ? end - 1 - j : j < n_masked ? first : first + j - n_tail; };
+  const auto block_of = [&](int j) __attribute__((always_inline)) { return j < n_tail ? end - 1 - j : j < n_masked ? first : first + j - n_tail; };
 
   floatx4 o[MT][2];        // O^T: head-dim 16mt + 4g + r, query 16qt + col
 #pragma unroll
@@ -149,26 +143,27 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
   float mc[2] = {-FLT_MAX, -FLT_MAX};   // probabilities are 2^(c2 s - mc); finite from the start, so that keys whose score is -inf get 0
 
   if (n_blocks > 0) {
-    // ---- the part of the table that these blocks need ----
+    // ---- places of the blocks in the order in which they are taken, by halves of a ring; past the last block it is repeated ----
     const int row_lo = lo & ~15, row_hi = (most - 1) & ~15;   // first rows of the tiles that hold rows somebody sees
-    const int first_page = max(first * kKeys, row_lo) >> c.log2_rows, n_pages = (min(end * kKeys - 1, row_hi) >> c.log2_rows) - first_page + 1;
-    const int32_t* const table = c.table + entry0 * c.table_stride + first_page;
-    const bool in_lds = n_pages <= kTableEntries;
-    if (in_lds) {
-      bool bad = false;
-      for (int i = tid; i < n_pages; i += 64 * kNW) {
-        int p = table[i];
+    const int32_t* const table = c.table + entry0 * c.table_stride;
+    const auto tile_row = [&](int blk, int t) __attribute__((always_inline)) { return min(max(blk * kKeys + 16 * t, row_lo), row_hi); };
+    const auto fill = [&](int j0) __attribute__((always_inline)) {   // those of blocks j0 .. j0 + kRing / 2, one a thread
+      const int blk = block_of(min(j0 + tid, n_blocks - 1));
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int r = tile_row(blk, t);
+        int p = table[r >> c.log2_rows];
         if ((unsigned)p >= (unsigned)c.pages) {
-          bad = true;
+          report(c);
+          bad_sh = 1;
           p = 0;
         }
-        table_sh[i] = p;
+        place_sh[(j0 + tid) % kRing][t] = p * c.stride_page + (r & ((1 << c.log2_rows) - 1)) * c.stride_row + h * c.stride_head;
       }
-      if (bad) {
-        report(c);
-        bad_sh = 1;
-      }
-    }
+    };
+    static_assert(kRing / 2 == 64 * kNW, "a thread a block");
+    fill(0);
+    fill(kRing / 2);
     __syncthreads();
 
     // LDS layout of a block: rows in groups of four, a group's 64-byte pieces row after row (piece x of row r at (r / 4) 8D + 256 x + 64 (r % 4)), the 16-byte
@@ -178,67 +173,49 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
     const int group_row = (GPI == 1 ? 4 * w : 4 * ((2 * w + (lane >> 5)) & 3)) + ((lane >> 2) & 3);   // row of this lane's piece within its tile
     const int cg = GPI == 1 ? w : 2 * w + (lane >> 5), piece = 4 * ((lane >> 4) & (KC - 1));
     const unsigned k_chunk = (piece + ((lane & 3) ^ (cg & 3))) * 16, v_chunk = (piece + ((lane & 3) ^ (2 * (cg & 1)))) * 16;
-    const unsigned k_src = group_row * (unsigned)c.stride_row + k_chunk, v_src = group_row * (unsigned)c.stride_row + v_chunk;
     const unsigned ks_lds = lds_addr_of(&Ks[0][0]), vs_lds = lds_addr_of(&Vs[0][0]);
-    const int in_page = (1 << c.log2_rows) - 1;
-    const auto tile_of = [&](int i) { return IPW == 2 ? i : w >> 1; };
-    const auto tile_row = [&](int blk, int i) { return min(max(blk * kKeys + 16 * tile_of(i), row_lo), row_hi); };
-    struct Entries { int p[IPW]; };
-    const auto entries = [&](int blk) {   // as they come out of memory, the same in all lanes
-      Entries e;
-#pragma unroll
-      for (int i = 0; i < IPW; ++i) {
-        const int x = (tile_row(blk, i) >> c.log2_rows) - first_page;
-        e.p[i] = in_lds ? table_sh[x] : table[x];
+    const uint8_t* const k_lane = c.k + group_row * c.stride_row + k_chunk;   // in a tile at place 0
+    const uint8_t* const v_lane = c.v + group_row * c.stride_row + v_chunk;
+    struct Places { int64_t at[IPW]; };   // of the tiles that this wave's copies take
+    const auto places_of = [&](int j) __attribute__((always_inline)) {
+      const int64_t* p = place_sh[j % kRing];
+      Places x;
+      if constexpr (IPW == 1) {
+        x.at[0] = p[w >> 1];
+      } else {
+        x.at[0] = p[0];
+        x.at[1] = p[1];
       }
-      return e;
+      return x;
     };
-    int64_t at[kNS][IPW];   // where the tiles of the block that goes to a slot begin in k and v
-    const auto place = [&](int slot, int blk, const Entries& e) {
+    const auto copy = [&](const uint8_t* from, const Places& p, int slot, unsigned lds) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < IPW; ++i) {
-        int p = __builtin_amdgcn_readfirstlane(e.p[i]);
-        if (!in_lds && (unsigned)p >= (unsigned)c.pages) {
-          report(c);
-          bad_sh = 1;
-          p = 0;
-        }
-        at[slot][i] = p * c.stride_page + (tile_row(blk, i) & in_page) * c.stride_row + h * c.stride_head;
-      }
+      for (int i = 0; i < IPW; ++i) load_to_lds(from + p.at[i], lds + (unsigned)((slot * BLK + (w + i * kNW) * 512) * 2));
     };
-    const auto copy = [&](const uint8_t* mem, int slot, int blk, bool masked, unsigned src, unsigned chunk_off, unsigned lds) {
-#pragma unroll
-      for (int i = 0; i < IPW; ++i) {
-        unsigned off = src;
-        if (masked) {
-          const int r0 = tile_row(blk, i);
-          off = min(max(r0 + group_row, lo), most - 1) - r0;
-          off = off * (unsigned)c.stride_row + chunk_off;
-        }
-        load_to_lds(uniform(mem + at[slot][i]), off, lds + (unsigned)((slot * BLK + (w + i * kNW) * 512) * 2));
-      }
-    };
-    const auto issue_k = [&](int slot, int j) {   // block number j in the order of processing
+    // Block number j in the order of processing, masked or not: rows that nobody sees are not read.  Copies past the last block repeat it into slots that
+    // nobody reads any more, so that every stage issues and awaits as many.
+    const auto issue = [&](const uint8_t* from, const Places& p, int slot, int j, unsigned lds) __attribute__((always_inline)) {
       const int x = min(j, n_blocks - 1);
-      copy(c.k, slot, block_of(x), x < n_masked, k_src, k_chunk, ks_lds);
-    };
-    const auto issue_v = [&](int slot, int j) {
-      const int x = min(j, n_blocks - 1);
-      copy(c.v, slot, block_of(x), x < n_masked, v_src, v_chunk, vs_lds);
-    };
-    // Copies past the last block repeat it into slots that nobody reads any more, so that every stage issues and awaits as many.
-    const auto where = [&](int j) { return block_of(min(j, n_blocks - 1)); };
+      if (x >= n_masked) return copy(from, p, slot, lds);
+      const int blk = block_of(x);
 #pragma unroll
-    for (int j = 0; j < kNS; ++j) place(j, where(j), entries(where(j)));
-    issue_k(0, 0);
-    issue_v(0, 0);
-    if (n_blocks > 1) {
-      issue_k(1, 1);
-      issue_k(2, 2);
-      issue_k(3, 3);
-      issue_v(1, 1);
+      for (int i = 0; i < IPW; ++i) {
+        const int r0 = tile_row(blk, IPW == 2 ? i : w >> 1), r = min(max(r0 + group_row, lo), most - 1) - r0;
+        load_to_lds(from + p.at[i] + (r - group_row) * c.stride_row, lds + (unsigned)((slot * BLK + (w + i * kNW) * 512) * 2));
+      }
+    };
+    {
+      const Places p0 = places_of(0), p1 = places_of(1), p2 = places_of(2), p3 = places_of(3);
+      issue(k_lane, p0, 0, 0, ks_lds);
+      issue(v_lane, p0, 0, 0, vs_lds);
+      if (n_blocks > 1) {
+        issue(k_lane, p1, 1, 1, ks_lds);
+        issue(k_lane, p2, 2, 2, ks_lds);
+        issue(k_lane, p3, 3, 3, ks_lds);
+        issue(v_lane, p1, 1, 1, vs_lds);
+      }
     }
-    Entries next = entries(where(kNS));
+    Places next_k = places_of(kNS), next_v = places_of(2);   // of the copies of the next stage
 
     // Q fragments (B operand of S^T = K Q^T): query 16 qt + col, head-dim slice [32kc + 8g, +8); consumed here, so that a wait for them does not drain the
     // copies that are meant to stay in flight later.
@@ -261,7 +238,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
     asm volatile("" : "+v"(ones));   // stays in registers
 
     struct Scores { floatx4 t[2][2]; };   // keys 16kt + 4g + r, query 16qt + col
-    const auto mask = [&](Scores& sc, int blk) {
+    const auto mask = [&](Scores& sc, int blk) __attribute__((always_inline)) {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -272,15 +249,15 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
             if (key < lo || key >= sees[qt]) sc.t[kt][qt][r] = -INFINITY;
         }
     };
-    const auto probs = [&](const Scores& sc, int qt, bf16x8& pf) {
+    const auto probs = [&](const Scores& sc, int qt, bf16x8& pf) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) pf[j] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc.t[j >> 2][qt][j & 3], c2, -mc[qt]));
     };
-    const auto too_large = [&](const bf16x8 (&pf)[2]) -> bool {
+    const auto too_large = [&](const bf16x8 (&pf)[2]) __attribute__((always_inline)) -> bool {
       const uintx4 x = __builtin_bit_cast(uintx4, pf[0]), y = __builtin_bit_cast(uintx4, pf[1]);
       return (((x[0] | x[1] | x[2]) | x[3] | y[0]) | y[1] | y[2] | y[3]) & 0x40004000u;
     };
-    const auto rescale = [&](const Scores& sc, bf16x8 (&pf)[2]) {
+    const auto rescale = [&](const Scores& sc, bf16x8 (&pf)[2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt) {
         float mx = sc.t[0][qt][0];
@@ -303,28 +280,29 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
       bf16x8 k[2];
       bf16x4 v[2][2];
     };
-    const auto load_frag = [&](Frags& f, const __bf16* Kt, const __bf16* Vt, int i, int p) {   // one LDS read, p 0 .. 5
+    const auto load_frag = [&](Frags& f, const __bf16* Kt, const __bf16* Vt, int i, int p) __attribute__((always_inline)) {   // one LDS read, p 0 .. 5
       if (p < 2) f.k[p] = *reinterpret_cast<const bf16x8*>(&Kt[16 * p * D + 128 * i + k_off]);
       else f.v[(p >> 1) - 1][p & 1] = lds_read_tr(&Vt[16 * (p & 1) * D + 128 * i + ((p >> 1) - 1 ? v_odd : v_even)]);
     };
-    const auto joined = [](const bf16x4 (&v)[2]) { return bf16x8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]}; };
-    const auto qk = [&](Scores& sn, const Frags& f, int kc, int n) {
+    const auto joined = [](const bf16x4 (&v)[2]) __attribute__((always_inline)) { return bf16x8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]}; };
+    const auto qk = [&](Scores& sn, const Frags& f, int kc, int n) __attribute__((always_inline)) {
       const int kt = n >> 1, qt = kt ^ (n & 1);
       sn.t[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.k[kt], qf[qt][kc], sn.t[kt][qt], 0, 0, 0);
     };
-    const auto pv = [&](const Frags& f, const bf16x8 (&p)[2], int i, int n) {
+    const auto pv = [&](const Frags& f, const bf16x8 (&p)[2], int i, int n) __attribute__((always_inline)) {
       const int m = n >> 1, qt = m ^ (n & 1);
       o[2 * i + m][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(joined(f.v[m]), p[qt], o[2 * i + m][qt], 0, 0, 0);
     };
-    const auto row_sums = [&](const bf16x8 (&p)[2], int qt) { ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[qt], ls[qt], 0, 0, 0); };
+    const auto row_sums = [&](const bf16x8 (&p)[2], int qt) __attribute__((always_inline)) { ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[qt], ls[qt], 0, 0, 0); };
 
     bf16x8 P[2][2];   // probabilities of block j in P[j & 1]: those of the previous block wait for their PV product
     Frags pre;        // operands of the next stage's first step
 
     // Stage j, slot S = j % 4 (compile time).  On entry sc = scores of block j, on exit those of block j + 1.  FIRST: j = 0 (no previous block).
-    auto stage = [&](auto slot_tag, auto first_tag, int j, Scores& sc) {
+    // FULL: blocks from j + 1 on are not masked.
+    auto stage = [&](auto slot_tag, auto first_tag, auto full_tag, int j, Scores& sc) __attribute__((always_inline)) {
       constexpr int S = decltype(slot_tag)::value;
-      constexpr bool FIRST = decltype(first_tag)::value;
+      constexpr bool FIRST = decltype(first_tag)::value, FULL = decltype(full_tag)::value;
       const __bf16* const Kt = &Ks[(S + 1) % kNS][0];
       const __bf16* const Vt = &Vs[(S + 3) % kNS][0];
       Scores sn;
@@ -333,7 +311,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
       bf16x8 (&pp)[2] = P[(S + 1) & 1], (&pf)[2] = P[S & 1];
       Frags f = pre, nx;
       float x[16];
-      auto vec_op = [&](auto t_tag) {
+      auto vec_op = [&](auto t_tag) __attribute__((always_inline)) {
         constexpr Step op = softmax_step(decltype(t_tag)::value);
         constexpr int i = op.index, qt = (i >> 3) & 1, jj = i & 7;
         if constexpr (op.kind == 0) x[i] = fmaf(sc.t[jj >> 2][qt][jj & 3], c2, -mc[qt]);
@@ -342,8 +320,11 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
       };
       constexpr int SLOTS = 8 * KC + 2, VEC_SLOTS = SLOTS - 3 * KC / 4;   // the vector work ends early: its test travels beside the last MFMAs
       bool large = false;
-      auto slot = [&](auto s_tag) {
+      auto slot = [&](auto s_tag) __attribute__((always_inline)) {
         constexpr int T = decltype(s_tag)::value, I = T / 8 < KC ? T / 8 : KC - 1, N = T - 8 * I;   // the last step has two more
+        // one wait for both K operands (lgkmcnt(4)) and one for both of V^T (lgkmcnt(2)) instead of one for each
+        if constexpr (N == 0) __builtin_amdgcn_s_waitcnt(0xC47F);
+        if constexpr (N == 4) __builtin_amdgcn_s_waitcnt(0xC27F);
         if constexpr (N < 4) qk(sn, f, I, N);
         else if constexpr (N < 8) { if (!FIRST) pv(f, pp, I, N - 4); }
         else { if (!FIRST) row_sums(pp, N - 8); }
@@ -358,19 +339,21 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
         __builtin_amdgcn_sched_barrier(0);
       };
       for_each<0, 4 * KC>(slot);
-      place(S, where(j + kNS), next);
       wait_and_sync<2 * IPW>();   // K(j + 2) and V(j) have landed: everything but what the previous stage issued
-      issue_k(S, j + kNS);
-      issue_v((S + 2) % kNS, j + 2);
-      next = entries(where(j + kNS + 1));
+      if constexpr (FULL) {
+        copy(k_lane, next_k, S, ks_lds);                   // K(j + 4)
+        copy(v_lane, next_v, (S + 2) % kNS, vs_lds);       // V(j + 2)
+      } else {
+        issue(k_lane, next_k, S, j + kNS, ks_lds);
+        issue(v_lane, next_v, (S + 2) % kNS, j + 2, vs_lds);
+      }
+      next_k = places_of(j + kNS + 1);
+      next_v = places_of(j + 3);
       __builtin_amdgcn_sched_barrier(0);
       for_each<4 * KC, SLOTS>(slot);
       pre = nx;
-      const bool masked = j + 1 < n_masked;
-      if (__builtin_expect(large || masked, 0)) {
-        if (large) rescale(sc, pf);
-        if (masked) mask(sn, block_of(j + 1));
-      }
+      if (__builtin_expect(large, 0)) rescale(sc, pf);
+      if (!FULL && j + 1 < n_masked) mask(sn, block_of(j + 1));
       sc = sn;
     };
 
@@ -392,20 +375,27 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
     using No = std::false_type;
     using Yes = std::true_type;
     if (n_blocks > 1) {
-      stage(std::integral_constant<int, 0>{}, Yes{}, 0, sc);
-      for (int j = 1;; j += 4) {
-        if (j >= n_blocks - 1) break;
-        stage(std::integral_constant<int, 1>{}, No{}, j, sc);
-        if (j + 1 >= n_blocks - 1) break;
-        stage(std::integral_constant<int, 2>{}, No{}, j + 1, sc);
-        if (j + 2 >= n_blocks - 1) break;
-        stage(std::integral_constant<int, 3>{}, No{}, j + 2, sc);
-        if (j + 3 >= n_blocks - 1) break;
-        stage(std::integral_constant<int, 0>{}, No{}, j + 3, sc);
-      }
+      stage(std::integral_constant<int, 0>{}, Yes{}, No{}, 0, sc);
+      int j = 1;
+      const auto four = [&](auto full_tag) __attribute__((always_inline)) {   // stages j .. j + 3; whether there are more
+        if (j >= n_blocks - 1) return false;
+        stage(std::integral_constant<int, 1>{}, No{}, full_tag, j, sc);
+        if (j + 1 >= n_blocks - 1) return false;
+        stage(std::integral_constant<int, 2>{}, No{}, full_tag, j + 1, sc);
+        if (j + 2 >= n_blocks - 1) return false;
+        stage(std::integral_constant<int, 3>{}, No{}, full_tag, j + 2, sc);
+        if (j + 3 >= n_blocks - 1) return false;
+        if (__builtin_expect((j + 3) % (kRing / 2) == 0, 0)) fill(j + 3 + kRing / 2);   // over those of blocks that are done
+        stage(std::integral_constant<int, 0>{}, No{}, full_tag, j + 3, sc);
+        j += 4;
+        return true;
+      };
+      bool more = true;
+      while (more && j + 1 < n_masked) more = four(No{});
+      while (more) more = four(Yes{});
     }
     // the last block: its probabilities, its PV product and the one of the block before
-    const auto pv_block = [&](const __bf16* Vt, const bf16x8 (&p)[2]) {
+    const auto pv_block = [&](const __bf16* Vt, const bf16x8 (&p)[2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < KC; ++i) {
         Frags f;
@@ -472,7 +462,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
     x[0] = __builtin_bit_cast(float, (unsigned)p << 16);
     if constexpr (E == 2) x[1] = __builtin_bit_cast(float, (unsigned)p & 0xFFFF0000u);
   };
-  const int32_t* const table = c.table + entry0 * c.table_stride;
+  const int32_t* const pages = c.table + entry0 * c.table_stride;
 #pragma unroll 1
   for (; again != 0; again &= again - 1) {
     const int x = w * 32 + __builtin_ctz(again);
@@ -483,7 +473,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
     const int key1 = min(q.sees, end * kKeys);
 #pragma unroll 1
     for (int key = max(lo, first * kKeys); key < key1; ++key) {
-      const int p = table[key >> c.log2_rows];
+      const int p = pages[key >> c.log2_rows];
       if ((unsigned)p >= (unsigned)c.pages) continue;
       const int64_t off = p * c.stride_page + (key & ((1 << c.log2_rows) - 1)) * c.stride_row + h * c.stride_head + E * 2 * lane;
       float kv[E], vv[E], s = 0.f;
