@@ -155,11 +155,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_pages(const AttnPagesArgs a)
     row[qt] = ((int64_t)b * c.heads + h) * GN + r;
     if (!there) row[qt] = -1 - row[qt];
   }
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) {
-    most = max(most, __shfl_xor(most, x, 64));
-    fewest = min(fewest, __shfl_xor(fewest, x, 64));
-  }
+  most = row_most(most);
+  fewest = row_fewest(fewest);
   most = __builtin_amdgcn_readfirstlane(most);
   fewest = __builtin_amdgcn_readfirstlane(fewest);
   uintx4 qf[NQ][R::kPieces];

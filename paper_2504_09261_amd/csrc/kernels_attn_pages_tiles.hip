@@ -114,11 +114,8 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
     }
     qrow[qt] = static_cast<const __bf16*>(a.q) + q.row * D + 8 * g;
   }
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) {
-    most = max(most, __shfl_xor(most, x, 64));
-    fewest = min(fewest, __shfl_xor(fewest, x, 64));
-  }
+  most = row_most(most);
+  fewest = row_fewest(fewest);
   if (lane == 0) {
     most_sh[w] = most;
     fewest_sh[w] = fewest;
