@@ -104,7 +104,7 @@ __device__ __forceinline__ bool find_work(const AttnPagesArgs& a, int part, int 
     for (int e = lane; e < entries_of(a, 1 - part); e += 64) other += entry_blocks(a, 1 - part, e);
     sum = fmaf(other, (float)entry_heads(a, 1 - part) * a.part[1 - part].tiles, sum);
   }
-  const int chunk = chunk_blocks(lanes_sum(sum), a.part[part].share, a.least);
+  const int chunk = chunk_blocks(lanes_sum(sum), a.part[part].share, a.part[part].least);
   int carry = 0;
   const auto look = [&](int e0, int blocks) __attribute__((always_inline)) {
     const int e = e0 + lane, chunks = e < n ? entry_chunks(blocks, chunk) : 0, incl = lanes_scan(chunks * heads), base = carry + incl - chunks * heads;

@@ -9,10 +9,7 @@
 // operand of S^T = K Q^T, a lane 16 bytes of a row at a time.  V^T wants keys side by side where memory has head-dim: a lane loads
 // the same 8 (head_dim 64: 4) elements of eight rows and turns the square around in registers, so that its elements are rows of 8 tiles of O^T.  Float32
 // enters the 16x16x4 matrix instruction as it is, whose operands need no turning.
-#include <cfloat>
-#include <type_traits>
-
-#include "attn_pages_device.h"
+#include "attn_pages_few.h"
 
 namespace hack {
 
@@ -20,419 +17,11 @@ namespace {
 
 using namespace dev;
 
-// ---- rows in registers ---------------------------------------------------------
-template <typename T, int D> struct Rows;
-template <int D> struct Rows<__bf16, D> {   // 32 rows
-  static constexpr int kRows = 32, kTiles = 2, kPieces = D / 32, kVRows = 8;
-  typedef std::conditional_t<D == 128, uintx4, uint2> VPiece;
-  uintx4 k[kTiles][kPieces];
-  VPiece v[kVRows];
-  // row of piece i in lane group g, within its tile, and the tile
-  static __device__ __forceinline__ int v_tile(int i) { return i >> 2; }
-  static __device__ __forceinline__ int v_row(int i, int g) { return 4 * g + (i & 3); }
-  __device__ __forceinline__ void load_v(int i, const uint8_t* base, unsigned off, int col) {
-    v[i] = *reinterpret_cast<const VPiece*>(base + off + col * (D / 8));
-  }
-  __device__ __forceinline__ void clear_v(int i) { v[i] = VPiece{}; }
-  static __device__ __forceinline__ unsigned word(const uintx4& x, int j) { return x[j]; }
-  static __device__ __forceinline__ unsigned word(const uint2& x, int j) { return j ? x.y : x.x; }
-  // The operand of tile mt: element mt of the lane's head-dims, in all eight rows.
-  __device__ __forceinline__ bf16x8 v_operand(int mt) const {
-    uintx4 x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(word(v[2 * i + 1], mt >> 1), word(v[2 * i], mt >> 1), mt & 1 ? 0x07060302u : 0x05040100u);
-    return __builtin_bit_cast(bf16x8, x);
-  }
-  __device__ __forceinline__ bool strange(int i) const {   // an infinity or a NaN
-    bool s = false;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) s |= (word(v[i], j) & 0x7F80u) == 0x7F80u || (word(v[i], j) & 0x7F800000u) == 0x7F800000u;
-    return s;
-  }
-  __device__ __forceinline__ void clear_strange(int i) {
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      unsigned x = word(v[i], j);
-      if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
-      if ((x & 0x7F800000u) == 0x7F800000u) x &= 0xFFFFu;
-      if constexpr (D == 128) v[i][j] = x;
-      else if (j) v[i].y = x;
-      else v[i].x = x;
-    }
-  }
-  // head-dim of row m of tile mt of O^T
-  static __device__ __forceinline__ int dim(int mt, int m) { return D / 16 * m + mt; }
-};
-template <int D> struct Rows<float, D> {   // 16 rows
-  static constexpr int kRows = 16, kTiles = 1, kPieces = D / 16, kVRows = 4;
-  uintx4 k[kTiles][kPieces];
-  floatx4 v[kVRows][D / 64];
-  static __device__ __forceinline__ int v_tile(int) { return 0; }
-  static __device__ __forceinline__ int v_row(int i, int g) { return 4 * g + i; }
-  __device__ __forceinline__ void load_v(int i, const uint8_t* base, unsigned off, int col) {
-#pragma unroll
-    for (int p = 0; p < D / 64; ++p) v[i][p] = *reinterpret_cast<const floatx4*>(base + off + 256 * p + 16 * col);
-  }
-  __device__ __forceinline__ void clear_v(int i) {
-#pragma unroll
-    for (int p = 0; p < D / 64; ++p) v[i][p] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
-  static __device__ __forceinline__ bool odd(float x) { return (__builtin_bit_cast(unsigned, x) & 0x7F800000u) == 0x7F800000u; }
-  __device__ __forceinline__ bool strange(int i) const {
-    bool s = false;
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) s |= odd(v[i][j >> 2][j & 3]);
-    return s;
-  }
-  __device__ __forceinline__ void clear_strange(int i) {
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j)
-      if (odd(v[i][j >> 2][j & 3])) v[i][j >> 2][j & 3] = 0.f;
-  }
-  static __device__ __forceinline__ int dim(int mt, int m) { return 64 * (mt >> 2) + 4 * m + (mt & 3); }
-};
-
-// floats of the four (float32) or D / 16 (bf16) head-dims that lie side by side, from dim(mt, m) on
-__device__ __forceinline__ void store_some(__bf16* p, const float* x, int n, float f) {
-  if (n == 8) {
-    bf16x8 y;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (__bf16)(x[i] * f);
-    *reinterpret_cast<bf16x8*>(p) = y;
-  } else {
-    *reinterpret_cast<bf16x4*>(p) = bf16x4{(__bf16)(x[0] * f), (__bf16)(x[1] * f), (__bf16)(x[2] * f), (__bf16)(x[3] * f)};
-  }
-}
-__device__ __forceinline__ void store_some(float* p, const float* x, int n, float f) {
-#pragma unroll
-  for (int i = 0; i < n; i += 4) *reinterpret_cast<floatx4*>(p + i) = floatx4{x[i] * f, x[i + 1] * f, x[i + 2] * f, x[i + 3] * f};
-}
-
 template <typename T, int D, int NQ>
 __global__ __launch_bounds__(kThreads, 2) void attn_pages(const AttnPagesArgs a) {
-  using R = Rows<T, D>;
-  constexpr bool kBf16 = sizeof(T) == 2;
-  constexpr int MT = D / 16, QROWS = 16 * NQ, SIDE = kBf16 ? MT : 4;   // head-dims of a lane that lie side by side
-  const Pages& c = a.c;
-  const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0;
-  const int part = (int)blockIdx.x >= grid0 ? 1 : 0, id = blockIdx.x - (part ? grid0 : 0), tiles = a.part[part].tiles;
-  // The tiles of an entry, head and chunk follow each other on an XCD (work-group id mod 8).
-  const int along = id >> 3, pair = (along / tiles) * 8 + (id & 7), tile = along % tiles;
-  Work work;
-  if (!find_work(a, part, pair, work)) return;
-  const int heads = entry_heads(a, part), chunk = work.local / heads;
-  if (work.local == 0 && tile == 0 && threadIdx.x == 0) a.plan[(part ? a.n_shared : 0) + work.entry] = make_int2(work.base, work.chunks);
-  const int b0 = part == 0 ? a.shared[work.entry].first : c.by_head ? work.entry / c.heads : work.entry;   // the first (or only) batch element
-  const int h = part == 1 && c.by_head ? work.entry % c.heads : work.local % heads;
-  const int group = part == 0 ? work.entry : group_of(a, b0), common = shared_rows(a, group);
-  const int entry0 = c.by_head ? b0 * c.heads + h : b0;     // of the table
-  const int lo = part ? common : 0;
-  const int GN = a.G * c.n, n_rows = part ? GN : a.shared[work.entry].count * GN;
-  if (tile * QROWS >= n_rows) return;
-  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-  __shared__ __attribute__((aligned(1024))) float ring[kWaves][16 * NQ * D];
-  __shared__ float m_sh[kWaves][QROWS], l_sh[kWaves][QROWS];
-
-  // ---- queries and the rows that they see ----
-  int sees[NQ];        // keys in front of it, of this part
-  int64_t row[NQ];     // of q and out; < 0: not computed
-  int most = 0, fewest = c.max_len;
-#pragma unroll
-  for (int qt = 0; qt < NQ; ++qt) {
-    const int j = min(tile * QROWS + 16 * qt + col, n_rows - 1), m = j / GN, r = j - m * GN, n = r % c.n, b = b0 + m;
-    const int fresh = fresh_of(c, b), len = rows_of(c, c.by_head ? b * c.heads + h : b);
-    const bool there = tile * QROWS + 16 * qt + col < n_rows && n < fresh;
-    sees[qt] = max(0, a.causal ? len - fresh + n + 1 : len);
-    if (part == 0) sees[qt] = min(sees[qt], common);
-    if (there) {
-      most = max(most, sees[qt]);
-      fewest = min(fewest, sees[qt]);
-    } else {
-      sees[qt] = 0;
-    }
-    row[qt] = ((int64_t)b * c.heads + h) * GN + r;
-    if (!there) row[qt] = -1 - row[qt];
-  }
-  most = row_most(most);
-  fewest = row_fewest(fewest);
-  most = __builtin_amdgcn_readfirstlane(most);
-  fewest = __builtin_amdgcn_readfirstlane(fewest);
-  uintx4 qf[NQ][R::kPieces];
-#pragma unroll
-  for (int qt = 0; qt < NQ; ++qt) {
-    const uint8_t* p = static_cast<const uint8_t*>(a.q) + (row[qt] < 0 ? -1 - row[qt] : row[qt]) * (D * (int)sizeof(T)) + 16 * g;
-#pragma unroll
-    for (int s = 0; s < R::kPieces; ++s) qf[qt][s] = *reinterpret_cast<const uintx4*>(p + 64 * s);
-  }
-
-  // ---- this wave's blocks of kRows keys: first + w, first + w + 4, ... ----
-  constexpr int PER = kKeys / R::kRows;
-  const int n_blocks = blocks_between(lo, most), begin = lo / kKeys;
-  const int first = (begin + chunk_at(n_blocks, work.chunks, chunk)) * PER, last = (begin + chunk_at(n_blocks, work.chunks, chunk + 1)) * PER;
-  const ConstInts table = as_const(c.table) + entry0 * c.table_stride;
-  const int in_page = (1 << c.log2_rows) - 1;
-  // Tiles of 16 rows lie in one page.  Tiles behind the last row that is seen, or in front of the first one, are the nearest again (their scores are masked).
-  const auto tile_row = [&](int blk, int t) { return max(min(blk * R::kRows + 16 * t, (most - 1) & ~15), lo & ~15); };
-  const auto pages_of = [&](int blk, int (&p)[R::kTiles]) {
-#pragma unroll
-    for (int t = 0; t < R::kTiles; ++t) p[t] = table[tile_row(blk, t) >> c.log2_rows];
-  };
-  const unsigned k_off = col * (unsigned)c.stride_row + 16 * g;
-  R rows;
-  int pg[R::kTiles], bad = 0, next_bad = 0;   // pages of the next block; tiles of this and of the next one whose page is none
-  int64_t at[R::kTiles];                  // of the next block's tiles in k and v
-  const auto place = [&](int blk) {
-    next_bad = 0;
-#pragma unroll
-    for (int t = 0; t < R::kTiles; ++t) {
-      int p = pg[t];
-      if (__builtin_expect((unsigned)p >= (unsigned)c.pages, 0)) {
-        p = 0;
-        next_bad |= 1 << t;
-      }
-      at[t] = p * c.stride_page + (tile_row(blk, t) & in_page) * c.stride_row + h * c.stride_head;
-    }
-    if (next_bad) report(c);
-  };
-  const auto load_k = [&]() {
-#pragma unroll
-    for (int t = 0; t < R::kTiles; ++t)
-#pragma unroll
-      for (int s = 0; s < R::kPieces; ++s) rows.k[t][s] = *reinterpret_cast<const uintx4*>(c.k + at[t] + k_off + 64 * s);
-  };
-  const auto load_v = [&]() {
-#pragma unroll
-    for (int i = 0; i < R::kVRows; ++i) rows.load_v(i, c.v + at[R::v_tile(i)], (unsigned)R::v_row(i, g) * (unsigned)c.stride_row, col);
-  };
-  int blk = first + w;
-  if (blk < last) {
-    pages_of(blk, pg);
-    place(blk);
-    load_k();
-    load_v();
-    if (blk + kWaves < last) pages_of(blk + kWaves, pg);
-  }
-
-  floatx4 o[MT][NQ];   // O^T: row m = 4 g + r of tile mt, query 16 qt + col
-  floatx4 ls[NQ];      // row sums of P, bf16: all rows hold the same; float32: those of the lane's keys in [0]
-  float mc[NQ];        // probabilities are 2^(c2 s - mc); finite from the start, so that keys whose score is -inf get 0
-  const float c2 = a.scale * kLog2eF;
-  bf16x8 ones;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
-#pragma unroll
-  for (int qt = 0; qt < NQ; ++qt) {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) o[mt][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
-    ls[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
-    mc[qt] = -FLT_MAX;
-  }
-
-  for (; blk < last; blk += kWaves) {
-    const bool more = blk + kWaves < last;
-    const int key0 = blk * R::kRows;
-    bad = next_bad;
-    floatx4 sc[R::kTiles][NQ];
-#pragma unroll
-    for (int t = 0; t < R::kTiles; ++t)
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-        sc[t][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < R::kPieces; ++s) {
-          if constexpr (kBf16) {
-            sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rows.k[t][s]), __builtin_bit_cast(bf16x8, qf[qt][s]), sc[t][qt], 0, 0, 0);
-          } else {
-            const floatx4 x = __builtin_bit_cast(floatx4, rows.k[t][s]), y = __builtin_bit_cast(floatx4, qf[qt][s]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], sc[t][qt], 0, 0, 0);
-          }
-        }
-      }
-    int64_t here[R::kTiles];
-#pragma unroll
-    for (int t = 0; t < R::kTiles; ++t) here[t] = at[t];
-    if (more) {
-      place(blk + kWaves);
-      load_k();
-      if (blk + 2 * kWaves < last) pages_of(blk + 2 * kWaves, pg);
-    }
-    const bool masked = key0 < lo || key0 + R::kRows > fewest || bad != 0;
-    bool apart = false;   // some queries see infinities or NaNs that others do not
-    if (masked) {
-#pragma unroll
-      for (int t = 0; t < R::kTiles; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int key = key0 + 16 * t + 4 * g + r;
-          const bool gone = key < lo || (bad >> t & 1);
-#pragma unroll
-          for (int qt = 0; qt < NQ; ++qt)
-            if (gone || key >= sees[qt]) sc[t][qt][r] = -INFINITY;
-        }
-      // Rows that no query of the tile sees may hold anything: their probabilities are zero, and the product must not meet a NaN.
-      bool strange = false;
-#pragma unroll
-      for (int i = 0; i < R::kVRows; ++i) {
-        const int t = R::v_tile(i), key = key0 + 16 * t + R::v_row(i, g);
-        if (key < lo || key >= most || (bad >> t & 1)) rows.clear_v(i);
-        strange |= key >= fewest && rows.strange(i);
-      }
-      apart = __any(strange);
-    }
-    // The reference is the largest score so far: the largest probabilities lie just below one, where bf16 rounds them finest.
-    float m_new[NQ];
-    bool moved = false;
-#pragma unroll
-    for (int qt = 0; qt < NQ; ++qt) {
-      float mx = sc[0][qt][0];
-#pragma unroll
-      for (int j = 1; j < 4 * R::kTiles; ++j) mx = maximum(mx, sc[j >> 2][qt][j & 3]);
-      m_new[qt] = maximum(mc[qt], quad_maximum(mx) * c2);
-      moved |= m_new[qt] != mc[qt];
-    }
-    if (__any(moved)) {
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-        const float f = __builtin_amdgcn_exp2f(mc[qt] - m_new[qt]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          ls[qt][r] *= f;
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) o[mt][qt][r] *= f;
-        }
-        mc[qt] = m_new[qt];
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < R::kTiles; ++t)
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sc[t][qt][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][qt][r], c2, -mc[qt]));
-    if (__builtin_expect(apart, 0)) {
-      // Each query takes what it sees: key by key, elements that are no numbers, and the product below goes without them.
-      float* const p_sh = &ring[w][0];   // [key, query]
-#pragma unroll
-      for (int t = 0; t < R::kTiles; ++t)
-#pragma unroll
-        for (int qt = 0; qt < NQ; ++qt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) p_sh[(16 * t + 4 * g + r) * QROWS + 16 * qt + col] = sc[t][qt][r];
-      wave_lds_order();
-#pragma unroll 1
-      for (int x = 0; x < R::kRows; ++x) {
-        const int key = key0 + x, t = x >> 4;
-        if (key < lo || key >= most || (bad >> t & 1)) continue;
-        const T* vr = reinterpret_cast<const T*>(c.v + (t ? here[R::kTiles - 1] : here[0]) + (x & 15) * c.stride_row);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float y = (float)vr[R::dim(mt, 4 * g + r)];
-            if ((__builtin_bit_cast(unsigned, y) & 0x7F800000u) != 0x7F800000u) continue;
-#pragma unroll
-            for (int qt = 0; qt < NQ; ++qt)
-              if (key < sees[qt]) o[mt][qt][r] += p_sh[x * QROWS + 16 * qt + col] * y;
-          }
-      }
-      wave_lds_order();
-#pragma unroll
-      for (int i = 0; i < R::kVRows; ++i) rows.clear_strange(i);
-    }
-    if constexpr (kBf16) {
-      bf16x8 pf[NQ];
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) pf[qt][j] = (__bf16)sc[j >> 2][qt][j & 3];
-        ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[qt], ls[qt], 0, 0, 0);   // sums over the numbers that the product below uses
-      }
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const bf16x8 vf = rows.v_operand(mt);
-#pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], o[mt][qt], 0, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) {
-          ls[qt][0] += sc[0][qt][r];
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-            o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(rows.v[r][mt >> 2][mt & 3], sc[0][qt][r], o[mt][qt], 0, 0, 0);
-        }
-    }
-    if (more) load_v();
-  }
-  if constexpr (!kBf16) {
-#pragma unroll
-    for (int qt = 0; qt < NQ; ++qt) {
-      ls[qt][0] += __shfl_xor(ls[qt][0], 16, 64);
-      ls[qt][0] += __shfl_xor(ls[qt][0], 32, 64);
-    }
-  }
-
-  // ---- merge the waves' partial results; wave w finishes rows 4 g + w of all tiles ----
-  wave_lds_order();
-  float4* const mine = reinterpret_cast<float4*>(&ring[w][0]) + lane;
-#pragma unroll
-  for (int qt = 0; qt < NQ; ++qt)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int m4 = 0; m4 < MT / 4; ++m4)
-        mine[((r * NQ + qt) * (MT / 4) + m4) * 64] = make_float4(o[4 * m4][qt][r], o[4 * m4 + 1][qt][r], o[4 * m4 + 2][qt][r], o[4 * m4 + 3][qt][r]);
-  if (g == 0) {
-#pragma unroll
-    for (int qt = 0; qt < NQ; ++qt) {
-      m_sh[w][16 * qt + col] = mc[qt];
-      l_sh[w][16 * qt + col] = ls[qt][0];
-    }
-  }
-  __syncthreads();
-  const bool whole = part == 1 && work.chunks == 1 && group < 0;
-  const int64_t slot = (int64_t)pair * tiles + tile;
-#pragma unroll
-  for (int qt = 0; qt < NQ; ++qt) {
-    float M = -FLT_MAX;
-#pragma unroll
-    for (int x = 0; x < kWaves; ++x) M = fmaxf(M, m_sh[x][16 * qt + col]);
-    float f[kWaves], L = 0.f;
-#pragma unroll
-    for (int x = 0; x < kWaves; ++x) {
-      f[x] = __builtin_amdgcn_exp2f(m_sh[x][16 * qt + col] - M);   // a wave without blocks has summed nothing
-      L = fmaf(f[x], l_sh[x][16 * qt + col], L);
-    }
-    float acc[MT];
-#pragma unroll
-    for (int m4 = 0; m4 < MT / 4; ++m4) {
-      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int x = 0; x < kWaves; ++x) {
-        const float4 p = reinterpret_cast<const float4*>(&ring[x][0])[((w * NQ + qt) * (MT / 4) + m4) * 64 + lane];
-        s.x = fmaf(f[x], p.x, s.x);
-        s.y = fmaf(f[x], p.y, s.y);
-        s.z = fmaf(f[x], p.z, s.z);
-        s.w = fmaf(f[x], p.w, s.w);
-      }
-      acc[4 * m4] = s.x; acc[4 * m4 + 1] = s.y; acc[4 * m4 + 2] = s.z; acc[4 * m4 + 3] = s.w;
-    }
-    if (row[qt] < 0) continue;
-    const float inv = sees[qt] > 0 ? 1.f / L : 0.f;
-    const int64_t prow = a.part[part].row0 + slot * QROWS + 16 * qt + col;
-#pragma unroll
-    for (int mt = 0; mt < MT; mt += SIDE) {
-      const int d = R::dim(mt, 4 * g + w);
-      if (whole) store_some(static_cast<T*>(a.out) + row[qt] * D + d, acc + mt, SIDE, inv);
-      else store_some(a.part_o + prow * D + d, acc + mt, SIDE, 1.f);
-    }
-    if (!whole && w == 0 && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(M, L);
-  }
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kFewLds<D, NQ>];
+  const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0, part = (int)blockIdx.x >= grid0 ? 1 : 0;
+  attn_pages_few<T, D, NQ>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
 }
 
 // Rows with partial results: ROWS of them a work-group, each by 256 / ROWS threads, D / 4 lanes a slot, which walk over its slots.
@@ -446,7 +35,7 @@ __global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a) {
   __shared__ float4 o_sh[ROWS][SIDE][LPR];
   __shared__ float2 ml_sh[ROWS][SIDE];
   bool mine = row < (int64_t)a.batch * c.heads * GN;
-  const int u = mine ? (int)(row / GN) : 0, r = (int)(row - (int64_t)u * GN), b = u / c.heads, h = u - b * c.heads, n = r % c.n;
+  const int u = mine ? (int)(row / GN) : 0, r = (int)(row - (int64_t)u * GN), b = u / c.heads, h = u - b * c.heads, n = r % c.n, x0 = n * a.G + r / c.n;
   const int entry = c.by_head ? u : b, group = mine ? group_of(a, b) : -1;
   const int2 own = a.plan[a.n_shared + entry];
   int2 common = make_int2(0, 0);
@@ -454,11 +43,12 @@ __global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a) {
   const int fresh = fresh_of(c, b);
   mine = mine && n < fresh && (group >= 0 || own.y > 1);
   const int slots = mine ? common.y + own.y : 0;
-  const int64_t j = group >= 0 ? (int64_t)(b - a.shared[group].first) * GN + r : 0;   // the row among its group's
-  // a part's slots are tiles of whole rows, one tile behind the other: query x of an entry is row x of its pair
+  // A part's slots are tiles of whole rows, one tile behind the other: query x of an entry is row x of its pair, and pairs of a head are its chunks.  The order of an
+  // entry's queries: by element, number, head.
+  const int64_t j = group >= 0 ? (int64_t)(b - a.shared[group].first) * GN + x0 : 0;
   const int64_t rows0 = (int64_t)a.part[0].tiles * a.part[0].queries, rows1 = (int64_t)a.part[1].tiles * a.part[1].queries;
-  const int64_t at0 = a.part[0].row0 + ((int64_t)common.x + h) * rows0 + j, step0 = c.heads * rows0;
-  const int64_t at1 = a.part[1].row0 + ((int64_t)own.x + (c.by_head ? 0 : h)) * rows1 + r, step1 = (c.by_head ? 1 : c.heads) * rows1;
+  const int64_t at0 = a.part[0].row0 + ((int64_t)common.x + (int64_t)h * common.y) * rows0 + j;
+  const int64_t at1 = a.part[1].row0 + ((int64_t)own.x + (c.by_head ? 0 : (int64_t)h * own.y)) * rows1 + x0;
   const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
   const float4* const po = reinterpret_cast<const float4*>(a.part_o) + lane;
   float M = -FLT_MAX, L = 0.f;
@@ -470,7 +60,7 @@ __global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int s = min(s0 + i * SIDE, slots - 1);
-      const int64_t at = s < common.y ? at0 + s * step0 : at1 + (s - common.y) * step1;
+      const int64_t at = s < common.y ? at0 + s * rows0 : at1 + (s - common.y) * rows1;
       x[i] = ml[at];
       p[i] = po[at * LPR];
     }
@@ -528,17 +118,14 @@ __global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a) {
 
 template <typename T, int D>
 void launch_some(hipStream_t s, bool merge, AttnPagesArgs& a) {
-  // parts of equal tiles go together
-  const int both = a.n_shared > 0 ? 3 : 2;
-  for (int left = both; left != 0; left &= ~a.parts) {
-    const int queries = a.part[left & 1 ? 0 : 1].queries;
-    a.parts = 0;
-    for (int p = 0; p < 2; ++p)
-      if ((left >> p & 1) && a.part[p].queries == queries) a.parts |= 1 << p;
+  const bool both = a.n_shared > 0;
+  a.parts = both ? 3 : 2;
+  if (a.part[1].queries == kPageTileQueries || (both && a.part[0].queries == kPageTileQueries)) {
+    launch_attn_pages_tiles(s, D, a);
+  } else {
     const dim3 grid((unsigned)(part_grid(a, 0) + part_grid(a, 1)));
-    if (queries == 16) hipLaunchKernelGGL((attn_pages<T, D, 1>), grid, dim3(kThreads), 0, s, a);
-    else if (queries == 32) hipLaunchKernelGGL((attn_pages<T, D, 2>), grid, dim3(kThreads), 0, s, a);
-    else launch_attn_pages_tiles(s, D, a);
+    if (a.part[1].queries == 16) hipLaunchKernelGGL((attn_pages<T, D, 1>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((attn_pages<T, D, 2>), grid, dim3(kThreads), 0, s, a);
   }
   if (!merge) return;
   const int64_t rows = (int64_t)a.batch * a.c.heads * a.G * a.c.n;

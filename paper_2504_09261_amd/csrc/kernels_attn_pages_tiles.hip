@@ -8,9 +8,7 @@
 // begins inside the shared rows) come first, their scores are masked, and rows that nobody sees are not copied: the nearest row that is seen stands in for them.
 // A masked row's probability is zero, which keeps it out of the sums unless its value is an infinity or NaN: an item whose results are no numbers, or
 // that met a page that is none, does these queries again row by row, and numbers among their results stand.
-#include <type_traits>
-
-#include "attn_pages_device.h"
+#include "attn_pages_few.h"
 
 namespace hack {
 
@@ -56,24 +54,26 @@ constexpr int steps_before(int s, int slots) {   // in front of slot s
   return t;
 }
 
+template <int D> constexpr int kTileLds = 2 * kNS * kKeys * D * 2 + kRing * 16 + (2 * kNW + 1) * 4;   // bytes
+
+// Work-group id of a part; lds: kTileLds bytes, 1024-byte aligned.
 template <int D>
-__global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesArgs a) {
+__device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int id, unsigned char* lds) {
   constexpr int KC = D / 32;        // MFMA steps over head_dim for S^T
   constexpr int MT = D / 16;        // 16-row tiles of O^T
   constexpr int IPW = D / 64;       // copy instructions per wave, block and tensor
   constexpr int BLK = kKeys * D;    // elements per block and tensor
   constexpr int QROWS = kPageTileQueries;
   const Pages& c = a.c;
-  const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0;
-  const int part = (int)blockIdx.x >= grid0 ? 1 : 0, id = blockIdx.x - (part ? grid0 : 0), tiles = a.part[part].tiles;
+  const int tiles = a.part[part].tiles;
   // The tiles of an entry, head and chunk follow each other on an XCD (work-group id mod 8), the last ones, which see the most rows, first.
   const int along = id >> 3, pair = (along / tiles) * 8 + (id & 7), tile = tiles - 1 - along % tiles;
   Work work;
   if (!find_work(a, part, pair, work)) return;
-  const int heads = entry_heads(a, part), chunk = work.local / heads;
+  const int chunk = work.local % work.chunks;
   if (work.local == 0 && tile == 0 && threadIdx.x == 0) a.plan[(part ? a.n_shared : 0) + work.entry] = make_int2(work.base, work.chunks);
   const int b0 = part == 0 ? a.shared[work.entry].first : c.by_head ? work.entry / c.heads : work.entry;
-  const int h = part == 1 && c.by_head ? work.entry % c.heads : work.local % heads;
+  const int h = part == 1 && c.by_head ? work.entry % c.heads : work.local / work.chunks;
   const int group = part == 0 ? work.entry : group_of(a, b0), common = shared_rows(a, group);
   const int entry0 = c.by_head ? b0 * c.heads + h : b0;     // of the table
   const int lo = part ? common : 0;
@@ -82,10 +82,12 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  __shared__ __attribute__((aligned(1024))) __bf16 Ks[kNS][BLK];
-  __shared__ __attribute__((aligned(1024))) __bf16 Vs[kNS][BLK];
-  __shared__ __attribute__((aligned(16))) int64_t place_sh[kRing][2];   // where the two tiles of a block begin in k and v, bytes
-  __shared__ int most_sh[kNW], fewest_sh[kNW], bad_sh;
+  __bf16 (&Ks)[kNS][BLK] = *reinterpret_cast<__bf16 (*)[kNS][BLK]>(lds);
+  __bf16 (&Vs)[kNS][BLK] = *reinterpret_cast<__bf16 (*)[kNS][BLK]>(lds + sizeof Ks);
+  int64_t (&place_sh)[kRing][2] = *reinterpret_cast<int64_t (*)[kRing][2]>(lds + 2 * sizeof Ks);   // where the two tiles of a block begin in k and v, bytes
+  int* const most_sh = reinterpret_cast<int*>(lds + 2 * sizeof Ks + sizeof place_sh);
+  int* const fewest_sh = most_sh + kNW;
+  int& bad_sh = most_sh[2 * kNW];
 
   // ---- queries and the rows that they see ----
   struct Query {
@@ -94,9 +96,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
     bool there;
   };
   const auto query = [&](int x) __attribute__((always_inline)) {
-    const int j = tile * QROWS + x, jj = min(j, n_rows - 1), m = jj / GN, r = jj - m * GN, n = r % c.n, b = b0 + m;
+    const int j = tile * QROWS + x, jj = min(j, n_rows - 1), m = jj / GN, r = jj - m * GN, n = r / a.G, b = b0 + m;
     const int fresh = fresh_of(c, b), len = rows_of(c, c.by_head ? b * c.heads + h : b);
-    Query q{((int64_t)b * c.heads + h) * GN + r, max(0, a.causal ? len - fresh + n + 1 : len), j < n_rows && n < fresh};
+    Query q{((int64_t)b * c.heads + h) * GN + (r - n * a.G) * c.n + n, max(0, a.causal ? len - fresh + n + 1 : len), j < n_rows && n < fresh};
     if (part == 0) q.sees = min(q.sees, common);
     if (!q.there) q.sees = 0;
     return q;
@@ -512,12 +514,35 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
   }
 }
 
+template <int D>
+__global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileLds<D>];
+  const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0, part = (int)blockIdx.x >= grid0 ? 1 : 0;
+  tile_part<D>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
+}
+
+// Shared rows by tiles, own rows by few queries: the products of the one beside the loads of the other.
+template <int D, int NQ>
+__global__ __launch_bounds__(64 * kNW, 2) void attn_pages_mixed(const AttnPagesArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[std::max(kTileLds<D>, kFewLds<D, NQ>)];
+  const int grid0 = (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles;
+  if ((int)blockIdx.x < grid0) tile_part<D>(a, 0, blockIdx.x, lds);
+  else attn_pages_few<__bf16, D, NQ>(a, 1, blockIdx.x - grid0, lds);
+}
+
+template <int D>
+void launch_some(hipStream_t s, const AttnPagesArgs& a) {
+  const dim3 grid((unsigned)(part_grid(a, 0) + part_grid(a, 1)));
+  if (a.part[1].queries == 16) hipLaunchKernelGGL((attn_pages_mixed<D, 1>), grid, dim3(64 * kNW), 0, s, a);
+  else if (a.part[1].queries == 32) hipLaunchKernelGGL((attn_pages_mixed<D, 2>), grid, dim3(64 * kNW), 0, s, a);
+  else hipLaunchKernelGGL((attn_pages_tiles<D>), grid, dim3(64 * kNW), 0, s, a);
+}
+
 }  // namespace
 
 void launch_attn_pages_tiles(hipStream_t s, int head_dim, const AttnPagesArgs& a) {
-  const dim3 grid((unsigned)(part_grid(a, 0) + part_grid(a, 1)));
-  if (head_dim == 64) hipLaunchKernelGGL((attn_pages_tiles<64>), grid, dim3(64 * kNW), 0, s, a);
-  else hipLaunchKernelGGL((attn_pages_tiles<128>), grid, dim3(64 * kNW), 0, s, a);
+  if (head_dim == 64) launch_some<64>(s, a);
+  else launch_some<128>(s, a);
 }
 
 }  // namespace hack

@@ -7,6 +7,8 @@ using namespace hack;
 
 namespace {
 
+int TUNE(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
+
 struct Dim { int64_t stride, count; };
 
 // Whether rows of `width` bytes at the multiples of nested dimensions (the widest first), and the same ones delta bytes on, keep clear of each other.
@@ -78,28 +80,33 @@ int tile_queries(const hack_ctx* ctx, int64_t queries) {
 // not known here, so all bounds hold for any up to max_len.  false: more work-groups than a launch takes.
 bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
   const int64_t H = a->c.heads, GN = (int64_t)a->G * a->c.n, units = (int64_t)a->batch * H;
-  const int64_t cuts = (((int64_t)a->c.max_len + kKeys - 1) / kKeys + a->least) / a->least;   // chunks of an entry at most
-  const auto lay_out = [&](AttnPart* p, int64_t queries, int64_t entries) -> int64_t {   // rows of partial results without a cut
-    p->queries = tile_queries(ctx, queries);
-    p->tiles = (int32_t)((queries + p->queries - 1) / p->queries);
-    return entries * p->tiles * p->queries;
+  AttnPart* const part = a->part;
+  const auto rows_of = [](const AttnPart& p, int64_t entries) { return entries * p.tiles * p.queries; };   // of partial results, without a cut
+  const auto lay_out = [&](int i, int64_t queries, int tile) {
+    part[i] = AttnPart{tile, (int32_t)((queries + tile - 1) / tile), 0, tile == kPageTileQueries ? TUNE("T_LEAST", 24) : TUNE("F_LEAST", 8), 0.f, 0};
   };
-  int64_t most = 0, shared_rows = 0;
-  for (int i = 0; i < a->n_shared; ++i) most = std::max(most, a->shared[i].count * GN);
-  const int64_t own_rows = lay_out(&a->part[1], GN, units);
-  if (a->n_shared) shared_rows = lay_out(&a->part[0], most, a->n_shared * H);
-  if (shared_rows + own_rows > ctx->part_rows) a->n_shared = 0, shared_rows = 0;   // no room to join the parts: every element reads all of its rows
-  const int64_t spare = (ctx->part_rows - shared_rows - own_rows) / (a->n_shared ? 2 : 1);   // rows that the chunks of a part may take beyond
+  int64_t most = 0, saved = 0;   // queries of a group; bytes that sharing spares
+  for (int i = 0; i < a->n_shared; ++i) {
+    const Shared& s = a->shared[i];
+    most = std::max(most, s.count * GN);
+    saved += (int64_t)(s.count - 1) * s.rows * H * 2 * ctx->cfg.head_dim * ctx->elem_bytes;
+  }
+  if (saved < ((int64_t)TUNE("SAVED", 16) << 20)) a->n_shared = 0;
+  const int own_tile = tile_queries(ctx, GN), shared_tile = tile_queries(ctx, most);
+  lay_out(1, GN, own_tile);
+  lay_out(0, most, shared_tile == kPageTileQueries ? shared_tile : own_tile);   // tiles of 16 and of 32 are not mixed
+  if (rows_of(part[0], a->n_shared * H) + rows_of(part[1], units) > ctx->part_rows) a->n_shared = 0;   // no room to join the parts: every element reads all of its rows
+  const int64_t shared_rows = rows_of(part[0], a->n_shared * H);
+  const int64_t spare = (ctx->part_rows - shared_rows - rows_of(part[1], units)) / (a->n_shared ? 2 : 1);   // rows that the chunks of a part may take beyond
+  const bool large = own_tile == kPageTileQueries || (a->n_shared && shared_tile == kPageTileQueries);
+  const int64_t want = (large || own_tile == 32 ? TUNE("T_WANT", 2) : TUNE("F_WANT", 3)) * (int64_t)ctx->cus;   // work-groups that the device holds at once
   int64_t rows = 0, groups = 0;
   for (int i = 0; i < 2; ++i) {
-    AttnPart& p = a->part[i];
+    AttnPart& p = part[i];
     const int64_t pairs = i ? units : a->n_shared * H;
-    if (pairs == 0) {
-      p = AttnPart{0, 1, 0, 0.f, 0};
-      continue;
-    }
-    const int64_t each = p.queries == 16 ? 3 : 2, more = std::min(each * ctx->cus, spare / p.queries);
-    p.share = more > 0 && cuts > 1 ? (float)more : 0.f;
+    const int64_t cuts = (((int64_t)a->c.max_len + kKeys - 1) / kKeys + p.least) / p.least;   // chunks of an entry at most
+    const int64_t more = std::min(want, spare / p.queries);
+    p.share = more > 0 && cuts > 1 && pairs > 0 ? (float)more : 0.f;
     p.pairs = (int32_t)std::min(pairs * cuts, p.share > 0.f ? (more + pairs * p.tiles) / p.tiles : pairs);
     p.row0 = rows;
     rows += (int64_t)p.pairs * p.tiles * p.queries;
@@ -206,7 +213,6 @@ extern "C" hack_status hack_attn_pages(hack_ctx* ctx, int32_t B, int32_t N, int3
   a.G = heads / H;
   a.causal = causal != 0;
   a.scale = scale;
-  a.least = 8;
   if (!plan_parts(ctx, &a)) return fail(ctx, HACK_ECAPACITY, "%lld queries are more than a launch takes", (long long)rows);
   launch_attn_pages(static_cast<hipStream_t>(stream), ctx->elem_bytes, d, a.part[1].share > 0.f || a.n_shared > 0, a);
   HIP_TRY(ctx, hipGetLastError());

@@ -44,6 +44,7 @@ struct AttnPart {
   int32_t queries;    // of a tile: 16, 32 or kPageTileQueries
   int32_t tiles;      // of an entry's queries
   int32_t pairs;      // (entry, head, chunk) at most
+  int32_t least;      // blocks of a chunk at least
   float share;        // work-groups that the blocks of its launch are cut for; 0: no cuts
   int64_t row0;       // first row of its partial results
 };
@@ -61,7 +62,6 @@ struct AttnPagesHead {
   int32_t n_shared;
   int32_t causal;
   float scale;
-  int32_t least;      // blocks of a chunk at least
   int32_t parts;      // of the launch, a bit each; set by launch_attn_pages
 };
 struct AttnPagesArgs : AttnPagesHead {
@@ -78,7 +78,7 @@ __host__ __device__ inline int entry_chunks(int blocks, int chunk) { return bloc
 constexpr int64_t pairs_grid(int64_t pairs, int64_t tiles) { return (pairs + 7) / 8 * 8 * tiles; }
 // merge: partial results may have to be joined.
 void launch_attn_pages(hipStream_t s, int elem_bytes, int head_dim, bool merge, AttnPagesArgs a);
-void launch_attn_pages_tiles(hipStream_t s, int head_dim, const AttnPagesArgs& a);   // a launch of tiles of kPageTileQueries queries, bf16
+void launch_attn_pages_tiles(hipStream_t s, int head_dim, const AttnPagesArgs& a);   // where a part has tiles of kPageTileQueries queries; bf16
 // Work-groups of part p in the launch.
 inline int64_t part_grid(const AttnPagesArgs& a, int p) { return a.parts >> p & 1 ? pairs_grid(a.part[p].pairs, a.part[p].tiles) : 0; }
 

@@ -309,7 +309,7 @@ int plans() {
           if (b >= a.shared[g].first && b < a.shared[g].first + a.shared[g].count) lo = a.shared[g].rows;
         blocks[1].push_back(blocks_between(lo, len[e]));
       }
-      const bool together = a.n_shared > 0 && a.part[0].queries == a.part[1].queries;   // parts of equal tiles are one launch
+      const bool together = a.n_shared > 0;   // both parts are one launch
       float total[2] = {};
       for (int part = 0; part < 2; ++part)
         for (int n : blocks[part]) total[part] += (float)mult[part] * a.part[part].tiles * n;
@@ -317,7 +317,7 @@ int plans() {
       int64_t pairs[2] = {}, rows = 0;
       bool joined = a.n_shared > 0;
       for (int part = 0; part < 2; ++part) {
-        const int chunk = chunk_blocks(total[part], a.part[part].share, a.least);
+        const int chunk = chunk_blocks(total[part], a.part[part].share, a.part[part].least);
         for (int n : blocks[part]) {
           pairs[part] += (int64_t)mult[part] * entry_chunks(n, chunk);
           joined |= entry_chunks(n, chunk) > 1;
