@@ -66,6 +66,15 @@ __device__ __forceinline__ float lanes_sum(float x) {   // in all lanes
   x += dpp_zero<0x143, 0xC>(x);
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
+__device__ __forceinline__ int lanes_most(int x) {   // of numbers from 0 on, in all lanes
+  x = max(x, dpp_zero<0x111, 0xF>(x));
+  x = max(x, dpp_zero<0x112, 0xF>(x));
+  x = max(x, dpp_zero<0x114, 0xF>(x));
+  x = max(x, dpp_zero<0x118, 0xF>(x));
+  x = max(x, dpp_zero<0x142, 0xA>(x));
+  x = max(x, dpp_zero<0x143, 0xC>(x));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 // Over the 16 lanes of a row, in all of them.
 template <int CTRL> __device__ __forceinline__ int dpp_mov(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true); }
 __device__ __forceinline__ int row_most(int x) {
@@ -92,19 +101,25 @@ __device__ __forceinline__ bool find_work(const AttnPagesArgs& a, int part, int 
   constexpr int kHeld = 4;
   int held[kHeld];
   float sum = 0.f;
+  int longest = 0;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
     held[i] = 64 * i + lane < n ? entry_blocks(a, part, 64 * i + lane) : 0;
     sum += held[i];
+    longest = max(longest, held[i]);
   }
-  for (int e = 64 * kHeld + lane; e < n; e += 64) sum += entry_blocks(a, part, e);
+  for (int e = 64 * kHeld + lane; e < n; e += 64) {
+    const int x = entry_blocks(a, part, e);
+    sum += x;
+    longest = max(longest, x);
+  }
   sum *= (float)heads * a.part[part].tiles;
   if (a.parts == 3) {
     float other = 0.f;
     for (int e = lane; e < entries_of(a, 1 - part); e += 64) other += entry_blocks(a, 1 - part, e);
     sum = fmaf(other, (float)entry_heads(a, 1 - part) * a.part[1 - part].tiles, sum);
   }
-  const int chunk = chunk_blocks(lanes_sum(sum), a.part[part].share, a.part[part].least);
+  const int chunk = chunk_blocks(lanes_sum(sum), lanes_most(longest), a.part[part]);
   int carry = 0;
   const auto look = [&](int e0, int blocks) __attribute__((always_inline)) {
     const int e = e0 + lane, chunks = e < n ? entry_chunks(blocks, chunk) : 0, incl = lanes_scan(chunks * heads), base = carry + incl - chunks * heads;

@@ -9,74 +9,116 @@
 namespace hack {
 namespace dev {
 
-// ---- rows in registers ---------------------------------------------------------
-template <typename T, int D> struct Rows;
-template <int D> struct Rows<__bf16, D> {   // 32 rows
-  static constexpr int kRows = 32, kTiles = 2, kPieces = D / 32, kVRows = 8;
-  typedef std::conditional_t<D == 128, uintx4, uint2> VPiece;
-  uintx4 k[kTiles][kPieces];
-  VPiece v[kVRows];
-  // row of piece i in lane group g, within its tile, and the tile
-  static __device__ __forceinline__ int v_tile(int i) { return i >> 2; }
-  static __device__ __forceinline__ int v_row(int i, int g) { return 4 * g + (i & 3); }
-  __device__ __forceinline__ void load_v(int i, const uint8_t* base, unsigned off, int col) {
-    v[i] = *reinterpret_cast<const VPiece*>(base + off + col * (D / 8));
+// ---- rows of a block -----------------------------------------------------------
+template <bool NT, typename V> __device__ __forceinline__ V load_piece(const uint8_t* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
+}
+
+// K: whole rows side by side in the lanes of a load, in chunks of 16 bytes, and through LDS into the order of the A operand.  Chunk c of row r lies at c ^ turn(r),
+// so that neither the writes (whole rows) nor the reads (16 rows at one chunk) meet a bank twice.  (A load of 16 rows' 64 bytes each into the operand's
+// registers needs no LDS, but reads half lines: 64 tokens over 643 MB 134 us, so 116.)
+template <typename T, int D, bool NT> struct KeyRows {
+  static constexpr int kRows = sizeof(T) == 2 ? 32 : 16, kChunks = D * (int)sizeof(T) / 16, kAtOnce = 64 / kChunks, kLoads = kRows / kAtOnce;
+  uintx4 x[kLoads];
+  static __device__ __forceinline__ int turn(int r) { return kChunks >= 16 ? r & 15 : (r >> 1) & 7; }
+  static constexpr int tile(int i) { return i * kAtOnce >> 4; }
+  // off: lane_offset.  (What is the same in all lanes goes into the base.)
+  static __device__ __forceinline__ unsigned lane_offset(unsigned stride, int lane) { return lane / kChunks * stride + 16 * (lane % kChunks); }
+  __device__ __forceinline__ void load(int i, const uint8_t* tile_base, unsigned stride, unsigned off) {
+    x[i] = load_piece<NT, uintx4>(tile_base + (uint64_t)((i * kAtOnce & 15) * stride) + off);
   }
-  __device__ __forceinline__ void clear_v(int i) { v[i] = VPiece{}; }
-  static __device__ __forceinline__ unsigned word(const uintx4& x, int j) { return x[j]; }
-  static __device__ __forceinline__ unsigned word(const uint2& x, int j) { return j ? x.y : x.x; }
-  // The operand of tile mt: element mt of the lane's head-dims, in all eight rows.
-  __device__ __forceinline__ bf16x8 v_operand(int mt) const {
-    uintx4 x;
+  __device__ __forceinline__ void put(uintx4* lds, int lane) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(word(v[2 * i + 1], mt >> 1), word(v[2 * i], mt >> 1), mt & 1 ? 0x07060302u : 0x05040100u);
-    return __builtin_bit_cast(bf16x8, x);
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * kAtOnce + lane / kChunks;
+      lds[r * kChunks + ((lane % kChunks) ^ turn(r))] = x[i];
+    }
   }
+  static __device__ __forceinline__ uintx4 get(const uintx4* lds, int t, int s, int col, int g) {   // chunk 4 s + g of row col of tile t
+    const int r = 16 * t + col;
+    return lds[r * kChunks + ((4 * s + g) ^ turn(r))];
+  }
+};
+
+// V: a lane's head-dims of the rows that the accumulators of S^T hold in its group of 16 lanes.
+template <typename T, int D, bool NT> struct ValueRows;
+template <int D, bool NT> struct ValueRows<__bf16, D, NT> {   // 32 rows: 8 head-dims of eight rows (128), or, until turned, of every second one (64)
+  static constexpr int kLoads = D / 16;
+  uintx4 x[kLoads];
+  static constexpr int tile(int i) { return i >= kLoads / 2; }
+  static __device__ __forceinline__ int row(int i, int g, int col) {   // within its tile
+    return D == 128 ? 4 * g + (i & 3) : 4 * g + 2 * (i & 1) + (col >> 3);
+  }
+  static __device__ __forceinline__ unsigned lane_offset(unsigned stride, int g, int col) { return row(0, g, col) * stride + 16 * (D == 128 ? col : col & 7); }
+  __device__ __forceinline__ void load(int i, const uint8_t* tile_base, unsigned stride, unsigned off) {
+    x[i] = load_piece<NT, uintx4>(tile_base + (uint64_t)(row(i, 0, 0) * stride) + off);
+  }
+  __device__ __forceinline__ void clear(int i) { x[i] = uintx4{0, 0, 0, 0}; }
   __device__ __forceinline__ bool strange(int i) const {   // an infinity or a NaN
     bool s = false;
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) s |= (word(v[i], j) & 0x7F80u) == 0x7F80u || (word(v[i], j) & 0x7F800000u) == 0x7F800000u;
+    for (int j = 0; j < 4; ++j) s |= (x[i][j] & 0x7F80u) == 0x7F80u || (x[i][j] & 0x7F800000u) == 0x7F800000u;
     return s;
   }
   __device__ __forceinline__ void clear_strange(int i) {
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      unsigned x = word(v[i], j);
-      if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
-      if ((x & 0x7F800000u) == 0x7F800000u) x &= 0xFFFFu;
-      if constexpr (D == 128) v[i][j] = x;
-      else if (j) v[i].y = x;
-      else v[i].x = x;
+    for (int j = 0; j < 4; ++j) {
+      if ((x[i][j] & 0x7F80u) == 0x7F80u) x[i][j] &= 0xFFFF0000u;
+      if ((x[i][j] & 0x7F800000u) == 0x7F800000u) x[i][j] &= 0xFFFFu;
     }
   }
+  // Operands of tiles 2 j and 2 j + 1 of O^T: elements 2 j and 2 j + 1 of the lane's head-dims in all eight rows.
+  __device__ __forceinline__ void operands(int j, int col, bf16x8 (&v)[2]) const {
+    uintx4 y[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      unsigned even_row, odd_row;
+      if constexpr (D == 128) {
+        even_row = x[2 * i][j];
+        odd_row = x[2 * i + 1][j];
+      } else {
+        // Lanes col and col ^ 8 hold the even and the odd rows of the same eight head-dims: each takes four of these in all rows.
+        const bool odd = col >> 3;
+        const unsigned keep = odd ? x[i][2 + j] : x[i][j], give = odd ? x[i][j] : x[i][2 + j];
+        const unsigned got = (unsigned)__builtin_amdgcn_update_dpp(0, (int)give, 0x128, 0xF, 0xF, true);   // row_ror 8
+        even_row = odd ? got : keep;
+        odd_row = odd ? keep : got;
+      }
+      y[0][i] = __builtin_amdgcn_perm(odd_row, even_row, 0x05040100u);
+      y[1][i] = __builtin_amdgcn_perm(odd_row, even_row, 0x07060302u);
+    }
+    v[0] = __builtin_bit_cast(bf16x8, y[0]);
+    v[1] = __builtin_bit_cast(bf16x8, y[1]);
+  }
   // head-dim of row m of tile mt of O^T
-  static __device__ __forceinline__ int dim(int mt, int m) { return D / 16 * m + mt; }
+  static __device__ __forceinline__ int dim(int mt, int m) { return D == 128 ? 8 * m + mt : 8 * (m & 7) + 4 * (m >> 3) + mt; }
 };
-template <int D> struct Rows<float, D> {   // 16 rows
-  static constexpr int kRows = 16, kTiles = 1, kPieces = D / 16, kVRows = 4;
-  uintx4 k[kTiles][kPieces];
-  floatx4 v[kVRows][D / 64];
-  static __device__ __forceinline__ int v_tile(int) { return 0; }
-  static __device__ __forceinline__ int v_row(int i, int g) { return 4 * g + i; }
-  __device__ __forceinline__ void load_v(int i, const uint8_t* base, unsigned off, int col) {
+template <int D, bool NT> struct ValueRows<float, D, NT> {   // 16 rows: four head-dims of each quarter (128) or all (64) of the head in four rows
+  static constexpr int kLoads = 4;
+  floatx4 x[kLoads][D / 64];
+  static constexpr int tile(int) { return 0; }
+  static __device__ __forceinline__ int row(int i, int g, int) { return 4 * g + i; }
+  static __device__ __forceinline__ unsigned lane_offset(unsigned stride, int g, int col) { return 4 * g * stride + 16 * col; }
+  __device__ __forceinline__ void load(int i, const uint8_t* tile_base, unsigned stride, unsigned off) {
 #pragma unroll
-    for (int p = 0; p < D / 64; ++p) v[i][p] = *reinterpret_cast<const floatx4*>(base + off + 256 * p + 16 * col);
+    for (int p = 0; p < D / 64; ++p) x[i][p] = load_piece<NT, floatx4>(tile_base + (uint64_t)(i * stride) + 256 * p + off);
   }
-  __device__ __forceinline__ void clear_v(int i) {
+  __device__ __forceinline__ void clear(int i) {
 #pragma unroll
-    for (int p = 0; p < D / 64; ++p) v[i][p] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < D / 64; ++p) x[i][p] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  static __device__ __forceinline__ bool odd(float x) { return (__builtin_bit_cast(unsigned, x) & 0x7F800000u) == 0x7F800000u; }
+  static __device__ __forceinline__ bool odd(float y) { return (__builtin_bit_cast(unsigned, y) & 0x7F800000u) == 0x7F800000u; }
   __device__ __forceinline__ bool strange(int i) const {
     bool s = false;
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) s |= odd(v[i][j >> 2][j & 3]);
+    for (int j = 0; j < D / 16; ++j) s |= odd(x[i][j >> 2][j & 3]);
     return s;
   }
   __device__ __forceinline__ void clear_strange(int i) {
 #pragma unroll
     for (int j = 0; j < D / 16; ++j)
-      if (odd(v[i][j >> 2][j & 3])) v[i][j >> 2][j & 3] = 0.f;
+      if (odd(x[i][j >> 2][j & 3])) x[i][j >> 2][j & 3] = 0.f;
   }
   static __device__ __forceinline__ int dim(int mt, int m) { return 64 * (mt >> 2) + 4 * m + (mt & 3); }
 };
@@ -99,10 +141,13 @@ __device__ __forceinline__ void store_some(float* p, const float* x, int n, floa
 
 template <int D, int NQ> constexpr int kFewLds = kWaves * 16 * NQ * (D + 2) * (int)sizeof(float);   // bytes
 
-// Work-group id of a part; lds: kFewLds bytes, 1024-byte aligned.
-template <typename T, int D, int NQ>
+// Work-group id of a part; lds: kFewLds bytes, 1024-byte aligned.  NT: rows are read once, past the caches.
+template <typename T, int D, int NQ, bool NT>
 __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part, int id, unsigned char* lds) {
-  using R = Rows<T, D>;
+  using Keys = KeyRows<T, D, NT>;
+  using Values = ValueRows<T, D, NT>;
+  constexpr int ROWS = Keys::kRows, TILES = ROWS / 16, PIECES = Keys::kChunks / 4;
+  static_assert(ROWS * D * (int)sizeof(T) <= 16 * NQ * D * (int)sizeof(float), "a wave's block of K fits where its results go");
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int MT = D / 16, QROWS = 16 * NQ, SIDE = kBf16 ? MT : 4;   // head-dims of a lane that lie side by side
   const Pages& c = a.c;
@@ -151,34 +196,36 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
   fewest = row_fewest(fewest);
   most = __builtin_amdgcn_readfirstlane(most);
   fewest = __builtin_amdgcn_readfirstlane(fewest);
-  uintx4 qf[NQ][R::kPieces];
+  uintx4 qf[NQ][PIECES];
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
     const uint8_t* p = static_cast<const uint8_t*>(a.q) + (row[qt] < 0 ? -1 - row[qt] : row[qt]) * (D * (int)sizeof(T)) + 16 * g;
 #pragma unroll
-    for (int s = 0; s < R::kPieces; ++s) qf[qt][s] = *reinterpret_cast<const uintx4*>(p + 64 * s);
+    for (int s = 0; s < PIECES; ++s) qf[qt][s] = *reinterpret_cast<const uintx4*>(p + 64 * s);
   }
 
   // ---- this wave's blocks of kRows keys: first + w, first + w + 4, ... ----
-  constexpr int PER = kKeys / R::kRows;
+  constexpr int PER = kKeys / ROWS;
   const int n_blocks = blocks_between(lo, most), begin = lo / kKeys;
   const int first = (begin + chunk_at(n_blocks, work.chunks, chunk)) * PER, last = (begin + chunk_at(n_blocks, work.chunks, chunk + 1)) * PER;
   const ConstInts table = as_const(c.table) + entry0 * c.table_stride;
   const int in_page = (1 << c.log2_rows) - 1;
   // Tiles of 16 rows lie in one page.  Tiles behind the last row that is seen, or in front of the first one, are the nearest again (their scores are masked).
-  const auto tile_row = [&](int blk, int t) { return max(min(blk * R::kRows + 16 * t, (most - 1) & ~15), lo & ~15); };
-  const auto pages_of = [&](int blk, int (&p)[R::kTiles]) {
+  const auto tile_row = [&](int blk, int t) { return max(min(blk * ROWS + 16 * t, (most - 1) & ~15), lo & ~15); };
+  const auto pages_of = [&](int blk, int (&p)[TILES]) {
 #pragma unroll
-    for (int t = 0; t < R::kTiles; ++t) p[t] = table[tile_row(blk, t) >> c.log2_rows];
+    for (int t = 0; t < TILES; ++t) p[t] = table[tile_row(blk, t) >> c.log2_rows];
   };
-  const unsigned k_off = col * (unsigned)c.stride_row + 16 * g;
-  R rows;
-  int pg[R::kTiles], bad = 0, next_bad = 0;   // pages of the next block; tiles of this and of the next one whose page is none
-  int64_t at[R::kTiles];                  // of the next block's tiles in k and v
+  Keys kr;
+  Values vr;
+  const unsigned stride = (unsigned)c.stride_row, k_off = Keys::lane_offset(stride, lane), v_off = Values::lane_offset(stride, g, col);
+  uintx4* const k_lds = reinterpret_cast<uintx4*>(&ring[w][0]);
+  int pg[TILES], bad = 0, next_bad = 0;   // pages of the next block; tiles of this and of the next one whose page is none
+  int64_t at[TILES];                  // of the next block's tiles in k and v
   const auto place = [&](int blk) {
     next_bad = 0;
 #pragma unroll
-    for (int t = 0; t < R::kTiles; ++t) {
+    for (int t = 0; t < TILES; ++t) {
       int p = pg[t];
       if (__builtin_expect((unsigned)p >= (unsigned)c.pages, 0)) {
         p = 0;
@@ -190,13 +237,11 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
   };
   const auto load_k = [&]() {
 #pragma unroll
-    for (int t = 0; t < R::kTiles; ++t)
-#pragma unroll
-      for (int s = 0; s < R::kPieces; ++s) rows.k[t][s] = *reinterpret_cast<const uintx4*>(c.k + at[t] + k_off + 64 * s);
+    for (int i = 0; i < Keys::kLoads; ++i) kr.load(i, c.k + at[Keys::tile(i)], stride, k_off);
   };
   const auto load_v = [&]() {
 #pragma unroll
-    for (int i = 0; i < R::kVRows; ++i) rows.load_v(i, c.v + at[R::v_tile(i)], (unsigned)R::v_row(i, g) * (unsigned)c.stride_row, col);
+    for (int i = 0; i < Values::kLoads; ++i) vr.load(i, c.v + at[Values::tile(i)], stride, v_off);
   };
   int blk = first + w;
   if (blk < last) {
@@ -224,38 +269,44 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
 
   for (; blk < last; blk += kWaves) {
     const bool more = blk + kWaves < last;
-    const int key0 = blk * R::kRows;
+    const int key0 = blk * ROWS;
     bad = next_bad;
-    floatx4 sc[R::kTiles][NQ];
+    wave_lds_order();   // the last reads of the block before
+    kr.put(k_lds, lane);
+    wave_lds_order();
+    int64_t here[TILES];
 #pragma unroll
-    for (int t = 0; t < R::kTiles; ++t)
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-        sc[t][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < R::kPieces; ++s) {
-          if constexpr (kBf16) {
-            sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rows.k[t][s]), __builtin_bit_cast(bf16x8, qf[qt][s]), sc[t][qt], 0, 0, 0);
-          } else {
-            const floatx4 x = __builtin_bit_cast(floatx4, rows.k[t][s]), y = __builtin_bit_cast(floatx4, qf[qt][s]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], sc[t][qt], 0, 0, 0);
-          }
-        }
-      }
-    int64_t here[R::kTiles];
-#pragma unroll
-    for (int t = 0; t < R::kTiles; ++t) here[t] = at[t];
+    for (int t = 0; t < TILES; ++t) here[t] = at[t];
     if (more) {
       place(blk + kWaves);
       load_k();
       if (blk + 2 * kWaves < last) pages_of(blk + 2 * kWaves, pg);
     }
-    const bool masked = key0 < lo || key0 + R::kRows > fewest || bad != 0;
+    floatx4 sc[TILES][NQ];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) sc[t][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < PIECES; ++s) {
+        const uintx4 k = Keys::get(k_lds, t, s, col, g);
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) {
+          if constexpr (kBf16) {
+            sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[qt][s]), sc[t][qt], 0, 0, 0);
+          } else {
+            const floatx4 x = __builtin_bit_cast(floatx4, k), y = __builtin_bit_cast(floatx4, qf[qt][s]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], sc[t][qt], 0, 0, 0);
+          }
+        }
+      }
+    }
+    const bool masked = key0 < lo || key0 + ROWS > fewest || bad != 0;
     bool apart = false;   // some queries see infinities or NaNs that others do not
     if (masked) {
 #pragma unroll
-      for (int t = 0; t < R::kTiles; ++t)
+      for (int t = 0; t < TILES; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int key = key0 + 16 * t + 4 * g + r;
@@ -267,10 +318,10 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
       // Rows that no query of the tile sees may hold anything: their probabilities are zero, and the product must not meet a NaN.
       bool strange = false;
 #pragma unroll
-      for (int i = 0; i < R::kVRows; ++i) {
-        const int t = R::v_tile(i), key = key0 + 16 * t + R::v_row(i, g);
-        if (key < lo || key >= most || (bad >> t & 1)) rows.clear_v(i);
-        strange |= key >= fewest && rows.strange(i);
+      for (int i = 0; i < Values::kLoads; ++i) {
+        const int t = Values::tile(i), key = key0 + 16 * t + Values::row(i, g, col);
+        if (key < lo || key >= most || (bad >> t & 1)) vr.clear(i);
+        strange |= key >= fewest && vr.strange(i);
       }
       apart = __any(strange);
     }
@@ -281,7 +332,7 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
     for (int qt = 0; qt < NQ; ++qt) {
       float mx = sc[0][qt][0];
 #pragma unroll
-      for (int j = 1; j < 4 * R::kTiles; ++j) mx = maximum(mx, sc[j >> 2][qt][j & 3]);
+      for (int j = 1; j < 4 * TILES; ++j) mx = maximum(mx, sc[j >> 2][qt][j & 3]);
       m_new[qt] = maximum(mc[qt], quad_maximum(mx) * c2);
       moved |= m_new[qt] != mc[qt];
     }
@@ -299,7 +350,7 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
       }
     }
 #pragma unroll
-    for (int t = 0; t < R::kTiles; ++t)
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
       for (int qt = 0; qt < NQ; ++qt)
 #pragma unroll
@@ -308,22 +359,22 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
       // Each query takes what it sees: key by key, elements that are no numbers, and the product below goes without them.
       float* const p_sh = &ring[w][0];   // [key, query]
 #pragma unroll
-      for (int t = 0; t < R::kTiles; ++t)
+      for (int t = 0; t < TILES; ++t)
 #pragma unroll
         for (int qt = 0; qt < NQ; ++qt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) p_sh[(16 * t + 4 * g + r) * QROWS + 16 * qt + col] = sc[t][qt][r];
       wave_lds_order();
 #pragma unroll 1
-      for (int x = 0; x < R::kRows; ++x) {
+      for (int x = 0; x < ROWS; ++x) {
         const int key = key0 + x, t = x >> 4;
         if (key < lo || key >= most || (bad >> t & 1)) continue;
-        const T* vr = reinterpret_cast<const T*>(c.v + (t ? here[R::kTiles - 1] : here[0]) + (x & 15) * c.stride_row);
+        const T* v_row = reinterpret_cast<const T*>(c.v + (t ? here[TILES - 1] : here[0]) + (x & 15) * c.stride_row);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float y = (float)vr[R::dim(mt, 4 * g + r)];
+            const float y = (float)v_row[Values::dim(mt, 4 * g + r)];
             if ((__builtin_bit_cast(unsigned, y) & 0x7F800000u) != 0x7F800000u) continue;
 #pragma unroll
             for (int qt = 0; qt < NQ; ++qt)
@@ -332,7 +383,7 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
       }
       wave_lds_order();
 #pragma unroll
-      for (int i = 0; i < R::kVRows; ++i) rows.clear_strange(i);
+      for (int i = 0; i < Values::kLoads; ++i) vr.clear_strange(i);
     }
     if constexpr (kBf16) {
       bf16x8 pf[NQ];
@@ -343,10 +394,13 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
         ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[qt], ls[qt], 0, 0, 0);   // sums over the numbers that the product below uses
       }
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const bf16x8 vf = rows.v_operand(mt);
+      for (int mt = 0; mt < MT; mt += 2) {
+        bf16x8 vf[2];
+        vr.operands(mt / 2, col, vf);
 #pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], o[mt][qt], 0, 0, 0);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int qt = 0; qt < NQ; ++qt) o[mt + i][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], pf[qt], o[mt + i][qt], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -356,7 +410,7 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
           ls[qt][0] += sc[0][qt][r];
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
-            o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(rows.v[r][mt >> 2][mt & 3], sc[0][qt][r], o[mt][qt], 0, 0, 0);
+            o[mt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr.x[r][mt >> 2][mt & 3], sc[0][qt][r], o[mt][qt], 0, 0, 0);
         }
     }
     if (more) load_v();
@@ -419,7 +473,7 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
     const int64_t prow = a.part[part].row0 + slot * QROWS + 16 * qt + col;
 #pragma unroll
     for (int mt = 0; mt < MT; mt += SIDE) {
-      const int d = R::dim(mt, 4 * g + w);
+      const int d = Values::dim(mt, 4 * g + w);
       if (whole) store_some(static_cast<T*>(a.out) + row[qt] * D + d, acc + mt, SIDE, inv);
       else store_some(a.part_o + prow * D + d, acc + mt, SIDE, 1.f);
     }

@@ -513,6 +513,7 @@ extern "C" hack_status hack_create(hack_ctx** out, const hack_config* cfg) {
     const int n = std::atoi(v);
     ctx->packed_queries = n == 16 || n == 32 || n == 128 ? n : 0;
   }
+  if (const char* v = std::getenv("HACK_ATTN_PAGES_SHARED")) ctx->share_bytes = std::max(std::atoll(v), 0ll);   // A/B and test override
   hipError_t e = hipSetDevice(cfg->device);
   const size_t n_ws = (size_t)cfg->max_units * ctx->ws_stride;
   if (e == hipSuccess) e = hipMalloc((void**)&ctx->importance, n_ws * sizeof(float));

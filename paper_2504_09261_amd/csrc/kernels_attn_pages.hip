@@ -17,11 +17,11 @@ namespace {
 
 using namespace dev;
 
-template <typename T, int D, int NQ>
-__global__ __launch_bounds__(kThreads, 2) void attn_pages(const AttnPagesArgs a) {
+template <typename T, int D, int NQ, bool NT>
+__global__ __launch_bounds__(kThreads, D == 128 ? 2 : NQ == 1 ? 4 : 3) void attn_pages(const AttnPagesArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kFewLds<D, NQ>];
   const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0, part = (int)blockIdx.x >= grid0 ? 1 : 0;
-  attn_pages_few<T, D, NQ>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
+  attn_pages_few<T, D, NQ, NT>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
 }
 
 // Rows with partial results: ROWS of them a work-group, each by 256 / ROWS threads, D / 4 lanes a slot, which walk over its slots.
@@ -124,8 +124,16 @@ void launch_some(hipStream_t s, bool merge, AttnPagesArgs& a) {
     launch_attn_pages_tiles(s, D, a);
   } else {
     const dim3 grid((unsigned)(part_grid(a, 0) + part_grid(a, 1)));
-    if (a.part[1].queries == 16) hipLaunchKernelGGL((attn_pages<T, D, 1>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((attn_pages<T, D, 2>), grid, dim3(kThreads), 0, s, a);
+    const bool once = reads_once(a);
+#define HACK_ATTN_PAGES(NQ, NT) hipLaunchKernelGGL((attn_pages<T, D, NQ, NT>), grid, dim3(kThreads), 0, s, a)
+    if (a.part[1].queries == 16) {
+      if (once) HACK_ATTN_PAGES(1, true);
+      else HACK_ATTN_PAGES(1, false);
+    } else {
+      if (once) HACK_ATTN_PAGES(2, true);
+      else HACK_ATTN_PAGES(2, false);
+    }
+#undef HACK_ATTN_PAGES
   }
   if (!merge) return;
   const int64_t rows = (int64_t)a.batch * a.c.heads * a.G * a.c.n;

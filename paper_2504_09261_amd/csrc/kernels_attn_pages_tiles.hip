@@ -522,20 +522,25 @@ __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesA
 }
 
 // Shared rows by tiles, own rows by few queries: the products of the one beside the loads of the other.
-template <int D, int NQ>
+template <int D, int NQ, bool NT>
 __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_mixed(const AttnPagesArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[std::max(kTileLds<D>, kFewLds<D, NQ>)];
   const int grid0 = (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles;
   if ((int)blockIdx.x < grid0) tile_part<D>(a, 0, blockIdx.x, lds);
-  else attn_pages_few<__bf16, D, NQ>(a, 1, blockIdx.x - grid0, lds);
+  else attn_pages_few<__bf16, D, NQ, NT>(a, 1, blockIdx.x - grid0, lds);
 }
 
 template <int D>
 void launch_some(hipStream_t s, const AttnPagesArgs& a) {
   const dim3 grid((unsigned)(part_grid(a, 0) + part_grid(a, 1)));
-  if (a.part[1].queries == 16) hipLaunchKernelGGL((attn_pages_mixed<D, 1>), grid, dim3(64 * kNW), 0, s, a);
-  else if (a.part[1].queries == 32) hipLaunchKernelGGL((attn_pages_mixed<D, 2>), grid, dim3(64 * kNW), 0, s, a);
+  const bool once = reads_once(a);
+#define HACK_ATTN_MIXED(NQ, NT) hipLaunchKernelGGL((attn_pages_mixed<D, NQ, NT>), grid, dim3(64 * kNW), 0, s, a)
+  if (a.part[1].queries == 16 && once) HACK_ATTN_MIXED(1, true);
+  else if (a.part[1].queries == 16) HACK_ATTN_MIXED(1, false);
+  else if (a.part[1].queries == 32 && once) HACK_ATTN_MIXED(2, true);
+  else if (a.part[1].queries == 32) HACK_ATTN_MIXED(2, false);
   else hipLaunchKernelGGL((attn_pages_tiles<D>), grid, dim3(64 * kNW), 0, s, a);
+#undef HACK_ATTN_MIXED
 }
 
 }  // namespace

@@ -7,8 +7,6 @@ using namespace hack;
 
 namespace {
 
-int TUNE(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
-
 struct Dim { int64_t stride, count; };
 
 // Whether rows of `width` bytes at the multiples of nested dimensions (the widest first), and the same ones delta bytes on, keep clear of each other.
@@ -83,7 +81,8 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
   AttnPart* const part = a->part;
   const auto rows_of = [](const AttnPart& p, int64_t entries) { return entries * p.tiles * p.queries; };   // of partial results, without a cut
   const auto lay_out = [&](int i, int64_t queries, int tile) {
-    part[i] = AttnPart{tile, (int32_t)((queries + tile - 1) / tile), 0, tile == kPageTileQueries ? TUNE("T_LEAST", 24) : TUNE("F_LEAST", 8), 0.f, 0};
+    const bool large = tile == kPageTileQueries;
+    part[i] = AttnPart{tile, (int32_t)((queries + tile - 1) / tile), 0, large ? 48 : 24, large ? 16 : 4, 0.f, 0.f, 0};
   };
   int64_t most = 0, saved = 0;   // queries of a group; bytes that sharing spares
   for (int i = 0; i < a->n_shared; ++i) {
@@ -91,7 +90,7 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
     most = std::max(most, s.count * GN);
     saved += (int64_t)(s.count - 1) * s.rows * H * 2 * ctx->cfg.head_dim * ctx->elem_bytes;
   }
-  if (saved < ((int64_t)TUNE("SAVED", 16) << 20)) a->n_shared = 0;
+  if (saved < ctx->share_bytes) a->n_shared = 0;
   const int own_tile = tile_queries(ctx, GN), shared_tile = tile_queries(ctx, most);
   lay_out(1, GN, own_tile);
   lay_out(0, most, shared_tile == kPageTileQueries ? shared_tile : own_tile);   // tiles of 16 and of 32 are not mixed
@@ -99,14 +98,15 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
   const int64_t shared_rows = rows_of(part[0], a->n_shared * H);
   const int64_t spare = (ctx->part_rows - shared_rows - rows_of(part[1], units)) / (a->n_shared ? 2 : 1);   // rows that the chunks of a part may take beyond
   const bool large = own_tile == kPageTileQueries || (a->n_shared && shared_tile == kPageTileQueries);
-  const int64_t want = (large || own_tile == 32 ? TUNE("T_WANT", 2) : TUNE("F_WANT", 3)) * (int64_t)ctx->cus;   // work-groups that the device holds at once
+  const int64_t want = (large ? 2 : 4) * (int64_t)ctx->cus;
   int64_t rows = 0, groups = 0;
   for (int i = 0; i < 2; ++i) {
     AttnPart& p = part[i];
     const int64_t pairs = i ? units : a->n_shared * H;
-    const int64_t cuts = (((int64_t)a->c.max_len + kKeys - 1) / kKeys + p.least) / p.least;   // chunks of an entry at most
+    const int64_t blocks = ((int64_t)a->c.max_len + kKeys - 1) / kKeys + 1, cuts = blocks <= p.uncut ? 1 : (blocks + p.least - 1) / p.least;   // chunks of an entry at most
     const int64_t more = std::min(want, spare / p.queries);
     p.share = more > 0 && cuts > 1 && pairs > 0 ? (float)more : 0.f;
+    p.fill = (float)std::min<int64_t>(more, ctx->cus);
     p.pairs = (int32_t)std::min(pairs * cuts, p.share > 0.f ? (more + pairs * p.tiles) / p.tiles : pairs);
     p.row0 = rows;
     rows += (int64_t)p.pairs * p.tiles * p.queries;

@@ -44,8 +44,10 @@ struct AttnPart {
   int32_t queries;    // of a tile: 16, 32 or kPageTileQueries
   int32_t tiles;      // of an entry's queries
   int32_t pairs;      // (entry, head, chunk) at most
+  int32_t uncut;      // entries of up to so many blocks are not cut where none is longer
   int32_t least;      // blocks of a chunk at least
   float share;        // work-groups that the blocks of its launch are cut for; 0: no cuts
+  float fill;         // work-groups that fill the device
   int64_t row0;       // first row of its partial results
 };
 constexpr int kPageTileQueries = 128;
@@ -67,18 +69,23 @@ struct AttnPagesHead {
 struct AttnPagesArgs : AttnPagesHead {
   Shared shared[kMostShared];
 };
-// How the kernels cut: blocks that hold rows lo to hi, blocks of a chunk where all entries have `total` (times heads and tiles of queries), chunks of an entry.
+// How the kernels cut: blocks that hold rows lo to hi; blocks of a chunk where the launch has `total` (times heads and tiles of queries) and the part's longest entry
+// `longest`; chunks of an entry.  Shorter chunks than kChunk only as far as work-groups are missing.
+constexpr float kChunk = 32.f;
 __host__ __device__ inline int blocks_between(int lo, int hi) { return hi > lo ? (hi + kKeys - 1) / kKeys - lo / kKeys : 0; }
-__host__ __device__ inline int chunk_blocks(float total, float share, int least) {
-  const float each = share > 0.f ? total / share : 1e9f;
-  const int whole = (int)(each < 1e9f ? each : 1e9f);
-  return whole < least ? least : whole + 1;
+__host__ __device__ inline int chunk_blocks(float total, int longest, const AttnPart& p) {
+  if (p.share == 0.f || longest <= p.uncut) return 1 << 30;
+  const float each = total / p.share, full = total / p.fill < kChunk ? total / p.fill : kChunk, most = each > full ? each : full;
+  const int whole = (int)(most < 1e9f ? most : 1e9f);
+  return whole < p.least ? p.least : whole + 1;
 }
 __host__ __device__ inline int entry_chunks(int blocks, int chunk) { return blocks > chunk ? chunks_of(blocks, chunk) : 1; }
 constexpr int64_t pairs_grid(int64_t pairs, int64_t tiles) { return (pairs + 7) / 8 * 8 * tiles; }
 // merge: partial results may have to be joined.
 void launch_attn_pages(hipStream_t s, int elem_bytes, int head_dim, bool merge, AttnPagesArgs a);
 void launch_attn_pages_tiles(hipStream_t s, int head_dim, const AttnPagesArgs& a);   // where a part has tiles of kPageTileQueries queries; bf16
+// Whether every row of K and V is read by one work-group, whose loads then pass the caches by.
+inline bool reads_once(const AttnPagesArgs& a) { return a.part[1].tiles == 1 && (!(a.parts & 1) || a.part[0].tiles == 1 || a.part[0].queries == kPageTileQueries); }
 // Work-groups of part p in the launch.
 inline int64_t part_grid(const AttnPagesArgs& a, int p) { return a.parts >> p & 1 ? pairs_grid(a.part[p].pairs, a.part[p].tiles) : 0; }
 

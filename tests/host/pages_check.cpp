@@ -226,12 +226,15 @@ int cache_refusals() {
 int attn_refusals() {
   Context c;
   hack_pages p = pages();
+  p.table_pages = p.table_stride = 2000;
+  p.len = at<int32_t>(kC + 0x10000);
   const auto run = [&](const hack_shared* s, int n, int B = 2, int N = 1, int heads = 8, void* out = at(kF), float scale = 0.1f) {
     return hack_attn_pages(c.ctx, B, N, heads, at(kE), &p, nullptr, 0, s, n, scale, out, kStream);
   };
-  const hack_shared both[] = {{0, 2, 640}}, each[] = {{0, 1, 64}, {1, 1, 64}};
+  const hack_shared both[] = {{0, 2, 100000}}, each[] = {{0, 1, 100000}, {1, 1, 100000}}, little[] = {{0, 2, 640}};
   CHECK(run(both, 1) == HACK_OK && stub::attentions.back().a.n_shared == 1 && stub::attentions.back().merge);
   CHECK(run(each, 2) == HACK_OK && stub::attentions.back().a.n_shared == 0);   // nothing is shared
+  CHECK(run(little, 1) == HACK_OK && stub::attentions.back().a.n_shared == 0); // not worth a launch that joins
   CHECK(run(both, 0) == HACK_OK && stub::attentions.back().a.n_shared == 0);
   REFUSED(HACK_EINVAL, hack_attn_pages(nullptr, 2, 1, 8, at(kE), &p, nullptr, 0, nullptr, 0, 0.1f, at(kF), kStream));
   REFUSED(HACK_EINVAL, hack_attn_pages(c.ctx, 2, 1, 8, nullptr, &p, nullptr, 0, nullptr, 0, 0.1f, at(kF), kStream));
@@ -253,7 +256,7 @@ int attn_refusals() {
   REFUSED(HACK_ECAPACITY, run(both, 1, 2, 513));
   REFUSED(HACK_EINVAL, run(both, 1, 1));   // a group beyond the batch
   const hack_shared wrong[][2] = {{{1, 1, 5}, {0, 1, 5}}, {{0, 2, 5}, {1, 1, 5}}, {{-1, 1, 5}, {1, 1, 5}}, {{0, 0, 5}, {1, 1, 5}},
-                                  {{0, 1, -1}, {1, 1, 5}}, {{0, 1, 20 * 64 + 1}, {1, 1, 5}}, {{0, INT32_MAX, 5}, {1, 1, 5}}};
+                                  {{0, 1, -1}, {1, 1, 5}}, {{0, 1, 2000 * 64 + 1}, {1, 1, 5}}, {{0, INT32_MAX, 5}, {1, 1, 5}}};
   for (const auto& w : wrong) REFUSED(HACK_EINVAL, run(w, 2));
   // more queries than a launch takes: 2^31 - 64 rows
   REFUSED(HACK_ECAPACITY, run(nullptr, 0, 2, 512, 4 << 19));
@@ -317,7 +320,8 @@ int plans() {
       int64_t pairs[2] = {}, rows = 0;
       bool joined = a.n_shared > 0;
       for (int part = 0; part < 2; ++part) {
-        const int chunk = chunk_blocks(total[part], a.part[part].share, a.part[part].least);
+        const int longest = blocks[part].empty() ? 0 : *std::max_element(blocks[part].begin(), blocks[part].end());
+        const int chunk = chunk_blocks(total[part], longest, a.part[part]);
         for (int n : blocks[part]) {
           pairs[part] += (int64_t)mult[part] * entry_chunks(n, chunk);
           joined |= entry_chunks(n, chunk) > 1;

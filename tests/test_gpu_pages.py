@@ -1,5 +1,7 @@
 """Caches in pages (appending with norm and rotation, attention for tokens, scales and causal prompts, shared prefixes) against plain implementations in
 64 bits, through the C ABI.  Tolerances count roundings: half a step of a type is finfo.eps / 2 relative, H below is float32's."""
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -14,10 +16,15 @@ pytestmark = pytest.mark.gpu
 def contexts():
     made = {}
 
-    def get(heads, d, dtype, units=64, queries=4096):
-        key = (heads, d, dtype, units, queries)
+    def get(heads, d, dtype, units=64, queries=4096, shared=None):
+        key = (heads, d, dtype, units, queries, shared)
         if key not in made:
-            made[key] = Hack(heads, d, dtype, units, 64, queries)
+            if shared is not None:
+                os.environ["HACK_ATTN_PAGES_SHARED"] = str(shared)      # read when a context is created
+            try:
+                made[key] = Hack(heads, d, dtype, units, 64, queries)
+            finally:
+                os.environ.pop("HACK_ATTN_PAGES_SHARED", None)
         return made[key]
     yield get
     for h in made.values():
@@ -170,9 +177,9 @@ def test_causal_attention_of_ragged_batches(contexts, dtype, d, page, layout, by
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d, page, by_head", [(64, 16, False), (128, 64, False), (128, 32, True)])
-@pytest.mark.parametrize("n, group", [(1, 1), (1, 8), (5, 3), (40, 1)])
+@pytest.mark.parametrize("n, group", [(1, 1), (1, 8), (5, 3), (40, 1), (60, 2)])
 def test_shared_rows(contexts, dtype, d, page, by_head, n, group):
-    hk = contexts(2, d, dtype)
+    hk = contexts(2, d, dtype, shared=0)
     g = torch.Generator(DEV).manual_seed(n + group)
     # groups of four and two, the rest alone; shared rows that end inside a page, an element shorter than what it shares
     lens = np.array([700, 513, 600, 530, 90, 200, 333, 64]) + n
@@ -196,7 +203,7 @@ def test_shared_rows(contexts, dtype, d, page, by_head, n, group):
 @pytest.mark.parametrize("dtype, d, batch, group, prefix", [("bf16", 128, 24, 8, 4100), ("f32", 64, 10, 4, 3000), ("bf16", 64, 3, 1, 9000)])
 def test_long_shared_prefix(contexts, dtype, d, batch, group, prefix):
     """Many queries of many elements over one prefix, cut into chunks, and ragged rows of their own."""
-    hk = contexts(2, d, dtype)
+    hk = contexts(2, d, dtype, shared=0)
     g = torch.Generator(DEV).manual_seed(batch)
     lens = prefix + (np.arange(batch) * 37) % 400
     pool = Pool(hk, lens, 64, g, shared=[(0, batch, prefix // 64 * 64)])
@@ -462,7 +469,7 @@ def test_serving_run(contexts, dtype, d, prefix):
     """A shared prefix, prompts of different lengths, then tokens: queries and keys of one projection, appended, then attended to; the tokens in a captured graph,
     whose lengths grow in device memory, with eager work between replays."""
     B, K, G, N, tokens = 3, 2, 2, 50, 40
-    hk = contexts(K, d, dtype)
+    hk = contexts(K, d, dtype, shared=0)
     g = torch.Generator(DEV).manual_seed(d)
     fresh = np.array([50, 13, 31])
     pool = Pool(hk, prefix + fresh, 16, g, shared=[(0, B, prefix)] if prefix else (), extra=tokens)
