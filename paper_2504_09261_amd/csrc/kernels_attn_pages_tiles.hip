@@ -56,8 +56,9 @@ constexpr int steps_before(int s, int slots) {   // in front of slot s
 
 template <int D> constexpr int kTileLds = 2 * kNS * kKeys * D * 2 + kRing * 16 + (2 * kNW + 1) * 4;   // bytes
 
-// Work-group id of a part; lds: kTileLds bytes, 1024-byte aligned.
-template <int D>
+// Work-group id of a part; lds: kTileLds bytes, 1024-byte aligned.  HALF: no tile has more than 64 queries, and waves without one stand aside, out of the way of
+// those that have (64 queries of 480 units over 604 to 668 rows at head_dim 64: 24.7 us, so 22.5; the code for it costs tiles of 128 up to 6 %).
+template <int D, bool HALF>
 __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int id, unsigned char* lds) {
   constexpr int KC = D / 32;        // MFMA steps over head_dim for S^T
   constexpr int MT = D / 16;        // 16-row tiles of O^T
@@ -105,11 +106,13 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   };
   int sees[2];
   int most = 0, fewest = c.max_len;
+  bool any = false;
   const __bf16* qrow[2];
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
     const Query q = query(w * 32 + 16 * qt + col);
     sees[qt] = q.sees;
+    any |= q.there;
     if (q.there) {
       most = max(most, q.sees);
       fewest = min(fewest, q.sees);
@@ -118,6 +121,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   }
   most = row_most(most);
   fewest = row_fewest(fewest);
+  const bool idle = HALF && __ballot(any) == 0;   // a wave without queries only copies
   if (lane == 0) {
     most_sh[w] = most;
     fewest_sh[w] = fewest;
@@ -216,204 +220,216 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
     }
     Places next_k = places_of(kNS), next_v = places_of(2);   // of the copies of the next stage
 
-    // Q fragments (B operand of S^T = K Q^T): query 16 qt + col, head-dim slice [32kc + 8g, +8); consumed here, so that a wait for them does not drain the
-    // copies that are meant to stay in flight later.
-    bf16x8 qf[2][KC];
-#pragma unroll
-    for (int qt = 0; qt < 2; ++qt)
-#pragma unroll
-      for (int kc = 0; kc < KC; ++kc) qf[qt][kc] = *reinterpret_cast<const bf16x8*>(qrow[qt] + 32 * kc);
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc) asm volatile("" ::"v"(qf[0][kc]), "v"(qf[1][kc]));
-
-    const float c2 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.scale * kLog2eF)));
-    const int e = col >> 2, qd = col & 3;
-    const int k_off = e * 4 * D + (col & 3) * 32 + (g ^ e) * 8;   // K operand: row 16kt + col, chunk 4kc + g
-    // V^T operand: rows 4g + e and 16 + 4g + e, head-dim 16mt + 4qd; even and odd mt
-    const int v_even = g * 4 * D + e * 32 + (2 * (g & 1) + (qd >> 1)) * 8 + 4 * (qd & 1), v_odd = v_even ^ 16;
-    bf16x8 ones;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
-    asm volatile("" : "+v"(ones));   // stays in registers
-
-    struct Scores { floatx4 t[2][2]; };   // keys 16kt + 4g + r, query 16qt + col
-    const auto mask = [&](Scores& sc, int blk) __attribute__((always_inline)) {
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int key = blk * kKeys + 16 * kt + 4 * g + r;
-#pragma unroll
-          for (int qt = 0; qt < 2; ++qt)
-            if (key < lo || key >= sees[qt]) sc.t[kt][qt][r] = -INFINITY;
-        }
-    };
-    const auto probs = [&](const Scores& sc, int qt, bf16x8& pf) __attribute__((always_inline)) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) pf[j] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc.t[j >> 2][qt][j & 3], c2, -mc[qt]));
-    };
-    const auto too_large = [&](const bf16x8 (&pf)[2]) __attribute__((always_inline)) -> bool {
-      const uintx4 x = __builtin_bit_cast(uintx4, pf[0]), y = __builtin_bit_cast(uintx4, pf[1]);
-      return (((x[0] | x[1] | x[2]) | x[3] | y[0]) | y[1] | y[2] | y[3]) & 0x40004000u;
-    };
-    const auto rescale = [&](const Scores& sc, bf16x8 (&pf)[2]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int qt = 0; qt < 2; ++qt) {
-        float mx = sc.t[0][qt][0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc.t[j >> 2][qt][j & 3]);
-        const float m_new = fmaxf(mc[qt], fmaf(quad_max(mx), c2, kHeadroom));
-        const float f = __builtin_amdgcn_exp2f(mc[qt] - m_new);
-        mc[qt] = m_new;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          ls[qt][r] *= f;
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) o[mt][qt][r] *= f;
-        }
-        probs(sc, qt, pf[qt]);
+    if (idle) {
+      dma_wait_but<0>();
+      __syncthreads();
+      for (int j = 0; j < n_blocks - 1; ++j) {
+        if (j > 0 && j % (kRing / 2) == 0) fill(j + kRing / 2);
+        wait_and_sync<2 * IPW>();
+        issue(k_lane, places_of(j + kNS), j % kNS, j + kNS, ks_lds);
+        issue(v_lane, places_of(j + 2), (j + 2) % kNS, j + 2, vs_lds);
       }
-    };
-    // Operands of step i of a stage: head-dim slice i of S^T and two head-dim tiles of O^T.
-    struct Frags {
-      bf16x8 k[2];
-      bf16x4 v[2][2];
-    };
-    const auto load_frag = [&](Frags& f, const __bf16* Kt, const __bf16* Vt, int i, int p) __attribute__((always_inline)) {   // one LDS read, p 0 .. 5
-      if (p < 2) f.k[p] = *reinterpret_cast<const bf16x8*>(&Kt[16 * p * D + 128 * i + k_off]);
-      else f.v[(p >> 1) - 1][p & 1] = lds_read_tr(&Vt[16 * (p & 1) * D + 128 * i + ((p >> 1) - 1 ? v_odd : v_even)]);
-    };
-    const auto joined = [](const bf16x4 (&v)[2]) __attribute__((always_inline)) { return bf16x8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]}; };
-    const auto qk = [&](Scores& sn, const Frags& f, int kc, int n) __attribute__((always_inline)) {
-      const int kt = n >> 1, qt = kt ^ (n & 1);
-      sn.t[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.k[kt], qf[qt][kc], sn.t[kt][qt], 0, 0, 0);
-    };
-    const auto pv = [&](const Frags& f, const bf16x8 (&p)[2], int i, int n) __attribute__((always_inline)) {
-      const int m = n >> 1, qt = m ^ (n & 1);
-      o[2 * i + m][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(joined(f.v[m]), p[qt], o[2 * i + m][qt], 0, 0, 0);
-    };
-    const auto row_sums = [&](const bf16x8 (&p)[2], int qt) __attribute__((always_inline)) { ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[qt], ls[qt], 0, 0, 0); };
-
-    bf16x8 P[2][2];   // probabilities of block j in P[j & 1]: those of the previous block wait for their PV product
-    Frags pre;        // operands of the next stage's first step
-
-    // Stage j, slot S = j % 4 (compile time).  On entry sc = scores of block j, on exit those of block j + 1.  FIRST: j = 0 (no previous block).
-    // FULL: blocks from j + 1 on are not masked.
-    auto stage = [&](auto slot_tag, auto first_tag, auto full_tag, int j, Scores& sc) __attribute__((always_inline)) {
-      constexpr int S = decltype(slot_tag)::value;
-      constexpr bool FIRST = decltype(first_tag)::value, FULL = decltype(full_tag)::value;
-      const __bf16* const Kt = &Ks[(S + 1) % kNS][0];
-      const __bf16* const Vt = &Vs[(S + 3) % kNS][0];
-      Scores sn;
+      wait_and_sync<0>();
+    } else {
+      // Q fragments (B operand of S^T = K Q^T): query 16 qt + col, head-dim slice [32kc + 8g, +8); consumed here, so that a wait for them does not drain the
+      // copies that are meant to stay in flight later.
+      bf16x8 qf[2][KC];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sn.t[i >> 1][i & 1] = floatx4{0.f, 0.f, 0.f, 0.f};
-      bf16x8 (&pp)[2] = P[(S + 1) & 1], (&pf)[2] = P[S & 1];
-      Frags f = pre, nx;
-      float x[16];
-      auto vec_op = [&](auto t_tag) __attribute__((always_inline)) {
-        constexpr Step op = softmax_step(decltype(t_tag)::value);
-        constexpr int i = op.index, qt = (i >> 3) & 1, jj = i & 7;
-        if constexpr (op.kind == 0) x[i] = fmaf(sc.t[jj >> 2][qt][jj & 3], c2, -mc[qt]);
-        else if constexpr (op.kind == 1) x[i] = __builtin_amdgcn_exp2f(x[i]);
-        else { pf[qt][jj] = (__bf16)x[i]; pf[qt][jj + 1] = (__bf16)x[i + 1]; }
+      for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) qf[qt][kc] = *reinterpret_cast<const bf16x8*>(qrow[qt] + 32 * kc);
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) asm volatile("" ::"v"(qf[0][kc]), "v"(qf[1][kc]));
+
+      const float c2 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.scale * kLog2eF)));
+      const int e = col >> 2, qd = col & 3;
+      const int k_off = e * 4 * D + (col & 3) * 32 + (g ^ e) * 8;   // K operand: row 16kt + col, chunk 4kc + g
+      // V^T operand: rows 4g + e and 16 + 4g + e, head-dim 16mt + 4qd; even and odd mt
+      const int v_even = g * 4 * D + e * 32 + (2 * (g & 1) + (qd >> 1)) * 8 + 4 * (qd & 1), v_odd = v_even ^ 16;
+      bf16x8 ones;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
+      asm volatile("" : "+v"(ones));   // stays in registers
+
+      struct Scores { floatx4 t[2][2]; };   // keys 16kt + 4g + r, query 16qt + col
+      const auto mask = [&](Scores& sc, int blk) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int key = blk * kKeys + 16 * kt + 4 * g + r;
+#pragma unroll
+            for (int qt = 0; qt < 2; ++qt)
+              if (key < lo || key >= sees[qt]) sc.t[kt][qt][r] = -INFINITY;
+          }
       };
-      constexpr int SLOTS = 8 * KC + 2, VEC_SLOTS = SLOTS - 3 * KC / 4;   // the vector work ends early: its test travels beside the last MFMAs
-      bool large = false;
-      auto slot = [&](auto s_tag) __attribute__((always_inline)) {
-        constexpr int T = decltype(s_tag)::value, I = T / 8 < KC ? T / 8 : KC - 1, N = T - 8 * I;   // the last step has two more
-        // one wait for both K operands (lgkmcnt(4)) and one for both of V^T (lgkmcnt(2)) instead of one for each
-        if constexpr (N == 0) __builtin_amdgcn_s_waitcnt(0xC47F);
-        if constexpr (N == 4) __builtin_amdgcn_s_waitcnt(0xC27F);
-        if constexpr (N < 4) qk(sn, f, I, N);
-        else if constexpr (N < 8) { if (!FIRST) pv(f, pp, I, N - 4); }
-        else { if (!FIRST) row_sums(pp, N - 8); }
-        for_each<steps_before(T, VEC_SLOTS), steps_before(T + 1, VEC_SLOTS)>(vec_op);
-        if constexpr (T == VEC_SLOTS) large = __any(too_large(pf));
-        if constexpr (N < 2 || (N >= 4 && N < 8)) {
-          constexpr int p = N < 2 ? N : N - 2;
-          if constexpr (I + 1 < KC) load_frag(nx, Kt, Vt, I + 1, p);
-          else load_frag(nx, &Ks[(S + 2) % kNS][0], &Vs[S][0], 0, p);
+      const auto probs = [&](const Scores& sc, int qt, bf16x8& pf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pf[j] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc.t[j >> 2][qt][j & 3], c2, -mc[qt]));
+      };
+      const auto too_large = [&](const bf16x8 (&pf)[2]) __attribute__((always_inline)) -> bool {
+        const uintx4 x = __builtin_bit_cast(uintx4, pf[0]), y = __builtin_bit_cast(uintx4, pf[1]);
+        return (((x[0] | x[1] | x[2]) | x[3] | y[0]) | y[1] | y[2] | y[3]) & 0x40004000u;
+      };
+      const auto rescale = [&](const Scores& sc, bf16x8 (&pf)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt) {
+          float mx = sc.t[0][qt][0];
+#pragma unroll
+          for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc.t[j >> 2][qt][j & 3]);
+          const float m_new = fmaxf(mc[qt], fmaf(quad_max(mx), c2, kHeadroom));
+          const float f = __builtin_amdgcn_exp2f(mc[qt] - m_new);
+          mc[qt] = m_new;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            ls[qt][r] *= f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) o[mt][qt][r] *= f;
+          }
+          probs(sc, qt, pf[qt]);
         }
-        if constexpr (N == 7 && I + 1 < KC) f = nx;
+      };
+      // Operands of step i of a stage: head-dim slice i of S^T and two head-dim tiles of O^T.
+      struct Frags {
+        bf16x8 k[2];
+        bf16x4 v[2][2];
+      };
+      const auto load_frag = [&](Frags& f, const __bf16* Kt, const __bf16* Vt, int i, int p) __attribute__((always_inline)) {   // one LDS read, p 0 .. 5
+        if (p < 2) f.k[p] = *reinterpret_cast<const bf16x8*>(&Kt[16 * p * D + 128 * i + k_off]);
+        else f.v[(p >> 1) - 1][p & 1] = lds_read_tr(&Vt[16 * (p & 1) * D + 128 * i + ((p >> 1) - 1 ? v_odd : v_even)]);
+      };
+      const auto joined = [](const bf16x4 (&v)[2]) __attribute__((always_inline)) { return bf16x8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]}; };
+      const auto qk = [&](Scores& sn, const Frags& f, int kc, int n) __attribute__((always_inline)) {
+        const int kt = n >> 1, qt = kt ^ (n & 1);
+        sn.t[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.k[kt], qf[qt][kc], sn.t[kt][qt], 0, 0, 0);
+      };
+      const auto pv = [&](const Frags& f, const bf16x8 (&p)[2], int i, int n) __attribute__((always_inline)) {
+        const int m = n >> 1, qt = m ^ (n & 1);
+        o[2 * i + m][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(joined(f.v[m]), p[qt], o[2 * i + m][qt], 0, 0, 0);
+      };
+      const auto row_sums = [&](const bf16x8 (&p)[2], int qt) __attribute__((always_inline)) { ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[qt], ls[qt], 0, 0, 0); };
+
+      bf16x8 P[2][2];   // probabilities of block j in P[j & 1]: those of the previous block wait for their PV product
+      Frags pre;        // operands of the next stage's first step
+
+      // Stage j, slot S = j % 4 (compile time).  On entry sc = scores of block j, on exit those of block j + 1.  FIRST: j = 0 (no previous block).
+      // FULL: blocks from j + 1 on are not masked.
+      auto stage = [&](auto slot_tag, auto first_tag, auto full_tag, int j, Scores& sc) __attribute__((always_inline)) {
+        constexpr int S = decltype(slot_tag)::value;
+        constexpr bool FIRST = decltype(first_tag)::value, FULL = decltype(full_tag)::value;
+        const __bf16* const Kt = &Ks[(S + 1) % kNS][0];
+        const __bf16* const Vt = &Vs[(S + 3) % kNS][0];
+        Scores sn;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sn.t[i >> 1][i & 1] = floatx4{0.f, 0.f, 0.f, 0.f};
+        bf16x8 (&pp)[2] = P[(S + 1) & 1], (&pf)[2] = P[S & 1];
+        Frags f = pre, nx;
+        float x[16];
+        auto vec_op = [&](auto t_tag) __attribute__((always_inline)) {
+          constexpr Step op = softmax_step(decltype(t_tag)::value);
+          constexpr int i = op.index, qt = (i >> 3) & 1, jj = i & 7;
+          if constexpr (op.kind == 0) x[i] = fmaf(sc.t[jj >> 2][qt][jj & 3], c2, -mc[qt]);
+          else if constexpr (op.kind == 1) x[i] = __builtin_amdgcn_exp2f(x[i]);
+          else { pf[qt][jj] = (__bf16)x[i]; pf[qt][jj + 1] = (__bf16)x[i + 1]; }
+        };
+        constexpr int SLOTS = 8 * KC + 2, VEC_SLOTS = SLOTS - 3 * KC / 4;   // the vector work ends early: its test travels beside the last MFMAs
+        bool large = false;
+        auto slot = [&](auto s_tag) __attribute__((always_inline)) {
+          constexpr int T = decltype(s_tag)::value, I = T / 8 < KC ? T / 8 : KC - 1, N = T - 8 * I;   // the last step has two more
+          // one wait for both K operands (lgkmcnt(4)) and one for both of V^T (lgkmcnt(2)) instead of one for each
+          if constexpr (N == 0) __builtin_amdgcn_s_waitcnt(0xC47F);
+          if constexpr (N == 4) __builtin_amdgcn_s_waitcnt(0xC27F);
+          if constexpr (N < 4) qk(sn, f, I, N);
+          else if constexpr (N < 8) { if (!FIRST) pv(f, pp, I, N - 4); }
+          else { if (!FIRST) row_sums(pp, N - 8); }
+          for_each<steps_before(T, VEC_SLOTS), steps_before(T + 1, VEC_SLOTS)>(vec_op);
+          if constexpr (T == VEC_SLOTS) large = __any(too_large(pf));
+          if constexpr (N < 2 || (N >= 4 && N < 8)) {
+            constexpr int p = N < 2 ? N : N - 2;
+            if constexpr (I + 1 < KC) load_frag(nx, Kt, Vt, I + 1, p);
+            else load_frag(nx, &Ks[(S + 2) % kNS][0], &Vs[S][0], 0, p);
+          }
+          if constexpr (N == 7 && I + 1 < KC) f = nx;
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        for_each<0, 4 * KC>(slot);
+        wait_and_sync<2 * IPW>();   // K(j + 2) and V(j) have landed: everything but what the previous stage issued
+        if constexpr (FULL) {
+          copy(k_lane, next_k, S, ks_lds);                   // K(j + 4)
+          copy(v_lane, next_v, (S + 2) % kNS, vs_lds);       // V(j + 2)
+        } else {
+          issue(k_lane, next_k, S, j + kNS, ks_lds);
+          issue(v_lane, next_v, (S + 2) % kNS, j + 2, vs_lds);
+        }
+        next_k = places_of(j + kNS + 1);
+        next_v = places_of(j + 3);
         __builtin_amdgcn_sched_barrier(0);
+        for_each<4 * KC, SLOTS>(slot);
+        pre = nx;
+        if (__builtin_expect(large, 0)) rescale(sc, pf);
+        if (!FULL && j + 1 < n_masked) mask(sn, block_of(j + 1));
+        sc = sn;
       };
-      for_each<0, 4 * KC>(slot);
-      wait_and_sync<2 * IPW>();   // K(j + 2) and V(j) have landed: everything but what the previous stage issued
-      if constexpr (FULL) {
-        copy(k_lane, next_k, S, ks_lds);                   // K(j + 4)
-        copy(v_lane, next_v, (S + 2) % kNS, vs_lds);       // V(j + 2)
-      } else {
-        issue(k_lane, next_k, S, j + kNS, ks_lds);
-        issue(v_lane, next_v, (S + 2) % kNS, j + 2, vs_lds);
-      }
-      next_k = places_of(j + kNS + 1);
-      next_v = places_of(j + 3);
-      __builtin_amdgcn_sched_barrier(0);
-      for_each<4 * KC, SLOTS>(slot);
-      pre = nx;
-      if (__builtin_expect(large, 0)) rescale(sc, pf);
-      if (!FULL && j + 1 < n_masked) mask(sn, block_of(j + 1));
-      sc = sn;
-    };
 
-    dma_wait_but<0>();
-    __syncthreads();
-    Scores sc;
+      dma_wait_but<0>();
+      __syncthreads();
+      Scores sc;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sc.t[i >> 1][i & 1] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 4; ++i) sc.t[i >> 1][i & 1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) {
-      Frags f;
-      for (int n = 0; n < 2; ++n) load_frag(f, &Ks[0][0], nullptr, kc, n);
-      for (int n = 0; n < 4; ++n) qk(sc, f, kc, n);
-    }
-    for (int n = 0; n < 2; ++n) load_frag(pre, &Ks[1][0], nullptr, 0, n);
-    for (int n = 2; n < 6; ++n) load_frag(pre, nullptr, &Vs[0][0], 0, n);
-    if (n_masked > 0) mask(sc, block_of(0));
-
-    using No = std::false_type;
-    using Yes = std::true_type;
-    if (n_blocks > 1) {
-      stage(std::integral_constant<int, 0>{}, Yes{}, No{}, 0, sc);
-      int j = 1;
-      const auto four = [&](auto full_tag) __attribute__((always_inline)) {   // stages j .. j + 3; whether there are more
-        if (j >= n_blocks - 1) return false;
-        stage(std::integral_constant<int, 1>{}, No{}, full_tag, j, sc);
-        if (j + 1 >= n_blocks - 1) return false;
-        stage(std::integral_constant<int, 2>{}, No{}, full_tag, j + 1, sc);
-        if (j + 2 >= n_blocks - 1) return false;
-        stage(std::integral_constant<int, 3>{}, No{}, full_tag, j + 2, sc);
-        if (j + 3 >= n_blocks - 1) return false;
-        if (__builtin_expect((j + 3) % (kRing / 2) == 0, 0)) fill(j + 3 + kRing / 2);   // over those of blocks that are done
-        stage(std::integral_constant<int, 0>{}, No{}, full_tag, j + 3, sc);
-        j += 4;
-        return true;
-      };
-      bool more = true;
-      while (more && j + 1 < n_masked) more = four(No{});
-      while (more) more = four(Yes{});
-    }
-    // the last block: its probabilities, its PV product and the one of the block before
-    const auto pv_block = [&](const __bf16* Vt, const bf16x8 (&p)[2]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < KC; ++i) {
+      for (int kc = 0; kc < KC; ++kc) {
         Frags f;
-        for (int n = 2; n < 6; ++n) load_frag(f, nullptr, Vt, i, n);
-        for (int n = 0; n < 4; ++n) pv(f, p, i, n);
+        for (int n = 0; n < 2; ++n) load_frag(f, &Ks[0][0], nullptr, kc, n);
+        for (int n = 0; n < 4; ++n) qk(sc, f, kc, n);
       }
-      row_sums(p, 0);
-      row_sums(p, 1);
-    };
-    if (n_blocks > 1) {
-      const bool odd = n_blocks & 1;   // the block before the last has an odd number
-      const bf16x8 pl[2] = {odd ? P[1][0] : P[0][0], odd ? P[1][1] : P[0][1]};
-      pv_block(&Vs[(n_blocks - 2) % kNS][0], pl);
+      for (int n = 0; n < 2; ++n) load_frag(pre, &Ks[1][0], nullptr, 0, n);
+      for (int n = 2; n < 6; ++n) load_frag(pre, nullptr, &Vs[0][0], 0, n);
+      if (n_masked > 0) mask(sc, block_of(0));
+
+      using No = std::false_type;
+      using Yes = std::true_type;
+      if (n_blocks > 1) {
+        stage(std::integral_constant<int, 0>{}, Yes{}, No{}, 0, sc);
+        int j = 1;
+        const auto four = [&](auto full_tag) __attribute__((always_inline)) {   // stages j .. j + 3; whether there are more
+          if (j >= n_blocks - 1) return false;
+          stage(std::integral_constant<int, 1>{}, No{}, full_tag, j, sc);
+          if (j + 1 >= n_blocks - 1) return false;
+          stage(std::integral_constant<int, 2>{}, No{}, full_tag, j + 1, sc);
+          if (j + 2 >= n_blocks - 1) return false;
+          stage(std::integral_constant<int, 3>{}, No{}, full_tag, j + 2, sc);
+          if (j + 3 >= n_blocks - 1) return false;
+          if (__builtin_expect((j + 3) % (kRing / 2) == 0, 0)) fill(j + 3 + kRing / 2);   // over those of blocks that are done
+          stage(std::integral_constant<int, 0>{}, No{}, full_tag, j + 3, sc);
+          j += 4;
+          return true;
+        };
+        bool more = true;
+        while (more && j + 1 < n_masked) more = four(No{});
+        while (more) more = four(Yes{});
+      }
+      // the last block: its probabilities, its PV product and the one of the block before
+      const auto pv_block = [&](const __bf16* Vt, const bf16x8 (&p)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < KC; ++i) {
+          Frags f;
+          for (int n = 2; n < 6; ++n) load_frag(f, nullptr, Vt, i, n);
+          for (int n = 0; n < 4; ++n) pv(f, p, i, n);
+        }
+        row_sums(p, 0);
+        row_sums(p, 1);
+      };
+      if (n_blocks > 1) {
+        const bool odd = n_blocks & 1;   // the block before the last has an odd number
+        const bf16x8 pl[2] = {odd ? P[1][0] : P[0][0], odd ? P[1][1] : P[0][1]};
+        pv_block(&Vs[(n_blocks - 2) % kNS][0], pl);
+      }
+      wait_and_sync<0>();
+      probs(sc, 0, P[0][0]);
+      probs(sc, 1, P[0][1]);
+      if (__any(too_large(P[0]))) rescale(sc, P[0]);
+      pv_block(&Vs[(n_blocks - 1) % kNS][0], P[0]);
     }
-    wait_and_sync<0>();
-    probs(sc, 0, P[0][0]);
-    probs(sc, 1, P[0][1]);
-    if (__any(too_large(P[0]))) rescale(sc, P[0]);
-    pv_block(&Vs[(n_blocks - 1) % kNS][0], P[0]);
   }
 
   // ---- normalise and store: a lane holds head-dim 16mt + 4g .. +4 of queries 16qt + col ----
@@ -514,11 +530,11 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   }
 }
 
-template <int D>
+template <int D, bool HALF>
 __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileLds<D>];
   const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0, part = (int)blockIdx.x >= grid0 ? 1 : 0;
-  tile_part<D>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
+  tile_part<D, HALF>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
 }
 
 // Shared rows by tiles, own rows by few queries: the products of the one beside the loads of the other.
@@ -526,7 +542,7 @@ template <int D, int NQ, bool NT>
 __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_mixed(const AttnPagesArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[std::max(kTileLds<D>, kFewLds<D, NQ>)];
   const int grid0 = (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles;
-  if ((int)blockIdx.x < grid0) tile_part<D>(a, 0, blockIdx.x, lds);
+  if ((int)blockIdx.x < grid0) tile_part<D, false>(a, 0, blockIdx.x, lds);
   else attn_pages_few<__bf16, D, NQ, NT>(a, 1, blockIdx.x - grid0, lds);
 }
 
@@ -539,7 +555,8 @@ void launch_some(hipStream_t s, const AttnPagesArgs& a) {
   else if (a.part[1].queries == 16) HACK_ATTN_MIXED(1, false);
   else if (a.part[1].queries == 32 && once) HACK_ATTN_MIXED(2, true);
   else if (a.part[1].queries == 32) HACK_ATTN_MIXED(2, false);
-  else hipLaunchKernelGGL((attn_pages_tiles<D>), grid, dim3(64 * kNW), 0, s, a);
+  else if (a.n_shared == 0 && a.G * a.c.n <= kPageTileQueries / 2) hipLaunchKernelGGL((attn_pages_tiles<D, true>), grid, dim3(64 * kNW), 0, s, a);
+  else hipLaunchKernelGGL((attn_pages_tiles<D, false>), grid, dim3(64 * kNW), 0, s, a);
 #undef HACK_ATTN_MIXED
 }
 

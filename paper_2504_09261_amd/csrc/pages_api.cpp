@@ -68,10 +68,13 @@ hack_status take_pages(hack_ctx* ctx, int32_t B, int32_t N, const hack_pages* c,
   return HACK_OK;
 }
 
-// Queries of a tile for so many queries of a cache.
-int tile_queries(const hack_ctx* ctx, int64_t queries) {
+// Queries of a tile for so many queries of each of `units` caches.  Tiles of 128 share every block through LDS, the smaller ones have every wave read its own.  Float32
+// takes 16 while 32 leave compute units without work: their matrix instructions are what a work-group's time goes by (64 units of 61 to 424 rows, 169
+// queries at head_dim 64: 384 work-groups of 32 queries 24.4 us, 704 of 16 19.9).
+int tile_queries(const hack_ctx* ctx, int64_t queries, int64_t units) {
   if (queries <= 16) return 16;
-  return ctx->cfg.dtype == HACK_F32 || queries <= 48 ? 32 : kPageTileQueries;
+  if (ctx->cfg.dtype == HACK_F32) return (queries + 31) / 32 * units < 3 * (int64_t)ctx->cus ? 16 : 32;
+  return queries <= 48 ? 32 : kPageTileQueries;
 }
 
 // How the parts of a call are laid out: tiles of queries, at most how many (entry, head, chunk) there may be, and where their partial results go.  Lengths are
@@ -91,12 +94,12 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
     saved += (int64_t)(s.count - 1) * s.rows * H * 2 * ctx->cfg.head_dim * ctx->elem_bytes;
   }
   if (saved < ctx->share_bytes) a->n_shared = 0;
-  const int own_tile = tile_queries(ctx, GN), shared_tile = tile_queries(ctx, most);
+  const int own_tile = tile_queries(ctx, GN, units), shared_tile = tile_queries(ctx, most, a->n_shared * H);
   lay_out(1, GN, own_tile);
   lay_out(0, most, shared_tile == kPageTileQueries ? shared_tile : own_tile);   // tiles of 16 and of 32 are not mixed
   if (rows_of(part[0], a->n_shared * H) + rows_of(part[1], units) > ctx->part_rows) a->n_shared = 0;   // no room to join the parts: every element reads all of its rows
   const int64_t shared_rows = rows_of(part[0], a->n_shared * H);
-  const int64_t spare = (ctx->part_rows - shared_rows - rows_of(part[1], units)) / (a->n_shared ? 2 : 1);   // rows that the chunks of a part may take beyond
+  int64_t spare = ctx->part_rows - shared_rows - rows_of(part[1], units);   // rows that chunks may take beyond, three quarters for those of shared rows
   const bool large = own_tile == kPageTileQueries || (a->n_shared && shared_tile == kPageTileQueries);
   const int64_t want = (large ? 2 : 4) * (int64_t)ctx->cus;
   int64_t rows = 0, groups = 0;
@@ -104,7 +107,8 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
     AttnPart& p = part[i];
     const int64_t pairs = i ? units : a->n_shared * H;
     const int64_t blocks = ((int64_t)a->c.max_len + kKeys - 1) / kKeys + 1, cuts = blocks <= p.uncut ? 1 : (blocks + p.least - 1) / p.least;   // chunks of an entry at most
-    const int64_t more = std::min(want, spare / p.queries);
+    const int64_t more = std::min(want, (i ? spare : spare * 3 / 4) / p.queries);
+    spare -= std::max<int64_t>(more, 0) * p.queries;
     p.share = more > 0 && cuts > 1 && pairs > 0 ? (float)more : 0.f;
     p.fill = (float)std::min<int64_t>(more, ctx->cus);
     p.pairs = (int32_t)std::min(pairs * cuts, p.share > 0.f ? (more + pairs * p.tiles) / p.tiles : pairs);

@@ -70,7 +70,7 @@ struct AttnPagesArgs : AttnPagesHead {
   Shared shared[kMostShared];
 };
 // How the kernels cut: blocks that hold rows lo to hi; blocks of a chunk where the launch has `total` (times heads and tiles of queries) and the part's longest entry
-// `longest`; chunks of an entry.  Shorter chunks than kChunk only as far as work-groups are missing.
+// `longest`; chunks of an entry.  Shorter chunks than kChunk only as far as compute units have no work-group.
 constexpr float kChunk = 32.f;
 __host__ __device__ inline int blocks_between(int lo, int hi) { return hi > lo ? (hi + kKeys - 1) / kKeys - lo / kKeys : 0; }
 __host__ __device__ inline int chunk_blocks(float total, int longest, const AttnPart& p) {
