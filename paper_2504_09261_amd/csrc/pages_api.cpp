@@ -68,13 +68,16 @@ hack_status take_pages(hack_ctx* ctx, int32_t B, int32_t N, const hack_pages* c,
   return HACK_OK;
 }
 
-// Queries of a tile for so many queries of each of `units` caches.  Tiles of 128 share every block through LDS, the smaller ones have every wave read its own.  Float32
-// takes 16 while 32 leave compute units without work: their matrix instructions are what a work-group's time goes by (64 units of 61 to 424 rows, 169
-// queries at head_dim 64: 384 work-groups of 32 queries 24.4 us, 704 of 16 19.9).
-int tile_queries(const hack_ctx* ctx, int64_t queries, int64_t units) {
+constexpr int kFewUncut = 24, kTilesUncut = 48;   // blocks of the longest entry up to which nothing is cut: joining the parts takes a launch of 4 us
+
+// Queries of a tile for so many queries of each of `units` caches.  Tiles of 128 share every block through LDS, in the smaller ones every wave reads blocks of its
+// own.  Us a call, tiles of 16 / 32 / 128, head_dim 128, 64 elements of 8 caches of 900 to 4000 rows, 20 queries 157 / 140 / 147; of 300 to 1500 rows, 32 queries
+// 73 / 64 / 61, 48 87 / 80 / 64, 80 114 / 97 / 70.  Where short caches leave compute units without a tile of 32, more tiles of 16 end earlier: 64 units of
+// 61 to 424 rows at head_dim 64, 17 queries 8.8 / 11.2 / 12.0, float32, 169 queries 18.0 / 22.7.
+int tile_queries(const hack_ctx* ctx, int64_t queries, int64_t units, int32_t max_len) {
   if (queries <= 16) return 16;
-  if (ctx->cfg.dtype == HACK_F32) return (queries + 31) / 32 * units < 3 * (int64_t)ctx->cus ? 16 : 32;
-  return queries <= 48 ? 32 : kPageTileQueries;
+  if (ctx->cfg.dtype != HACK_F32 && queries > 32) return kPageTileQueries;
+  return max_len < kFewUncut * kKeys && (queries + 31) / 32 * units < 3 * (int64_t)ctx->cus ? 16 : 32;
 }
 
 // How the parts of a call are laid out: tiles of queries, at most how many (entry, head, chunk) there may be, and where their partial results go.  Lengths are
@@ -85,7 +88,7 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
   const auto rows_of = [](const AttnPart& p, int64_t entries) { return entries * p.tiles * p.queries; };   // of partial results, without a cut
   const auto lay_out = [&](int i, int64_t queries, int tile) {
     const bool large = tile == kPageTileQueries;
-    part[i] = AttnPart{tile, (int32_t)((queries + tile - 1) / tile), 0, large ? 48 : 24, large ? 16 : 4, 0.f, 0.f, 0};
+    part[i] = AttnPart{tile, (int32_t)((queries + tile - 1) / tile), 0, large ? kTilesUncut : kFewUncut, large ? 16 : 4, 0.f, 0.f, 0};
   };
   int64_t most = 0, saved = 0;   // queries of a group; bytes that sharing spares
   for (int i = 0; i < a->n_shared; ++i) {
@@ -94,7 +97,7 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
     saved += (int64_t)(s.count - 1) * s.rows * H * 2 * ctx->cfg.head_dim * ctx->elem_bytes;
   }
   if (saved < ctx->share_bytes) a->n_shared = 0;
-  const int own_tile = tile_queries(ctx, GN, units), shared_tile = tile_queries(ctx, most, a->n_shared * H);
+  const int own_tile = tile_queries(ctx, GN, units, a->c.max_len), shared_tile = tile_queries(ctx, most, a->n_shared * H, a->c.max_len);
   lay_out(1, GN, own_tile);
   lay_out(0, most, shared_tile == kPageTileQueries ? shared_tile : own_tile);   // tiles of 16 and of 32 are not mixed
   if (rows_of(part[0], a->n_shared * H) + rows_of(part[1], units) > ctx->part_rows) a->n_shared = 0;   // no room to join the parts: every element reads all of its rows
