@@ -514,8 +514,8 @@ hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, const void* 
  *
  * What only a running kernel can see is reported as HACK_EINVAL by hack_check and the next
  * call, once: a page number outside [0, pages) (rows there are left out: not stored, not
- * seen), a length outside [0, max_len] or a number of new rows outside [0, N] (brought to
- * the nearest of these).  Entries of a table behind a sequence's last row are not read. */
+ * seen), a length outside [0, max_len] or a number of new rows outside [0, N] (attention takes the
+ * nearest of these, appending stores nothing).  Entries of a table behind a sequence's last row are not read. */
 typedef struct {
   void* k;              /* DEVICE element (page p, row r, head h, i) at p stride_page + r stride_row + h stride_head + i */
   void* v;              /* DEVICE the same; rows of K and V may lie in turn in one allocation */
@@ -564,7 +564,8 @@ typedef struct {
  *   heads   of q, a multiple G of H: query heads G h .. G h + G - 1 read cache h
  *   q, out  DEVICE [B, heads, N, head_dim]
  *   shared  HOST n_shared groups in ascending order, none in two of them; NULL: none.  Rows that a group shares are read
- *           once for all of it where that is faster, from the first element's pages.  Lengths count them: an element whose length is smaller sees that many.
+ *           once for all of it where that is faster, from the pages that the first element's table has for them (whatever its length).  Lengths count them: an element
+           whose length is smaller sees that many.
  * Sums are in float32, softmax in one pass; results are reproducible bit for bit from call to call with the same
  * lengths, groups and max_len.  out must not share memory with q or the cache.
  * Errors: HACK_EINVAL, HACK_ECAPACITY (B or N beyond max_units / H, max_queries, more than 256 groups, more queries than a

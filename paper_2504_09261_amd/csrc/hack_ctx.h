@@ -161,7 +161,7 @@ inline hack_status device_report(hack_ctx* ctx) {
   if (f && f[2]) {
     f[2] = 0;
     return fail(ctx, HACK_EINVAL, "an earlier call over a cache in pages met a page number outside the cache (rows there were left out), or a "
-                                  "length or a number of new rows out of range (taken as the nearest that is not)");
+                                  "length or a number of new rows out of range (attention took the nearest that is not, appending stored nothing)");
   }
   return HACK_OK;
 }

@@ -12,6 +12,20 @@ namespace {
 
 using namespace dev;
 
+// A length or a number of new rows that is out of range stores nothing: the rows that it would name are others'.
+__device__ __forceinline__ int stored_rows(const Pages& c, int entry) {
+  const int len = c.len[entry];
+  if (__builtin_expect((unsigned)len <= (unsigned)c.max_len, 1)) return len;
+  report(c);
+  return 0;   // no row lies in front of the sequence's first
+}
+__device__ __forceinline__ int stored_fresh(const Pages& c, int b) {
+  if (!c.fresh) return c.n;
+  const int fresh = c.fresh[b];
+  if (__builtin_expect((unsigned)fresh <= (unsigned)c.n, 1)) return fresh;
+  report(c);
+  return 0;
+}
 // Where row r of a table's sequence lies; NULL where it lies nowhere.
 __device__ __forceinline__ uint8_t* find_row(const Pages& c, uint8_t* mem, int entry, int r) {
   if (r < 0) return nullptr;
@@ -31,7 +45,7 @@ template <typename T> struct ToPages {
   int unit0, back;    // by_head: the first head's unit; rows between the sequence's end and this one
   __device__ __forceinline__ T* operator()(int h) const {
     uint8_t* p = row;
-    if (c.by_head) p = find_row(c, mem, unit0 + h, rows_of(c, unit0 + h) - back);
+    if (c.by_head) p = find_row(c, mem, unit0 + h, stored_rows(c, unit0 + h) - back);
     return p ? reinterpret_cast<T*>(p + h * c.stride_head) : nullptr;
   }
 };
@@ -41,8 +55,8 @@ __global__ __launch_bounds__(kRotateThreads) void append_rows(const AppendArgs a
   const int b = blockIdx.x / a.all_groups;
   unsigned x = blockIdx.x - (unsigned)b * a.all_groups;
   const int which = x < a.groups[0] ? 0 : x < a.groups[1] ? 1 : 2;   // q, k, v
-  const int fresh = fresh_of(a.c, b);
-  const int first = a.c.by_head ? 0 : rows_of(a.c, b) - fresh;   // row of the first new one
+  const int fresh = stored_fresh(a.c, b);
+  const int first = a.c.by_head ? 0 : stored_rows(a.c, b) - fresh;   // row of the first new one
   const int pos0 = a.own_rows ? first : 0;
   if (which == 0) {
     turn_rows<T, D, HALF, NORM, STREAM>(a, a.t[0], b, x, a.rot_dim, pos0, [&](int64_t n) {

@@ -198,7 +198,7 @@ extern "C" hack_status hack_attn_pages(hack_ctx* ctx, int32_t B, int32_t N, int3
   PageMemory mem;
   if ((st = take_pages(ctx, B, N, cache, fresh, &a.c, &mem)) != HACK_OK) return st;
   const int64_t GN = (int64_t)(heads / H) * N, rows = (int64_t)B * H * GN;
-  if (rows > ((int64_t)1 << 31) - 64) return fail(ctx, HACK_ECAPACITY, "%lld queries are more than a launch takes", (long long)rows);
+  if (rows > ((int64_t)1 << 31) - 2 * kPageTileQueries) return fail(ctx, HACK_ECAPACITY, "%lld queries are more than a launch takes", (long long)rows);
   const Range from = range_of(q, rows, (int64_t)d * ctx->elem_bytes), to = range_of(out, rows, (int64_t)d * ctx->elem_bytes);
   for (const Range& r : {from, mem.k, mem.v, mem.table, mem.len, mem.fresh})
     if (to.meets(r)) return fail(ctx, HACK_EINVAL, "out shares memory with what is read");

@@ -239,22 +239,23 @@ def test_long_causal_prompts(contexts, dtype, d, n, group):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("n", [9, 150])
+@pytest.mark.parametrize("n, old, shared", [(9, 40, 0), (150, 40, 0), (9, 3000, 0), (150, 3000, 0), (150, 2000, 1008)])
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
-def test_what_is_not_seen_does_not_matter(contexts, dtype, d, n, value):
-    """A new row that is no number reaches the queries from it on, and none before."""
-    hk = contexts(2, d, dtype)
+def test_what_is_not_seen_does_not_matter(contexts, dtype, d, n, old, shared, value):
+    """A new row that is no number reaches the queries from it on, and none before; in a whole result and in the parts of a cut one."""
+    hk = contexts(2, d, dtype, shared=0)
     g = torch.Generator(DEV).manual_seed(n)
-    pool = Pool(hk, [n + 100, n + 40], 16, g)
+    groups = [(0, 2, shared)] if shared else []
+    pool = Pool(hk, [n + old + 60, n + old], 16, g, shared=groups)
     at = n // 2 + 1
     clean = queries((2, 2, n, d), dtype, g)
     fine = torch.full_like(clean, 9.0)
-    hk.attn_pages(clean, pool.cache, 0.1, fine, causal=True)
-    page, row, head = pool.where(1, 1, 40 + at, 41 + at)
+    hk.attn_pages(clean, pool.cache, 0.1, fine, causal=True, shared=groups)
+    page, row, head = pool.where(1, 1, old + at, old + at + 1)
     old = pool.v[page, row, head].clone()
     pool.v[page, row, head, 5] = value
     out = torch.full_like(clean, 9.0)
-    hk.attn_pages(clean, pool.cache, 0.1, out, causal=True)
+    hk.attn_pages(clean, pool.cache, 0.1, out, causal=True, shared=groups)
     same = torch.ones_like(out, dtype=torch.bool)
     same[1, 1, :, 5] = False
     assert torch.equal(out[same], fine[same]), (out[same] != fine[same]).sum()
@@ -264,7 +265,7 @@ def test_what_is_not_seen_does_not_matter(contexts, dtype, d, n, value):
     out[1, 1, at:, 5] = fine[1, 1, at:, 5]
     check_attention(pool, clean, out, float(np.float32(0.1)), True)
     pool.k[page, row, head, 5] = value            # a score that is no number, or infinite
-    hk.attn_pages(clean, pool.cache, 0.1, out, causal=True)
+    hk.attn_pages(clean, pool.cache, 0.1, out, causal=True, shared=groups)
     same[1, 1, :, 5] = True
     same[1, 1, at:] = False
     assert torch.equal(out[same], fine[same])
@@ -286,17 +287,17 @@ def test_scores_of_minus_infinity_are_not_an_empty_row(contexts, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n", [1, 40])
-def test_pages_and_lengths_that_are_none(contexts, dtype, n):
+@pytest.mark.parametrize("n, length", [(1, 200), (40, 200), (1, 5000), (40, 5000)])
+def test_pages_and_lengths_that_are_none(contexts, dtype, n, length):
     """Rows in a page that is none are left out, lengths are brought into range, and both are reported once."""
     hk = contexts(2, 128, dtype)
     g = torch.Generator(DEV).manual_seed(3)
-    pool = Pool(hk, [300, 200], 32, g)
-    hole = Pool(hk, [300, 168], 32, g)           # the second sequence of `pool` without its page 2
+    pool = Pool(hk, [300, length], 32, g)
+    hole = Pool(hk, [300, length - 32], 32, g)   # the second sequence of `pool` without its page 2
     for h in range(2):
         for m, o in ((pool.k, hole.k), (pool.v, hole.v)):
-            rows = m[pool.where(1, h, 0, 200)]
-            o[hole.where(1, h, 0, 168)] = torch.cat([rows[:64], rows[96:]])
+            rows = m[pool.where(1, h, 0, length)]
+            o[hole.where(1, h, 0, length - 32)] = torch.cat([rows[:64], rows[96:]])
     q = queries((2, 4, n, 128), dtype, g)
     for bad in (-1, pool.n_pages, 1 << 30):
         pool.table[1, 2] = bad
@@ -320,7 +321,13 @@ def test_pages_and_lengths_that_are_none(contexts, dtype, n):
     with pytest.raises(HackError):
         hk.check()
     assert (out[0] == 0).all()
-    pool.len.copy_(torch.tensor([300, 200]))
+    pool.len.copy_(torch.tensor([300, length]))
+    for fresh in ([n + 1, n], [n, -1]):
+        hk.attn_pages(q, pool.cache, 0.1, out, fresh=torch.tensor(fresh, dtype=torch.int32, device=DEV))
+        torch.cuda.synchronize()
+        with pytest.raises(HackError):
+            hk.check()
+    pool.len.copy_(torch.tensor([300, length]))
     hk.attn_pages(q, pool.cache, 0.1, out)
     check_attention(pool, q, out, float(np.float32(0.1)))
     hk.check()
@@ -443,7 +450,7 @@ def test_append_to_pages_that_are_none(contexts):
     before = [pool.k.clone(), pool.v.clone()]
     pool.table[0, 5] = pool.n_pages
     pool.table[1, 4] = -3
-    pool.len[1] = 1 << 20                        # brought to max_len, whose last entries are no pages
+    pool.len[1] = 1 << 20                        # out of range: nothing of it is stored
     k, v = (torch.randn((2, 2, 40, 64), generator=g, device=DEV).bfloat16() for _ in range(2))
     hk.append_pages(k, v, pool.cache)
     torch.cuda.synchronize()
@@ -456,11 +463,60 @@ def test_append_to_pages_that_are_none(contexts):
             at = pool.where(0, h, 60, 100)
             keep = torch.from_numpy(np.arange(60, 100) // 16 != 5).to(DEV)
             want[at[0][keep], at[1][keep], at[2][keep]] = x[0, h][keep]
-        cap = pool.table.shape[1] * 16            # the second sequence's last 40 rows: entries 4 (in place of a page) to the end
-        for r in range(cap - 40, cap):
-            p = int(pool.table[1, r // 16])
-            assert not 0 <= p < pool.n_pages
         assert torch.equal(m.nan_to_num(7.0), want.nan_to_num(7.0))
+    # numbers of new rows
+    pool.table[0, 5] = int(pool.np_table[0, 0, 5])
+    pool.len.copy_(torch.tensor([100, 70]))
+    before = [pool.k.clone(), pool.v.clone()]
+    for fresh in ([41, -1], [-1, 1 << 30]):
+        hk.append_pages(2 * k, 2 * v, pool.cache, fresh=torch.tensor(fresh, dtype=torch.int32, device=DEV))
+        torch.cuda.synchronize()
+        with pytest.raises(HackError):
+            hk.check()
+        for m, o in zip((pool.k, pool.v), before):
+            assert torch.equal(m.nan_to_num(7.0), o.nan_to_num(7.0))
+
+
+def test_views(contexts):
+    """Tables with rows apart, a bound on lengths, queries in place, heads of a wider pool, another stream."""
+    hk = contexts(2, 64, "bf16")
+    g = torch.Generator(DEV).manual_seed(6)
+    pool = Pool(hk, [90, 300, 7], 16, g)
+    q = queries((3, 4, 5, 64), "bf16", g)
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    hk.attn_pages(q, pool.cache, 0.1, want, causal=True)
+    wide = torch.full((3, 50), -1, dtype=torch.int32, device=DEV)
+    wide[:, 3:3 + pool.table.shape[1]] = pool.table
+    for table, most in ((wide[:, 3:3 + pool.table.shape[1]], 0), (wide[:, 3:22], 300), (wide[:, 3:22], 304)):
+        cache = PagedCache(pool.k, pool.v, table, pool.len, most)
+        hk.attn_pages(q, cache, 0.1, out, causal=True)
+        assert torch.equal(out, want)
+    cache = PagedCache(pool.k, pool.v, wide[:, 3:21], pool.len)      # 288 rows: one length is out of range
+    hk.attn_pages(q, cache, 0.1, out, causal=True)
+    torch.cuda.synchronize()
+    with pytest.raises(HackError):
+        hk.check()
+    assert torch.equal(out[::2], want[::2])
+    # two of four heads of a pool
+    four = [torch.full((pool.n_pages, 16, 4, 64), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    four[0][:, :, 1:3], four[1][:, :, 1:3] = pool.k, pool.v
+    hk.attn_pages(q, PagedCache(four[0][:, :, 1:3], four[1][:, :, 1:3], pool.table, pool.len), 0.1, out, causal=True)
+    assert torch.equal(out, want)
+    # queries turned in place
+    rope = Rope.scaled(64)
+    k, v = (torch.randn((3, 2, 5, 64), generator=g, device=DEV).bfloat16() for _ in range(2))
+    x, y = q.clone(), torch.empty_like(q)
+    hk.append_pages(k, v, pool.cache, rope=rope, q=q, q_out=y)
+    hk.append_pages(k, v, pool.cache, rope=rope, q=x, q_out=x)
+    assert torch.equal(x, y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        hk.attn_pages(q, pool.cache, 0.1, out, causal=True)
+    side.synchronize()
+    hk.attn_pages(q, pool.cache, 0.1, want, causal=True)
+    assert torch.equal(out, want)
+    hk.check()
 
 
 # ---- a run of both, graphs, streams ---------------------------------------------
