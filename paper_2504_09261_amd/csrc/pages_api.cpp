@@ -112,7 +112,9 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
     const int64_t blocks = ((int64_t)a->c.max_len + kKeys - 1) / kKeys + 1, cuts = blocks <= p.uncut ? 1 : (blocks + p.least - 1) / p.least;   // chunks of an entry at most
     const int64_t more = std::min(want, (i ? spare : spare * 3 / 4) / p.queries);
     spare -= std::max<int64_t>(more, 0) * p.queries;
-    p.share = more > 0 && cuts > 1 && pairs > 0 ? (float)more : 0.f;
+    // A chunk has a `more`-th of all blocks at least, so no entry is cut whose heads and tiles are as many: the longest one alone brings so many times its blocks.
+    const bool never = (i && a->c.by_head ? 1 : H) * p.tiles >= more;
+    p.share = !never && cuts > 1 && pairs > 0 ? (float)more : 0.f;
     p.fill = (float)std::min<int64_t>(more, ctx->cus);
     p.pairs = (int32_t)std::min(pairs * cuts, p.share > 0.f ? (more + pairs * p.tiles) / p.tiles : pairs);
     p.row0 = rows;
