@@ -1,5 +1,13 @@
-// Attention over caches in pages, few queries (tiles of 16 and 32), as the kernels that have tiles of these alone and beside larger ones share it.  HIP device
-// code only.
+// Attention over caches in pages, few queries (tiles of 16 and 32), as the kernels that have such tiles alone and beside larger ones share it: O = Softmax(scale Q K^T) V
+// over the rows that a query sees.  HIP device code only.
+//
+// A work-group takes 16 NQ queries and a chunk of keys, its four waves every fourth block (32 keys, float32 16), each by itself.  S^T = K Q^T, one softmax update a block, O^T +=
+// V^T P^T: the probabilities go from the accumulators into the B operand.  V^T wants keys side by side where memory has head-dim: a lane loads the
+// same 8 elements of eight rows (at head_dim 64, of four, and trades halves with a neighbour) and turns the square around in registers.  Float32 enters the
+// 16x16x4 matrix instruction as it is, whose operands need no turning.  The next block is loaded into the registers of this one as soon as they are free, the
+// page numbers of the one behind it are under way by then.
+// Bound by reading the cache: two work-groups keep 128 KB a compute unit under way.  Of the 137 us of one token over 643 MB, whole rows side by side in a load took 15 (K through
+// LDS; 16 rows' 64 bytes each before), loads past the caches 5.
 #pragma once
 
 #include <type_traits>
@@ -290,15 +298,19 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
 #pragma unroll
       for (int s = 0; s < PIECES; ++s) {
         const uintx4 k = Keys::get(k_lds, t, s, col, g);
+        if constexpr (kBf16) {
 #pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) {
-          if constexpr (kBf16) {
+          for (int qt = 0; qt < NQ; ++qt)
             sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[qt][s]), sc[t][qt], 0, 0, 0);
-          } else {
-            const floatx4 x = __builtin_bit_cast(floatx4, k), y = __builtin_bit_cast(floatx4, qf[qt][s]);
+        } else {
+          const floatx4 x = __builtin_bit_cast(floatx4, k);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], sc[t][qt], 0, 0, 0);
-          }
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int qt = 0; qt < NQ; ++qt) {
+              const floatx4 y = __builtin_bit_cast(floatx4, qf[qt][s]);
+              sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], sc[t][qt], 0, 0, 0);
+            }
         }
       }
     }

@@ -1,14 +1,9 @@
-// Attention over caches in pages: O = Softmax(scale Q K^T) V over the rows that a query sees, for few queries of a cache (single tokens, small scales) and
-// in float32 contexts for all.
+// Attention over caches in pages for few queries of a cache (single tokens, small scales) and in float32 contexts for all, and the merge of partial results
+// (the arithmetic: attn_pages_few.h; many queries: kernels_attn_pages_tiles.hip).
 //
-// Lengths lie in device memory, so the work is cut there: every work-group sums up the blocks of 32 keys of all entries (groups with shared rows; batch
-// elements, or units, with their own), which gives the length of a chunk, and finds the entry, head, chunk and tile of queries that are its own.
-// Partial results of an entry's chunks, and of shared and own rows, are joined by a launch of their own.
-//
-// A work-group takes 16 NQ queries and a chunk of keys, its four waves every fourth block, each by itself, and no LDS until the end: K comes from memory as the A
-// operand of S^T = K Q^T, a lane 16 bytes of a row at a time.  V^T wants keys side by side where memory has head-dim: a lane loads
-// the same 8 (head_dim 64: 4) elements of eight rows and turns the square around in registers, so that its elements are rows of 8 tiles of O^T.  Float32
-// enters the 16x16x4 matrix instruction as it is, whose operands need no turning.
+// Measured, bf16, head_dim 128: one token of 64 elements with 32 heads over 8 caches of 900 to 4000 rows, 643 MB, 112 us (5.7 TB/s; a plain kernel that only
+// reads reaches 5.9), 64 heads over 8 caches of 131071 rows, 537 MB, 95; float32, head_dim 64: 64 units of 61 to 424 rows, 169 queries 18 us, of which the
+// products are 5: the start of a work-group, 5 us, and uneven units.
 #include "attn_pages_few.h"
 
 namespace hack {
@@ -17,6 +12,7 @@ namespace {
 
 using namespace dev;
 
+// At head_dim 128 two work-groups a compute unit with all the registers they ask for (three: some spill, 643 MB 120 -> 123 us, float32 122 -> 132).
 template <typename T, int D, int NQ, bool NT>
 __global__ __launch_bounds__(kThreads, D == 128 ? 2 : NQ == 1 ? 4 : 3) void attn_pages(const AttnPagesArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kFewLds<D, NQ>];
@@ -24,7 +20,9 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 2 : NQ == 1 ? 4 : 3) void attn
   attn_pages_few<T, D, NQ, NT>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
 }
 
-// Rows with partial results: ROWS of them a work-group, each by 256 / ROWS threads, D / 4 lanes a slot, which walk over its slots.
+// Joins the partial results of rows: ROWS of them a work-group, each by 256 / ROWS threads, D / 4 lanes a slot, which walk over its slots.  With references m_i, sums l_i
+// and outputs o_i of a row's slots, o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Bound by reading the slots (6144 rows of 11 or 12: 38 MB, 8 us); where rows are few, the way of one
+// through them counts, and a work-group takes one.
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void attn_pages_merge(const AttnPagesArgs a) {
   constexpr int LPR = D / 4, SIDE = 256 / LPR / ROWS;   // slots of a row at a time

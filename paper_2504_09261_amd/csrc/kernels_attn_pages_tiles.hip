@@ -8,6 +8,11 @@
 // begins inside the shared rows) come first, their scores are masked, and rows that nobody sees are not copied: the nearest row that is seen stands in for them.
 // A masked row's probability is zero, which keeps it out of the sums unless its value is an infinity or NaN: an item whose results are no numbers, or
 // that met a page that is none, does these queries again row by row, and numbers among their results stand.
+//
+// Bound by the matrix cores and the vector work beside them.  Measured, head_dim 128: 3000 causal queries of 32 heads over 4001 to 7001 rows of 8 caches 248 to 258 us (1.05 to 1.09
+// PFLOP/s; a large library product reaches 1.2), without the mask 314 (1.10).  At head_dim 64 the exponentials of a block stand beside half the products: the same at 64, 174 us
+// (0.78).  Places computed from the table in every stage, copies with scalar bases, masks in every stage: 479 us for the 310 that the form here took then; queries in the
+// order number, head instead of head, number, so that an item's last blocks are few and items are in order of their lengths: 310 -> 270.
 #include "attn_pages_few.h"
 
 namespace hack {

@@ -2,7 +2,9 @@
 // in the same launch.
 //
 // The arithmetic and the lanes' share of a row are those of the rotation (rotate_device.h); a token's place is its sequence's table entry.  Memory-bound: every
-// row is read and written once.
+// row is read and written once.  Measured, bf16: 16384 tokens of 32 + 8 + 8 heads of 128 out of one projection 79 us (403 MB, 5.1 TB/s of the 6.2 of a plain elementwise kernel),
+// 32 x 256 of 30 + 30 + 30 heads of 64, normed and turned in two axes, into pages of 16 rows 42 us (189 MB, 4.5 TB/s; a plain kernel of this size 5.4), one
+// token of each of 64 sequences 4.5 us.  More or fewer tokens or heads a work-group, the next head's loads ahead of this one's arithmetic: within 3 %.
 #include "pages_device.h"
 #include "rotate_device.h"
 
