@@ -106,13 +106,16 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
   // of 128 two, which is what it holds.  Shorter chunks than kChunk are worth it only up to one a compute unit: 8 units of 20000 rows in 296 chunks 26.3 us, in 256 22.3.
   int64_t spare = ctx->part_rows - shared_rows - rows_of(part[1], units);   // rows that chunks may take beyond, three quarters for those of shared rows
   const bool large = own_tile == kPageTileQueries || (a->n_shared && shared_tile == kPageTileQueries);
-  const int64_t want = (large ? 2 : 4) * (int64_t)ctx->cus;
+  // Float32 tiles of 32, whose products bound them: one, less half of what entries' last chunks may add (8 units of 20000 rows, 100 queries, four / two / one 144 / 121 /
+  // 125 us, 16 at head_dim 64, 32 queries 60 / 60 / 51, 32 of 2000 to 9000 rows 70 / 70 / 70, less the half 51).
+  const int64_t uncut = units * part[1].tiles;
+  const int64_t want = ctx->cfg.dtype == HACK_F32 && own_tile == 32 ? ctx->cus - std::min<int64_t>(uncut / 2, ctx->cus / 4) : (large ? 2 : 4) * (int64_t)ctx->cus;
   int64_t rows = 0, groups = 0;
   for (int i = 0; i < 2; ++i) {
     AttnPart& p = part[i];
     const int64_t pairs = i ? units : a->n_shared * H;
     const int64_t blocks = ((int64_t)a->c.max_len + kKeys - 1) / kKeys + 1, cuts = blocks <= p.uncut ? 1 : (blocks + p.least - 1) / p.least;   // chunks of an entry at most
-    const int64_t more = std::min(want, (i ? spare : spare * 3 / 4) / p.queries);
+    const int64_t more = pairs ? std::min(want, (i ? spare : spare * 3 / 4) / p.queries) : 0;
     spare -= std::max<int64_t>(more, 0) * p.queries;
     // A chunk has a `more`-th of all blocks at least, so no entry is cut whose heads and tiles are as many: the longest one alone brings so many times its blocks.
     const bool never = (i && a->c.by_head ? 1 : H) * p.tiles >= more;
