@@ -214,6 +214,39 @@ def test_long_shared_prefix(contexts, dtype, d, batch, group, prefix):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("by_head", [False, True])
+@pytest.mark.parametrize("n, n_groups", [(1, 3), (1, 40), (40, 40)])
+def test_many_sequences_and_groups(contexts, dtype, by_head, n, n_groups):
+    """More sequences than a wave keeps the blocks of, more groups than it looks through one by one, a few long caches that are cut."""
+    batch = 300
+    hk = contexts(2, 64, dtype, units=2 * batch, shared=0)
+    g = torch.Generator(DEV).manual_seed(n_groups)
+    lens = 70 + (np.arange(batch) * 29) % 60
+    lens[[7, 150, 260, 299]] = (2900, 1777, 3100, 2500)
+    shared = [(7 * i + 1, 5, 64 if i % 3 else 48) for i in range(n_groups)]
+    pool = Pool(hk, np.stack([lens, lens[::-1]], 1) if by_head else lens, 16, g, by_head, shared=shared)
+    q = queries((batch, 4, n, 64), dtype, g)
+    for groups in (shared, None):
+        out = torch.full_like(q, 9.0)
+        hk.attn_pages(q, pool.cache, 0.125, out, causal=True, shared=groups)
+        check_attention(pool, q, out, 0.125, True)
+    hk.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 40])
+def test_largest_pages(contexts, dtype, n):
+    hk = contexts(2, 64, dtype)
+    g = torch.Generator(DEV).manual_seed(n)
+    pool = Pool(hk, [65536 + 300, 41], 65536, g)
+    q = queries((2, 4, n, 64), dtype, g)
+    out = torch.full_like(q, 9.0)
+    hk.attn_pages(q, pool.cache, 0.125, out, causal=True)
+    check_attention(pool, q, out, 0.125, True)
+    hk.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_few_queries_over_one_long_cache(contexts, dtype, d):
     hk = contexts(1, d, dtype)
