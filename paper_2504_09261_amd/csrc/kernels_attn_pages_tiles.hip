@@ -34,26 +34,26 @@ __device__ __forceinline__ void for_each(F&& f) {
   }
 }
 
-// Vector work of a stage in the order of issue: 16 scores a lane become probabilities, dependent operations two elements apart.
+// Vector work of a stage in the order of issue: E scores a lane become probabilities, dependent operations two elements apart.
 struct Step {
   int kind, index;   // 0 multiply-add, 1 exponential, 2 conversion of elements index and index + 1
 };
-constexpr int kSteps = 40, kStepCycles = 16 * 4 + 16 * 8 + 8 * 4;
-constexpr Step softmax_step(int t) {
+template <int E> constexpr Step softmax_step(int t) {
   int n = 0;
-  for (int j = -2; j < 18; ++j) {
-    if (j >= 0 && j < 16 && n++ == t) return Step{1, j};
-    if (j + 2 < 16 && n++ == t) return Step{0, j + 2};
+  for (int j = -2; j < E + 2; ++j) {
+    if (j >= 0 && j < E && n++ == t) return Step{1, j};
+    if (j + 2 < E && n++ == t) return Step{0, j + 2};
     if (j >= 2 && j % 2 == 0 && n++ == t) return Step{2, j - 2};
   }
   return Step{-1, 0};
 }
-constexpr int steps_before(int s, int slots) {   // in front of slot s
+template <int E> constexpr int steps_before(int s, int slots) {   // in front of slot s
+  constexpr int kSteps = E + E + E / 2, kCycles = E * 4 + E * 8 + E / 2 * 4;
   if (s >= slots) return kSteps;
   int c = 0, t = 0;
   while (t < kSteps) {
-    c += softmax_step(t).kind == 1 ? 8 : 4;
-    if (c * slots > kStepCycles * s) break;
+    c += softmax_step<E>(t).kind == 1 ? 8 : 4;
+    if (c * slots > kCycles * s) break;
     ++t;
   }
   return t;
@@ -61,9 +61,8 @@ constexpr int steps_before(int s, int slots) {   // in front of slot s
 
 template <int D> constexpr int kTileLds = 2 * kNS * kKeys * D * 2 + kRing * 16 + (2 * kNW + 1) * 4;   // bytes
 
-// Work-group id of a part; lds: kTileLds bytes, 1024-byte aligned.  HALF: no tile has more than 64 queries, and waves without one stand aside, out of the way of
-// those that have (64 queries of 480 units over 604 to 668 rows at head_dim 64: 24.7 us, so 22.5; the code for it costs tiles of 128 up to 6 %).
-template <int D, bool HALF>
+// Work-group id of a part; lds: kTileLds bytes, 1024-byte aligned.  QT: tiles of 16 queries a wave, 2, or 1 where no item has more than 64 queries.
+template <int D, int QT>
 __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int id, unsigned char* lds) {
   constexpr int KC = D / 32;        // MFMA steps over head_dim for S^T
   constexpr int MT = D / 16;        // 16-row tiles of O^T
@@ -109,15 +108,13 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
     if (!q.there) q.sees = 0;
     return q;
   };
-  int sees[2];
+  int sees[QT];
   int most = 0, fewest = c.max_len;
-  bool any = false;
-  const __bf16* qrow[2];
+  const __bf16* qrow[QT];
 #pragma unroll
-  for (int qt = 0; qt < 2; ++qt) {
-    const Query q = query(w * 32 + 16 * qt + col);
+  for (int qt = 0; qt < QT; ++qt) {
+    const Query q = query(16 * (QT * w + qt) + col);
     sees[qt] = q.sees;
-    any |= q.there;
     if (q.there) {
       most = max(most, q.sees);
       fewest = min(fewest, q.sees);
@@ -126,7 +123,6 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   }
   most = row_most(most);
   fewest = row_fewest(fewest);
-  const bool idle = HALF && __ballot(any) == 0;   // a wave without queries only copies
   if (lane == 0) {
     most_sh[w] = most;
     fewest_sh[w] = fewest;
@@ -144,11 +140,18 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   const int n_tail = end - full_end, n_head = first < full_end && first * kKeys < lo ? 1 : 0, n_masked = n_tail + n_head;
   const auto block_of = [&](int j) __attribute__((always_inline)) { return j < n_tail ? end - 1 - j : j < n_masked ? first : first + j - n_tail; };
 
-  floatx4 o[MT][2];        // O^T: head-dim 16mt + 4g + r, query 16qt + col
+  floatx4 o[MT][QT];       // O^T: head-dim 16mt + 4g + r, query 16qt + col
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) o[mt][0] = o[mt][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-  floatx4 ls[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};   // row sums of P (equal in all four rows)
-  float mc[2] = {-FLT_MAX, -FLT_MAX};   // probabilities are 2^(c2 s - mc); finite from the start, so that keys whose score is -inf get 0
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) o[mt][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  floatx4 ls[QT];   // row sums of P (equal in all four rows)
+  float mc[QT];     // probabilities are 2^(c2 s - mc); finite from the start, so that keys whose score is -inf get 0
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    ls[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    mc[qt] = -FLT_MAX;
+  }
 
   if (n_blocks > 0) {
     // ---- places of the blocks in the order in which they are taken, by halves of a ring; past the last block it is repeated ----
@@ -225,26 +228,16 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
     }
     Places next_k = places_of(kNS), next_v = places_of(2);   // of the copies of the next stage
 
-    if (idle) {
-      dma_wait_but<0>();
-      __syncthreads();
-      for (int j = 0; j < n_blocks - 1; ++j) {
-        if (j > 0 && j % (kRing / 2) == 0) fill(j + kRing / 2);
-        wait_and_sync<2 * IPW>();
-        issue(k_lane, places_of(j + kNS), j % kNS, j + kNS, ks_lds);
-        issue(v_lane, places_of(j + 2), (j + 2) % kNS, j + 2, vs_lds);
-      }
-      wait_and_sync<0>();
-    } else {
+    {
       // Q fragments (B operand of S^T = K Q^T): query 16 qt + col, head-dim slice [32kc + 8g, +8); consumed here, so that a wait for them does not drain the
       // copies that are meant to stay in flight later.
-      bf16x8 qf[2][KC];
+      bf16x8 qf[QT][KC];
 #pragma unroll
-      for (int qt = 0; qt < 2; ++qt)
+      for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
         for (int kc = 0; kc < KC; ++kc) qf[qt][kc] = *reinterpret_cast<const bf16x8*>(qrow[qt] + 32 * kc);
 #pragma unroll
-      for (int kc = 0; kc < KC; ++kc) asm volatile("" ::"v"(qf[0][kc]), "v"(qf[1][kc]));
+      for (int kc = 0; kc < KC; ++kc) asm volatile("" ::"v"(qf[0][kc]), "v"(qf[QT - 1][kc]));
 
       const float c2 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.scale * kLog2eF)));
       const int e = col >> 2, qd = col & 3;
@@ -256,7 +249,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
       for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
       asm volatile("" : "+v"(ones));   // stays in registers
 
-      struct Scores { floatx4 t[2][2]; };   // keys 16kt + 4g + r, query 16qt + col
+      struct Scores { floatx4 t[2][QT]; };   // keys 16kt + 4g + r, query 16qt + col
       const auto mask = [&](Scores& sc, int blk) __attribute__((always_inline)) {
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -264,7 +257,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
           for (int r = 0; r < 4; ++r) {
             const int key = blk * kKeys + 16 * kt + 4 * g + r;
 #pragma unroll
-            for (int qt = 0; qt < 2; ++qt)
+            for (int qt = 0; qt < QT; ++qt)
               if (key < lo || key >= sees[qt]) sc.t[kt][qt][r] = -INFINITY;
           }
       };
@@ -272,13 +265,13 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
 #pragma unroll
         for (int j = 0; j < 8; ++j) pf[j] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc.t[j >> 2][qt][j & 3], c2, -mc[qt]));
       };
-      const auto too_large = [&](const bf16x8 (&pf)[2]) __attribute__((always_inline)) -> bool {
-        const uintx4 x = __builtin_bit_cast(uintx4, pf[0]), y = __builtin_bit_cast(uintx4, pf[1]);
+      const auto too_large = [&](const bf16x8 (&pf)[QT]) __attribute__((always_inline)) -> bool {
+        const uintx4 x = __builtin_bit_cast(uintx4, pf[0]), y = __builtin_bit_cast(uintx4, pf[QT - 1]);
         return (((x[0] | x[1] | x[2]) | x[3] | y[0]) | y[1] | y[2] | y[3]) & 0x40004000u;
       };
-      const auto rescale = [&](const Scores& sc, bf16x8 (&pf)[2]) __attribute__((always_inline)) {
+      const auto rescale = [&](const Scores& sc, bf16x8 (&pf)[QT]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int qt = 0; qt < 2; ++qt) {
+        for (int qt = 0; qt < QT; ++qt) {
           float mx = sc.t[0][qt][0];
 #pragma unroll
           for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc.t[j >> 2][qt][j & 3]);
@@ -305,16 +298,16 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
       };
       const auto joined = [](const bf16x4 (&v)[2]) __attribute__((always_inline)) { return bf16x8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]}; };
       const auto qk = [&](Scores& sn, const Frags& f, int kc, int n) __attribute__((always_inline)) {
-        const int kt = n >> 1, qt = kt ^ (n & 1);
+        const int kt = QT == 1 ? n : n >> 1, qt = QT == 1 ? 0 : kt ^ (n & 1);
         sn.t[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.k[kt], qf[qt][kc], sn.t[kt][qt], 0, 0, 0);
       };
-      const auto pv = [&](const Frags& f, const bf16x8 (&p)[2], int i, int n) __attribute__((always_inline)) {
-        const int m = n >> 1, qt = m ^ (n & 1);
+      const auto pv = [&](const Frags& f, const bf16x8 (&p)[QT], int i, int n) __attribute__((always_inline)) {
+        const int m = QT == 1 ? n : n >> 1, qt = QT == 1 ? 0 : m ^ (n & 1);
         o[2 * i + m][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(joined(f.v[m]), p[qt], o[2 * i + m][qt], 0, 0, 0);
       };
-      const auto row_sums = [&](const bf16x8 (&p)[2], int qt) __attribute__((always_inline)) { ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[qt], ls[qt], 0, 0, 0); };
+      const auto row_sums = [&](const bf16x8 (&p)[QT], int qt) __attribute__((always_inline)) { ls[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[qt], ls[qt], 0, 0, 0); };
 
-      bf16x8 P[2][2];   // probabilities of block j in P[j & 1]: those of the previous block wait for their PV product
+      bf16x8 P[2][QT];  // probabilities of block j in P[j & 1]: those of the previous block wait for their PV product
       Frags pre;        // operands of the next stage's first step
 
       // Stage j, slot S = j % 4 (compile time).  On entry sc = scores of block j, on exit those of block j + 1.  FIRST: j = 0 (no previous block).
@@ -326,38 +319,42 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
         const __bf16* const Vt = &Vs[(S + 3) % kNS][0];
         Scores sn;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sn.t[i >> 1][i & 1] = floatx4{0.f, 0.f, 0.f, 0.f};
-        bf16x8 (&pp)[2] = P[(S + 1) & 1], (&pf)[2] = P[S & 1];
+        for (int i = 0; i < 2 * QT; ++i) sn.t[i & 1][i >> 1] = floatx4{0.f, 0.f, 0.f, 0.f};
+        bf16x8 (&pp)[QT] = P[(S + 1) & 1], (&pf)[QT] = P[S & 1];
         Frags f = pre, nx;
-        float x[16];
+        constexpr int E = 8 * QT;
+        float x[E];
         auto vec_op = [&](auto t_tag) __attribute__((always_inline)) {
-          constexpr Step op = softmax_step(decltype(t_tag)::value);
+          constexpr Step op = softmax_step<E>(decltype(t_tag)::value);
           constexpr int i = op.index, qt = (i >> 3) & 1, jj = i & 7;
           if constexpr (op.kind == 0) x[i] = fmaf(sc.t[jj >> 2][qt][jj & 3], c2, -mc[qt]);
           else if constexpr (op.kind == 1) x[i] = __builtin_amdgcn_exp2f(x[i]);
           else { pf[qt][jj] = (__bf16)x[i]; pf[qt][jj + 1] = (__bf16)x[i + 1]; }
         };
-        constexpr int SLOTS = 8 * KC + 2, VEC_SLOTS = SLOTS - 3 * KC / 4;   // the vector work ends early: its test travels beside the last MFMAs
+        constexpr int STEP = 4 * QT, SLOTS = STEP * KC + QT, VEC_SLOTS = SLOTS - 3 * KC / 4;   // the vector work ends early: its test travels beside the last MFMAs
         bool large = false;
         auto slot = [&](auto s_tag) __attribute__((always_inline)) {
-          constexpr int T = decltype(s_tag)::value, I = T / 8 < KC ? T / 8 : KC - 1, N = T - 8 * I;   // the last step has two more
+          constexpr int T = decltype(s_tag)::value, I = T / STEP < KC ? T / STEP : KC - 1, N = T - STEP * I;   // the last step has QT more
           // one wait for both K operands (lgkmcnt(4)) and one for both of V^T (lgkmcnt(2)) instead of one for each
           if constexpr (N == 0) __builtin_amdgcn_s_waitcnt(0xC47F);
-          if constexpr (N == 4) __builtin_amdgcn_s_waitcnt(0xC27F);
-          if constexpr (N < 4) qk(sn, f, I, N);
-          else if constexpr (N < 8) { if (!FIRST) pv(f, pp, I, N - 4); }
-          else { if (!FIRST) row_sums(pp, N - 8); }
-          for_each<steps_before(T, VEC_SLOTS), steps_before(T + 1, VEC_SLOTS)>(vec_op);
+          if constexpr (N == 2 * QT) __builtin_amdgcn_s_waitcnt(0xC27F);
+          if constexpr (N < 2 * QT) qk(sn, f, I, N);
+          else if constexpr (N < STEP) { if (!FIRST) pv(f, pp, I, N - 2 * QT); }
+          else { if (!FIRST) row_sums(pp, N - STEP); }
+          for_each<steps_before<E>(T, VEC_SLOTS), steps_before<E>(T + 1, VEC_SLOTS)>(vec_op);
           if constexpr (T == VEC_SLOTS) large = __any(too_large(pf));
-          if constexpr (N < 2 || (N >= 4 && N < 8)) {
-            constexpr int p = N < 2 ? N : N - 2;
-            if constexpr (I + 1 < KC) load_frag(nx, Kt, Vt, I + 1, p);
-            else load_frag(nx, &Ks[(S + 2) % kNS][0], &Vs[S][0], 0, p);
+          if constexpr (N < 2 || (N >= 2 * QT && N < STEP)) {
+            constexpr int READS = N < 2 ? 1 : 2 / QT, p = N < 2 ? N : 2 + READS * (N - 2 * QT);
+#pragma unroll
+            for (int i = 0; i < READS; ++i) {
+              if constexpr (I + 1 < KC) load_frag(nx, Kt, Vt, I + 1, p + i);
+              else load_frag(nx, &Ks[(S + 2) % kNS][0], &Vs[S][0], 0, p + i);
+            }
           }
-          if constexpr (N == 7 && I + 1 < KC) f = nx;
+          if constexpr (N == STEP - 1 && I + 1 < KC) f = nx;
           __builtin_amdgcn_sched_barrier(0);
         };
-        for_each<0, 4 * KC>(slot);
+        for_each<0, 2 * QT * KC>(slot);
         wait_and_sync<2 * IPW>();   // K(j + 2) and V(j) have landed: everything but what the previous stage issued
         if constexpr (FULL) {
           copy(k_lane, next_k, S, ks_lds);                   // K(j + 4)
@@ -369,7 +366,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
         next_k = places_of(j + kNS + 1);
         next_v = places_of(j + 3);
         __builtin_amdgcn_sched_barrier(0);
-        for_each<4 * KC, SLOTS>(slot);
+        for_each<2 * QT * KC, SLOTS>(slot);
         pre = nx;
         if (__builtin_expect(large, 0)) rescale(sc, pf);
         if (!FULL && j + 1 < n_masked) mask(sn, block_of(j + 1));
@@ -380,12 +377,13 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
       __syncthreads();
       Scores sc;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sc.t[i >> 1][i & 1] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 2 * QT; ++i) sc.t[i & 1][i >> 1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kc = 0; kc < KC; ++kc) {
         Frags f;
         for (int n = 0; n < 2; ++n) load_frag(f, &Ks[0][0], nullptr, kc, n);
-        for (int n = 0; n < 4; ++n) qk(sc, f, kc, n);
+#pragma unroll
+        for (int n = 0; n < 2 * QT; ++n) qk(sc, f, kc, n);
       }
       for (int n = 0; n < 2; ++n) load_frag(pre, &Ks[1][0], nullptr, 0, n);
       for (int n = 2; n < 6; ++n) load_frag(pre, nullptr, &Vs[0][0], 0, n);
@@ -414,24 +412,30 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
         while (more) more = four(Yes{});
       }
       // the last block: its probabilities, its PV product and the one of the block before
-      const auto pv_block = [&](const __bf16* Vt, const bf16x8 (&p)[2]) __attribute__((always_inline)) {
+      const auto pv_block = [&](const __bf16* Vt, const bf16x8 (&p)[QT]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < KC; ++i) {
           Frags f;
           for (int n = 2; n < 6; ++n) load_frag(f, nullptr, Vt, i, n);
-          for (int n = 0; n < 4; ++n) pv(f, p, i, n);
+#pragma unroll
+          for (int n = 0; n < 2 * QT; ++n) pv(f, p, i, n);
         }
-        row_sums(p, 0);
-        row_sums(p, 1);
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) row_sums(p, qt);
       };
       if (n_blocks > 1) {
         const bool odd = n_blocks & 1;   // the block before the last has an odd number
-        const bf16x8 pl[2] = {odd ? P[1][0] : P[0][0], odd ? P[1][1] : P[0][1]};
+        bf16x8 pl[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          const bf16x8 even_p = P[0][qt], odd_p = P[1][qt];
+          pl[qt] = odd ? odd_p : even_p;
+        }
         pv_block(&Vs[(n_blocks - 2) % kNS][0], pl);
       }
       wait_and_sync<0>();
-      probs(sc, 0, P[0][0]);
-      probs(sc, 1, P[0][1]);
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) probs(sc, qt, P[0][qt]);
       if (__any(too_large(P[0]))) rescale(sc, P[0]);
       pv_block(&Vs[(n_blocks - 1) % kNS][0], P[0]);
     }
@@ -441,10 +445,10 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   const bool whole = part == 1 && work.chunks == 1 && group < 0;
   const int64_t row0 = a.part[part].row0 + ((int64_t)pair * tiles + tile) * QROWS;   // of partial results
   const bool mixed = fewest < min(most, end * kKeys);   // rows that some query does not see and another does
-  unsigned odd[2] = {0, 0};   // queries whose results are no numbers
+  unsigned odd = 0;   // the wave's queries whose results are no numbers
 #pragma unroll
-  for (int qt = 0; qt < 2; ++qt) {
-    const Query q = query(w * 32 + 16 * qt + col);
+  for (int qt = 0; qt < QT; ++qt) {
+    const Query q = query(16 * (QT * w + qt) + col);
     if (mixed) {
       float x = ls[qt][0] * 0.f;
 #pragma unroll
@@ -452,12 +456,12 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
 #pragma unroll
         for (int r = 0; r < 4; ++r) x = fmaf(o[mt][qt][r], 0.f, x);
       const uint64_t b = __ballot(q.there && x != 0.f);   // NaN
-      odd[qt] = (unsigned)((b | b >> 16 | b >> 32 | b >> 48) & 0xFFFFu);
+      odd |= (unsigned)((b | b >> 16 | b >> 32 | b >> 48) & 0xFFFFu) << 16 * qt;
     }
     if (!q.there) continue;
     const float inv = q.sees > 0 ? 1.f / ls[qt][0] : 0.f;
     __bf16* const orow = static_cast<__bf16*>(a.out) + q.row * D;
-    const int64_t prow = row0 + w * 32 + 16 * qt + col;
+    const int64_t prow = row0 + 16 * (QT * w + qt) + col;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       if (whole) {
@@ -472,7 +476,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
     if (!whole && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(mc[qt], ls[qt][0]);
   }
   __syncthreads();
-  unsigned again = bad_sh ? ~0u : odd[0] | odd[1] << 16;   // of the wave's queries
+  unsigned again = bad_sh ? ~0u >> (32 - 16 * QT) : odd;
   if (__builtin_expect(again == 0 || n_blocks <= 0, 1)) return;
 
   // ---- row by row: a query of the wave after the other, D / 64 elements of the head a lane ----
@@ -485,7 +489,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   const int32_t* const pages = c.table + entry0 * c.table_stride;
 #pragma unroll 1
   for (; again != 0; again &= again - 1) {
-    const int x = w * 32 + __builtin_ctz(again);
+    const int x = 16 * QT * w + __builtin_ctz(again);
     const Query q = query(x);
     if (!q.there) continue;
     float qv[E], acc[E] = {}, M = -FLT_MAX, L = 0.f;
@@ -535,11 +539,11 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   }
 }
 
-template <int D, bool HALF>
+template <int D, int QT>
 __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileLds<D>];
   const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0, part = (int)blockIdx.x >= grid0 ? 1 : 0;
-  tile_part<D, HALF>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
+  tile_part<D, QT>(a, part, blockIdx.x - (part ? grid0 : 0), lds);
 }
 
 // Shared rows by tiles, own rows by few queries: the products of the one beside the loads of the other.
@@ -547,7 +551,7 @@ template <int D, int NQ, bool NT>
 __global__ __launch_bounds__(64 * kNW, 2) void attn_pages_mixed(const AttnPagesArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[std::max(kTileLds<D>, kFewLds<D, NQ>)];
   const int grid0 = (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles;
-  if ((int)blockIdx.x < grid0) tile_part<D, false>(a, 0, blockIdx.x, lds);
+  if ((int)blockIdx.x < grid0) tile_part<D, 2>(a, 0, blockIdx.x, lds);
   else attn_pages_few<__bf16, D, NQ, NT>(a, 1, blockIdx.x - grid0, lds);
 }
 
@@ -560,8 +564,8 @@ void launch_some(hipStream_t s, const AttnPagesArgs& a) {
   else if (a.part[1].queries == 16) HACK_ATTN_MIXED(1, false);
   else if (a.part[1].queries == 32 && once) HACK_ATTN_MIXED(2, true);
   else if (a.part[1].queries == 32) HACK_ATTN_MIXED(2, false);
-  else if (a.n_shared == 0 && a.G * a.c.n <= kPageTileQueries / 2) hipLaunchKernelGGL((attn_pages_tiles<D, true>), grid, dim3(64 * kNW), 0, s, a);
-  else hipLaunchKernelGGL((attn_pages_tiles<D, false>), grid, dim3(64 * kNW), 0, s, a);
+  else if (a.n_shared == 0 && a.G * a.c.n <= kPageTileQueries / 2) hipLaunchKernelGGL((attn_pages_tiles<D, 1>), grid, dim3(64 * kNW), 0, s, a);
+  else hipLaunchKernelGGL((attn_pages_tiles<D, 2>), grid, dim3(64 * kNW), 0, s, a);
 #undef HACK_ATTN_MIXED
 }
 
