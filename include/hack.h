@@ -560,7 +560,8 @@ typedef struct {
  * Query n < fresh[b] sees the len[b] rows of its sequence, or, causal, the first
  * len[b] - fresh[b] + n + 1 of them (the last fresh[b] rows are the queries' own).  A query
  * that sees no row gives zeros; queries from fresh[b] on are not computed and `out` is left
- * as it is there.  What rows hold that a query does not see (infinities and NaN too) does not reach it.
+ * as it is there.  What rows hold that a query does not see (infinities and NaN too) does not reach it (beyond the
+ * order in which it is summed up).
  *   heads   of q, a multiple G of H: query heads G h .. G h + G - 1 read cache h
  *   q, out  DEVICE [B, heads, N, head_dim]
  *   shared  HOST n_shared groups in ascending order, none in two of them; NULL: none.  Rows that a group shares are read

@@ -118,7 +118,7 @@ template <typename T, int D>
 void launch_some(hipStream_t s, bool merge, AttnPagesArgs& a) {
   const bool both = a.n_shared > 0;
   a.parts = both ? 3 : 2;
-  if (a.part[1].queries == kPageTileQueries || (both && a.part[0].queries == kPageTileQueries)) {
+  if (a.part[1].queries >= kHalfTileQueries || (both && a.part[0].queries >= kHalfTileQueries)) {
     launch_attn_pages_tiles(s, D, a);
   } else {
     const dim3 grid((unsigned)(part_grid(a, 0) + part_grid(a, 1)));

@@ -1,4 +1,4 @@
-// Attention over caches in pages for many queries, bf16: work items of 128 queries, four waves of 32, which share every block of 32 keys through LDS (few
+// Attention over caches in pages for many queries, bf16: work items of 128 queries, four waves of 32, or of 64, four waves of 16, which share every block of 32 keys through LDS (few
 // queries, float32 contexts and the merge of partial results: kernels_attn_pages.hip).
 //
 // The stage is that of the 128-query kernel over contiguous rows: scores of block j + 1, probabilities of block j and PV product of block j - 1 side by
@@ -59,16 +59,17 @@ template <int E> constexpr int steps_before(int s, int slots) {   // in front of
   return t;
 }
 
-template <int D> constexpr int kTileLds = 2 * kNS * kKeys * D * 2 + kRing * 16 + (2 * kNW + 1) * 4;   // bytes
+template <int D> constexpr int kTileLds = 2 * kNS * kKeys * D * 2 + kRing * 16;   // bytes
 
-// Work-group id of a part; lds: kTileLds bytes, 1024-byte aligned.  QT: tiles of 16 queries a wave, 2, or 1 where no item has more than 64 queries.
+// Work-group id of a part; lds: kTileLds bytes, 1024-byte aligned.  QT: tiles of 16 queries a wave, 2 (items of 128) or 1 (64; four work-groups a compute unit at
+// head_dim 64, where LDS holds just as many.  64 queries of 480 units over 604 to 668 rows there: 19.6 us, by two waves of 32 22.7).
 template <int D, int QT>
 __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int id, unsigned char* lds) {
   constexpr int KC = D / 32;        // MFMA steps over head_dim for S^T
   constexpr int MT = D / 16;        // 16-row tiles of O^T
   constexpr int IPW = D / 64;       // copy instructions per wave, block and tensor
   constexpr int BLK = kKeys * D;    // elements per block and tensor
-  constexpr int QROWS = kPageTileQueries;
+  constexpr int QROWS = 64 * QT;
   const Pages& c = a.c;
   const int tiles = a.part[part].tiles;
   // The tiles of an entry, head and chunk follow each other on an XCD (work-group id mod 8), the last ones, which see the most rows, first.
@@ -90,9 +91,11 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   __bf16 (&Ks)[kNS][BLK] = *reinterpret_cast<__bf16 (*)[kNS][BLK]>(lds);
   __bf16 (&Vs)[kNS][BLK] = *reinterpret_cast<__bf16 (*)[kNS][BLK]>(lds + sizeof Ks);
   int64_t (&place_sh)[kRing][2] = *reinterpret_cast<int64_t (*)[kRing][2]>(lds + 2 * sizeof Ks);   // where the two tiles of a block begin in k and v, bytes
-  int* const most_sh = reinterpret_cast<int*>(lds + 2 * sizeof Ks + sizeof place_sh);
+  // In front of the first copies, and behind the last reads, the waves' words lie where K does.
+  int* const most_sh = reinterpret_cast<int*>(lds);
   int* const fewest_sh = most_sh + kNW;
-  int& bad_sh = most_sh[2 * kNW];
+  int* const bad_sh = fewest_sh + kNW;
+  bool bad = false;   // this thread met a page that is none
 
   // ---- queries and the rows that they see ----
   struct Query {
@@ -127,7 +130,6 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
     most_sh[w] = most;
     fewest_sh[w] = fewest;
   }
-  if (tid == 0) bad_sh = 0;
   __syncthreads();
   most = __builtin_amdgcn_readfirstlane(max(max(most_sh[0], most_sh[1]), max(most_sh[2], most_sh[3])));
   fewest = __builtin_amdgcn_readfirstlane(min(min(fewest_sh[0], fewest_sh[1]), min(fewest_sh[2], fewest_sh[3])));
@@ -166,7 +168,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
         int p = table[r >> c.log2_rows];
         if ((unsigned)p >= (unsigned)c.pages) {
           report(c);
-          bad_sh = 1;
+          bad = true;
           p = 0;
         }
         place_sh[(j0 + tid) % kRing][t] = p * c.stride_page + (r & ((1 << c.log2_rows) - 1)) * c.stride_row + h * c.stride_head;
@@ -475,8 +477,11 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
     }
     if (!whole && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(mc[qt], ls[qt][0]);
   }
+  const bool wave_bad = __any(bad);
+  if (lane == 0) bad_sh[w] = wave_bad;
   __syncthreads();
-  unsigned again = bad_sh ? ~0u >> (32 - 16 * QT) : odd;
+  const bool any_bad = (bad_sh[0] | bad_sh[1] | bad_sh[2] | bad_sh[3]) != 0;
+  unsigned again = any_bad ? ~0u >> (32 - 16 * QT) : odd;
   if (__builtin_expect(again == 0 || n_blocks <= 0, 1)) return;
 
   // ---- row by row: a query of the wave after the other, D / 64 elements of the head a lane ----
@@ -523,10 +528,10 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
       const float inv = q.sees > 0 ? 1.f / L : 0.f;
 #pragma unroll
       for (int i = 0; i < E; ++i)
-        if (bad_sh || (float)orow[i] * 0.f != 0.f) orow[i] = (__bf16)(acc[i] * inv);
+        if (any_bad || (float)orow[i] * 0.f != 0.f) orow[i] = (__bf16)(acc[i] * inv);
     } else {
       const float m = ml[0], l = ml[1];
-      const bool all_of_it = bad_sh || l * 0.f != 0.f;
+      const bool all_of_it = any_bad || l * 0.f != 0.f;
       const float f = all_of_it ? 1.f : __builtin_amdgcn_exp2f(M - m);
 #pragma unroll
       for (int i = 0; i < E; ++i)
@@ -564,7 +569,7 @@ void launch_some(hipStream_t s, const AttnPagesArgs& a) {
   else if (a.part[1].queries == 16) HACK_ATTN_MIXED(1, false);
   else if (a.part[1].queries == 32 && once) HACK_ATTN_MIXED(2, true);
   else if (a.part[1].queries == 32) HACK_ATTN_MIXED(2, false);
-  else if (a.n_shared == 0 && a.G * a.c.n <= kPageTileQueries / 2) hipLaunchKernelGGL((attn_pages_tiles<D, 1>), grid, dim3(64 * kNW), 0, s, a);
+  else if (a.part[1].queries == kHalfTileQueries) hipLaunchKernelGGL((attn_pages_tiles<D, 1>), grid, dim3(64 * kNW), 0, s, a);
   else hipLaunchKernelGGL((attn_pages_tiles<D, 2>), grid, dim3(64 * kNW), 0, s, a);
 #undef HACK_ATTN_MIXED
 }

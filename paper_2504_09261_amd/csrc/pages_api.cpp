@@ -74,9 +74,13 @@ constexpr int kFewUncut = 24, kTilesUncut = 48;   // blocks of the longest entry
 // own.  Us a call, tiles of 16 / 32 / 128, head_dim 128, 64 elements of 8 caches of 900 to 4000 rows, 20 queries 157 / 140 / 147; of 300 to 1500 rows, 32 queries
 // 73 / 64 / 61, 48 87 / 80 / 64, 80 114 / 97 / 70.  Where short caches leave compute units without a tile of 32, more tiles of 16 end earlier: 64 units of
 // 61 to 424 rows at head_dim 64, 17 queries 8.8 / 11.2 / 12.0, float32, 169 queries 18.0 / 22.7.
+// Tiles of 64 instead of 128 as long as the device holds all of them at once, four a compute unit at head_dim 64 and two at 128: twice the work-groups, whose stages
+// are half the work, but read all of K and V again.  64 / 128: head_dim 128, 32 units of 680 rows, 256 queries 17.1 / 23.0, a causal prompt of 300 11.1 / 15.2, 64 units,
+// 676 queries (704 work-groups of 64) 36.4 / 34.6; head_dim 64, 16 units of 3900 rows, as many queries (976) 91 / 99, 480 units, 256 queries (1920) 57 / 50.
 int tile_queries(const hack_ctx* ctx, int64_t queries, int64_t units, int32_t max_len) {
   if (queries <= 16) return 16;
-  if (ctx->cfg.dtype != HACK_F32 && queries > 32) return kPageTileQueries;
+  if (ctx->cfg.dtype != HACK_F32 && queries > 32)
+    return queries <= kHalfTileQueries || (queries + kHalfTileQueries - 1) / kHalfTileQueries * units <= (ctx->cfg.head_dim == 64 ? 4 : 2) * (int64_t)ctx->cus ? kHalfTileQueries : kPageTileQueries;
   return max_len < kFewUncut * kKeys && (queries + 31) / 32 * units < 3 * (int64_t)ctx->cus ? 16 : 32;
 }
 
@@ -87,7 +91,7 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
   AttnPart* const part = a->part;
   const auto rows_of = [](const AttnPart& p, int64_t entries) { return entries * p.tiles * p.queries; };   // of partial results, without a cut
   const auto lay_out = [&](int i, int64_t queries, int tile) {
-    const bool large = tile == kPageTileQueries;
+    const bool large = tile >= kHalfTileQueries;
     part[i] = AttnPart{tile, (int32_t)((queries + tile - 1) / tile), 0, large ? kTilesUncut : kFewUncut, large ? 16 : 4, 0.f, 0.f, 0};
   };
   int64_t most = 0, saved = 0;   // queries of a group; bytes that sharing spares
@@ -97,15 +101,19 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
     saved += (int64_t)(s.count - 1) * s.rows * H * 2 * ctx->cfg.head_dim * ctx->elem_bytes;
   }
   if (saved < ctx->share_bytes) a->n_shared = 0;
-  const int own_tile = tile_queries(ctx, GN, units, a->c.max_len), shared_tile = tile_queries(ctx, most, a->n_shared * H, a->c.max_len);
+  int own_tile = tile_queries(ctx, GN, units, a->c.max_len), shared_tile = own_tile;
+  if (a->n_shared > 0) {   // tiles of 16 and of 32 are not mixed, nor those of 64 and of 128
+    if (tile_queries(ctx, most, a->n_shared * H, a->c.max_len) >= kHalfTileQueries) shared_tile = kPageTileQueries;
+    if (own_tile >= kHalfTileQueries) own_tile = kPageTileQueries;
+  }
   lay_out(1, GN, own_tile);
-  lay_out(0, most, shared_tile == kPageTileQueries ? shared_tile : own_tile);   // tiles of 16 and of 32 are not mixed
+  lay_out(0, most, shared_tile);
   if (rows_of(part[0], a->n_shared * H) + rows_of(part[1], units) > ctx->part_rows) a->n_shared = 0;   // no room to join the parts: every element reads all of its rows
   const int64_t shared_rows = rows_of(part[0], a->n_shared * H);
   // Work-groups that blocks are cut for: of few queries four a compute unit (two, three, four, six: 643 MB 121, 120, 119, 118 us, one long cache 105, 107, 103, 106),
   // of 128 two, which is what it holds.  Shorter chunks than kChunk are worth it only up to one a compute unit: 8 units of 20000 rows in 296 chunks 26.3 us, in 256 22.3.
   int64_t spare = ctx->part_rows - shared_rows - rows_of(part[1], units);   // rows that chunks may take beyond, three quarters for those of shared rows
-  const bool large = own_tile == kPageTileQueries || (a->n_shared && shared_tile == kPageTileQueries);
+  const bool large = std::max(own_tile, shared_tile) >= kHalfTileQueries;
   // Float32 tiles of 32, whose products bound them: one, less half of what entries' last chunks may add (8 units of 20000 rows, 100 queries, four / two / one 144 / 121 /
   // 125 us, 16 at head_dim 64, 32 queries 60 / 60 / 51, 32 of 2000 to 9000 rows 70 / 70 / 70, less the half 51).
   const int64_t uncut = units * part[1].tiles;

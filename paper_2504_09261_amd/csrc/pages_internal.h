@@ -41,7 +41,7 @@ struct Shared {
 };
 // The shared rows of groups (0) and the rows that every batch element, or head of it, has alone (1).
 struct AttnPart {
-  int32_t queries;    // of a tile: 16, 32 or kPageTileQueries
+  int32_t queries;    // of a tile: 16 or 32 by few queries, kHalfTileQueries or kPageTileQueries by tiles
   int32_t tiles;      // of an entry's queries
   int32_t pairs;      // (entry, head, chunk) at most
   int32_t uncut;      // entries of up to so many blocks are not cut where none is longer
@@ -50,7 +50,7 @@ struct AttnPart {
   float fill;         // work-groups that fill the device
   int64_t row0;       // first row of its partial results
 };
-constexpr int kPageTileQueries = 128;
+constexpr int kHalfTileQueries = 64, kPageTileQueries = 128;
 struct AttnPagesHead {
   Pages c;
   const void* q;
@@ -83,7 +83,7 @@ __host__ __device__ inline int entry_chunks(int blocks, int chunk) { return bloc
 constexpr int64_t pairs_grid(int64_t pairs, int64_t tiles) { return (pairs + 7) / 8 * 8 * tiles; }
 // merge: partial results may have to be joined.
 void launch_attn_pages(hipStream_t s, int elem_bytes, int head_dim, bool merge, AttnPagesArgs a);
-void launch_attn_pages_tiles(hipStream_t s, int head_dim, const AttnPagesArgs& a);   // where a part has tiles of kPageTileQueries queries; bf16
+void launch_attn_pages_tiles(hipStream_t s, int head_dim, const AttnPagesArgs& a);   // where a part has tiles of kHalfTileQueries or kPageTileQueries; bf16
 // Whether every row of K and V is read by one work-group, whose loads then pass the caches by.
 inline bool reads_once(const AttnPagesArgs& a) { return a.part[1].tiles == 1 && (!(a.parts & 1) || a.part[0].tiles == 1 || a.part[0].queries == kPageTileQueries); }
 // Work-groups of part p in the launch.

@@ -233,6 +233,43 @@ def test_many_sequences_and_groups(contexts, dtype, by_head, n, n_groups):
     hk.check()
 
 
+@pytest.mark.parametrize("d, n, longest", [(64, 65, 300), (128, 65, 300), (128, 130, 2500), (64, 100, 2500)])
+def test_more_queries_than_the_device_holds_at_once(contexts, d, n, longest):
+    """Queries of so many caches that they are taken in the largest tiles, whole and cut; a value that is no number reaches the queries behind it only."""
+    batch, heads = 66, 8
+    hk = contexts(heads, d, "bf16", units=batch * heads)
+    g = torch.Generator(DEV).manual_seed(n)
+    lens = n + (np.arange(batch) * 37) % 150
+    lens[[5, 40]] = (longest, n // 2)
+    fresh = np.full(batch, n)
+    fresh[::7] = np.arange(len(fresh[::7])) * 6 % (n + 1)
+    pool = Pool(hk, lens, 32, g)
+    q = queries((batch, heads, n, d), "bf16", g)
+    f = torch.from_numpy(fresh.astype(np.int32)).to(DEV)
+    fine = torch.full_like(q, 9.0)
+    hk.attn_pages(q, pool.cache, 0.1, fine, causal=True, fresh=f)
+    check_attention(pool, q, fine, float(np.float32(0.1)), True, fresh)
+    out = torch.full_like(q, 9.0)
+    hk.attn_pages(q, pool.cache, 0.1, out)
+    check_attention(pool, q, out, float(np.float32(0.1)))
+    places = [pool.where(b, 3, int(lens[b]) - n + 30, int(lens[b]) - n + 31) for b in (5, 9)]   # new row 30 of each
+    values = [pool.v[p].clone() for p in places]
+    for page, at, head in places:
+        pool.v[page, at, head, 7] = float("nan")
+    out.fill_(9.0)
+    hk.attn_pages(q, pool.cache, 0.1, out, causal=True, fresh=f)
+    same = torch.ones_like(out, dtype=torch.bool)
+    for b in (5, 9):
+        same[b, 3, :, 7] = False
+        assert fresh[b] == n and torch.isnan(out[b, 3, 30:, 7]).all()
+        out[b, 3, 30:, 7] = fine[b, 3, 30:, 7]
+    assert torch.equal(out[same], fine[same])
+    for p, v in zip(places, values):
+        pool.v[p] = v
+    check_attention(pool, q, out, float(np.float32(0.1)), True, fresh)   # queries in front of it: summed again in float32, so within the roundings
+    hk.check()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [1, 40])
 def test_largest_pages(contexts, dtype, n):
