@@ -452,12 +452,13 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   for (int qt = 0; qt < QT; ++qt) {
     const Query q = query(16 * (QT * w + qt) + col);
     if (mixed) {
-      float x = ls[qt][0] * 0.f;
+      float x = 0.f;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) x = fmaf(o[mt][qt][r], 0.f, x);
-      const uint64_t b = __ballot(q.there && x != 0.f);   // NaN
+      // NaN among the sums of rows, beside a number as the sum of probabilities, into which no row goes that is not seen: where that is none, the results are right.
+      const uint64_t b = __ballot(q.there && x != 0.f && ls[qt][0] * 0.f == 0.f);
       odd |= (unsigned)((b | b >> 16 | b >> 32 | b >> 48) & 0xFFFFu) << 16 * qt;
     }
     if (!q.there) continue;
