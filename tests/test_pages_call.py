@@ -43,8 +43,8 @@ def entries():
     SEEN.clear()
 
 
-STRUCT = binding.hack_pages(1024, 2048, 9, 16, 3072, 192, 64, 512, 5, 6, 640, 0, 70)     # one, so that its address stays
-FIELDS = (1024, 2048, 9, 16, 3072, 192, 64, 512, 5, 6, 640, 0, 70)
+STRUCT = binding.hack_pages(1024, 2048, 9, 16, 3200, 192, 64, 512, 5, 6, 640, 0, 70)     # one, so that its address stays
+FIELDS = (1024, 2048, 9, 16, 3200, 192, 64, 512, 5, 6, 640, 0, 70)
 
 
 def info(device=1, dtype=BF16, head_dim=64, heads=3, rows=2):
