@@ -94,10 +94,14 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
     const bool large = tile >= kHalfTileQueries;
     part[i] = AttnPart{tile, (int32_t)((queries + tile - 1) / tile), 0, large ? kTilesUncut : kFewUncut, large ? 16 : 4, 0.f, 0.f, 0};
   };
-  int64_t most = 0, saved = 0;   // queries of a group; bytes that sharing spares
+  int64_t most = 0, saved = 0, members = 0;   // queries of a group; bytes that sharing spares; batch elements in groups
+  int32_t fewest = a->c.max_len, longest = 0; // shared rows of a group
   for (int i = 0; i < a->n_shared; ++i) {
     const Shared& s = a->shared[i];
     most = std::max(most, s.count * GN);
+    members += s.count;
+    fewest = std::min(fewest, s.rows);
+    longest = std::max(longest, s.rows);
     saved += (int64_t)(s.count - 1) * s.rows * H * 2 * ctx->cfg.head_dim * ctx->elem_bytes;
   }
   if (saved < ctx->share_bytes) a->n_shared = 0;
@@ -122,7 +126,8 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
   for (int i = 0; i < 2; ++i) {
     AttnPart& p = part[i];
     const int64_t pairs = i ? units : a->n_shared * H;
-    const int64_t blocks = ((int64_t)a->c.max_len + kKeys - 1) / kKeys + 1, cuts = blocks <= p.uncut ? 1 : (blocks + p.least - 1) / p.least;   // chunks of an entry at most
+    const int64_t rows_most = i == 0 ? longest : a->n_shared && members == a->batch ? a->c.max_len - fewest : a->c.max_len;   // of an entry
+    const int64_t blocks = (rows_most + kKeys - 1) / kKeys + 1, cuts = blocks <= p.uncut ? 1 : (blocks + p.least - 1) / p.least;   // chunks of an entry at most
     const int64_t more = pairs ? std::min(want, (i ? spare : spare * 3 / 4) / p.queries) : 0;
     spare -= std::max<int64_t>(more, 0) * p.queries;
     // A chunk has a `more`-th of all blocks at least, so no entry is cut whose heads and tiles are as many: the longest one alone brings so many times its blocks.
