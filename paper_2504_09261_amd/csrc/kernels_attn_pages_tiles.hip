@@ -6,8 +6,9 @@
 // 16-row tile, which lie in one page, so it has a base of its own, which is read a stage ahead out of a ring in LDS that the
 // threads fill from the table, 256 blocks at a time.  Blocks with rows that some query of the item does not see (the last ones, causal; a first one that
 // begins inside the shared rows) come first, their scores are masked, and rows that nobody sees are not copied: the nearest row that is seen stands in for them.
-// A masked row's probability is zero, which keeps it out of the sums unless its value is an infinity or NaN: an item whose results are no numbers, or
-// that met a page that is none, does these queries again row by row, and numbers among their results stand.
+// A masked row's probability is zero, which keeps it out of the sums unless its value is an infinity or NaN (its own, or that of the seen row that stands in for
+// it: zero times an infinity is NaN, whoever sees the row): an item that had masked blocks and whose results are no numbers, or that met a page that is none, does
+// these queries again row by row, and numbers among their results stand.
 //
 // Bound by the matrix cores and the vector work beside them.  Measured, head_dim 128: 3000 causal queries of 32 heads over 4001 to 7001 rows of 8 caches 248 to 258 us (1.05 to 1.09
 // PFLOP/s; a large library product reaches 1.2), without the mask 314 (1.10).  At head_dim 64 the exponentials of a block stand beside half the products: the same at 64, 174 us
@@ -446,12 +447,11 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   // ---- normalise and store: a lane holds head-dim 16mt + 4g .. +4 of queries 16qt + col ----
   const bool whole = part == 1 && work.chunks == 1 && group < 0;
   const int64_t row0 = a.part[part].row0 + ((int64_t)pair * tiles + tile) * QROWS;   // of partial results
-  const bool mixed = fewest < min(most, end * kKeys);   // rows that some query does not see and another does
   unsigned odd = 0;   // the wave's queries whose results are no numbers
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
     const Query q = query(16 * (QT * w + qt) + col);
-    if (mixed) {
+    if (n_masked > 0) {
       float x = 0.f;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)

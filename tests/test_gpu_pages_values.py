@@ -1,0 +1,54 @@
+"""Caches in pages where rows hold values that are no numbers, pages are none or lengths are out of range: what reaches a query, what is stored, and that such a
+call stays about as fast as another one.  Plain implementations in 64 bits; the tolerances are those of tests/test_gpu_pages.py."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_operators import DEV
+from tests.test_gpu_pages import Pool, check_attention, contexts, queries  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+def scale_of(d):
+    return float(np.float32(d ** -0.5))
+
+
+def put(pool, b, h, row, col, value):
+    """An element of V, in every sequence's page of that row; what was there."""
+    at = pool.where(b, h, row, row + 1)
+    old = pool.v[at].clone()
+    pool.v[at[0], at[1], at[2], col] = value
+    return lambda: pool.v.__setitem__(at, old)
+
+
+# ---- rows that all queries see, in blocks that end or begin with rows that none sees ----
+@pytest.mark.parametrize("value", [INF, -INF])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [16, 40, 130])
+@pytest.mark.parametrize("length, prefix", [(1, 0), (17, 0), (65, 0), (81, 0), (3009, 0), (3025, 0), (3025, 1009), (1100, 1025), (1057, 1041)])
+def test_infinities_that_all_queries_see(contexts, value, d, n, length, prefix):  # noqa: F811
+    """An infinity in a row that every query sees is the result's, not a NaN, wherever the row lies: at the end of a sequence or on either side of a shared prefix's
+    end; the other elements stay as they are."""
+    hk = contexts(2, d, "bf16", shared=0)
+    g = torch.Generator(DEV).manual_seed(length + n)
+    groups = [(0, 2, prefix)] if prefix else []
+    lens = [length, length + 7 if prefix else length // 2 + 3]
+    pool = Pool(hk, lens, 16, g, shared=groups)
+    q = queries((2, 4, n, d), "bf16", g)
+    fine, out = torch.full_like(q, 9.0), torch.full_like(q, 9.0)
+    hk.attn_pages(q, pool.cache, d ** -0.5, fine, shared=groups)
+    check_attention(pool, q, fine, scale_of(d))
+    rows = sorted({r for r in (0, length - 1, (length - 1) // 16 * 16, (length - 1) // 32 * 32, prefix - 1, prefix) if 0 <= r < length})
+    for i, r in enumerate(rows):                 # each in a column of its own
+        for b in ((0, 1) if r < prefix else (0,)):
+            put(pool, b, 1, r, 3 * i, value)
+    hk.attn_pages(q, pool.cache, d ** -0.5, out, shared=groups)
+    same = torch.ones_like(out, dtype=torch.bool)
+    for i, r in enumerate(rows):
+        for b in ((0, 1) if r < prefix else (0,)):
+            assert (out[b, 2:, :, 3 * i] == value).all(), (b, r, out[b, 2:, :, 3 * i].unique())
+            same[b, 2:, :, 3 * i] = False
+    assert torch.equal(out[same], fine[same])
+    hk.check()
