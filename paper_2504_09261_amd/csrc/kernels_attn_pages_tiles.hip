@@ -7,8 +7,8 @@
 // threads fill from the table, 256 blocks at a time.  Blocks with rows that some query of the item does not see (the last ones, causal; a first one that
 // begins inside the shared rows) come first, their scores are masked, and rows that nobody sees are not copied: the nearest row that is seen stands in for them.
 // A masked row's probability is zero, which keeps it out of the sums unless its value is an infinity or NaN (its own, or that of the seen row that stands in for
-// it: zero times an infinity is NaN, whoever sees the row): an item that had masked blocks and whose results are no numbers, or that met a page that is none, does
-// these queries again row by row, and numbers among their results stand.
+// it: zero times an infinity is NaN, whoever sees the row): an item whose results are no numbers, and that finds values that are none in the rows of its masked
+// blocks, or that met a page that is none, does these queries again row by row, and numbers among their results stand.
 //
 // Bound by the matrix cores and the vector work beside them.  Measured, head_dim 128: 3000 causal queries of 32 heads over 4001 to 7001 rows of 8 caches 248 to 258 us (1.05 to 1.09
 // PFLOP/s; a large library product reaches 1.2), without the mask 314 (1.10).  At head_dim 64 the exponentials of a block stand beside half the products: the same at 64, 174 us
@@ -95,7 +95,8 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   // In front of the first copies, and behind the last reads, the waves' words lie where K does.
   int* const most_sh = reinterpret_cast<int*>(lds);
   int* const fewest_sh = most_sh + kNW;
-  int* const bad_sh = fewest_sh + kNW;
+  int* const again_sh = fewest_sh + kNW;
+  int* const strange_sh = again_sh + kNW;
   bool bad = false;   // this thread met a page that is none
 
   // ---- queries and the rows that they see ----
@@ -478,12 +479,32 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
     }
     if (!whole && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(mc[qt], ls[qt][0]);
   }
+  // Results that are no numbers may be what the queries see: only rows of masked blocks can have brought them to queries that do not see these rows.
   const bool wave_bad = __any(bad);
-  if (lane == 0) bad_sh[w] = wave_bad;
+  if (lane == 0) again_sh[w] = (wave_bad ? 2 : 0) | (odd != 0 ? 1 : 0);
   __syncthreads();
-  const bool any_bad = (bad_sh[0] | bad_sh[1] | bad_sh[2] | bad_sh[3]) != 0;
+  const int found = again_sh[0] | again_sh[1] | again_sh[2] | again_sh[3];
+  if (__builtin_expect(found == 0 || n_blocks <= 0, 1)) return;
+  const bool any_bad = found & 2;
+  if (!any_bad) {
+    const int32_t* const table = c.table + entry0 * c.table_stride;
+    constexpr int PIECES = D / 8;   // of 16 bytes in a row
+    bool strange = false;
+    for (int64_t x = tid; x < (int64_t)n_masked * (kKeys * PIECES); x += kNW * 64) {
+      const int key = block_of((int)(x / (kKeys * PIECES))) * kKeys + (int)(x / PIECES % kKeys);
+      if (key < lo || key >= most) continue;
+      const int p = table[key >> c.log2_rows];
+      if ((unsigned)p >= (unsigned)c.pages) continue;
+      const uintx4 v = *reinterpret_cast<const uintx4*>(c.v + p * c.stride_page + (key & ((1 << c.log2_rows) - 1)) * c.stride_row + h * c.stride_head + x % PIECES * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) strange |= (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
+    }
+    const bool wave_strange = __any(strange);
+    if (lane == 0) strange_sh[w] = wave_strange;
+    __syncthreads();
+    if (!(strange_sh[0] | strange_sh[1] | strange_sh[2] | strange_sh[3])) return;
+  }
   unsigned again = any_bad ? ~0u >> (32 - 16 * QT) : odd;
-  if (__builtin_expect(again == 0 || n_blocks <= 0, 1)) return;
 
   // ---- row by row: a query of the wave after the other, D / 64 elements of the head a lane ----
   constexpr int E = D / 64;

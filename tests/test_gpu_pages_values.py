@@ -23,6 +23,18 @@ def put(pool, b, h, row, col, value):
     return lambda: pool.v.__setitem__(at, old)
 
 
+def median_ms(call, times=5):
+    ms = []
+    for _ in range(times):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        call()
+        b.record()
+        torch.cuda.synchronize()
+        ms.append(a.elapsed_time(b))
+    return sorted(ms)[len(ms) // 2]
+
+
 # ---- rows that all queries see, in blocks that end or begin with rows that none sees ----
 @pytest.mark.parametrize("value", [INF, -INF])
 @pytest.mark.parametrize("d", [64, 128])
@@ -52,3 +64,40 @@ def test_infinities_that_all_queries_see(contexts, value, d, n, length, prefix):
             same[b, 2:, :, 3 * i] = False
     assert torch.equal(out[same], fine[same])
     hk.check()
+
+
+# ---- rows behind a prompt ----
+def nan_behind_a_prompt(contexts, d, heads, row):  # noqa: F811
+    """A NaN in V reaches the queries that see its row and no other, and the call takes about as long as without it; four heads: in tiles of 64 queries, many: of 128."""
+    n, length = 1000, 3000
+    hk = contexts(heads, d, "bf16", units=128)
+    g = torch.Generator(DEV).manual_seed(row)
+    pool = Pool(hk, [length], 64, g)
+    q = queries((1, heads, n, d), "bf16", g)
+    fine, out = torch.full_like(q, 9.0), torch.full_like(q, 9.0)
+
+    def call(to):
+        hk.attn_pages(q, pool.cache, d ** -0.5, to, causal=True)
+    call(fine)
+    clean = median_ms(lambda: call(fine))
+    back = put(pool, 0, 1, row, 5, float("nan"))
+    call(out)
+    strange = median_ms(lambda: call(out))
+    same = torch.ones_like(out, dtype=torch.bool)
+    same[0, 1, :, 5] = False
+    assert torch.equal(out[same], fine[same])
+    first = max(0, row - (length - n))           # the first query that sees it
+    assert torch.isnan(out[0, 1, first:, 5]).all()
+    out[0, 1, first:, 5] = fine[0, 1, first:, 5]
+    back()
+    check_attention(pool, q, out, scale_of(d), True)
+    hk.check()
+    assert strange < 8 * clean + 0.3, (clean, strange)
+
+
+HEADS = pytest.mark.parametrize("d, heads", [(64, 4), (128, 4), (64, 72), (128, 40)])
+
+
+@HEADS
+def test_a_nan_that_all_queries_see(contexts, d, heads):  # noqa: F811
+    nan_behind_a_prompt(contexts, d, heads, 0)
