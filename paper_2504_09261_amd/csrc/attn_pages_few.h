@@ -1,4 +1,5 @@
-// Attention over caches in pages, few queries (tiles of 16 and 32), as the kernels that have such tiles alone and beside larger ones share it: O = Softmax(scale Q K^T) V
+// Attention over caches in pages, few queries (tiles of 16 and 32), as the kernels that have such tiles alone, beside larger ones and in
+// place of results of larger ones share it: O = Softmax(scale Q K^T) V
 // over the rows that a query sees.  HIP device code only.
 //
 // A work-group takes 16 NQ queries and a chunk of keys, its four waves every fourth block (32 keys, float32 16), each by itself.  S^T = K Q^T, one softmax update a block, O^T +=
@@ -147,11 +148,31 @@ __device__ __forceinline__ void store_some(float* p, const float* x, int n, floa
   for (int i = 0; i < n; i += 4) *reinterpret_cast<floatx4*>(p + i) = floatx4{x[i] * f, x[i + 1] * f, x[i + 2] * f, x[i + 3] * f};
 }
 
+// Elements that are no numbers alone are replaced.
+template <typename T> __device__ __forceinline__ void mend_some(T* p, const float* x, int n, float f) {
+#pragma unroll
+  for (int i = 0; i < n; ++i)
+    if ((float)p[i] * 0.f != 0.f) p[i] = (T)(x[i] * f);
+}
+
 template <int D, int NQ> constexpr int kFewLds = kWaves * 16 * NQ * (D + 2) * (int)sizeof(float);   // bytes
 
-// Work-group id of a part; lds: kFewLds bytes, 1024-byte aligned.  NT: rows are read once, past the caches.
-template <typename T, int D, int NQ, bool NT>
-__device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part, int id, unsigned char* lds) {
+// What a work-group takes: queries of an entry and head from number query0 on, and a chunk of the keys.
+struct FewItem {
+  int b0, h, entry0;     // the first (or only) batch element; row of the table
+  int group, common;     // whose shared rows the element has, and how many these are
+  int lo, n_rows;        // first row of this part, queries of the entry
+  int query0;
+  int chunks, chunk;
+  int64_t row0;          // of the partial results of query0
+  // MEND: the chunk is blocks first to end of kKeys keys; all: results of a tile are replaced, not only their elements that are no numbers
+  int first, end;
+  bool all;
+};
+
+// lds: kFewLds bytes, 1024-byte aligned.  NT: rows are read once, past the caches.  MEND: over results of a tile, which stand in `out` or among the partial results.
+template <typename T, int D, int NQ, bool NT, bool MEND>
+__device__ __forceinline__ void few_queries(const AttnPagesArgs& a, int part, const FewItem& item, unsigned char* lds) {
   using Keys = KeyRows<T, D, NT>;
   using Values = ValueRows<T, D, NT>;
   constexpr int ROWS = Keys::kRows, TILES = ROWS / 16, PIECES = Keys::kChunks / 4;
@@ -159,21 +180,10 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int MT = D / 16, QROWS = 16 * NQ, SIDE = kBf16 ? MT : 4;   // head-dims of a lane that lie side by side
   const Pages& c = a.c;
-  const int tiles = a.part[part].tiles;
-  // The tiles of an entry, head and chunk follow each other on an XCD (work-group id mod 8).
-  const int along = id >> 3, pair = (along / tiles) * 8 + (id & 7), tile = along % tiles;
-  Work work;
-  if (!find_work(a, part, pair, work)) return;
-  const int chunk = work.local % work.chunks;
-  if (work.local == 0 && tile == 0 && threadIdx.x == 0) a.plan[(part ? a.n_shared : 0) + work.entry] = make_int2(work.base, work.chunks);
-  const int b0 = part == 0 ? a.shared[work.entry].first : c.by_head ? work.entry / c.heads : work.entry;   // the first (or only) batch element
-  const int h = part == 1 && c.by_head ? work.entry % c.heads : work.local / work.chunks;
-  const int group = part == 0 ? work.entry : group_of(a, b0), common = shared_rows(a, group);
-  const int entry0 = c.by_head ? b0 * c.heads + h : b0;     // of the table
-  const int lo = part ? common : 0;
-  const int GN = a.G * c.n, n_rows = part ? GN : a.shared[work.entry].count * GN;
-  if (tile * QROWS >= n_rows) return;
-  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int b0 = item.b0, h = item.h, entry0 = item.entry0, group = item.group, common = item.common, lo = item.lo, n_rows = item.n_rows, GN = a.G * c.n;
+  int tid = threadIdx.x;
+  if constexpr (MEND) asm volatile("" : "+v"(tid));   // what follows from it does not stay in registers through the tile's stages
+  const int lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   float (&ring)[kWaves][16 * NQ * D] = *reinterpret_cast<float (*)[kWaves][16 * NQ * D]>(lds);
@@ -186,9 +196,9 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
   int most = 0, fewest = c.max_len;
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
-    const int j = min(tile * QROWS + 16 * qt + col, n_rows - 1), m = j / GN, r = j - m * GN, n = r / a.G, b = b0 + m;
+    const int j = min(item.query0 + 16 * qt + col, n_rows - 1), m = j / GN, r = j - m * GN, n = r / a.G, b = b0 + m;
     const int fresh = fresh_of(c, b), len = rows_of(c, c.by_head ? b * c.heads + h : b);
-    const bool there = tile * QROWS + 16 * qt + col < n_rows && n < fresh;
+    const bool there = item.query0 + 16 * qt + col < n_rows && n < fresh;
     sees[qt] = max(0, a.causal ? len - fresh + n + 1 : len);
     if (part == 0) sees[qt] = min(sees[qt], common);
     if (there) {
@@ -215,7 +225,8 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
   // ---- this wave's blocks of kRows keys: first + w, first + w + 4, ... ----
   constexpr int PER = kKeys / ROWS;
   const int n_blocks = blocks_between(lo, most), begin = lo / kKeys;
-  const int first = (begin + chunk_at(n_blocks, work.chunks, chunk)) * PER, last = (begin + chunk_at(n_blocks, work.chunks, chunk + 1)) * PER;
+  const int first = (MEND ? item.first : begin + chunk_at(n_blocks, item.chunks, item.chunk)) * PER;
+  const int last = (MEND ? min(item.end, begin + n_blocks) : begin + chunk_at(n_blocks, item.chunks, item.chunk + 1)) * PER;
   const ConstInts table = as_const(c.table) + entry0 * c.table_stride;
   const int in_page = (1 << c.log2_rows) - 1;
   // Tiles of 16 rows lie in one page.  Tiles behind the last row that is seen, or in front of the first one, are the nearest again (their scores are masked).
@@ -453,18 +464,17 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
     }
   }
   __syncthreads();
-  const bool whole = part == 1 && work.chunks == 1 && group < 0;
-  const int64_t slot = (int64_t)pair * tiles + tile;
+  const bool whole = part == 1 && item.chunks == 1 && group < 0;
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
     float M = -FLT_MAX;
 #pragma unroll
     for (int x = 0; x < kWaves; ++x) M = fmaxf(M, m_sh[x][16 * qt + col]);
-    float f[kWaves], L = 0.f;
+    float fw[kWaves], L = 0.f;
 #pragma unroll
     for (int x = 0; x < kWaves; ++x) {
-      f[x] = __builtin_amdgcn_exp2f(m_sh[x][16 * qt + col] - M);   // a wave without blocks has summed nothing
-      L = fmaf(f[x], l_sh[x][16 * qt + col], L);
+      fw[x] = __builtin_amdgcn_exp2f(m_sh[x][16 * qt + col] - M);   // a wave without blocks has summed nothing
+      L = fmaf(fw[x], l_sh[x][16 * qt + col], L);
     }
     float acc[MT];
 #pragma unroll
@@ -473,24 +483,52 @@ __device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part,
 #pragma unroll
       for (int x = 0; x < kWaves; ++x) {
         const float4 p = reinterpret_cast<const float4*>(&ring[x][0])[((w * NQ + qt) * (MT / 4) + m4) * 64 + lane];
-        s.x = fmaf(f[x], p.x, s.x);
-        s.y = fmaf(f[x], p.y, s.y);
-        s.z = fmaf(f[x], p.z, s.z);
-        s.w = fmaf(f[x], p.w, s.w);
+        s.x = fmaf(fw[x], p.x, s.x);
+        s.y = fmaf(fw[x], p.y, s.y);
+        s.z = fmaf(fw[x], p.z, s.z);
+        s.w = fmaf(fw[x], p.w, s.w);
       }
       acc[4 * m4] = s.x; acc[4 * m4 + 1] = s.y; acc[4 * m4 + 2] = s.z; acc[4 * m4 + 3] = s.w;
     }
     if (row[qt] < 0) continue;
     const float inv = sees[qt] > 0 ? 1.f / L : 0.f;
-    const int64_t prow = a.part[part].row0 + slot * QROWS + 16 * qt + col;
+    const int64_t prow = item.row0 + 16 * qt + col;
+    const bool some = MEND && !item.all;
+    float f = 1.f;
+    if (some && !whole) f = __builtin_amdgcn_exp2f(M - a.part_ml[2 * prow]);   // to the reference that stays
 #pragma unroll
     for (int mt = 0; mt < MT; mt += SIDE) {
       const int d = Values::dim(mt, 4 * g + w);
-      if (whole) store_some(static_cast<T*>(a.out) + row[qt] * D + d, acc + mt, SIDE, inv);
+      if (some && whole) mend_some(static_cast<T*>(a.out) + row[qt] * D + d, acc + mt, SIDE, inv);
+      else if (some) mend_some(a.part_o + prow * D + d, acc + mt, SIDE, f);
+      else if (whole) store_some(static_cast<T*>(a.out) + row[qt] * D + d, acc + mt, SIDE, inv);
       else store_some(a.part_o + prow * D + d, acc + mt, SIDE, 1.f);
     }
-    if (!whole && w == 0 && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(M, L);
+    if (!some && !whole && w == 0 && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(M, L);
   }
+}
+
+// Work-group id of a part; lds: kFewLds bytes, 1024-byte aligned.
+template <typename T, int D, int NQ, bool NT>
+__device__ __forceinline__ void attn_pages_few(const AttnPagesArgs& a, int part, int id, unsigned char* lds) {
+  constexpr int QROWS = 16 * NQ;
+  const Pages& c = a.c;
+  const int tiles = a.part[part].tiles;
+  // The tiles of an entry, head and chunk follow each other on an XCD (work-group id mod 8).
+  const int along = id >> 3, pair = (along / tiles) * 8 + (id & 7), tile = along % tiles;
+  Work work;
+  if (!find_work(a, part, pair, work)) return;
+  const int chunk = work.local % work.chunks;
+  if (work.local == 0 && tile == 0 && threadIdx.x == 0) a.plan[(part ? a.n_shared : 0) + work.entry] = make_int2(work.base, work.chunks);
+  const int b0 = part == 0 ? a.shared[work.entry].first : c.by_head ? work.entry / c.heads : work.entry;   // the first (or only) batch element
+  const int h = part == 1 && c.by_head ? work.entry % c.heads : work.local / work.chunks;
+  const int group = part == 0 ? work.entry : group_of(a, b0), common = shared_rows(a, group);
+  const int entry0 = c.by_head ? b0 * c.heads + h : b0;     // of the table
+  const int lo = part ? common : 0;
+  const int GN = a.G * c.n, n_rows = part ? GN : a.shared[work.entry].count * GN;
+  if (tile * QROWS >= n_rows) return;
+  few_queries<T, D, NQ, NT, false>(a, part, FewItem{b0, h, entry0, group, common, lo, n_rows, tile * QROWS, work.chunks, chunk,
+                                                    a.part[part].row0 + ((int64_t)pair * tiles + tile) * QROWS, 0, 0, false}, lds);
 }
 
 }  // namespace dev

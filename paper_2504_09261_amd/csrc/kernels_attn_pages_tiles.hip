@@ -7,8 +7,10 @@
 // threads fill from the table, 256 blocks at a time.  Blocks with rows that some query of the item does not see (the last ones, causal; a first one that
 // begins inside the shared rows) come first, their scores are masked, and rows that nobody sees are not copied: the nearest row that is seen stands in for them.
 // A masked row's probability is zero, which keeps it out of the sums unless its value is an infinity or NaN (its own, or that of the seen row that stands in for
-// it: zero times an infinity is NaN, whoever sees the row): an item whose results are no numbers, and that finds values that are none in the rows of its masked
-// blocks, or that met a page that is none, does these queries again row by row, and numbers among their results stand.
+// it: zero times an infinity is NaN, whoever sees the row).  An item whose results are no numbers, and that finds values that are none in the rows of its masked
+// blocks, does the queries of these waves again as few queries do it (attn_pages_few.h), and numbers among their results stand; one that met a page that is none
+// does all of its queries again.  1000 causal queries of 72 heads of 64 over 3000 rows 94 us; with a NaN that some queries of an item see 234, with a page that is none 765
+// (key by key in each wave, query after query: 42.5 ms).
 //
 // Bound by the matrix cores and the vector work beside them.  Measured, head_dim 128: 3000 causal queries of 32 heads over 4001 to 7001 rows of 8 caches 248 to 258 us (1.05 to 1.09
 // PFLOP/s; a large library product reaches 1.2), without the mask 314 (1.10).  At head_dim 64 the exponentials of a block stand beside half the products: the same at 64, 174 us
@@ -448,7 +450,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   // ---- normalise and store: a lane holds head-dim 16mt + 4g .. +4 of queries 16qt + col ----
   const bool whole = part == 1 && work.chunks == 1 && group < 0;
   const int64_t row0 = a.part[part].row0 + ((int64_t)pair * tiles + tile) * QROWS;   // of partial results
-  unsigned odd = 0;   // the wave's queries whose results are no numbers
+  bool odd = false;   // queries of the wave have results that are no numbers
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
     const Query q = query(16 * (QT * w + qt) + col);
@@ -459,8 +461,7 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
 #pragma unroll
         for (int r = 0; r < 4; ++r) x = fmaf(o[mt][qt][r], 0.f, x);
       // NaN among the sums of rows, beside a number as the sum of probabilities, into which no row goes that is not seen: where that is none, the results are right.
-      const uint64_t b = __ballot(q.there && x != 0.f && ls[qt][0] * 0.f == 0.f);
-      odd |= (unsigned)((b | b >> 16 | b >> 32 | b >> 48) & 0xFFFFu) << 16 * qt;
+      odd |= __any(q.there && x != 0.f && ls[qt][0] * 0.f == 0.f);
     }
     if (!q.there) continue;
     const float inv = q.sees > 0 ? 1.f / ls[qt][0] : 0.f;
@@ -481,11 +482,12 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
   }
   // Results that are no numbers may be what the queries see: only rows of masked blocks can have brought them to queries that do not see these rows.
   const bool wave_bad = __any(bad);
-  if (lane == 0) again_sh[w] = (wave_bad ? 2 : 0) | (odd != 0 ? 1 : 0);
+  if (lane == 0) again_sh[w] = (wave_bad ? 15 : 0) | (odd ? 16 << w : 0);
   __syncthreads();
   const int found = again_sh[0] | again_sh[1] | again_sh[2] | again_sh[3];
-  if (__builtin_expect(found == 0 || n_blocks <= 0, 1)) return;
-  const bool any_bad = found & 2;
+  if (__builtin_expect(found == 0, 1)) return;
+  const bool any_bad = found & 15;
+  const int todo = any_bad ? 15 : found >> 4;   // waves
   if (!any_bad) {
     const int32_t* const table = c.table + entry0 * c.table_stride;
     constexpr int PIECES = D / 8;   // of 16 bytes in a row
@@ -504,70 +506,20 @@ __device__ __forceinline__ void tile_part(const AttnPagesArgs& a, int part, int 
     __syncthreads();
     if (!(strange_sh[0] | strange_sh[1] | strange_sh[2] | strange_sh[3])) return;
   }
-  unsigned again = any_bad ? ~0u >> (32 - 16 * QT) : odd;
-
-  // ---- row by row: a query of the wave after the other, D / 64 elements of the head a lane ----
-  constexpr int E = D / 64;
-  typedef std::conditional_t<E == 2, unsigned, unsigned short> Piece;
-  const auto unpack = [](Piece p, float (&x)[E]) {
-    x[0] = __builtin_bit_cast(float, (unsigned)p << 16);
-    if constexpr (E == 2) x[1] = __builtin_bit_cast(float, (unsigned)p & 0xFFFF0000u);
-  };
-  const int32_t* const pages = c.table + entry0 * c.table_stride;
+  // 16 queries after the other, all waves at each (32 at a time: the kernels spill).
+  static_assert(kFewLds<D, 1> <= kTileLds<D>, "few queries fit in a tile's LDS");
 #pragma unroll 1
-  for (; again != 0; again &= again - 1) {
-    const int x = 16 * QT * w + __builtin_ctz(again);
-    const Query q = query(x);
-    if (!q.there) continue;
-    float qv[E], acc[E] = {}, M = -FLT_MAX, L = 0.f;
-    unpack(*reinterpret_cast<const Piece*>(static_cast<const __bf16*>(a.q) + q.row * D + E * lane), qv);
-    const int key1 = min(q.sees, end * kKeys);
-#pragma unroll 1
-    for (int key = max(lo, first * kKeys); key < key1; ++key) {
-      const int p = pages[key >> c.log2_rows];
-      if ((unsigned)p >= (unsigned)c.pages) continue;
-      const int64_t off = p * c.stride_page + (key & ((1 << c.log2_rows) - 1)) * c.stride_row + h * c.stride_head + E * 2 * lane;
-      float kv[E], vv[E], s = 0.f;
-      unpack(*reinterpret_cast<const Piece*>(c.k + off), kv);
-      unpack(*reinterpret_cast<const Piece*>(c.v + off), vv);
-#pragma unroll
-      for (int i = 0; i < E; ++i) s = fmaf(qv[i], kv[i], s);
-#pragma unroll
-      for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i, 64);
-      s *= a.scale * kLog2eF;
-      const float m = maximum(M, s), f = __builtin_amdgcn_exp2f(M - m), pr = __builtin_amdgcn_exp2f(s - m);
-      M = m;
-      L = fmaf(L, f, pr);
-#pragma unroll
-      for (int i = 0; i < E; ++i) acc[i] = fmaf(pr, vv[i], acc[i] * f);
-    }
-    // Numbers among the results stand, unless a page was none or the sum of probabilities is no number.
-    const int64_t prow = row0 + x;
-    __bf16* const orow = static_cast<__bf16*>(a.out) + q.row * D + E * lane;
-    float* const po = a.part_o + prow * D + E * lane;
-    float* const ml = a.part_ml + 2 * prow;
-    if (whole) {
-      const float inv = q.sees > 0 ? 1.f / L : 0.f;
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (any_bad || (float)orow[i] * 0.f != 0.f) orow[i] = (__bf16)(acc[i] * inv);
-    } else {
-      const float m = ml[0], l = ml[1];
-      const bool all_of_it = any_bad || l * 0.f != 0.f;
-      const float f = all_of_it ? 1.f : __builtin_amdgcn_exp2f(M - m);
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (all_of_it || po[i] * 0.f != 0.f) po[i] = acc[i] * f;
-      if (all_of_it && lane == 0) {
-        ml[0] = M;
-        ml[1] = L;
-      }
-    }
+  for (int x = 0; x < QT * kNW; ++x) {
+    if (!(todo >> x / QT & 1)) continue;
+    __syncthreads();
+    few_queries<__bf16, D, 1, false, true>(a, part, FewItem{b0, h, entry0, group, common, lo, n_rows, tile * QROWS + 16 * x, work.chunks, chunk, row0 + 16 * x, first, end,
+                                                            any_bad}, lds);
   }
 }
 
+// Work-groups a compute unit: as many as LDS and the registers that they ask for allow.
 template <int D, int QT>
-__global__ __launch_bounds__(64 * kNW, 2) void attn_pages_tiles(const AttnPagesArgs a) {
+__global__ __launch_bounds__(64 * kNW, D == 128 ? 2 : QT == 1 ? 4 : 3) void attn_pages_tiles(const AttnPagesArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileLds<D>];
   const int grid0 = a.parts & 1 ? (a.part[0].pairs + 7) / 8 * 8 * a.part[0].tiles : 0, part = (int)blockIdx.x >= grid0 ? 1 : 0;
   tile_part<D, QT>(a, part, blockIdx.x - (part ? grid0 : 0), lds);

@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_operators import DEV
+from paper_2504_09261_amd.binding import HackError
+from tests.test_gpu_operators import DEV, H, HALF_STEP
 from tests.test_gpu_pages import Pool, check_attention, contexts, queries  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -101,3 +102,85 @@ HEADS = pytest.mark.parametrize("d, heads", [(64, 4), (128, 4), (64, 72), (128, 
 @HEADS
 def test_a_nan_that_all_queries_see(contexts, d, heads):  # noqa: F811
     nan_behind_a_prompt(contexts, d, heads, 0)
+
+
+# ---- rows that are masked for some queries ----
+@HEADS
+@pytest.mark.parametrize("row", [1999, 2500, 2999])
+def test_a_nan_that_some_queries_see(contexts, d, heads, row):  # noqa: F811
+    nan_behind_a_prompt(contexts, d, heads, row)
+
+
+# ---- pages that are none ----
+def check_without(pool, q, out, scale, causal, gone):
+    """As check_attention, with rows that are left out: gone[b] is a list of rows of batch element b."""
+    B, heads, N, d = q.shape
+    G = heads // pool.heads
+    for b in range(B):
+        for h in range(pool.heads):
+            k, v = pool.rows(b, h)
+            n = k.shape[0]
+            x, got = (t[b, h * G:(h + 1) * G].double().reshape(-1, d) for t in (q, out))
+            sees = (n - N + 1 + torch.arange(N, device=DEV) if causal else torch.full((N,), n, device=DEV)).repeat(G)[:, None]
+            hidden = torch.arange(n, device=DEV) >= sees
+            hidden[:, torch.tensor(gone[b], dtype=torch.int64, device=DEV)] = True
+            p = torch.softmax((x @ k.T.contiguous() * scale).masked_fill(hidden, -INF), -1)
+            size = torch.where(hidden, 0.0, x.abs() @ k.abs().T.contiguous()).amax(-1, keepdim=True)
+            want = p @ v
+            tol = (2 * 2.0 ** -8 + 2 * scale * (d + 4) * H * size + 1e-5) * (p @ v.abs()) * 1.01 + HALF_STEP["bf16"] * 1.01 * want.abs() + 2.0 ** -111 * (1 + v.abs().sum(0))
+            err = (got - want).abs()
+            assert (err <= tol).all(), (b, h, float((err / tol).max()))
+
+
+@HEADS
+@pytest.mark.parametrize("page", [0, 20, 46])
+def test_prompt_over_a_page_that_is_none(contexts, d, heads, page):  # noqa: F811
+    """Its rows are left out, the other elements of the batch are as they were, and the call takes about as long as another one."""
+    n, lens = 500, [3000, 1300]
+    hk = contexts(heads, d, "bf16", units=144)
+    g = torch.Generator(DEV).manual_seed(page)
+    pool = Pool(hk, lens, 64, g)
+    q = queries((2, heads, n, d), "bf16", g)
+    fine, out = torch.full_like(q, 9.0), torch.full_like(q, 9.0)
+
+    def call(to):
+        hk.attn_pages(q, pool.cache, d ** -0.5, to, causal=True)
+    call(fine)
+    clean = median_ms(lambda: call(fine))
+    rows = [list(range(64 * page, min(64 * page + 64, 3000))), []]
+    pool.table[0, page] = pool.n_pages
+    call(out)
+    torch.cuda.synchronize()
+    with pytest.raises(HackError):
+        hk.check()
+    check_without(pool, q, out, scale_of(d), True, rows)
+    assert torch.equal(out[1], fine[1])
+
+    def again():
+        call(out)
+        torch.cuda.synchronize()
+        with pytest.raises(HackError):
+            hk.check()
+    assert median_ms(again) < 16 * clean + 0.5, clean
+    hk.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n, length", [(40, 1500), (130, 1500), (130, 40)])
+def test_shared_pages_that_are_none(contexts, d, n, length):  # noqa: F811
+    """A page of the shared rows, and one of an element's own."""
+    prefix = 1024
+    hk = contexts(2, d, "bf16", shared=0)
+    g = torch.Generator(DEV).manual_seed(n)
+    groups = [(0, 2, prefix)]
+    pool = Pool(hk, [prefix + length, prefix + length + 9], 16, g, shared=groups)
+    q = queries((2, 4, n, d), "bf16", g)
+    out = torch.full_like(q, 9.0)
+    pool.table[0, 5] = -1                        # rows that all read by the first element's table
+    pool.table[1, prefix // 16 + 1] = 1 << 30
+    hk.attn_pages(q, pool.cache, d ** -0.5, out, shared=groups)
+    torch.cuda.synchronize()
+    with pytest.raises(HackError):
+        hk.check()
+    common = list(range(80, 96))
+    check_without(pool, q, out, scale_of(d), False, [common, common + list(range(prefix + 16, prefix + 32))])
