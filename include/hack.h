@@ -515,7 +515,8 @@ hack_status hack_attn_packed(hack_ctx* ctx, int32_t B, int32_t N_k, const void* 
  * What only a running kernel can see is reported as HACK_EINVAL by hack_check and the next
  * call, once: a page number outside [0, pages) (rows there are left out: not stored, not
  * seen, and a query that is left without any gives no numbers), a length outside [0, max_len] or a number of new rows outside [0, N] (attention takes the
- * nearest of these, appending stores nothing).  Entries of a table behind a sequence's last row are not read. */
+ * nearest of these; appending stores nothing of that sequence, q->out included, or, by_head, nothing of the
+ * head whose length it is).  Entries of a table behind a sequence's last row are not read. */
 typedef struct {
   void* k;              /* DEVICE element (page p, row r, head h, i) at p stride_page + r stride_row + h stride_head + i */
   void* v;              /* DEVICE the same; rows of K and V may lie in turn in one allocation */

@@ -14,12 +14,12 @@ namespace {
 
 using namespace dev;
 
-// A length or a number of new rows that is out of range stores nothing: the rows that it would name are others'.
+// A length or a number of new rows that is out of range stores nothing, no queries either: the rows and positions that it would name are others'.
 __device__ __forceinline__ int stored_rows(const Pages& c, int entry) {
   const int len = c.len[entry];
   if (__builtin_expect((unsigned)len <= (unsigned)c.max_len, 1)) return len;
   report(c);
-  return 0;   // no row lies in front of the sequence's first
+  return -1;   // no row lies in front of the sequence's first
 }
 __device__ __forceinline__ int stored_fresh(const Pages& c, int b) {
   if (!c.fresh) return c.n;
@@ -57,8 +57,8 @@ __global__ __launch_bounds__(kRotateThreads) void append_rows(const AppendArgs a
   const int b = blockIdx.x / a.all_groups;
   unsigned x = blockIdx.x - (unsigned)b * a.all_groups;
   const int which = x < a.groups[0] ? 0 : x < a.groups[1] ? 1 : 2;   // q, k, v
-  const int fresh = stored_fresh(a.c, b);
-  const int first = a.c.by_head ? 0 : stored_rows(a.c, b) - fresh;   // row of the first new one
+  const int len = a.c.by_head ? 0 : stored_rows(a.c, b), fresh = len < 0 ? 0 : stored_fresh(a.c, b);
+  const int first = a.c.by_head ? 0 : len - fresh;   // row of the first new one
   const int pos0 = a.own_rows ? first : 0;
   if (which == 0) {
     turn_rows<T, D, HALF, NORM, STREAM>(a, a.t[0], b, x, a.rot_dim, pos0, [&](int64_t n) {

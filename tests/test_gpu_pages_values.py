@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2504_09261_amd.binding import HackError
+from paper_2504_09261_amd.binding import HackError, Rope
 from tests.test_gpu_operators import DEV, H, HALF_STEP
 from tests.test_gpu_pages import Pool, check_attention, contexts, queries  # noqa: F401
 
@@ -184,3 +184,35 @@ def test_shared_pages_that_are_none(contexts, d, n, length):  # noqa: F811
         hk.check()
     common = list(range(80, 96))
     check_without(pool, q, out, scale_of(d), False, [common, common + list(range(prefix + 16, prefix + 32))])
+
+
+# ---- appending with lengths or numbers of new rows that are out of range ----
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("given", [False, True])
+def test_queries_of_sequences_out_of_range_are_left(contexts, dtype, given):  # noqa: F811
+    """Appending stores nothing of such a sequence, its queries included, so a caller that turns them in place still has them."""
+    hk = contexts(2, 64, dtype)
+    g = torch.Generator(DEV).manual_seed(3)
+    pool = Pool(hk, [100, 70, 90], 16, g)
+    rope, n = Rope.scaled(64), 40
+    q, k, v = (queries((3, h, n, 64), dtype, g, 1.0) for h in (4, 2, 2))
+    pos = torch.arange(n, dtype=torch.int32, device=DEV) if given else None
+    want = torch.full_like(q, 9.0)
+    hk.append_pages(k, v, pool.cache, rope=rope, pos=pos, q=q, q_out=want, norm="rms")
+    hk.check()
+    for lens, fresh in (([100, 1 << 20, 90], None), ([100, -1, 90], None), ([100, 70, 90], [n, n + 1, n]), ([100, 70, 90], [n, -1, n])):
+        pool.len.copy_(torch.tensor(lens))
+        f = None if fresh is None else torch.tensor(fresh, dtype=torch.int32, device=DEV)
+        before = [pool.k.clone(), pool.v.clone()]
+        for in_place in (False, True):
+            x = q.clone()
+            out = x if in_place else torch.full_like(q, 9.0)
+            hk.append_pages(k, v, pool.cache, rope=rope, pos=pos, fresh=f, q=x, q_out=out, norm="rms")
+            torch.cuda.synchronize()
+            with pytest.raises(HackError):
+                hk.check()
+            assert torch.equal(out[::2], want[::2])
+            assert torch.equal(out[1], q[1]) if in_place else (out[1] == 9.0).all()
+        for m, o in zip((pool.k, pool.v), before):
+            assert torch.equal(m.nan_to_num(7.0), o.nan_to_num(7.0))
+    hk.check()
