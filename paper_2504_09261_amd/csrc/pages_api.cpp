@@ -105,14 +105,21 @@ bool plan_parts(const hack_ctx* ctx, AttnPagesArgs* a) {
     saved += (int64_t)(s.count - 1) * s.rows * H * 2 * ctx->cfg.head_dim * ctx->elem_bytes;
   }
   if (saved < ctx->share_bytes) a->n_shared = 0;
-  int own_tile = tile_queries(ctx, GN, units, a->c.max_len), shared_tile = own_tile;
-  if (a->n_shared > 0) {   // tiles of 16 and of 32 are not mixed, nor those of 64 and of 128
-    if (tile_queries(ctx, most, a->n_shared * H, a->c.max_len) >= kHalfTileQueries) shared_tile = kPageTileQueries;
-    if (own_tile >= kHalfTileQueries) own_tile = kPageTileQueries;
+  int own_tile, shared_tile;
+  const auto choose_tiles = [&]() {
+    own_tile = shared_tile = tile_queries(ctx, GN, units, a->c.max_len);
+    if (a->n_shared > 0) {   // tiles of 16 and of 32 are not mixed, nor those of 64 and of 128
+      if (tile_queries(ctx, most, a->n_shared * H, a->c.max_len) >= kHalfTileQueries) shared_tile = kPageTileQueries;
+      if (own_tile >= kHalfTileQueries) own_tile = kPageTileQueries;
+    }
+    lay_out(1, GN, own_tile);
+    lay_out(0, most, shared_tile);
+  };
+  choose_tiles();
+  if (rows_of(part[0], a->n_shared * H) + rows_of(part[1], units) > ctx->part_rows && a->n_shared > 0) {
+    a->n_shared = 0;   // no room to join the parts: every element reads all of its rows
+    choose_tiles();
   }
-  lay_out(1, GN, own_tile);
-  lay_out(0, most, shared_tile);
-  if (rows_of(part[0], a->n_shared * H) + rows_of(part[1], units) > ctx->part_rows) a->n_shared = 0;   // no room to join the parts: every element reads all of its rows
   const int64_t shared_rows = rows_of(part[0], a->n_shared * H);
   // Work-groups that blocks are cut for: of few queries four a compute unit (two, three, four, six: 643 MB 121, 120, 119, 118 us, one long cache 105, 107, 103, 106),
   // of 128 two, which is what it holds.  Shorter chunks than kChunk are worth it only up to one a compute unit: 8 units of 20000 rows in 296 chunks 26.3 us, in 256 22.3.

@@ -341,6 +341,40 @@ int plans() {
   return 0;
 }
 
+// Groups whose partial results find no room: every element reads its rows by itself, in the tiles that it has without groups.
+int dropped_groups() {
+  const auto call = [](int dtype, int heads, int batch, int group, int queries, int rows, int own, bool shared, int32_t (&form)[3]) {
+    Context c(dtype, heads, batch * heads, 600);
+    c.ctx->cus = 256;
+    if (dtype == HACK_BF16) c.ctx->part_rows = 512 * 2 * 128;
+    hack_pages p = pages();
+    p.stride_head = kD;
+    p.stride_row = heads * kD;
+    p.stride_page = 64ll * heads * kD;
+    p.table_pages = p.table_stride = (rows + own + 63) / 64;
+    p.table = at<int32_t>(0x80000000000);
+    p.len = at<int32_t>(0xF00000000000);
+    const hack_shared s{0, batch, rows};
+    stub::attentions.clear();
+    if (hack_attn_pages(c.ctx, batch, queries, heads * group, at(kE << 8), &p, nullptr, 0, &s, shared, 0.1f, at(kF << 8), kStream) != HACK_OK) return false;
+    const AttnPagesArgs& a = stub::attentions.back().a;
+    form[0] = a.n_shared;
+    form[1] = a.part[1].queries;
+    form[2] = a.part[1].pairs;
+    return true;
+  };
+  int32_t with[3], without[3];
+  CHECK(call(HACK_BF16, 30, 8, 1, 64, 4096, 155, true, with) && with[0] == 1 && with[1] == kPageTileQueries);   // room: tiles as large as those of the shared rows
+  const struct { int dtype, heads, batch, group, queries, rows; } none[] = {{HACK_BF16, 30, 32, 1, 64, 4096}, {HACK_BF16, 8, 1024, 1, 1, 8192}, {HACK_BF16, 8, 64, 4, 33, 4096},
+                                                                            {HACK_F32, 32, 64, 1, 1, 4096}, {HACK_F32, 8, 256, 4, 1, 4096}};
+  for (const auto& x : none) {
+    CHECK(call(x.dtype, x.heads, x.batch, x.group, x.queries, x.rows, 155, true, with) && call(x.dtype, x.heads, x.batch, x.group, x.queries, x.rows, 155, false, without));
+    printf("%d queries of %d x %d: tiles of %d, without groups %d\n", x.queries, x.heads, x.batch, with[1], without[1]);
+    CHECK(with[0] == 0 && with[1] == without[1] && with[2] == without[2]);
+  }
+  return 0;
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -350,6 +384,7 @@ int main(int argc, char** argv) {
   if (name == "cache_refusals") r = cache_refusals();
   if (name == "attn_refusals") r = attn_refusals();
   if (name == "plans") r = plans();
+  if (name == "dropped_groups") r = dropped_groups();
   if (r == 0) printf("ok\n");
   return r;
 }

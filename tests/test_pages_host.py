@@ -22,3 +22,8 @@ def program(tmp_path_factory):
 def test_host_side(program, name):
     r = subprocess.run([str(program), name], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip().endswith("ok") and not r.stderr, r.stdout + r.stderr[-2000:]
+
+
+def test_groups_without_room(program):
+    r = subprocess.run([str(program), "dropped_groups"], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip().endswith("ok") and not r.stderr, r.stdout + r.stderr[-2000:]
