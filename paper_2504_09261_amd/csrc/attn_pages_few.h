@@ -178,6 +178,9 @@ __device__ __forceinline__ void few_queries(const AttnPagesArgs& a, int part, co
   constexpr int ROWS = Keys::kRows, TILES = ROWS / 16, PIECES = Keys::kChunks / 4;
   static_assert(ROWS * D * (int)sizeof(T) <= 16 * NQ * D * (int)sizeof(float), "a wave's block of K fits where its results go");
   constexpr bool kBf16 = sizeof(T) == 2;
+  // Sums that a float32 score is made of, each over a quarter of the products: one after the other 128 roundings add up where 32 do (one token of 2 caches in each of 4
+  // elements, 1249 to 1787 rows: 1.5e-6 off, so 6e-7; products over as many elements in a tree 5e-7).  32 queries have no registers for them, and are as far off as large products are.
+  constexpr int SUMS = !kBf16 && NQ == 1 ? 4 : 1;
   constexpr int MT = D / 16, QROWS = 16 * NQ, SIDE = kBf16 ? MT : 4;   // head-dims of a lane that lie side by side
   const Pages& c = a.c;
   const int b0 = item.b0, h = item.h, entry0 = item.entry0, group = item.group, common = item.common, lo = item.lo, n_rows = item.n_rows, GN = a.G * c.n;
@@ -304,15 +307,16 @@ __device__ __forceinline__ void few_queries(const AttnPagesArgs& a, int part, co
     floatx4 sc[TILES][NQ];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
+      floatx4 some[SUMS][NQ];
 #pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) sc[t][qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < SUMS * NQ; ++i) some[i / NQ][i % NQ] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < PIECES; ++s) {
         const uintx4 k = Keys::get(k_lds, t, s, col, g);
         if constexpr (kBf16) {
 #pragma unroll
           for (int qt = 0; qt < NQ; ++qt)
-            sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[qt][s]), sc[t][qt], 0, 0, 0);
+            some[0][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[qt][s]), some[0][qt], 0, 0, 0);
         } else {
           const floatx4 x = __builtin_bit_cast(floatx4, k);
 #pragma unroll
@@ -320,9 +324,14 @@ __device__ __forceinline__ void few_queries(const AttnPagesArgs& a, int part, co
 #pragma unroll
             for (int qt = 0; qt < NQ; ++qt) {
               const floatx4 y = __builtin_bit_cast(floatx4, qf[qt][s]);
-              sc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], sc[t][qt], 0, 0, 0);
+              some[i % SUMS][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], some[i % SUMS][qt], 0, 0, 0);
             }
         }
+      }
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+        if constexpr (SUMS == 4) some[0][qt] = (some[0][qt] + some[1][qt]) + (some[2][qt] + some[3][qt]);
+        sc[t][qt] = some[0][qt];
       }
     }
     const bool masked = key0 < lo || key0 + ROWS > fewest || bad != 0;

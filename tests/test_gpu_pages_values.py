@@ -233,3 +233,26 @@ def test_groups_without_room(contexts, dtype, batch, heads, group, n):  # noqa: 
         hk.attn_pages(q[:count], cache, 0.125, out, causal=True, shared=[(0, count, prefix)])
         check_attention(pool, q[:count], out, 0.125, True)
     hk.check()
+
+
+# ---- float32 scores ----
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 16])
+def test_small_products_beside_a_large_one(contexts, d, n):  # noqa: F811
+    """A float32 score of 2^20 and d - 1 products of 3 2^-8, of which not even four reach half a step of 2^20 (2^-4): only those in the sum of a quarter that the large
+    product is in are lost, (d / 4 - 1) 3 2^-8 of the score, and the three additions of the quarters round by 2^-4 at most.  Beside it a key whose score is 2^20, and whose
+    value is 0: the result is the weight of the first one."""
+    hk = contexts(1, d, "f32")
+    g = torch.Generator(DEV).manual_seed(d)
+    pool = Pool(hk, [2], 16, g)
+    pool.k[pool.where(0, 0, 0, 2)] = 0.0
+    page, row, head = pool.where(0, 0, 0, 2)
+    pool.k[page[0], row[0], head[0]] = 3 * 2.0 ** -8
+    pool.k[page, row, head, 0] = 2.0 ** 20
+    pool.v[page, row, head] = torch.tensor([[1.0], [0.0]], device=DEV)
+    q = torch.ones((1, 1, n, d), device=DEV)
+    out = torch.full_like(q, 9.0)
+    hk.attn_pages(q, pool.cache, 2.0, out)
+    more, off = (d - 1) * 3 * 2.0 ** -8, (d / 4 - 1) * 3 * 2.0 ** -8 + 3 * 2.0 ** -4
+    lo, hi = (1 / (1 + np.exp(-2.0 * x)) for x in (more - off, more + off))
+    assert (out >= lo - 1e-5).all() and (out <= hi + 1e-5).all(), (float(out[0, 0, 0, 0]), lo, hi)
