@@ -166,7 +166,7 @@ def test_prompt_over_a_page_that_is_none(contexts, d, heads, page):  # noqa: F81
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("n, length", [(40, 1500), (130, 1500), (130, 40)])
+@pytest.mark.parametrize("n, length", [(1, 1500), (16, 1500), (40, 1500), (130, 1500), (130, 40)])
 def test_shared_pages_that_are_none(contexts, d, n, length):  # noqa: F811
     """A page of the shared rows, and one of an element's own."""
     prefix = 1024
@@ -219,14 +219,14 @@ def test_queries_of_sequences_out_of_range_are_left(contexts, dtype, given):  # 
 
 
 # ---- groups whose partial results find no room ----
-@pytest.mark.parametrize("dtype, batch, heads, group, n", [("bf16", 64, 8, 4, 33), ("f32", 256, 8, 4, 1)])
-def test_groups_without_room(contexts, dtype, batch, heads, group, n):  # noqa: F811
+@pytest.mark.parametrize("dtype, d, batch, heads, group, n", [("bf16", 128, 64, 8, 4, 33), ("bf16", 64, 64, 8, 4, 33), ("f32", 64, 256, 8, 4, 1)])
+def test_groups_without_room(contexts, dtype, d, batch, heads, group, n):  # noqa: F811
     """Every element reads the shared rows by itself then, and they are the same; half of the batch in a group finds room."""
-    hk = contexts(heads, 64, dtype, units=batch * heads, shared=0)
+    hk = contexts(heads, d, dtype, units=batch * heads, shared=0)
     g = torch.Generator(DEV).manual_seed(batch)
     prefix, lens = 64, 70 + n + (np.arange(batch) * 29) % 200
     pool = Pool(hk, lens, 16, g, shared=[(0, batch, prefix)])
-    q = queries((batch, group * heads, n, 64), dtype, g)
+    q = queries((batch, group * heads, n, d), dtype, g)
     for count in (batch, batch // 4):
         out = torch.full_like(q[:count], 9.0)
         cache = PagedCache(pool.k, pool.v, pool.table[:count], pool.len[:count])
