@@ -565,10 +565,14 @@ typedef struct {
  * order in which it is summed up).
  *   heads   of q, a multiple G of H: query heads G h .. G h + G - 1 read cache h
  *   q, out  DEVICE [B, heads, N, head_dim]
- *   shared  HOST n_shared groups in ascending order, none in two of them; NULL: none.  Rows that a group shares are read
- *           once for all of it where that is faster, from the pages that the first element's table has for them (whatever its length).  Lengths count them: an element
-           whose length is smaller sees that many.
- * Sums are in float32, softmax in one pass; results are reproducible bit for bit from call to call with the same
+ *   shared  HOST n_shared groups in ascending order, none in two of them; NULL: none.  Lengths count the shared
+ *           rows: an element whose length is smaller sees that many.  Rows that a group shares are read once for all of it, from the
+ *           pages that the first element's table has for them (whatever its length), if that spares enough reading
+ *           (64 MiB) and the partial results of all queries have room in the context's workspace (131072 rows or more in
+ *           bf16 contexts, 32768 in float32 ones, counted in tiles of 16 to 128 queries); else every element
+ *           reads them by its own table.  So the tables of all elements name pages that hold these rows.
+ * Scores, softmax statistics and sums are in float32, softmax in one pass; bf16 contexts round the probabilities to bf16, for
+ * the product with V and for their sum alike.  Results are reproducible bit for bit from call to call with the same
  * lengths, groups and max_len.  out must not share memory with q or the cache.
  * Errors: HACK_EINVAL, HACK_ECAPACITY (B or N beyond max_units / H, max_queries, more than 256 groups, more queries than a
  * launch takes). */

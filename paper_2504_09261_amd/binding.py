@@ -534,7 +534,7 @@ class Hack:
 
     def attn_pages(self, q, cache: PagedCache, scale: float, out, causal: bool = False, fresh=None, shared=None):
         """q: [B, G heads, N, head_dim], G query heads to each cache; the first fresh[b] queries (None: all) see their sequence's rows, causal: those up to their own.
-        shared: (first, count, rows) of batch elements that have the same first rows."""
+        shared: (first, count, rows) of batch elements that have the same first rows, by the table of each."""
         st = _ops_call.attn_pages(_ops_addr["attn_pages"], self.ctx and self.ctx.value, self._info, q, cache._info, fresh, causal, shared, scale, out, _stream())
         if st != 0:
             self._check(st)

@@ -35,7 +35,9 @@ constexpr int kIotaRows = 32768;                 // rows a unit that keeps every
 // takes 0.16 us (launches that give up after 4096 and 16384 polls: 695 and 2662 us), so the wait lasts 96 ms; real ones last a few
 // microseconds, longer only where other work keeps the unit's other work-groups from running.
 constexpr int kScoreSpinLimit = 600000;
-constexpr int64_t kF32PartRows = 2048 * 16;      // partial results of units that attention over a packed cache cuts, fp32 contexts: 2048 work-groups of 16 queries
+// Rows of partial results in fp32 contexts, 2048 work-groups of 16 queries: of units that attention over a packed cache cuts, and of entries that attention over
+// caches in pages cuts or whose shared rows it reads apart (without room for them it shares and cuts nothing).
+constexpr int64_t kF32PartRows = 2048 * 16;
 
 }  // namespace
 
@@ -553,7 +555,7 @@ extern "C" hack_status hack_create(hack_ctx** out, const hack_config* cfg) {
     if (e == hipSuccess) e = hipMalloc((void**)&ctx->part_count, (n_part / 2) * sizeof(unsigned));
     if (e == hipSuccess) e = hipMemset(ctx->part_count, 0, (n_part / 2) * sizeof(unsigned));
   }
-  if (e == hipSuccess && cfg->dtype == HACK_F32) {   // attention over packed caches alone cuts units
+  if (e == hipSuccess && cfg->dtype == HACK_F32) {   // attention over packed caches and over caches in pages
     ctx->part_rows = kF32PartRows;
     e = hipMalloc((void**)&ctx->part_o, (size_t)ctx->part_rows * cfg->head_dim * sizeof(float));
     if (e == hipSuccess) e = hipMalloc((void**)&ctx->part_ml, (size_t)ctx->part_rows * 2 * sizeof(float));

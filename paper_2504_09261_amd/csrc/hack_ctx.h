@@ -76,7 +76,8 @@ struct hack_ctx {
   int attn_slots = 0;            // work-groups of the streamed kernel the device holds at once
   float* part_o = nullptr;       // [2 * attn_slots, 128, head_dim] unnormalised partial outputs (fp32 contexts: [part_rows, head_dim])
   float* part_ml = nullptr;      // [2 * attn_slots, 2, 128] their references and normalisers ([part_rows, 2])
-  int64_t part_rows = 0;         // rows of part_o
+  int64_t part_rows = 0;         // rows of part_o, for attention over packed caches and over caches in pages too: what finds no room there is not cut, and groups of the
+                                 // latter do not share
   // Rows of K and V that sharing must spare a call of attention over caches in pages, bytes (HACK_ATTN_PAGES_SHARED): partial results are joined by a launch of their own, and
   // reading again what others have just read is not reading memory.  Us a call, 32 + 8 heads of 128, own rows up to 700, apart / shared: 16 elements behind 1024
   // rows (63 MB) 22.6 / 27.6, 64 behind 256 (66 MB) 30.9 / 30.4, 8 behind 4096 (117 MB) 34.3 / 22.8, 64 behind 512 (132 MB) 42.9 / 30.8.
