@@ -453,16 +453,17 @@ PyObject* attn_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
   hack_shared groups[kMost];
   Py_ssize_t n_groups = 0;
   if (a[7] != Py_None) {
-    PyObject* f = PySequence_Fast(a[7], "shared: a list of (first, count, rows)");
+    // Tuples, which nothing changes while numbers are taken out of them: an __index__ may run any code.
+    PyObject* f = PySequence_Tuple(a[7]);
     if (!f) return nullptr;
-    n_groups = PySequence_Fast_GET_SIZE(f);
+    n_groups = PyTuple_GET_SIZE(f);
     bool ok = n_groups <= kMost || refuse("shared: too many groups");
     for (Py_ssize_t i = 0; ok && i < n_groups; ++i) {
-      PyObject* g = PySequence_Fast(PySequence_Fast_GET_ITEM(f, i), "shared: a list of (first, count, rows)");
-      ok = g && (PySequence_Fast_GET_SIZE(g) == 3 || refuse("shared: a list of (first, count, rows)"));
+      PyObject* g = PySequence_Tuple(PyTuple_GET_ITEM(f, i));
+      ok = g && (PyTuple_GET_SIZE(g) == 3 || refuse("shared: a list of (first, count, rows)"));
       if (ok)
-        ok = int32_arg(PySequence_Fast_GET_ITEM(g, 0), &groups[i].first) && int32_arg(PySequence_Fast_GET_ITEM(g, 1), &groups[i].count) &&
-             int32_arg(PySequence_Fast_GET_ITEM(g, 2), &groups[i].rows);
+        ok = int32_arg(PyTuple_GET_ITEM(g, 0), &groups[i].first) && int32_arg(PyTuple_GET_ITEM(g, 1), &groups[i].count) &&
+             int32_arg(PyTuple_GET_ITEM(g, 2), &groups[i].rows);
       Py_XDECREF(g);
     }
     Py_DECREF(f);

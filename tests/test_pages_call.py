@@ -122,3 +122,20 @@ def test_wrong_calls():
     with pytest.raises(TypeError):
         attn(scale="x")
     assert not SEEN
+
+
+def test_groups_that_change_while_they_are_read():
+    groups = []
+
+    class Clears:
+        def __init__(self, n, what):
+            self.n, self.what = n, what
+
+        def __index__(self):
+            self.what.clear()
+            return self.n
+    inner = []
+    inner += [Clears(0, inner), 1, 5]
+    groups += [inner, (Clears(1, groups), 1, 9), (2, 1, 3)]
+    assert attn(shared=groups) == 0
+    assert SEEN.pop()[8] == [(0, 1, 5), (1, 1, 9), (2, 1, 3)] and not groups and not inner
