@@ -12,7 +12,7 @@
 // does all of its queries again.  1000 causal queries of 72 heads of 64 over 3000 rows 94 us; with a NaN that some queries of an item see 234, with a page that is none 765
 // (key by key in each wave, query after query: 42.5 ms).
 //
-// Bound by the matrix cores and the vector work beside them.  Measured, head_dim 128: 3000 causal queries of 32 heads over 4001 to 7001 rows of 8 caches 248 to 255 us (1.06 to 1.09
+// Bound by the matrix cores and the vector work beside them.  Measured, head_dim 128: 3000 causal queries of 32 heads over 4001 to 7001 rows of 8 caches 243 to 261 us (1.04 to 1.11
 // PFLOP/s; a large library product reaches 1.2), without the mask 314 (1.10).  At head_dim 64 the exponentials of a block stand beside half the products: the same at 64, 160 to 163 us
 // (0.83 to 0.84).  A third of the LDS' active cycles are the K reads' two-way bank conflicts, as in the kernel over contiguous rows, where a placement without them is no faster.  Places computed from the table in every stage, copies with scalar bases, masks in every stage: 479 us for the 310 that the form here took then; queries in the
 // order number, head instead of head, number, so that an item's last blocks are few and items are in order of their lengths: 310 -> 270.
